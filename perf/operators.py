@@ -284,7 +284,8 @@ def _handles(st):
         st.rope = hsa.rope(c["rot"], layout=c["layout"], theta=THETA, axis_dims=_axes(c) if c["axes"] else None,
                            amplitude=AMPLITUDE[c["scaling"]], **scaled)
     if c["kind"] in ("write8", "attn8"):
-        st.cache = hsa.HsaCache8(c["batch"], c["heads"], c["d"], c["page"], _dtype(c), DEV, kv_heads=c["kv"],
+        heads = c["heads"] if c["kind"] == "attn8" else c["kv"]  # an append has no query heads
+        st.cache = hsa.HsaCache8(c["batch"], heads, c["d"], c["page"], _dtype(c), DEV, kv_heads=c["kv"],
                                  k=x.cache.k, v=x.cache.v, k_exp=x.cache.k_exp, v_exp=x.cache.v_exp,
                                  page_table=x.page_table, rope=st.rope)
     elif c["kind"] == "write":
