@@ -630,6 +630,148 @@ hsa_status_t hsa_forward_linformer(const hsa_config_t* cfg, const void* q, int32
                                    const float* g_sp, void* o, int32_t* sel_out, void* ws,
                                    size_t ws_bytes, void* stream);
 
+/*
+ * Rotary positions. Pair i of a head's first rot_dim dims is turned by the angle
+ * x * f_i, x the token's position on the pair's axis:
+ *   (a, b) -> A (a cos - b sin, b cos + a sin);
+ * the dims from rot_dim on are copied. Half layout: pair i is dims (i, i +
+ * rot_dim / 2); interleaved: (2 i, 2 i + 1). With one axis, f_i = theta^(-2 i /
+ * rot_dim). With 2 or 3 axes (frame, row, column of a video token) the
+ * pairs are divided among them in order, axis_dim[a] dims (even, summing to rot_dim) to axis
+ * a, and the j-th pair of axis a has f = theta^(-2 j / axis_dim[a]).
+ * Scaled for long contexts: LINEAR divides every f by factor; PARTS divides
+ * the slow ones only: with r = orig_len f / (2 pi) turns over the original length and
+ * w = (r - low) / (high - low) clamped to [0, 1], f becomes w f + (1 - w) f /
+ * factor. Angles are fp64 up to their reduction, cosines, sines and products
+ * fp32, and the result is rounded once to the type of the call.
+ */
+#define HSA_ROPE_HALF 0
+#define HSA_ROPE_INTERLEAVED 1
+#define HSA_ROPE_UNSCALED 0
+#define HSA_ROPE_LINEAR 1
+#define HSA_ROPE_PARTS 2
+
+typedef struct hsa_rope {
+  int32_t rot_dim;     /* even, in [2, head_dim] */
+  int32_t layout;      /* HSA_ROPE_HALF or HSA_ROPE_INTERLEAVED */
+  int32_t axes;        /* 1, 2 or 3 */
+  int32_t axis_dim[3]; /* dims of each axis (axes > 1) */
+  int32_t scaling;     /* HSA_ROPE_UNSCALED, _LINEAR or _PARTS */
+  int32_t orig_len;    /* PARTS: original context length, >= 1 */
+  double theta;        /* > 0 */
+  double factor;       /* LINEAR, PARTS: > 0 */
+  double low, high;    /* PARTS: 0 <= low < high */
+  double amplitude;    /* A; 0 means 1 */
+} hsa_rope_t;
+
+/*
+ * hsa_rope_apply -- turns the heads of n tokens of every batch entry (queries
+ * before an attention call, or keys that no cache takes).
+ * x: device, cfg->dtype, [B, n, heads, d] with the given strides in elements between batch
+ * entries and between tokens (>= 0; the heads of a token are contiguous), so that it may
+ * be a part of a fused projection. o: as x with its own strides; o may be x
+ * itself with the same strides, and must not overlap it otherwise. heads: 1 ..
+ * HSA_MAX_HEADS (cfg->num_heads is not used). pos: device int32 [B, n, axes], or NULL: token i of
+ * entry b is at first[b] + i (first: device int32 [B], NULL: 0; one axis only).
+ * inverse != 0 turns by the opposite angles. That is the transposed map:
+ * given the gradient of o it gives the gradient of x. Errors: INVALID_ARG (NULL, a
+ * bad rope or stride), UNSUPPORTED (sizes). n == 0 is a no-op.
+ */
+hsa_status_t hsa_rope_apply(const hsa_config_t* cfg, const hsa_rope_t* rope, const void* x,
+                            int64_t x_batch_stride, int64_t x_token_stride, int32_t n,
+                            int32_t heads, const int32_t* pos, const int32_t* first,
+                            int32_t inverse, void* o, int64_t o_batch_stride,
+                            int64_t o_token_stride, void* stream);
+
+/*
+ * hsa_token_write -- appends any run of tokens to the pool, keys rotated on the
+ * way (hsa_page_write without whole pages): tokens i < count[b] of batch entry
+ * b become tokens first[b] + i of its sequence, token t in page t / P of its
+ * row of the page table. Tokens outside [0, max_pages * P) are dropped; the rest of
+ * the pages stays as it was. rope: NULL for keys as they are; pos as in
+ * hsa_rope_apply, its default the token's place in the sequence.
+ * k_src, v_src: device, cfg->dtype, [B, n, H, d] with strides in elements as in
+ * hsa_rope_apply. first: device int32 [B], NULL: 0. count: device int32 [B] in
+ * [0, n], NULL: n. No two entries of a call may write to the same page. Errors as
+ * hsa_rope_apply. n == 0 is a no-op. Kernels read first and count, so a
+ * captured call follows them.
+ */
+hsa_status_t hsa_token_write(const hsa_config_t* cfg, const hsa_kv_pool_t* pool,
+                             const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
+                             int64_t k_token_stride, const void* v_src, int64_t v_batch_stride,
+                             int64_t v_token_stride, int32_t n, const int32_t* pos,
+                             const int32_t* first, const int32_t* count, void* stream);
+
+/*
+ * 8-bit cache: pages of OCP e4m3 codes with a power-of-two scale for each block of
+ * HSA_CACHE8_BLOCK tokens of a page (the last one may be shorter) and key head, keys and
+ * values apart. A number is code * 2^(exponent byte - 127). A page takes half
+ * the bytes of a bf16 one.
+ */
+#define HSA_CACHE8_BLOCK 64
+
+typedef struct hsa_cache8 {
+  void* k;                   /* device uint8 [num_slots, kv_heads, P, d] */
+  void* v;                   /* device uint8 [num_slots, kv_heads, d, P], d-major */
+  void* k_exp;               /* device uint8 [num_slots, kv_heads, ceil(P / HSA_CACHE8_BLOCK)] */
+  void* v_exp;
+  const int32_t* page_table; /* device [B, max_pages] */
+  int32_t num_slots;
+  int32_t max_pages;         /* max_pages * P < 2^31 - 128 */
+  int32_t kv_heads;          /* divides cfg->num_heads (the query heads) */
+} hsa_cache8_t;
+
+/*
+ * hsa_cache8_write -- hsa_token_write into the 8-bit cache: k_src, v_src are
+ * [B, n, kv_heads, d]. A block's scale 2^e has the smallest e in [-100, 120] with 448 *
+ * 2^e >= its largest finite magnitude (keys after the rotation, in fp32); codes are rounded to
+ * nearest even, infinities to the largest code, NaN to a NaN code (0x7f or 0xff). A block whose
+ * first tokens an earlier call wrote keeps the larger of its scale and the one the
+ * new tokens need; if that grows, the older codes are scaled down by the power of two, which
+ * rounds only those that become subnormal. A block written from its first
+ * token on starts anew, whatever its memory held.
+ */
+hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache,
+                              const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
+                              int64_t k_token_stride, const void* v_src, int64_t v_batch_stride,
+                              int64_t v_token_stride, int32_t n, const int32_t* pos,
+                              const int32_t* first, const int32_t* count, void* stream);
+
+/*
+ * hsa_cache8_attn -- exact softmax attention over the 8-bit cache (the sparse
+ * branch of hsa_sparse_attn for that cache, and what a model that decodes token by token
+ * calls): per batch entry and key head the listed pages are sel[b][hk][0..) (up to the first
+ * entry outside [0, max_pages), at most k_h[hk]) followed by pages
+ * [cur_first_page, cur_first_page + n_cur_pages). Query head h reads key head
+ * h / (num_heads / kv_heads). Query i of entry b sees the tokens t of the listed
+ * pages with t < kv_len[b] and, with causal != 0, t <= kv_len[b] - q_len[b] + i
+ * (query i is the sequence's token at that place):
+ *   o[b][i][h] = sum_t softmax_t(scale * q_i . k_t) v_t     (cfg->dtype)
+ *   lse[b][h][i] = log sum_t exp(scale * q_i . k_t)          (fp32, nullable)
+ * A query that sees no token gets o = 0 and lse = -inf. What lies in a page at or past
+ * kv_len is never used, whatever it holds.
+ * q, o: device [B, n_q, num_heads, d], 16-byte aligned. kv_len: device int32
+ * [B], NULL: every token of the listed pages (causal: (cur_first_page +
+ * n_cur_pages) * P). q_len: device int32 [B] in [0, n_q], NULL: n_q; rows of o and
+ * lse at or past q_len[b] stay as they were. sel: device int32 [B, kv_heads, k_max], NULL
+ * with k_max == 0. k_h: host int32 [kv_heads] in [0, k_max], NULL: k_max.
+ * Products of bf16 operands (codes are exact in bf16) summed in fp32; bf16 rounds
+ * the softmax weights to bf16; fp32 splits queries and weights into three bf16 parts,
+ * so that nothing but fp32 sums rounds. Sums are joined in a fixed order: the same
+ * call gives the same bits. ws: hsa_cache8_attn_workspace_size(...) bytes, 256-byte aligned.
+ * Errors: INVALID_ARG (NULL, sizes below 0, an empty list: k_max == 0 and
+ * n_cur_pages == 0), OUT_OF_RANGE (pages beyond max_pages), UNSUPPORTED
+ * (sizes, alignment), WORKSPACE. n_q == 0 is a no-op. Kernels read kv_len and q_len,
+ * so a captured call follows them.
+ */
+size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                      int32_t k_max, int32_t n_cur_pages);
+hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
+                             const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
+                             const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
+                             const int32_t* kv_len, const int32_t* q_len, int32_t causal,
+                             void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

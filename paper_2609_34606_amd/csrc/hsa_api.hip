@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <mutex>
 #include <vector>
 
@@ -1178,6 +1179,281 @@ hsa_status_t hsa_forward_noalloc(const hsa_config_t* cfg, const void* q, int32_t
   return forward_body(cfg, q, n_q, pool, n_cand, n_cur_pages, k_h, k_max, kv_state, k_state,
                       page_kmean, g_lin, g_sp, o, sel_out, base,
                       f32_scratch(base, HSA_NOALLOC_SCRATCH_BYTES, forward_need(cfg, n_q, k_max)), s);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- rotary positions, tokens, 8-bit cache
+namespace {
+
+// Largest grid of a launch in x (workgroups), and in y (batch entries).
+constexpr int64_t kMaxGrid = 0x7fffffff, kMaxGridY = 65535;
+
+hsa_status_t check_strides(int64_t batch, int64_t token) {
+  return batch < 0 || token < 0 ? HSA_ERR_INVALID_ARG : HSA_OK;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+hsa_status_t check_cache8(const hsa_config_t* c, const hsa_cache8_t* a) {
+  if (!a || !a->k || !a->v || !a->k_exp || !a->v_exp || !a->page_table) return HSA_ERR_INVALID_ARG;
+  if (a->num_slots < 1 || a->max_pages < 1 || a->kv_heads < 1) return HSA_ERR_INVALID_ARG;
+  if (c->num_heads % a->kv_heads != 0) return HSA_ERR_INVALID_ARG;
+  if (!aligned16(a->k) || !aligned16(a->v)) return HSA_ERR_UNSUPPORTED;
+  return HSA_OK;
+}
+
+// A sequence's tokens are counted in 32 bits, with room for a tile past the end.
+hsa_status_t check_table(const hsa_config_t* c, int32_t max_pages) {
+  return (int64_t)max_pages * c->page_size >= (1LL << 31) - 128 ? HSA_ERR_UNSUPPORTED : HSA_OK;
+}
+
+// With HSA_CHECK=1: n int32 values of device memory (`missing` where there are none).
+hsa_status_t fetch(const int32_t* dev, size_t n, int32_t missing, std::vector<int32_t>& out) {
+  out.assign(n, missing);
+  if (dev && hipMemcpy(out.data(), dev, n * 4, hipMemcpyDeviceToHost) != hipSuccess) return HSA_ERR_DEVICE;
+  return HSA_OK;
+}
+
+// With HSA_CHECK=1: every token that a write appends must lie in a page that maps
+// to a slot, and every page that an attention call reads must.
+hsa_status_t validate_tokens(const hsa_config_t* c, const int32_t* page_table, int num_slots, int max_pages,
+                             const int32_t* first, const int32_t* count, int n, hipStream_t s) {
+  if (!check_env()) return HSA_OK;
+  try {
+    std::vector<int32_t> pt, f, k;
+    if (hipStreamSynchronize(s) != hipSuccess) return HSA_ERR_DEVICE;
+    if (fetch(page_table, (size_t)c->batch * max_pages, 0, pt) != HSA_OK || fetch(first, c->batch, 0, f) != HSA_OK ||
+        fetch(count, c->batch, n, k) != HSA_OK)
+      return HSA_ERR_DEVICE;
+    for (int b = 0; b < c->batch; ++b) {
+      if (k[b] < 0 || k[b] > n) return HSA_ERR_OUT_OF_RANGE;
+      if (k[b] == 0) continue;
+      if (f[b] < 0 || (int64_t)f[b] + k[b] > (int64_t)max_pages * c->page_size) return HSA_ERR_OUT_OF_RANGE;
+      for (int64_t i = f[b] / c->page_size; i <= ((int64_t)f[b] + k[b] - 1) / c->page_size; ++i) {
+        const int32_t slot = pt[(size_t)b * max_pages + i];
+        if (slot < 0 || slot >= num_slots) return HSA_ERR_OUT_OF_RANGE;
+      }
+    }
+  } catch (const std::exception&) {
+    return HSA_ERR_DEVICE;
+  }
+  return HSA_OK;
+}
+
+hsa_status_t validate_cache8(const hsa_config_t* c, const hsa_cache8_t* a, const int32_t* sel, int k_max,
+                             const int32_t* k_h, int cur_first, int n_cur, const int32_t* kv_len, hipStream_t s) {
+  if (!check_env()) return HSA_OK;
+  try {
+    std::vector<int32_t> pt, len, rows;
+    if (hipStreamSynchronize(s) != hipSuccess) return HSA_ERR_DEVICE;
+    if (fetch(a->page_table, (size_t)c->batch * a->max_pages, 0, pt) != HSA_OK ||
+        fetch(kv_len, c->batch, a->max_pages * c->page_size, len) != HSA_OK ||
+        fetch(sel, (size_t)c->batch * a->kv_heads * k_max, -1, rows) != HSA_OK)
+      return HSA_ERR_DEVICE;
+    for (int b = 0; b < c->batch; ++b) {
+      auto bad = [&](int page) {
+        const int32_t slot = pt[(size_t)b * a->max_pages + page];
+        return (int64_t)page * c->page_size < len[b] && (slot < 0 || slot >= a->num_slots);
+      };
+      for (int i = cur_first; i < cur_first + n_cur; ++i)
+        if (bad(i)) return HSA_ERR_OUT_OF_RANGE;
+      for (int h = 0; h < a->kv_heads; ++h)
+        for (int i = 0; i < (k_h ? k_h[h] : k_max); ++i) {
+          const int32_t e = rows[((size_t)b * a->kv_heads + h) * k_max + i];
+          if (e < 0 || e >= a->max_pages) break;
+          if (bad(e)) return HSA_ERR_OUT_OF_RANGE;
+        }
+    }
+  } catch (const std::exception&) {
+    return HSA_ERR_DEVICE;
+  }
+  return HSA_OK;
+}
+
+// What the two append calls share, once the destination is filled in.
+hsa_status_t run_token_write(const hsa_config_t* cfg, TokenWriteParams& p, const hsa_rope_t* rope,
+                             const void* k_src, int64_t k_batch, int64_t k_token, const void* v_src,
+                             int64_t v_batch, int64_t v_token, int32_t n, const int32_t* pos,
+                             const int32_t* first, const int32_t* count, bool eight, void* stream) {
+  if (!k_src || !v_src || n < 0) return HSA_ERR_INVALID_ARG;
+  if (check_strides(k_batch, k_token) != HSA_OK || check_strides(v_batch, v_token) != HSA_OK)
+    return HSA_ERR_INVALID_ARG;
+  if (rope) {
+    if (!rope_table(rope, cfg->head_dim, false, pos, first, p.table)) return HSA_ERR_INVALID_ARG;
+  } else {
+    p.table.layout = HSA_ROPE_HALF;
+    p.table.rot = 0;
+  }
+  hsa_status_t st = check_table(cfg, p.max_pages);
+  if (st != HSA_OK) return st;
+  if (cfg->batch > kMaxGridY || token_write_units(n, cfg->page_size) * p.H > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  if (n == 0) return HSA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_tokens(cfg, p.page_table, p.num_slots, p.max_pages, first, count, n, s)) != HSA_OK) return st;
+  p.k_src = k_src;
+  p.v_src = v_src;
+  p.k_batch = k_batch;
+  p.k_token = k_token;
+  p.v_batch = v_batch;
+  p.v_token = v_token;
+  p.first = first;
+  p.count = count;
+  p.P = cfg->page_size;
+  p.n = n;
+  return from_hip(launch_token_write(cfg->dtype, cfg->head_dim, cfg->batch, eight, p, s));
+}
+
+// The parts of an attention call's parameters that its plan follows from.
+hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_most,
+                              int32_t n_cur_pages, Cache8AttnParams& p) {
+  p.H = cfg->num_heads;
+  p.Hk = kv_heads;
+  p.G = cfg->num_heads / kv_heads;
+  p.P = cfg->page_size;
+  p.d = cfg->head_dim;
+  p.n_q = n_q;
+  p.n_cur = n_cur_pages;
+  if ((int64_t)n_q * p.G >= 1 << 30) return HSA_ERR_UNSUPPORTED;
+  plan_cache8(p, cfg->dtype, cfg->batch, k_most);
+  if (cfg->batch > kMaxGridY || (int64_t)p.n_split * p.n_rt * p.Hk > kMaxGrid || (int64_t)n_q * p.H > kMaxGrid)
+    return HSA_ERR_UNSUPPORTED;
+  return HSA_OK;
+}
+
+size_t cache8_ws(const hsa_config_t* cfg, const Cache8AttnParams& p) {
+  return align_up(cache8_part_bytes(cfg->batch, p.Hk, p.n_split, p.part_rows, p.d));
+}
+
+}  // namespace
+
+extern "C" {
+
+hsa_status_t hsa_rope_apply(const hsa_config_t* cfg, const hsa_rope_t* rope, const void* x,
+                            int64_t x_batch_stride, int64_t x_token_stride, int32_t n,
+                            int32_t heads, const int32_t* pos, const int32_t* first,
+                            int32_t inverse, void* o, int64_t o_batch_stride,
+                            int64_t o_token_stride, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if (!rope || !x || !o || n < 0 || heads < 1) return HSA_ERR_INVALID_ARG;
+  if (check_strides(x_batch_stride, x_token_stride) != HSA_OK ||
+      check_strides(o_batch_stride, o_token_stride) != HSA_OK)
+    return HSA_ERR_INVALID_ARG;
+  RopeParams p{};
+  if (!rope_table(rope, cfg->head_dim, inverse != 0, pos, first, p.table)) return HSA_ERR_INVALID_ARG;
+  if (heads > HSA_MAX_HEADS || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
+  if ((int64_t)n * heads * cfg->head_dim > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  if (n == 0) return HSA_OK;
+  p.x = x;
+  p.o = o;
+  p.x_batch = x_batch_stride;
+  p.x_token = x_token_stride;
+  p.o_batch = o_batch_stride;
+  p.o_token = o_token_stride;
+  p.n = n;
+  p.heads = heads;
+  p.d = cfg->head_dim;
+  return from_hip(launch_rope(cfg->dtype, cfg->batch, p, static_cast<hipStream_t>(stream)));
+}
+
+hsa_status_t hsa_token_write(const hsa_config_t* cfg, const hsa_kv_pool_t* pool,
+                             const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
+                             int64_t k_token_stride, const void* v_src, int64_t v_batch_stride,
+                             int64_t v_token_stride, int32_t n, const int32_t* pos,
+                             const int32_t* first, const int32_t* count, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_pool(pool)) != HSA_OK) return st;
+  TokenWriteParams p{};
+  // the pool is the caller's device memory; this call is one of those that write it
+  p.k = const_cast<void*>(pool->k);
+  p.v = const_cast<void*>(pool->v);
+  p.page_table = pool->page_table;
+  p.num_slots = pool->num_slots;
+  p.max_pages = pool->max_pages;
+  p.H = cfg->num_heads;
+  return run_token_write(cfg, p, rope, k_src, k_batch_stride, k_token_stride, v_src, v_batch_stride,
+                         v_token_stride, n, pos, first, count, false, stream);
+}
+
+hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache,
+                              const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
+                              int64_t k_token_stride, const void* v_src, int64_t v_batch_stride,
+                              int64_t v_token_stride, int32_t n, const int32_t* pos,
+                              const int32_t* first, const int32_t* count, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  TokenWriteParams p{};
+  p.k = cache->k;
+  p.v = cache->v;
+  p.k_exp = static_cast<uint8_t*>(cache->k_exp);
+  p.v_exp = static_cast<uint8_t*>(cache->v_exp);
+  p.page_table = cache->page_table;
+  p.num_slots = cache->num_slots;
+  p.max_pages = cache->max_pages;
+  p.H = cache->kv_heads;
+  return run_token_write(cfg, p, rope, k_src, k_batch_stride, k_token_stride, v_src, v_batch_stride,
+                         v_token_stride, n, pos, first, count, true, stream);
+}
+
+size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                      int32_t k_max, int32_t n_cur_pages) {
+  if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return 0;
+  if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return 0;
+  Cache8AttnParams p{};
+  if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, p) != HSA_OK) return 0;
+  return cache8_ws(cfg, p);
+}
+
+hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
+                             const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
+                             const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
+                             const int32_t* kv_len, const int32_t* q_len, int32_t causal,
+                             void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  if (!q || !o || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
+  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
+  if (k_h)
+    for (int h = 0; h < cache->kv_heads; ++h)
+      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)cur_first_page + n_cur_pages > cache->max_pages) return HSA_ERR_OUT_OF_RANGE;
+  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
+  if ((st = check_table(cfg, cache->max_pages)) != HSA_OK) return st;
+  if (n_q == 0) return HSA_OK;
+  Cache8AttnParams p{};
+  if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, p)) != HSA_OK) return st;
+  const size_t need = cache8_ws(cfg, p);
+  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_cache8(cfg, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK)
+    return st;
+  p.q = q;
+  p.k = static_cast<const uint8_t*>(cache->k);
+  p.v = static_cast<const uint8_t*>(cache->v);
+  p.k_exp = static_cast<const uint8_t*>(cache->k_exp);
+  p.v_exp = static_cast<const uint8_t*>(cache->v_exp);
+  p.page_table = cache->page_table;
+  p.sel = sel;
+  p.kv_len = kv_len;
+  p.q_len = q_len;
+  p.o = o;
+  p.lse = lse;
+  p.num_slots = cache->num_slots;
+  p.max_pages = cache->max_pages;
+  p.k_max = k_max;
+  p.cur_first = cur_first_page;
+  p.causal = causal != 0;
+  p.sm_scale = softmax_scale(cfg);
+  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
+  for (int h = 0; h < cache->kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * p.d;
+  return from_hip(launch_cache8_attention(cfg->dtype, cfg->head_dim, cfg->batch, p, s));
 }
 
 }  // extern "C"

@@ -175,6 +175,79 @@ hipError_t launch_page_write(int dtype, int d, int B, const PageWriteParams& p, 
 // number of positions covered by whole cubes.
 int cube_order(int T, int H, int W, int ct, int ch, int cw, int32_t* src_of);
 
+// ------------------------------------------------------------ rotary positions
+struct RopeTable {
+  double turns[64];         // turns (of 2 pi) per position of each pair, negative for the inverse
+  int8_t axis[64];          // which position of the token turns the pair
+  int32_t rot, layout, axes;  // rot = 0: nothing turns
+  float amplitude;
+  const int32_t* pos;       // [B, n, axes] nullable: token i of entry b is at first[b] + i
+  const int32_t* first;     // [B] nullable: 0
+};
+
+struct RopeParams {
+  RopeTable table;
+  const void* x;            // element strides between batch entries and tokens; heads of
+  void* o;                  // a token are contiguous
+  int64_t x_batch, x_token, o_batch, o_token;
+  int32_t n, heads, d;
+  int32_t n_items, n_groups;  // set by the launch
+};
+
+// Fills t from the caller's description, false if that is invalid.
+bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, const int32_t* first, RopeTable& t);
+hipError_t launch_rope(int dtype, int B, const RopeParams& p, hipStream_t s);
+
+// ------------------------------------------------------------ token append
+struct TokenWriteParams {
+  RopeTable table;            // of the keys; its positions default to the cache's
+  const void* k_src;          // element strides as in RopeParams
+  const void* v_src;
+  int64_t k_batch, k_token, v_batch, v_token;
+  void* k;                    // [num_slots, H, P, d] pool keys, or codes
+  void* v;                    // [num_slots, H, d, P]
+  uint8_t* k_exp;             // [num_slots, H, ceil(P / 64)] (8-bit cache)
+  uint8_t* v_exp;
+  const int32_t* page_table;  // [B, max_pages]
+  const int32_t* first;       // [B] nullable
+  const int32_t* count;       // [B] nullable
+  int32_t H, P, n, num_slots, max_pages;
+};
+
+int64_t token_write_units(int64_t n, int P);
+// eight: into the 8-bit cache, else into the pool in the source's type
+hipError_t launch_token_write(int dtype, int d, int B, bool eight, const TokenWriteParams& p, hipStream_t s);
+
+// ------------------------------------------------------------ attention over the 8-bit cache
+struct Cache8AttnParams {
+  const void* q;              // [B, n_q, H, d]
+  const uint8_t* k;           // codes [num_slots, Hk, P, d]
+  const uint8_t* v;           // codes [num_slots, Hk, d, P]
+  const uint8_t* k_exp;       // [num_slots, Hk, nb]
+  const uint8_t* v_exp;
+  const int32_t* page_table;  // [B, max_pages]
+  const int32_t* sel;         // [B, Hk, k_max]
+  const int32_t* kv_len;      // [B] nullable
+  const int32_t* q_len;       // [B] nullable
+  void* o;                    // [B, n_q, H, d]
+  float* lse;                 // [B, H, n_q] nullable
+  float* part_o;              // [B, Hk, n_split, part_rows, d] (n_split > 1)
+  float* part_ml;             // [B, Hk, n_split, part_rows, 2] reference maximum and sum
+  int32_t H, Hk, G, P, d, n_q, num_slots, max_pages, k_max, cur_first, n_cur, causal;
+  float sm_scale, scale_log2;
+  int16_t k_h[HSA_MAX_HEADS]; // most pages of each key head's sel row
+  // set by plan_cache8
+  int32_t nb;                 // scale blocks per page
+  int32_t tpp, ppt;           // 64-key tiles per page; pages per tile
+  int32_t rows_per_item, n_rt, part_rows;
+  int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
+};
+
+// Plans the launch for lists of at most max_list_sel selected pages.
+void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel);
+size_t cache8_part_bytes(int64_t B, int64_t Hk, int64_t n_split, int64_t part_rows, int64_t d);
+hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s);
+
 // ------------------------------------------------------------ attention
 enum AttnMode : int32_t {
   ATTN_FINAL = 0,   // fused linear branch + gated merge, write o (dtype)

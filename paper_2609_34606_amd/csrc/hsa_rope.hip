@@ -1,0 +1,112 @@
+// Rotary positions (queries, or keys outside a cache): pair i of a head is
+// turned by the angle position * frequency_i.
+//
+// Every element is read and written once, so the launch is bound by memory (by
+// its own latency for few tokens). The angle's cosine and sine cost about 35 instructions
+// a pair; a thread computes those of one item (up to E pairs of a token) once and
+// applies them to kHeads heads, whose loads are in flight together. Neighbouring
+// lanes take neighbouring 16-byte pieces of a head.
+#include <math.h>
+
+#include "hsa_rope.h"
+
+namespace hsa {
+namespace {
+
+template <typename T, int kHeads>
+__global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
+  constexpr int E = Pack<T>::E;
+  const RopeTable& r = p.table;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+  const uint32_t row = id / p.n_items;                 // (token, head group)
+  const int j = (int)(id - row * p.n_items);
+  const uint32_t tok = row / p.n_groups;
+  if (tok >= (uint32_t)p.n) return;
+  const int t = (int)tok, h0 = (int)(row - tok * p.n_groups) * kHeads, b = blockIdx.y;
+  const RopeItem it = rope_item<T>(r.layout, r.rot, p.d, j);
+  const T* x = static_cast<const T*>(p.x) + (int64_t)b * p.x_batch + (int64_t)t * p.x_token + it.a;
+  T* o = static_cast<T*>(p.o) + (int64_t)b * p.o_batch + (int64_t)t * p.o_token + it.a;
+  float v[kHeads][E], w[kHeads][E];
+#pragma unroll
+  for (int k = 0; k < kHeads; ++k) {
+    const int h = min(h0 + k, p.heads - 1);
+    load_some<T>(x + h * p.d, it.n, v[k]);
+    if (it.pairs) load_some<T>(x + h * p.d + r.rot / 2, it.n, w[k]);
+  }
+  int32_t pos[3];
+  rope_positions(r, b, t, p.n, pos);
+  float c[E], s[E];
+  rope_item_angles<T>(r, it, pos, c, s);
+#pragma unroll
+  for (int k = 0; k < kHeads; ++k) {
+    if (h0 + k >= p.heads) break;
+    rope_turn<T>(r, it, c, s, v[k], w[k]);
+    store_some<T>(o + (h0 + k) * p.d, it.n, v[k]);
+    if (it.pairs) store_some<T>(o + (h0 + k) * p.d + r.rot / 2, it.n, w[k]);
+  }
+}
+
+template <typename T>
+hipError_t launch(RopeParams p, int B, hipStream_t s) {
+  p.n_items = rope_items<T>(p.table.layout, p.table.rot, p.d);
+  const int k = p.heads >= 4 && (int64_t)B * p.n * p.n_items * ((p.heads + 3) / 4) >= 65536 ? 4 : 1;
+  p.n_groups = (p.heads + k - 1) / k;
+  const int64_t threads = (int64_t)p.n * p.n_groups * p.n_items;
+  const dim3 grid((uint32_t)((threads + 255) / 256), B);
+  if (k == 4) rope_kernel<T, 4><<<grid, 256, 0, s>>>(p);
+  else rope_kernel<T, 1><<<grid, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope(int dtype, int B, const RopeParams& p, hipStream_t s) {
+  return dtype == HSA_DTYPE_BF16 ? launch<uint16_t>(p, B, s) : launch<float>(p, B, s);
+}
+
+bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, const int32_t* first, RopeTable& t) {
+  constexpr double kTau = 6.28318530717958647692;
+  if (r->rot_dim < 2 || r->rot_dim > d || r->rot_dim % 2) return false;
+  if (r->layout != HSA_ROPE_HALF && r->layout != HSA_ROPE_INTERLEAVED) return false;
+  if (r->axes < 1 || r->axes > 3 || (r->axes > 1 && !pos)) return false;
+  int dims[3] = {r->rot_dim, 0, 0}, sum = 0;
+  if (r->axes > 1)
+    for (int a = 0; a < r->axes; ++a) {
+      dims[a] = r->axis_dim[a];
+      if (dims[a] < 2 || dims[a] % 2 || dims[a] > r->rot_dim) return false;
+      sum += dims[a];
+    }
+  if (r->axes > 1 && sum != r->rot_dim) return false;
+  if (!(r->theta > 0.0) || isinf(r->theta) || !isfinite(r->amplitude)) return false;
+  if (r->scaling != HSA_ROPE_UNSCALED && (!(r->factor > 0.0) || isinf(r->factor))) return false;
+  if (r->scaling == HSA_ROPE_PARTS) {
+    if (!(r->low >= 0.0) || !(r->high > r->low) || isinf(r->high) || r->orig_len < 1) return false;
+  } else if (r->scaling != HSA_ROPE_UNSCALED && r->scaling != HSA_ROPE_LINEAR) {
+    return false;
+  }
+  int i = 0;
+  for (int a = 0; a < r->axes; ++a)
+    for (int k = 0; k < dims[a] / 2; ++k, ++i) {
+      double f = pow(r->theta, -2.0 * k / dims[a]);
+      if (r->scaling == HSA_ROPE_LINEAR) {
+        f /= r->factor;
+      } else if (r->scaling == HSA_ROPE_PARTS) {
+        const double turns = r->orig_len * f / kTau;
+        double w = (turns - r->low) / (r->high - r->low);
+        w = w < 0.0 ? 0.0 : (w > 1.0 ? 1.0 : w);
+        f = w * f + (1.0 - w) * f / r->factor;
+      }
+      if (!isfinite(f)) return false;
+      t.turns[i] = (inverse ? -f : f) / kTau;
+      t.axis[i] = (int8_t)a;
+    }
+  t.rot = r->rot_dim;
+  t.layout = r->layout;
+  t.axes = r->axes;
+  t.amplitude = r->amplitude == 0.0 ? 1.f : (float)r->amplitude;
+  t.pos = pos;
+  t.first = first;
+  return true;
+}
+
+}  // namespace hsa

@@ -41,6 +41,18 @@ class HsaKvPool(ctypes.Structure):
                 ("num_slots", c_i32), ("max_pages", c_i32)]
 
 
+class HsaRope(ctypes.Structure):
+    _fields_ = [("rot_dim", c_i32), ("layout", c_i32), ("axes", c_i32), ("axis_dim", c_i32 * 3),
+                ("scaling", c_i32), ("orig_len", c_i32), ("theta", ctypes.c_double),
+                ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("amplitude", ctypes.c_double)]
+
+
+class HsaCache8Pool(ctypes.Structure):
+    _fields_ = [("k", c_vp), ("v", c_vp), ("k_exp", c_vp), ("v_exp", c_vp), ("page_table", c_vp),
+                ("num_slots", c_i32), ("max_pages", c_i32), ("kv_heads", c_i32)]
+
+
 class HsaError(RuntimeError):
     def __init__(self, fn: str, status: int):
         super().__init__(f"{fn} failed: {STATUS.get(status, status)}")
@@ -160,6 +172,20 @@ def lib():
     L.hsa_forward_selected.restype = ctypes.c_int
     L.hsa_forward_selected.argtypes = [P(HsaConfig), c_vp, c_i32, P(HsaKvPool), c_vp, c_i32, c_vp,
                                        c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    c_i64 = ctypes.c_int64
+    L.hsa_rope_apply.restype = ctypes.c_int
+    L.hsa_rope_apply.argtypes = [P(HsaConfig), P(HsaRope), c_vp, c_i64, c_i64, c_i32, c_i32, c_vp, c_vp,
+                                 c_i32, c_vp, c_i64, c_i64, c_vp]
+    for n, pool in (("hsa_token_write", HsaKvPool), ("hsa_cache8_write", HsaCache8Pool)):
+        f = getattr(L, n)
+        f.restype = ctypes.c_int
+        f.argtypes = [P(HsaConfig), P(pool), P(HsaRope), c_vp, c_i64, c_i64, c_vp, c_i64, c_i64, c_i32,
+                      c_vp, c_vp, c_vp, c_vp]
+    L.hsa_cache8_attn_workspace_size.restype = c_sz
+    L.hsa_cache8_attn_workspace_size.argtypes = [P(HsaConfig), c_i32, c_i32, c_i32, c_i32]
+    L.hsa_cache8_attn.restype = ctypes.c_int
+    L.hsa_cache8_attn.argtypes = [P(HsaConfig), c_vp, c_i32, P(HsaCache8Pool), c_vp, c_i32, c_vp, c_i32,
+                                  c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
     _lib = L
     return L
 
@@ -177,7 +203,7 @@ def _ptr(t) -> Optional[int]:
 
 def _out(t, n: int, dtype: str, what: str) -> Optional[int]:
     """Pointer of an optional output of at least n elements of dtype
-    ('int32' or 'float64'), or None."""
+    ('int32', 'float32' or 'float64'), or None."""
     if t is None:
         return None
     if hasattr(t, "dtype") and str(t.dtype) != f"torch.{dtype}":
@@ -562,6 +588,166 @@ def hsa_forward_retrieval(cfg, q, n_q, pool, prompt_emb, chunk_emb, emb_dim, n_c
                                      0 if ws is None else ws.numel(), _stream(stream))
     if check:
         _check("hsa_forward_retrieval", st)
+    return st
+
+
+# ------------------------------------------------------------------ rotary positions, tokens, 8-bit cache
+CACHE8_BLOCK = 64  # tokens of a page that share a scale (HSA_CACHE8_BLOCK)
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "parts": 2}
+
+
+def rope(rot_dim: int, layout: str = "half", theta: float = 10000.0, axis_dims: Optional[Sequence[int]] = None,
+         scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 32.0, orig_len: int = 0,
+         amplitude: float = 1.0) -> HsaRope:
+    """Rotary positions (hsa_rope_t of include/hsa.h): the first rot_dim dims of
+    a head in pairs (i, i + rot_dim/2) ("half") or (2i, 2i+1) ("interleaved").
+    axis_dims: dims of each of 2 or 3 position axes. scaling: "none", "linear"
+    (every frequency / factor) or "parts" (only those that turn fewer than `high`
+    times over orig_len, wholly below `low`). amplitude multiplies the result."""
+    if layout not in _LAYOUTS or scaling not in _SCALINGS:
+        raise ValueError(f"unknown layout {layout!r} or scaling {scaling!r}")
+    dims = [int(x) for x in axis_dims] if axis_dims is not None else [int(rot_dim)]
+    if not 1 <= len(dims) <= 3 or sum(dims) != rot_dim:
+        raise ValueError(f"axis_dims {dims} must be 1 to 3 numbers that sum to rot_dim = {rot_dim}")
+    return HsaRope(rot_dim, _LAYOUTS[layout], len(dims), (c_i32 * 3)(*(dims + [0, 0])[:3]), _SCALINGS[scaling],
+                   orig_len, theta, factor, low, high, amplitude)
+
+
+def cache8_pool(k, v, k_exp, v_exp, page_table, cfg: HsaConfig) -> HsaCache8Pool:
+    """The 8-bit cache's descriptor after checking its tensors: k [slots, Hk, P, d],
+    v [slots, Hk, d, P], k_exp and v_exp [slots, Hk, ceil(P / 64)] uint8,
+    page_table [B, max_pages] int32."""
+    slots, kv = int(k.shape[0]), int(k.shape[1])
+    P, d = cfg.page_size, cfg.head_dim
+    nb = -(-P // CACHE8_BLOCK)
+    for name, t, shape in (("k", k, (slots, kv, P, d)), ("v", v, (slots, kv, d, P)),
+                           ("k_exp", k_exp, (slots, kv, nb)), ("v_exp", v_exp, (slots, kv, nb))):
+        if tuple(t.shape) != shape or str(t.dtype) != "torch.uint8":
+            raise ValueError(f"{name} must be torch.uint8 {shape}, got {t.dtype} {tuple(t.shape)}")
+    if page_table.dim() != 2 or page_table.shape[0] != cfg.batch or str(page_table.dtype) != "torch.int32":
+        raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "
+                         f"{page_table.dtype} {tuple(page_table.shape)}")
+    return HsaCache8Pool(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), _ptr(page_table), slots,
+                         int(page_table.shape[-1]), kv)
+
+
+def _i32s(t, n: int, what: str) -> Optional[int]:
+    """Pointer of an int32 tensor of n elements, or None."""
+    if t is None:
+        return None
+    if hasattr(t, "dtype") and (str(t.dtype) != "torch.int32" or t.numel() != n):
+        raise ValueError(f"{what} must hold {n} int32 values, got {tuple(t.shape)} {t.dtype}")
+    return _ptr(t)
+
+
+def _strided(cfg, t, n: int, heads: int, what: str):
+    """(pointer, batch stride, token stride) of a [B, n, heads, d] tensor whose
+    heads are contiguous within a token."""
+    if tuple(t.shape) != (cfg.batch, n, heads, cfg.head_dim) or str(t.dtype) != _elem_dtype(cfg):
+        raise ValueError(f"{what} must be {_elem_dtype(cfg)} {(cfg.batch, n, heads, cfg.head_dim)}, got "
+                         f"{t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if t.numel() and (st[3] != 1 or (heads > 1 and st[2] != cfg.head_dim)):
+        raise ValueError(f"{what}: the heads of a token must be contiguous, got strides {st}")
+    return t.data_ptr(), st[0], st[1]
+
+
+def _one_device(*tensors):
+    """The device of the tensors among the arguments (None and addresses skipped)."""
+    dev = None
+    for t in tensors:
+        d = getattr(t, "device", None)
+        if d is None:
+            continue
+        if dev is None:
+            dev = d
+        elif d != dev:
+            raise ValueError(f"tensors on {dev} and {d}")
+    return dev
+
+
+def _call(fn, dev, stream, *args) -> int:
+    """fn(*args, stream) with the tensors' device current (kernels launch there)."""
+    import torch
+    if dev is None or dev.type != "cuda" or dev.index == torch.cuda.current_device():
+        return fn(*args, _stream(stream))
+    with torch.cuda.device(dev):
+        return fn(*args, _stream(stream))
+
+
+def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None,
+                   check=True) -> int:
+    """Turns x [B, n, heads, d] by its tokens' positions (pos int32 [B, n, axes], or
+    first int32 [B] + the token's index) into o (x itself, or apart from it).
+    inverse: by the opposite angles, the gradient's map."""
+    heads = int(x.shape[2]) if x.dim() == 4 else 0
+    xp, xb, xt = _strided(cfg, x, n, heads, "x")
+    op, ob, ot = _strided(cfg, o, n, heads, "o")
+    dev = _one_device(x, o, pos, first)
+    st = _call(lib().hsa_rope_apply, dev, stream, ctypes.byref(cfg), ctypes.byref(rope), xp, xb, xt, n, heads,
+               _i32s(pos, cfg.batch * n * rope.axes, "pos"), _i32s(first, cfg.batch, "first"),
+               int(bool(inverse)), op, ob, ot)
+    if check:
+        _check("hsa_rope_apply", st)
+    return st
+
+
+def _token_write(name, cfg, pool, heads, k_src, v_src, n, rope, pos, first, count, stream, check) -> int:
+    kp, kb, kt = _strided(cfg, k_src, n, heads, "k_src")
+    vp, vb, vt = _strided(cfg, v_src, n, heads, "v_src")
+    dev = _one_device(k_src, v_src, pos, first, count)
+    st = _call(getattr(lib(), name), dev, stream, ctypes.byref(cfg), ctypes.byref(pool),
+               None if rope is None else ctypes.byref(rope), kp, kb, kt, vp, vb, vt, n,
+               None if rope is None else _i32s(pos, cfg.batch * n * rope.axes, "pos"),
+               _i32s(first, cfg.batch, "first"), _i32s(count, cfg.batch, "count"))
+    if check:
+        _check(name, st)
+    return st
+
+
+def hsa_token_write(cfg, pool, k_src, v_src, n, first=None, count=None, rope=None, pos=None, stream=None,
+                    check=True) -> int:
+    """Append tokens: k_src / v_src [B, n, H, d] become tokens first[b] + i, i <
+    count[b], of each sequence in the pool, keys turned by rope on the way."""
+    return _token_write("hsa_token_write", cfg, pool, cfg.num_heads, k_src, v_src, n, rope, pos, first, count,
+                        stream, check)
+
+
+def hsa_cache8_write(cfg, cache, k_src, v_src, n, first=None, count=None, rope=None, pos=None, stream=None,
+                     check=True) -> int:
+    """hsa_token_write into the 8-bit cache: k_src / v_src [B, n, kv_heads, d]."""
+    return _token_write("hsa_cache8_write", cfg, cache, cache.kv_heads, k_src, v_src, n, rope, pos, first, count,
+                        stream, check)
+
+
+def hsa_cache8_attn_workspace_size(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int) -> int:
+    return lib().hsa_cache8_attn_workspace_size(ctypes.byref(cfg), n_q, kv_heads, k_max, n_cur_pages)
+
+
+def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, kv_len=None,
+                    q_len=None, causal=False, ws=None, stream=None, check=True) -> int:
+    """Attention of q [B, n_q, H, d] over the 8-bit cache's listed pages: sel int32 [B,
+    kv_heads, k_max], then [cur_first_page, + n_cur_pages); tokens below kv_len[b]."""
+    qp, op = _rows(cfg, q, n_q, "q"), _rows(cfg, o, n_q, "o")
+    lp = None if lse is None else _out(lse, cfg.batch * cfg.num_heads * n_q, "float32", "lse")
+    sp = _i32s(sel, cfg.batch * cache.kv_heads * k_max, "sel")
+    kvp, qlp = _i32s(kv_len, cfg.batch, "kv_len"), _i32s(q_len, cfg.batch, "q_len")
+    if k_h is not None and len(k_h) != cache.kv_heads:
+        raise ValueError(f"k_h must hold {cache.kv_heads} budgets, got {len(k_h)}")
+    dev = _one_device(q, o, lse, sel, kv_len, q_len, ws)
+    if ws is None:
+        ws = _workspace(hsa_cache8_attn_workspace_size(cfg, n_q, cache.kv_heads, k_max, n_cur_pages), q.device)
+        if ws is not None and stream is not None:  # not reused before that stream is done with it
+            import torch
+            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else
+                             torch.cuda.ExternalStream(int(stream), device=q.device))
+    _keep, kp = _budgets(k_h)
+    st = _call(lib().hsa_cache8_attn, dev, stream, ctypes.byref(cfg), qp, n_q, ctypes.byref(cache), sp, k_max, kp,
+               cur_first_page, n_cur_pages, kvp, qlp, int(bool(causal)), op, lp, _ptr(ws),
+               0 if ws is None else ws.numel())
+    if check:
+        _check("hsa_cache8_attn", st)
     return st
 
 

@@ -78,6 +78,12 @@ class HsaLayer:
         _h.hsa_state_update(self.cfg, self.pool, first_page, n_pages, self.kv_state,
                             self.k_state, self.page_kmean, ws=ws, stream=stream)
 
+    def write_tokens(self, k, v, first=None, count=None, rope=None, pos=None, stream=None):
+        """Append tokens: k, v [B, n, H, d] become tokens first[b] + i, i < count[b],
+        of each sequence (int32 [B]; default 0 and n), keys turned by rope."""
+        _h.hsa_token_write(self.cfg, self.pool, k, v, k.shape[1], first=first, count=count, rope=rope, pos=pos,
+                           stream=stream)
+
     def forward(self, q, n_cand: int, n_cur: int, k_h: Sequence[int], k_max: Optional[int] = None,
                 g_lin=None, g_sp=None, out=None, sel_out=None, stream=None):
         B, n_q = q.shape[0], q.shape[1]
@@ -133,4 +139,62 @@ class HsaLayer:
                                  n_cur, k_h, k_max, self.page_kmean, g_lin, g_sp, out,
                                  tau_min=tau_min, tau_max=tau_max, sel_out=sel_out, ws=ws,
                                  stream=stream)
+        return out
+
+
+class HsaCache8:
+    """Paged 8-bit KV cache of one layer: e4m3 codes k [slots, Hk, P, d] and v
+    [slots, Hk, d, P], exponent bytes of the scales of 64-token blocks k_exp, v_exp [slots,
+    Hk, ceil(P / 64)], page_table [B, max_pages]; tensors not given are allocated. The tensors stay
+    the same over the cache's life (fill the page table in place). ``heads`` are the query heads,
+    kv_heads (default: as many) the cached ones. rope turns the keys that are
+    written and the queries given to ``rotate``.
+    """
+
+    def __init__(self, batch: int, heads: int, head_dim: int, page_size: int, dtype, device,
+                 kv_heads: Optional[int] = None, k=None, v=None, k_exp=None, v_exp=None, page_table=None,
+                 num_slots: int = 0, max_pages: int = 0, sm_scale: float = 0.0, rope=None):
+        import torch
+        self.torch = torch
+        self.device = torch.device(device)
+        self.cfg = _h.config(batch, heads, head_dim, page_size, dtype, sm_scale)
+        kv = heads if kv_heads is None else kv_heads
+        nb = -(-page_size // _h.CACHE8_BLOCK)
+        u8 = dict(dtype=torch.uint8, device=device)
+        if k is None:
+            k = torch.empty((num_slots, kv, page_size, head_dim), **u8)
+            v = torch.empty((num_slots, kv, head_dim, page_size), **u8)
+            k_exp, v_exp = torch.empty((num_slots, kv, nb), **u8), torch.empty((num_slots, kv, nb), **u8)
+        if page_table is None:
+            page_table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
+        if int(k.shape[1]) != kv:
+            raise ValueError(f"k must hold {kv} heads, got {tuple(k.shape)}")
+        _h._one_device(k, v, k_exp, v_exp, page_table)
+        self.k, self.v, self.k_exp, self.v_exp, self.page_table = k, v, k_exp, v_exp, page_table
+        self.rope = rope
+        self.pool = _h.cache8_pool(k, v, k_exp, v_exp, page_table, self.cfg)
+
+    def rotate(self, q, pos=None, first=None, out=None, inverse: bool = False, stream=None):
+        """q [B, n, heads, d] turned by its tokens' positions."""
+        if out is None:
+            out = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _h.hsa_rope_apply(self.cfg, self.rope, q, q.shape[1], out, pos=pos, first=first, inverse=inverse,
+                          stream=stream)
+        return out
+
+    def write(self, k, v, first=None, count=None, pos=None, stream=None):
+        """Append tokens: k, v [B, n, kv_heads, d] become tokens first[b] + i, i <
+        count[b], of each sequence (int32 [B]; default 0 and n)."""
+        _h.hsa_cache8_write(self.cfg, self.pool, k, v, k.shape[1], first=first, count=count, rope=self.rope, pos=pos,
+                            stream=stream)
+
+    def attend(self, q, n_pages: int, first_page: int = 0, sel=None, k_h: Optional[Sequence[int]] = None, kv_len=None,
+               q_len=None, causal: bool = False, out=None, lse=None, stream=None):
+        """Attention of q [B, n_q, heads, d] over the selected pages (sel int32 [B,
+        kv_heads, k_max], at most k_h of each head) and pages [first_page, + n_pages)."""
+        if out is None:
+            out = self.torch.empty_like(q)
+        _h.hsa_cache8_attn(self.cfg, q, q.shape[1], self.pool, sel, 0 if sel is None else int(sel.shape[-1]), k_h,
+                           first_page, n_pages, out, lse=lse, kv_len=kv_len, q_len=q_len, causal=causal,
+                           stream=stream)
         return out

@@ -1,0 +1,267 @@
+"""Token appends, to the pool in its own type and to the 8-bit cache, against the
+fp64 oracle.
+
+Values and unrotated keys are copied or rounded once from what they are:
+equal to the oracle's codes and exponents. A rotated key is off by up to 8 * 2^-24 (|a| +
+|b|) before its rounding (see test_gpu_rope.py): its code is then within half a
+step (2^-4 of the number, or 2^-10 below the smallest normal one) plus that.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34606_amd as P
+from oracle import hsa_cache8_oracle as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def source(seed, B, n, H, d, dt, fused, spread=0.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((B, n, 2, H, d), generator=g) * torch.exp(spread * torch.randn((B, n, 2, H, 1), generator=g))
+    x = x.to(dt).to(DEV)
+    k, v = x[:, :, 0], x[:, :, 1]
+    return (k, v) if fused else (k.contiguous(), v.contiguous())
+
+
+def host(x):
+    return x.cpu().double().numpy()
+
+
+def table(seed, B, pages, extra=2):
+    g = np.random.default_rng(seed)
+    slots = g.permutation(B * pages + extra)[:B * pages].reshape(B, pages).astype(np.int32)
+    return slots, B * pages + extra
+
+
+def cache(seed, B, H, d, P_, dt, pages, rope=None, kv=None, garbage=True):
+    pt, slots = table(seed, B, pages)
+    c = P.HsaCache8(B, H, d, P_, dt, DEV, kv_heads=kv, num_slots=slots, max_pages=pages, rope=rope)
+    c.page_table.copy_(torch.from_numpy(pt))
+    if garbage:  # whatever memory holds: every code, NaN too
+        g = torch.Generator().manual_seed(seed)
+        for t in (c.k, c.v, c.k_exp, c.v_exp):
+            t.copy_(torch.randint(0, 256, t.shape, generator=g, dtype=torch.uint8))
+    return c, pt
+
+
+def arrays(c):
+    return {n: getattr(c, n).cpu().numpy().copy() for n in ("k", "v", "k_exp", "v_exp")}
+
+
+def one_nan(codes):
+    """Codes with one NaN: 0x7f and 0xff both stand for it."""
+    return np.where((codes & 127) == 127, 127, codes)
+
+
+def same(c, want, keys_too=True):
+    got = arrays(c)
+    for n in ("v_exp", "k_exp"):
+        assert np.array_equal(got[n], want[n]), n
+    for n in ("v", "k") if keys_too else ("v",):
+        assert np.array_equal(one_nan(got[n]), one_nan(want[n])), n
+
+
+def check_keys(c, want, exact, size):
+    """Written key codes within their bound, all others as they were."""
+    got = arrays(c)["k"]
+    wrote = ~np.isnan(exact["k"])
+    assert np.array_equal(got[~wrote], want["k"][~wrote])
+    x = exact["k"][wrote]
+    bound = np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10) + 8 * 2.0 ** -24 * size
+    assert (np.abs(O.decode(got[wrote]) - x) <= bound).all()
+    # and nearly all of them the oracle's own
+    assert np.mean(got[wrote] != want["k"][wrote]) < 1e-4
+
+
+# ---------------------------------------------------------------- pool
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P_,n,first,count,fused", [
+    (8, 1, [0, 17], [1, 1], False),
+    (64, 70, [61, 0], [70, 3], True),
+    (72, 200, [5, 71], [200, 133], True),
+    (200, 33, [180, 199], [33, 0], False),
+    (392, 777, [3, 391], [777, 390], True),
+])
+def test_pool_append(dt, d, P_, n, first, count, fused):
+    print(dt, d, P_, n, first, count, flush=True)
+    B, H = 2, 3
+    pages = (max(first) + n) // P_ + 2
+    pt, slots = table(n, B, pages)
+    layer = P.HsaLayer(B, H, d, P_, dt, DEV, num_slots=slots, max_pages=pages)
+    layer.page_table.copy_(torch.from_numpy(pt))
+    g = torch.Generator().manual_seed(1)
+    layer.k_pool.copy_(torch.randn(layer.k_pool.shape, generator=g))
+    layer.v_pool.copy_(torch.randn(layer.v_pool.shape, generator=g))
+    k, v = source(n, B, n, H, d, dt, fused)
+    wk, wv = host(layer.k_pool), host(layer.v_pool)
+    layer.write_tokens(k, v, i32(first), count=i32(count))
+    O.write_tokens(wk, wv, pt, host(k), host(v), first, count)
+    assert np.array_equal(host(layer.k_pool), wk) and np.array_equal(host(layer.v_pool), wv)
+    # rotated: the keys within their rounding, the values as before
+    rope = P.rope(d // 2 + 10, layout="interleaved" if d == 64 else "half")
+    pos = O.places(first, n)
+    kw = dict(rot=d // 2 + 10, layout="interleaved" if d == 64 else "half")
+    turned = O.rope(host(k), pos, **kw)
+    layer.write_tokens(k, v, i32(first), count=i32(count), rope=rope)
+    O.write_tokens(wk, wv, pt, turned, host(v), first, count)
+    eps = 2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -24
+    big = float(k.abs().max())
+    assert (np.abs(host(layer.k_pool) - wk) <= eps * np.abs(wk) + 16 * 2.0 ** -24 * big).all()
+    assert np.array_equal(host(layer.v_pool), wv)
+
+
+def test_pool_append_equals_page_write():
+    """Whole pages: the two appends leave the same bits."""
+    B, H, d, P_, n_pages = 2, 5, 128, 104, 3
+    pt, slots = table(3, B, 5)
+    layers = [P.HsaLayer(B, H, d, P_, torch.bfloat16, DEV, num_slots=slots, max_pages=5) for _ in range(2)]
+    k, v = source(8, B, n_pages * P_, H, d, torch.bfloat16, False)
+    for la in layers:
+        la.page_table.copy_(torch.from_numpy(pt))
+        la.k_pool.zero_()
+        la.v_pool.zero_()
+    layers[0].write_tokens(k, v, i32([P_, P_]))
+    P.hsa_page_write(layers[1].cfg, layers[1].pool, k, v, 1, n_pages)
+    assert torch.equal(layers[0].k_pool, layers[1].k_pool) and torch.equal(layers[0].v_pool, layers[1].v_pool)
+
+
+# ---------------------------------------------------------------- 8-bit cache
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P_,n,first,count,fused", [
+    (8, 1, [0, 17], [1, 1], False),
+    (16, 50, [3, 16], [50, 31], True),
+    (64, 70, [61, 0], [70, 3], True),
+    (72, 200, [5, 71], [200, 133], False),
+    (200, 33, [180, 199], [33, 0], True),
+    (392, 777, [3, 391], [777, 390], True),
+])
+def test_cache8_append(dt, d, P_, n, first, count, fused):
+    print(dt, d, P_, n, first, count, flush=True)
+    B, H = 2, 3
+    c, pt = cache(n + P_, B, H, d, P_, dt, (max(first) + n) // P_ + 2)
+    # the blocks that the append continues hold tokens of an earlier one
+    for b, f in enumerate(first):
+        if f:
+            k, v = source(b, B, f, H, d, dt, False, 1.0)
+            c.write(k, v, count=i32([f if i == b else 0 for i in range(B)]))
+    want = arrays(c)
+    k, v = source(n, B, n, H, d, dt, fused, 1.0)
+    c.write(k, v, i32(first), count=i32(count))
+    O.write8(want, pt, host(k), host(v), first, count)
+    same(c, want)
+
+
+@pytest.mark.parametrize("layout,rot,axes", [("half", 128, None), ("interleaved", 128, [44, 42, 42]), ("half", 90, None),
+                                             ("interleaved", 70, None)])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_cache8_append_rotated(dt, layout, rot, axes):
+    B, H, d, P_, n = 2, 3, 128, 200, 311
+    first, count = [37, 0], [311, 290]
+    c, pt = cache(5, B, H, d, P_, dt, 3, rope=P.rope(rot, layout=layout, axis_dims=axes))
+    k, v = source(6, B, 37, H, d, dt, False)
+    c.write(k, v, count=i32([37, 0]), pos=torch.zeros((B, 37, 3), dtype=torch.int32, device=DEV) if axes else None)
+    want = arrays(c)
+    k, v = source(7, B, n, H, d, dt, True)
+    pos = None
+    where = O.places(first, n)
+    if axes:
+        g = torch.Generator().manual_seed(3)
+        pos = torch.randint(0, 200, (B, n, 3), generator=g).to(torch.int32)
+        where, pos = pos.numpy().astype(np.int64), pos.to(DEV)
+    c.write(k, v, i32(first), count=i32(count), pos=pos)
+    turned = O.rope(host(k), where, rot, layout, axis_dims=axes)
+    exact = O.write8(want, pt, turned, host(v), first, count)
+    same(c, want, keys_too=False)
+    check_keys(c, want, exact, 448.0 * 2)  # |a| + |b| in units of the scale
+
+
+def test_cache8_single_tokens_grow_the_scale():
+    """Tokens one at a time, each up to 2^12 times the ones before: older codes are
+    scaled down, some to subnormals and zero."""
+    B, H, d, P_ = 3, 2, 64, 80
+    for dt in (torch.bfloat16, torch.float32):
+        c, pt = cache(11, B, H, d, P_, dt, 3)
+        want = arrays(c)
+        g = np.random.default_rng(4)
+        for t in range(90):
+            k, v = source(100 + t, B, 1, H, d, dt, False)
+            scale = torch.from_numpy(2.0 ** g.integers(-6, 6, (B, 1, H, 1)) * (2.0 ** 12 if t % 23 == 20 else 1.0)).to(DEV)
+            k, v = (k * scale).to(dt), (v * scale.flip(0)).to(dt)
+            at = [t, max(0, t - 50), 40 + t]
+            count = [1, int(t >= 50), int(t < 60)]
+            c.write(k, v, i32(at), count=i32(count))
+            O.write8(want, pt, host(k), host(v), at, count)
+        same(c, want)
+
+
+def test_cache8_special_values():
+    """Zeros, infinities and NaN, tiny and huge numbers."""
+    B, H, d, P_ = 1, 2, 64, 128
+    c, pt = cache(12, B, H, d, P_, torch.float32, 2)
+    want = arrays(c)
+    k, v = source(13, B, 200, H, d, torch.float32, False)
+    k[:, :64] = 0.0
+    k[0, 70, 0, 3], k[0, 71, 1, 5], k[0, 80, 0, 9] = float("inf"), float("-inf"), float("nan")
+    v[0, 5, 0, 3], v[0, 6, 0, 60], v[0, 7, 1, 0] = float("-inf"), float("nan"), float("inf")
+    k[:, 128:] *= 1e-37
+    v[:, 128:] *= 1e37
+    v[:, 64:128] *= 2.0 ** -120
+    c.write(k, v)
+    O.write8(want, pt, host(k), host(v), [0], [200])
+    same(c, want)
+
+
+def test_cache8_tokens_outside_the_table_are_dropped():
+    B, H, d, P_ = 3, 2, 64, 40
+    c, pt = cache(14, B, H, d, P_, torch.bfloat16, 2)
+    want = arrays(c)
+    k, v = source(15, B, 30, H, d, torch.bfloat16, False)
+    first, count = [-10, 70, 200], [30, 30, 30]
+    c.write(k, v, i32(first), count=i32(count))
+    O.write8(want, pt, host(k), host(v), first, count)
+    same(c, want)
+
+
+def test_rewriting_the_same_tokens_is_idempotent():
+    B, H, d, P_ = 1, 3, 128, 256
+    c, pt = cache(16, B, H, d, P_, torch.bfloat16, 2, rope=P.rope(128))
+    k, v = source(17, B, 100, H, d, torch.bfloat16, False)
+    c.write(k, v, i32([0]))
+    k2, v2 = source(18, B, 90, H, d, torch.bfloat16, False, 1.0)
+    c.write(k2, v2, i32([100]))
+    once = arrays(c)
+    c.write(k2, v2, i32([100]))
+    same(c, once)
+
+
+def test_captured_appends_follow_their_lengths():
+    """A captured step of one token, replayed: each replay reads first from the
+    device; other work and synchronisations in between."""
+    B, H, d, P_ = 2, 2, 64, 24
+    c, pt = cache(19, B, H, d, P_, torch.bfloat16, 3, rope=P.rope(64))
+    e, _ = cache(19, B, H, d, P_, torch.bfloat16, 3, rope=P.rope(64))
+    layer = P.HsaLayer(B, H, d, P_, torch.bfloat16, DEV, num_slots=8, max_pages=3, page_table=c.page_table)
+    layer.k_pool.zero_(), layer.v_pool.zero_()
+    eager = P.HsaLayer(B, H, d, P_, torch.bfloat16, DEV, num_slots=8, max_pages=3, page_table=c.page_table)
+    eager.k_pool.zero_(), eager.v_pool.zero_()
+    first = i32([0, 10])
+    k, v = source(20, B, 1, H, d, torch.bfloat16, False)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.write(k, v, first)
+        layer.write_tokens(k, v, first, rope=c.rope)
+    for t in range(30):
+        k2, v2 = source(30 + t, B, 1, H, d, torch.bfloat16, False)
+        k.copy_(k2), v.copy_(v2)
+        first.copy_(torch.tensor([t, 10 + t]))
+        graph.replay()
+        e.write(k2, v2, first)
+        eager.write_tokens(k2, v2, first, rope=c.rope)
+        torch.cuda.synchronize()
+        same(c, arrays(e))
+        assert torch.equal(layer.k_pool, eager.k_pool) and torch.equal(layer.v_pool, eager.v_pool)
