@@ -177,7 +177,7 @@ int cube_order(int T, int H, int W, int ct, int ch, int cw, int32_t* src_of);
 
 // ------------------------------------------------------------ rotary positions
 struct RopeTable {
-  double turns[64];         // turns (of 2 pi) per position of each pair, negative for the inverse
+  double quarters[64];      // quarter turns per position of each pair, negative for the inverse
   int8_t axis[64];          // which position of the token turns the pair
   int32_t rot, layout, axes;  // rot = 0: nothing turns
   float amplitude;
@@ -212,6 +212,7 @@ struct TokenWriteParams {
   const int32_t* first;       // [B] nullable
   const int32_t* count;       // [B] nullable
   int32_t H, P, n, num_slots, max_pages;
+  int32_t item_shift;         // set by the launch: 2^this threads share a token's key row
 };
 
 int64_t token_write_units(int64_t n, int P);

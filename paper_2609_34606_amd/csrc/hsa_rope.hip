@@ -3,7 +3,7 @@
 //
 // Every element is read and written once, so the launch is bound by memory (by
 // its own latency for few tokens). The angle's cosine and sine cost about 35 instructions
-// a pair; a thread computes those of one item (up to E pairs of a token) once and
+// a pair; a thread computes those of one item (rope_mode) of a token once and
 // applies them to kHeads heads, whose loads are in flight together. Neighbouring
 // lanes take neighbouring 16-byte pieces of a head.
 #include <math.h>
@@ -13,55 +13,60 @@
 namespace hsa {
 namespace {
 
-template <typename T, int kHeads>
+template <typename T, int kMode, int kHeads>
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
-  constexpr int E = Pack<T>::E;
+  using Item = RopeItem<T, kMode>;
   const RopeTable& r = p.table;
   const uint32_t id = blockIdx.x * 256u + threadIdx.x;
   const uint32_t row = id / p.n_items;                 // (token, head group)
-  const int j = (int)(id - row * p.n_items);
   const uint32_t tok = row / p.n_groups;
   if (tok >= (uint32_t)p.n) return;
   const int t = (int)tok, h0 = (int)(row - tok * p.n_groups) * kHeads, b = blockIdx.y;
-  const RopeItem it = rope_item<T>(r.layout, r.rot, p.d, j);
-  const T* x = static_cast<const T*>(p.x) + (int64_t)b * p.x_batch + (int64_t)t * p.x_token + it.a;
-  T* o = static_cast<T*>(p.o) + (int64_t)b * p.o_batch + (int64_t)t * p.o_token + it.a;
-  float v[kHeads][E], w[kHeads][E];
+  Item it;
+  it.set(r, (int)(id - row * p.n_items));
+  const T* x = static_cast<const T*>(p.x) + (int64_t)b * p.x_batch + (int64_t)t * p.x_token;
+  T* o = static_cast<T*>(p.o) + (int64_t)b * p.o_batch + (int64_t)t * p.o_token;
+  typename Item::El::Raw ra[kHeads], rb[kHeads];
+#pragma unroll
+  for (int k = 0; k < kHeads; ++k) it.load(x + min(h0 + k, p.heads - 1) * p.d, ra[k], rb[k]);
+  it.frequencies(r);
+  float c[Item::NP], s[Item::NP];
+  it.angles(r, rope_positions(r, b, t, p.n), c, s);
 #pragma unroll
   for (int k = 0; k < kHeads; ++k) {
-    const int h = min(h0 + k, p.heads - 1);
-    load_some<T>(x + h * p.d, it.n, v[k]);
-    if (it.pairs) load_some<T>(x + h * p.d + r.rot / 2, it.n, w[k]);
-  }
-  int32_t pos[3];
-  rope_positions(r, b, t, p.n, pos);
-  float c[E], s[E];
-  rope_item_angles<T>(r, it, pos, c, s);
-#pragma unroll
-  for (int k = 0; k < kHeads; ++k) {
-    if (h0 + k >= p.heads) break;
-    rope_turn<T>(r, it, c, s, v[k], w[k]);
-    store_some<T>(o + (h0 + k) * p.d, it.n, v[k]);
-    if (it.pairs) store_some<T>(o + (h0 + k) * p.d + r.rot / 2, it.n, w[k]);
+    if (h0 + k < p.heads) {
+      float u[Item::N], v[Item::N];
+      it.result(ra[k], rb[k], c, s, u, v);
+      it.store(o + (h0 + k) * p.d, u, v);
+    }
   }
 }
 
-template <typename T>
+template <typename T, int kMode>
 hipError_t launch(RopeParams p, int B, hipStream_t s) {
-  p.n_items = rope_items<T>(p.table.layout, p.table.rot, p.d);
+  p.n_items = RopeItem<T, kMode>::count(p.table.rot, p.d);
   const int k = p.heads >= 4 && (int64_t)B * p.n * p.n_items * ((p.heads + 3) / 4) >= 65536 ? 4 : 1;
   p.n_groups = (p.heads + k - 1) / k;
   const int64_t threads = (int64_t)p.n * p.n_groups * p.n_items;
   const dim3 grid((uint32_t)((threads + 255) / 256), B);
-  if (k == 4) rope_kernel<T, 4><<<grid, 256, 0, s>>>(p);
-  else rope_kernel<T, 1><<<grid, 256, 0, s>>>(p);
+  if (k == 4) rope_kernel<T, kMode, 4><<<grid, 256, 0, s>>>(p);
+  else rope_kernel<T, kMode, 1><<<grid, 256, 0, s>>>(p);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_as(const RopeParams& p, int B, hipStream_t s) {
+  switch (rope_mode<T>(p.table)) {
+    case kRopeHalves: return launch<T, kRopeHalves>(p, B, s);
+    case kRopeInterleaved: return launch<T, kRopeInterleaved>(p, B, s);
+    default: return launch<T, kRopeSingle>(p, B, s);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_rope(int dtype, int B, const RopeParams& p, hipStream_t s) {
-  return dtype == HSA_DTYPE_BF16 ? launch<uint16_t>(p, B, s) : launch<float>(p, B, s);
+  return dtype == HSA_DTYPE_BF16 ? launch_as<uint16_t>(p, B, s) : launch_as<float>(p, B, s);
 }
 
 bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, const int32_t* first, RopeTable& t) {
@@ -97,7 +102,7 @@ bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, co
         f = w * f + (1.0 - w) * f / r->factor;
       }
       if (!isfinite(f)) return false;
-      t.turns[i] = (inverse ? -f : f) / kTau;
+      t.quarters[i] = 4.0 * (inverse ? -f : f) / kTau;
       t.axis[i] = (int8_t)a;
     }
   t.rot = r->rot_dim;

@@ -3,9 +3,8 @@
 // position on the way: into the pool in its own type, or into the 8-bit cache.
 //
 // A workgroup takes one block of up to 64 tokens of a page (the tokens that share
-// a scale) of one head: its keys turn in registers, its values are transposed through LDS into
-// the d-major rows. For the 8-bit cache the turned keys wait in LDS in fp32 for the block's
-// largest magnitude. A block that holds older tokens keeps its scale or
+// a scale) of one head: its keys turn in registers, where they wait for the block's largest
+// magnitude, its values are transposed through LDS into the d-major rows. A block that holds older tokens keeps its scale or
 // grows it by a power of two; then, and only then, the older codes are read and
 // written again (exact unless they become subnormal).
 // Bound: HBM (the step's tokens read once, the codes written once); few
@@ -24,27 +23,28 @@ __device__ __forceinline__ float finite_max(float m, float x) {
   return x < INFINITY ? fmaxf(m, x) : m;
 }
 
-template <typename T>
-struct Vec16u;
-template <>
-struct Vec16u<uint16_t> {
-  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
-};
-template <>
-struct Vec16u<float> {
-  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
-};
+// N codes of x in units of 1 / inv.
+template <int N>
+__device__ __forceinline__ void store_codes(uint8_t* p, const float (&x)[N], float inv) {
+  if constexpr (N == 1) {
+    *p = (uint8_t)codes4(x[0] * inv, 0.f, 0.f, 0.f);
+  } else {
+    uint32_t* w = reinterpret_cast<uint32_t*>(p);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      w[i] = codes4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+  }
+}
 
-template <typename T, int D, bool kEight>
+template <typename T, int D, bool kEight, int kMode>
 __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
-  using V16 = typename Vec16u<T>::type;
-  constexpr int E = Pack<T>::E;
+  using V16 = typename Vec16<T>::type;
+  using Item = RopeItem<T, kMode>;
+  constexpr int E = 16 / (int)sizeof(T);
   constexpr int CPR = D / E;                      // 16-byte chunks per token
   constexpr int NLD = kTok * CPR / 256;           // value chunks per thread
   constexpr int RW = D * (int)sizeof(T) / 4 + 1;  // dwords per value row: one more than d, so that rows fall on their own banks
-  constexpr int KS = D + 4;                       // floats per key row
   __shared__ uint32_t vs[kTok * RW];
-  __shared__ __attribute__((aligned(16))) float ks[kEight ? kTok * KS : 4];
   __shared__ float amax[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int unit = blockIdx.x / p.H, h = blockIdx.x % p.H, b = blockIdx.y;
@@ -86,50 +86,56 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
     const int t = min((tid + 256 * l) / CPR, ntok - 1);
     v[l] = *reinterpret_cast<const V16*>(vsrc + (int64_t)t * p.v_token + tid % CPR * E);
   }
-  // keys: two items (rope_items) at a time
+  // keys: a thread has one item (RopeItem) of every 256 >> item_shift tokens; its turned
+  // elements stay in registers until the block's scale is known
   float mk = 0.f, mv = 0.f;
   const RopeTable& r = p.table;
-  const int n_items = rope_items<T>(r.layout, r.rot, D);
+  const int step = 256 >> p.item_shift;
+  const int j = tid & ((1 << p.item_shift) - 1), tk = tid >> p.item_shift;
+  Item it;
+  it.set(r, j);
+  const bool mine = j < Item::count(r.rot, D);
   T* kdst = static_cast<T*>(p.k) + (head * p.P + boff) * D;
-  for (int x0 = tid; x0 < ntok * n_items; x0 += 512) {
-    RopeItem it[2];
-    int t[2];
-    float a[2][E], w[2][E];
+  constexpr int NK = kMode == kRopeSingle ? 1 : kTok * D / E / 256;
+  float ku[NK][Item::N], kw[NK][Item::N];
+  auto turned = [&](int t, const typename Item::El::Raw& ra, const typename Item::El::Raw& rb, float (&u)[Item::N],
+                    float (&w)[Item::N]) {
+    float cs[Item::NP], sn[Item::NP];
+    it.angles(r, rope_positions(r, b, i0 + t, p.n), cs, sn);
+    it.result(ra, rb, cs, sn, u, w);
+  };
+  auto largest = [&](const float (&u)[Item::N], const float (&w)[Item::N]) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const int x = min(x0 + 256 * y, ntok * n_items - 1);
-      t[y] = x / n_items;
-      it[y] = rope_item<T>(r.layout, r.rot, D, x - t[y] * n_items);
-      const T* src = ksrc + (int64_t)t[y] * p.k_token + it[y].a;
-      load_some<T>(src, it[y].n, a[y]);
-      if (it[y].pairs) load_some<T>(src + r.rot / 2, it[y].n, w[y]);
+    for (int i = 0; i < Item::N; ++i) {
+      mk = finite_max(mk, u[i]);
+      if (kMode != kRopeInterleaved && it.turn) mk = finite_max(mk, w[i]);
     }
+  };
+  if constexpr (kMode != kRopeSingle) {
+    typename Item::El::Raw ra[NK], rb[NK];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      if (x0 + 256 * y >= ntok * n_items) break;
-      int32_t pos[3];
-      rope_positions(r, b, i0 + t[y], p.n, pos);
-      float cs[E], sn[E];
-      rope_item_angles<T>(r, it[y], pos, cs, sn);
-      rope_turn<T>(r, it[y], cs, sn, a[y], w[y]);
-      const int row = o0 + t[y];
-      if constexpr (kEight) {
-        float* dst = ks + row * KS + it[y].a;
+    for (int k = 0; k < NK; ++k)
+      if (mine) it.load(ksrc + (int64_t)min(tk + k * step, ntok - 1) * p.k_token, ra[k], rb[k]);
+    if (mine) {
+      it.frequencies(r);
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          if (i >= it[y].n) break;
-          dst[i] = a[y][i];
-          mk = finite_max(mk, a[y][i]);
-          if (it[y].pairs) {
-            dst[r.rot / 2 + i] = w[y][i];
-            mk = finite_max(mk, w[y][i]);
-          }
+      for (int k = 0; k < NK; ++k) {
+        const int t = tk + k * step;
+        if (t < ntok) {
+          turned(t, ra[k], rb[k], ku[k], kw[k]);
+          if constexpr (kEight) largest(ku[k], kw[k]);
+          else it.store(kdst + (size_t)(o0 + t) * D, ku[k], kw[k]);
         }
-      } else {
-        T* dst = kdst + (size_t)row * D + it[y].a;
-        store_some<T>(dst, it[y].n, a[y]);
-        if (it[y].pairs) store_some<T>(dst + r.rot / 2, it[y].n, w[y]);
       }
+    }
+  } else if (mine) {
+    it.frequencies(r);
+    for (int t = tk; t < ntok; t += step) {
+      typename Item::El::Raw ra, rb;
+      it.load(ksrc + (int64_t)t * p.k_token, ra, rb);
+      turned(t, ra, rb, ku[0], kw[0]);
+      if constexpr (kEight) largest(ku[0], kw[0]);
+      else it.store(kdst + (size_t)(o0 + t) * D, ku[0], kw[0]);
     }
   }
 #pragma unroll
@@ -211,28 +217,35 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
     if (tid == 0) p.k_exp[head * nb + blk] = (uint8_t)(ek + 127);
     if (tid == 64) p.v_exp[head * nb + blk] = (uint8_t)(ev + 127);
     {
-      const bool grow = o0 > 0 && ek > ek_old;
-      const float inv = pow2i(-ek), shift = pow2i(ek_old - ek);
-      const int r0 = grow ? 0 : o0;
-      for (int x = tid; x < (o1 - r0) * (D / 16); x += 256) {
-        const int row = r0 + x / (D / 16), d0 = x % (D / 16) * 16;
-        u32x4* dst = reinterpret_cast<u32x4*>(kc + (size_t)row * D + d0);
-        u32x4 w;
-        if (row >= o0) {
-          const f32x4* src = reinterpret_cast<const f32x4*>(ks + row * KS + d0);
+      const float inv = pow2i(-ek);
+      auto put = [&](int t, const float (&u)[Item::N], const float (&w)[Item::N]) {
+        uint8_t* row = kc + (size_t)(o0 + t) * D;
+        store_codes<Item::N>(row + it.a, u, inv);
+        if (kMode != kRopeInterleaved && it.turn) store_codes<Item::N>(row + it.b, w, inv);
+      };
+      if constexpr (kMode != kRopeSingle) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 y = src[i];
-            w[i] = codes4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-          }
-        } else {
-          const u32x4 was = *dst;
+        for (int k = 0; k < NK; ++k)
+          if (mine && tk + k * step < ntok) put(tk + k * step, ku[k], kw[k]);
+      } else if (mine) {
+        for (int t = tk; t < ntok; t += step) {  // (turned again: one pair a thread is too many to keep)
+          typename Item::El::Raw ra, rb;
+          it.load(ksrc + (int64_t)t * p.k_token, ra, rb);
+          turned(t, ra, rb, ku[0], kw[0]);
+          put(t, ku[0], kw[0]);
+        }
+      }
+      if (o0 > 0 && ek > ek_old) {  // the older rows, scaled down
+        const float shift = pow2i(ek_old - ek);
+        for (int x = tid; x < o0 * (D / 16); x += 256) {
+          u32x4* dst = reinterpret_cast<u32x4*>(kc + 16 * x);
+          u32x4 w = *dst;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            w[i] = codes4(code_to_f32(was[i] & 255u) * shift, code_to_f32(was[i] >> 8 & 255u) * shift,
-                          code_to_f32(was[i] >> 16 & 255u) * shift, code_to_f32(was[i] >> 24) * shift);
+            w[i] = codes4(code_to_f32(w[i] & 255u) * shift, code_to_f32(w[i] >> 8 & 255u) * shift,
+                          code_to_f32(w[i] >> 16 & 255u) * shift, code_to_f32(w[i] >> 24) * shift);
+          *dst = w;
         }
-        *dst = w;
       }
     }
     {
@@ -240,6 +253,16 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
       const float inv = pow2i(-ev), shift = pow2i(ev_old - ev);
       const int r0 = grow ? 0 : o0;
       constexpr int EPW = 4 / sizeof(T);  // dims per dword
+      if (!grow && ntok <= 4) {
+        // a few tokens (of a step that decodes): an element a thread
+        for (int x = tid; x < ntok * D; x += 256) {
+          const int t = o0 + x / D, e = x % D;
+          const uint32_t raw = vs[t * RW + e / EPW];
+          const float y = (sizeof(T) == 4 ? __uint_as_float(raw) : (e & 1 ? bf16_hi(raw) : bf16_lo(raw))) * inv;
+          vc[(size_t)e * p.P + t] = (uint8_t)codes4(y, y, y, y);
+        }
+        return;
+      }
       // runs of 16 tokens of a dword of dims
       for (int x = tid; x < 4 * (RW - 1); x += 256) {
         const int g0 = x % 4 * 16, w = x / 4;
@@ -274,10 +297,26 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
   }
 }
 
+template <typename T, int D, bool kEight, int kMode>
+void launch_mode(dim3 grid, TokenWriteParams p, hipStream_t s) {
+  const int n = RopeItem<T, kMode>::count(p.table.rot, D);
+  while (1 << p.item_shift < n) ++p.item_shift;
+  token_write_kernel<T, D, kEight, kMode><<<grid, 256, 0, s>>>(p);
+}
+
+template <typename T, int D, bool kEight>
+void launch_as(dim3 grid, const TokenWriteParams& p, hipStream_t s) {
+  switch (rope_mode<T>(p.table)) {
+    case kRopeHalves: return launch_mode<T, D, kEight, kRopeHalves>(grid, p, s);
+    case kRopeInterleaved: return launch_mode<T, D, kEight, kRopeInterleaved>(grid, p, s);
+    default: return launch_mode<T, D, kEight, kRopeSingle>(grid, p, s);
+  }
+}
+
 template <typename T, int D>
 void launch_for(bool eight, dim3 grid, const TokenWriteParams& p, hipStream_t s) {
-  if (eight) token_write_kernel<T, D, true><<<grid, 256, 0, s>>>(p);
-  else token_write_kernel<T, D, false><<<grid, 256, 0, s>>>(p);
+  if (eight) launch_as<T, D, true>(grid, p, s);
+  else launch_as<T, D, false>(grid, p, s);
 }
 
 }  // namespace

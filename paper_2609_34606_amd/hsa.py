@@ -632,48 +632,55 @@ def cache8_pool(k, v, k_exp, v_exp, page_table, cfg: HsaConfig) -> HsaCache8Pool
                          int(page_table.shape[-1]), kv)
 
 
-def _i32s(t, n: int, what: str) -> Optional[int]:
-    """Pointer of an int32 tensor of n elements, or None."""
+# The calls below may serve a single token, where the host's time counts: their checks
+# compare types, shapes and devices without building strings or objects.
+def _i32s(t, n: int, dev: int, what: str) -> Optional[int]:
+    """Address of a contiguous int32 tensor of n elements on device dev, or None."""
     if t is None:
         return None
-    if hasattr(t, "dtype") and (str(t.dtype) != "torch.int32" or t.numel() != n):
-        raise ValueError(f"{what} must hold {n} int32 values, got {tuple(t.shape)} {t.dtype}")
-    return _ptr(t)
+    import torch
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must hold {n} contiguous int32 values, got {tuple(t.shape)} {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}, not on the call's device")
+    return t.data_ptr()
 
 
-def _strided(cfg, t, n: int, heads: int, what: str):
-    """(pointer, batch stride, token stride) of a [B, n, heads, d] tensor whose
+def _strided(cfg, t, n: int, heads: int, dev: Optional[int], what: str):
+    """(address, batch stride, token stride, device) of a [B, n, heads, d] tensor whose
     heads are contiguous within a token."""
-    if tuple(t.shape) != (cfg.batch, n, heads, cfg.head_dim) or str(t.dtype) != _elem_dtype(cfg):
-        raise ValueError(f"{what} must be {_elem_dtype(cfg)} {(cfg.batch, n, heads, cfg.head_dim)}, got "
+    import torch
+    d = cfg.head_dim
+    if t.dtype is not (torch.bfloat16 if cfg.dtype == HSA_DTYPE_BF16 else torch.float32) or \
+            t.shape != (cfg.batch, n, heads, d):
+        raise ValueError(f"{what} must be {_elem_dtype(cfg)} {(cfg.batch, n, heads, d)}, got "
                          f"{t.dtype} {tuple(t.shape)}")
-    st = t.stride()
-    if t.numel() and (st[3] != 1 or (heads > 1 and st[2] != cfg.head_dim)):
-        raise ValueError(f"{what}: the heads of a token must be contiguous, got strides {st}")
-    return t.data_ptr(), st[0], st[1]
+    sb, st, sh, sd = t.stride()
+    if (sd != 1 or (sh != d and heads > 1)) and t.numel():
+        raise ValueError(f"{what}: the heads of a token must be contiguous, got strides {t.stride()}")
+    at = t.get_device()
+    if dev is not None and at != dev:
+        raise ValueError(f"{what} is on {t.device}, not on the call's device")
+    return t.data_ptr(), sb, st, at
 
 
-def _one_device(*tensors):
-    """The device of the tensors among the arguments (None and addresses skipped)."""
-    dev = None
-    for t in tensors:
-        d = getattr(t, "device", None)
-        if d is None:
-            continue
-        if dev is None:
-            dev = d
-        elif d != dev:
-            raise ValueError(f"tensors on {dev} and {d}")
-    return dev
+def _contiguous(cfg, t, n: int, dev: Optional[int], what: str):
+    """(address, device) of a contiguous [B, n, num_heads, d] tensor."""
+    p, _, _, at = _strided(cfg, t, n, cfg.num_heads, dev, what)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return p, at
 
 
-def _call(fn, dev, stream, *args) -> int:
+def _call(fn, dev: int, stream, *args) -> int:
     """fn(*args, stream) with the tensors' device current (kernels launch there)."""
     import torch
-    if dev is None or dev.type != "cuda" or dev.index == torch.cuda.current_device():
-        return fn(*args, _stream(stream))
-    with torch.cuda.device(dev):
-        return fn(*args, _stream(stream))
+    if dev < 0:
+        raise ValueError("the tensors must be on a GPU")
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call(fn, dev, stream, *args)
+    return fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
 
 
 def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None,
@@ -681,26 +688,24 @@ def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stre
     """Turns x [B, n, heads, d] by its tokens' positions (pos int32 [B, n, axes], or
     first int32 [B] + the token's index) into o (x itself, or apart from it).
     inverse: by the opposite angles, the gradient's map."""
-    heads = int(x.shape[2]) if x.dim() == 4 else 0
-    xp, xb, xt = _strided(cfg, x, n, heads, "x")
-    op, ob, ot = _strided(cfg, o, n, heads, "o")
-    dev = _one_device(x, o, pos, first)
+    heads = x.shape[2] if x.dim() == 4 else 0
+    xp, xb, xt, dev = _strided(cfg, x, n, heads, None, "x")
+    op, ob, ot, _ = _strided(cfg, o, n, heads, dev, "o")
     st = _call(lib().hsa_rope_apply, dev, stream, ctypes.byref(cfg), ctypes.byref(rope), xp, xb, xt, n, heads,
-               _i32s(pos, cfg.batch * n * rope.axes, "pos"), _i32s(first, cfg.batch, "first"),
-               int(bool(inverse)), op, ob, ot)
+               _i32s(pos, cfg.batch * n * rope.axes, dev, "pos"), _i32s(first, cfg.batch, dev, "first"),
+               1 if inverse else 0, op, ob, ot)
     if check:
         _check("hsa_rope_apply", st)
     return st
 
 
-def _token_write(name, cfg, pool, heads, k_src, v_src, n, rope, pos, first, count, stream, check) -> int:
-    kp, kb, kt = _strided(cfg, k_src, n, heads, "k_src")
-    vp, vb, vt = _strided(cfg, v_src, n, heads, "v_src")
-    dev = _one_device(k_src, v_src, pos, first, count)
-    st = _call(getattr(lib(), name), dev, stream, ctypes.byref(cfg), ctypes.byref(pool),
+def _token_write(name, fn, cfg, pool, heads, k_src, v_src, n, rope, pos, first, count, stream, check) -> int:
+    kp, kb, kt, dev = _strided(cfg, k_src, n, heads, None, "k_src")
+    vp, vb, vt, _ = _strided(cfg, v_src, n, heads, dev, "v_src")
+    st = _call(fn, dev, stream, ctypes.byref(cfg), ctypes.byref(pool),
                None if rope is None else ctypes.byref(rope), kp, kb, kt, vp, vb, vt, n,
-               None if rope is None else _i32s(pos, cfg.batch * n * rope.axes, "pos"),
-               _i32s(first, cfg.batch, "first"), _i32s(count, cfg.batch, "count"))
+               None if rope is None else _i32s(pos, cfg.batch * n * rope.axes, dev, "pos"),
+               _i32s(first, cfg.batch, dev, "first"), _i32s(count, cfg.batch, dev, "count"))
     if check:
         _check(name, st)
     return st
@@ -710,15 +715,15 @@ def hsa_token_write(cfg, pool, k_src, v_src, n, first=None, count=None, rope=Non
                     check=True) -> int:
     """Append tokens: k_src / v_src [B, n, H, d] become tokens first[b] + i, i <
     count[b], of each sequence in the pool, keys turned by rope on the way."""
-    return _token_write("hsa_token_write", cfg, pool, cfg.num_heads, k_src, v_src, n, rope, pos, first, count,
-                        stream, check)
+    return _token_write("hsa_token_write", lib().hsa_token_write, cfg, pool, cfg.num_heads, k_src, v_src, n, rope,
+                        pos, first, count, stream, check)
 
 
 def hsa_cache8_write(cfg, cache, k_src, v_src, n, first=None, count=None, rope=None, pos=None, stream=None,
                      check=True) -> int:
     """hsa_token_write into the 8-bit cache: k_src / v_src [B, n, kv_heads, d]."""
-    return _token_write("hsa_cache8_write", cfg, cache, cache.kv_heads, k_src, v_src, n, rope, pos, first, count,
-                        stream, check)
+    return _token_write("hsa_cache8_write", lib().hsa_cache8_write, cfg, cache, cache.kv_heads, k_src, v_src, n,
+                        rope, pos, first, count, stream, check)
 
 
 def hsa_cache8_attn_workspace_size(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int) -> int:
@@ -729,23 +734,37 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
                     q_len=None, causal=False, ws=None, stream=None, check=True) -> int:
     """Attention of q [B, n_q, H, d] over the 8-bit cache's listed pages: sel int32 [B,
     kv_heads, k_max], then [cur_first_page, + n_cur_pages); tokens below kv_len[b]."""
-    qp, op = _rows(cfg, q, n_q, "q"), _rows(cfg, o, n_q, "o")
-    lp = None if lse is None else _out(lse, cfg.batch * cfg.num_heads * n_q, "float32", "lse")
-    sp = _i32s(sel, cfg.batch * cache.kv_heads * k_max, "sel")
-    kvp, qlp = _i32s(kv_len, cfg.batch, "kv_len"), _i32s(q_len, cfg.batch, "q_len")
+    import torch
+    B = cfg.batch
+    qp, dev = _contiguous(cfg, q, n_q, None, "q")
+    op, _ = _contiguous(cfg, o, n_q, dev, "o")
+    if lse is None:
+        lp = None
+    else:
+        if lse.dtype is not torch.float32 or lse.shape != (B, cfg.num_heads, n_q) or not lse.is_contiguous():
+            raise ValueError(f"lse must be contiguous float32 {(B, cfg.num_heads, n_q)}, got {lse.dtype} "
+                             f"{tuple(lse.shape)}")
+        if lse.get_device() != dev:
+            raise ValueError(f"lse is on {lse.device}, not on the call's device")
+        lp = lse.data_ptr()
+    sp = _i32s(sel, B * cache.kv_heads * k_max, dev, "sel")
+    kvp, qlp = _i32s(kv_len, B, dev, "kv_len"), _i32s(q_len, B, dev, "q_len")
     if k_h is not None and len(k_h) != cache.kv_heads:
         raise ValueError(f"k_h must hold {cache.kv_heads} budgets, got {len(k_h)}")
-    dev = _one_device(q, o, lse, sel, kv_len, q_len, ws)
-    if ws is None:
-        ws = _workspace(hsa_cache8_attn_workspace_size(cfg, n_q, cache.kv_heads, k_max, n_cur_pages), q.device)
-        if ws is not None and stream is not None:  # not reused before that stream is done with it
-            import torch
-            ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else
-                             torch.cuda.ExternalStream(int(stream), device=q.device))
     _keep, kp = _budgets(k_h)
+    if ws is None:
+        nbytes = lib().hsa_cache8_attn_workspace_size(ctypes.byref(cfg), n_q, cache.kv_heads, k_max, n_cur_pages)
+        wp = None
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            wp = ws.data_ptr()
+            if stream is not None and dev >= 0:  # not reused before that stream is done with it
+                ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else
+                                 torch.cuda.ExternalStream(int(stream), device=q.device))
+    else:
+        wp, nbytes = _ptr(ws), ws.numel() * ws.element_size()
     st = _call(lib().hsa_cache8_attn, dev, stream, ctypes.byref(cfg), qp, n_q, ctypes.byref(cache), sp, k_max, kp,
-               cur_first_page, n_cur_pages, kvp, qlp, int(bool(causal)), op, lp, _ptr(ws),
-               0 if ws is None else ws.numel())
+               cur_first_page, n_cur_pages, kvp, qlp, 1 if causal else 0, op, lp, wp, nbytes)
     if check:
         _check("hsa_cache8_attn", st)
     return st

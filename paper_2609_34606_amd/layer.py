@@ -169,7 +169,8 @@ class HsaCache8:
             page_table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
         if int(k.shape[1]) != kv:
             raise ValueError(f"k must hold {kv} heads, got {tuple(k.shape)}")
-        _h._one_device(k, v, k_exp, v_exp, page_table)
+        if len({t.device for t in (k, v, k_exp, v_exp, page_table)}) > 1:
+            raise ValueError("the cache's tensors must be on one device")
         self.k, self.v, self.k_exp, self.v_exp, self.page_table = k, v, k_exp, v_exp, page_table
         self.rope = rope
         self.pool = _h.cache8_pool(k, v, k_exp, v_exp, page_table, self.cfg)
