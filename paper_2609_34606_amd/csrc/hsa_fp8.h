@@ -36,13 +36,24 @@ __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t lo, uint32_t hi, float s
                __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
 }
 
-// Code of x in units of the scale, rounded to nearest even: infinities go to
-// the largest number (e4m3 has none), NaN stays NaN.
-__device__ __forceinline__ float saturate(float x) { return x != x ? x : fminf(fmaxf(x, -kCodeMax), kCodeMax); }
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(a), saturate(b), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(c), saturate(d), w, true);
-  return (uint32_t)w;
+// Codes of numbers in units of a scale 2^e, rounded to nearest even; low byte first. The
+// caller's scale leaves no finite number above the largest code; saturate()
+// takes the infinities there first (e4m3 has none). NaN gives a NaN code.
+__device__ __forceinline__ float saturate(float x, float most) { return x != x ? x : fminf(fmaxf(x, -most), most); }
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t codes2(float a, float b, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, scale, false));
+}
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float scale) {
+  i16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, w);
+}
+// the same of two pairs of bf16 numbers
+__device__ __forceinline__ uint32_t codes4_bf16(uint32_t ab, uint32_t cd, float scale) {
+  i16x2 w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(i16x2{0, 0}, __builtin_bit_cast(bf16x2, ab), scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, cd), scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 // One code as a number.
 __device__ __forceinline__ float code_to_f32(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }

@@ -212,7 +212,8 @@ struct TokenWriteParams {
   const int32_t* first;       // [B] nullable
   const int32_t* count;       // [B] nullable
   int32_t H, P, n, num_slots, max_pages;
-  int32_t item_shift;         // set by the launch: 2^this threads share a token's key row
+  int32_t item_shift, heads;  // set by the launch: 2^item_shift threads share a token's key
+                              // row; heads a workgroup
 };
 
 int64_t token_write_units(int64_t n, int P);

@@ -96,16 +96,17 @@ struct Elems<T, 1> {
 
 // How a token's head is cut into items, by what the rotated part allows:
 //   halves       16 bytes of first elements and the 16 of their partners, rot / 2 dims on
-//                (rot / 2 a multiple of the elements in 16 bytes);
+//                (rot / 2 a multiple of the elements in 16 bytes); "part" where dims
+//                are left to copy, which takes up to twice the items;
 //   interleaved  16 bytes of whole pairs (rot a multiple);
 //   single       one pair, of either layout (any rot).
 // Items of the copied dims follow, 16 bytes or one element each.
-enum RopeMode { kRopeHalves = 0, kRopeInterleaved = 1, kRopeSingle = 2 };
+enum RopeMode { kRopeHalves = 0, kRopeInterleaved = 1, kRopeSingle = 2, kRopePart = 3 };
 
 template <typename T>
-inline int rope_mode(const RopeTable& r) {
+inline int rope_mode(const RopeTable& r, int d) {
   constexpr int E = 16 / sizeof(T);
-  if (r.layout == HSA_ROPE_HALF) return r.rot / 2 % E == 0 ? kRopeHalves : kRopeSingle;
+  if (r.layout == HSA_ROPE_HALF) return r.rot / 2 % E ? kRopeSingle : (r.rot == d ? kRopeHalves : kRopePart);
   return r.rot % E == 0 ? kRopeInterleaved : kRopeSingle;
 }
 
@@ -136,7 +137,7 @@ struct RopeItem {
     }
   }
   __device__ __forceinline__ void frequencies(const RopeTable& r) {
-    const bool halves = kMode == kRopeHalves || (kMode == kRopeSingle && r.layout == HSA_ROPE_HALF);
+    const bool halves = kMode != kRopeInterleaved && r.layout == HSA_ROPE_HALF;
     const int i0 = turn ? (halves ? a : a / 2) : 0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) f[i] = r.quarters[i0 + i];

@@ -56,8 +56,9 @@ hipError_t launch(RopeParams p, int B, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_as(const RopeParams& p, int B, hipStream_t s) {
-  switch (rope_mode<T>(p.table)) {
-    case kRopeHalves: return launch<T, kRopeHalves>(p, B, s);
+  switch (rope_mode<T>(p.table, p.d)) {
+    case kRopeHalves:
+    case kRopePart: return launch<T, kRopePart>(p, B, s);
     case kRopeInterleaved: return launch<T, kRopeInterleaved>(p, B, s);
     default: return launch<T, kRopeSingle>(p, B, s);
   }
