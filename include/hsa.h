@@ -762,7 +762,8 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  * Errors: INVALID_ARG (NULL, sizes below 0, an empty list: k_max == 0 and
  * n_cur_pages == 0), OUT_OF_RANGE (pages beyond max_pages), UNSUPPORTED
  * (sizes, alignment), WORKSPACE. n_q == 0 is a no-op. Kernels read kv_len and q_len,
- * so a captured call follows them.
+ * so a captured call follows them. k_max is at most HSA_MAX_LIST; a size of 0 means that no
+ * workspace is needed (or invalid input).
  */
 size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
                                       int32_t k_max, int32_t n_cur_pages);

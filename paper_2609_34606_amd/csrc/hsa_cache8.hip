@@ -8,6 +8,10 @@
 // key head h is head h G + r % G of query r / G, so a step of one token
 // reads every code once. Codes become bf16 matrix operands on the way (exactly:
 // see hsa_fp8.h), so keys and values are never in HBM in more than 8 bits.
+#include <limits.h>
+
+#include <type_traits>
+
 #include "hsa_cache8.h"
 
 namespace hsa {
@@ -15,7 +19,7 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;  // waves of a few-rows workgroup
+constexpr int kMaxSplit = 256;  // pieces of one item
 
 // D[16x16] += A[16x32] * B[32x16]. Lane l supplies A row (l % 16), k =
 // 8*(l/16)..+8, and B column (l % 16), same k range. Result register r of
@@ -75,7 +79,7 @@ __device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
 // from HBM to the registers of the wave that uses them, 16 bytes a lane; a
 // score block's rows are read in 64-byte pieces, a value block's too.
 // Bound: HBM (2 d bytes a token and key head).
-template <typename T, int D, int kCols, int kParts, bool kSmallP>
+template <typename T, int D, int kCols, int kParts, bool kSmallP, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
@@ -85,7 +89,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
   __shared__ float msm[kWaves][kRows], lsm[kWaves][kRows];
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int item = blockIdx.x / p.n_split, split = blockIdx.x - item * p.n_split, b = blockIdx.y;
+  // Workgroup i runs on XCD i % 8. Pieces of one sequence and head come n_items apart, and
+  // sequences begin one apart, so that no XCD gets only last pieces, which short
+  // sequences lack (32 sequences of 1 to 16384 tokens: %%% us, pieces together 154).
+  const int n_items = p.Hk * p.n_rt, b = blockIdx.y;
+  const int x0 = (int)((blockIdx.x + blockIdx.y) % gridDim.x);
+  const int split = x0 / n_items, item = x0 - split * n_items;
   const int rt = item / p.Hk, h = item - rt * p.Hk;
   const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, lane);
   if (w.rows <= 0) return;
@@ -128,20 +137,30 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
 
   u32x4 kc[4][C], vc[M];  // codes of a tile's keys and values
   float ksc[2], vsc[2];   // their scales (granules of 8 keys: two a lane)
-  int tok[2];             // logical token of the lane's keys 0..7 and 8..15
-  bool ok[2];             // whether they are tokens of a listed page
+  int tok[2];             // logical token of the lane's keys 0..7 and 8..15; none
+                          // (INT_MAX) where they are no token of a listed page
+  bool masked;            // whether some query does not see all of the tile
 
   const int rho = 4 * (c16 >> 2);  // key row of the lane in score block i: 4 rho + 4 i + c16 % 4
-  int li = 0, kt = 0;              // list position and tile within its page
+  int li = 0, kt = 0, li_next = 0, kt_next = 0;  // list position and tile within its page
   if constexpr (!kSmallP) {
     li = (t_lo + wave) / p.tpp;
     kt = (t_lo + wave) - li * p.tpp;
   }
-  int lp = 0, slot = 0;
-  auto locate = [&](int t) {
+  // The tile's page, and that of the wave's next tile: looked up a tile ahead.
+  int lp = 0, slot = 0, lp_next = 0, slot_next = 0;
+  auto look_ahead = [&](int t) {
     if constexpr (!kSmallP) {
-      lp = page_of(li);
-      slot = slot_of(lp);
+      kt_next = kt + kWaves;
+      li_next = li;
+      while (kt_next >= p.tpp) {
+        kt_next -= p.tpp;
+        ++li_next;
+      }
+      if (t + kWaves < t_hi) {
+        lp_next = page_of(li_next);
+        slot_next = slot_of(lp_next);
+      }
     }
   };
   auto load_keys = [&](int t) {
@@ -181,12 +200,6 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
         vc[m] = u32x4{x[0], x[1], x[2], x[3]};
       }
       vsc[0] = vsc[1] = scale_of(p.v_exp[head * p.nb + kt]);
-      const int first = lp * p.P + w0 + 16 * g;
-      tok[0] = first;
-      tok[1] = first + 8;
-      // a tile that the page's end shifts back repeats keys of the one before
-      ok[0] = w0 + 16 * g >= kt * 64;
-      ok[1] = w0 + 16 * g + 8 >= kt * 64;
     } else {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -194,8 +207,6 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
         const int page = page_v(p, w, selrow, a.li);
         const size_t head = (size_t)slot_v(p, ptrow, page) * p.Hk + h;
         vsc[u] = scale_of(p.v_exp[head * p.nb]);
-        tok[u] = page * p.P + a.off;
-        ok[u] = a.ok;
         const uint8_t* vb = p.v + (head * D + c16) * p.P + a.off;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
@@ -206,23 +217,36 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
       }
     }
   };
-  auto advance = [&]() {
+  // what the mask of the tile needs, once its place is known
+  auto place = [&](int t) {
     if constexpr (!kSmallP) {
-      kt += kWaves;
-      while (kt >= p.tpp) {
-        kt -= p.tpp;
-        ++li;
+      const int w0 = min(kt * 64, p.P - 64), first = lp * p.P + w0 + 16 * g;
+      // a tile that the page's end shifts back repeats keys of the one before
+      tok[0] = w0 + 16 * g >= kt * 64 ? first : INT_MAX - 8;
+      tok[1] = w0 + 16 * g + 8 >= kt * 64 ? first + 8 : INT_MAX - 8;
+      masked = kt * 64 > p.P - 64 || lp * p.P + kt * 64 + 64 > lim_first;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const Cache8Granule a = cache8_granule(p, w, t, 2 * g + u);
+        tok[u] = a.ok ? page_v(p, w, selrow, a.li) * p.P + a.off : INT_MAX - 8;
       }
+      masked = true;
     }
   };
 
+  if (t_lo + wave < t_hi) {
+    if constexpr (!kSmallP) {
+      lp = page_of(li);
+      slot = slot_of(lp);
+    }
+    load_keys(t_lo + wave);
+    load_values(t_lo + wave);
+  }
   for (int t = t_lo + wave; t < t_hi; t += kWaves) {
-    locate(t);
-    load_keys(t);
-    load_values(t);
-    bool masked = true;
-    if constexpr (!kSmallP)
-      masked = kt * 64 > p.P - 64 || lp * p.P + kt * 64 + 64 > lim_first;
+    look_ahead(t);
+    place(t);
+    const bool more = t + kWaves < t_hi;
     f32x4 s[kCols][4];
 #pragma unroll
     for (int n = 0; n < kCols; ++n)
@@ -240,21 +264,25 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
 #pragma unroll
             for (int k = 0; k < kParts; ++k) s[n][i] = mfma16(a, qf[n][c][u][k], s[n][i]);
         }
+    // the next tile's keys take the registers of these
+    lp = lp_next;
+    slot = slot_next;
+    li = li_next;
+    kt = kt_next;
+    if (more) load_keys(t + kWaves);
     if (masked) {
 #pragma unroll
       for (int n = 0; n < kCols; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int u = i >> 1, j = 4 * (i & 1) + r;
-            if (!ok[u] || tok[u] + j >= lim[n]) s[n][i][r] = -INFINITY;
-          }
+          for (int r = 0; r < 4; ++r)
+            if (tok[i >> 1] >= lim[n] - (4 * (i & 1) + r)) s[n][i][r] = -INFINITY;
       // Codes past the last token any row sees may be anything; a weight of 0 would
       // not take a NaN out.
 #pragma unroll
       for (int m = 0; m < M; ++m) {
-        const int n0 = ok[0] ? clampi(w.lim - tok[0], 0, 8) : 0, n1 = ok[1] ? clampi(w.lim - tok[1], 0, 8) : 0;
+        const int n0 = clampi(w.lim - min(tok[0], w.lim), 0, 8), n1 = clampi(w.lim - min(tok[1], w.lim), 0, 8);
         const u32x4 lo = keep_codes(vc[m], n0), hi = keep_codes(u32x4{0, 0, vc[m][2], vc[m][3]}, 8 + n1);
         vc[m] = u32x4{lo[0], lo[1], hi[2], hi[3]};
       }
@@ -316,10 +344,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
 #pragma unroll
           for (int k = 0; k < kParts; ++k) acc[n][m] = mfma16(a, pk[n][u][k], acc[n][m]);
       }
-    advance();
+    if (more) load_values(t + kWaves);
   }
 
-  // Join the waves: 16 rows at a time through LDS, then 16 threads a row.
+  // Join the waves: 16 rows at a time through LDS, then kShare threads a row.
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
     l_run[n] += __shfl_xor(l_run[n], 16);
@@ -329,7 +357,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
       lsm[wave][16 * n + c16] = l_run[n];
     }
   }
-  const int col = tid >> 4, d0 = (tid & 15) * (D / 16);
+  constexpr int kShare = 4 * kWaves;  // threads a row
+  constexpr int N = D / kShare;       // dims each
+  const int col = tid / kShare, d0 = tid % kShare * N;
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
     if (n > 0) __syncthreads();
@@ -341,79 +371,505 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
     float m_all = msm[0][row];
 #pragma unroll
     for (int x = 1; x < kWaves; ++x) m_all = fmaxf(m_all, msm[x][row]);
-    float l = 0.f, o[D / 16] = {};
+    float l = 0.f, o[N] = {};
 #pragma unroll
     for (int x = 0; x < kWaves; ++x) {
       const float wt = __builtin_amdgcn_exp2f((msm[x][row] - m_all) * c2);
       l += wt * lsm[x][row];
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) o[e] += wt * osm[(x * 16 + col) * OS + d0 + e];
+      for (int e = 0; e < N; ++e) o[e] += wt * osm[(x * 16 + col) * OS + d0 + e];
     }
     if (i >= w.q_len) continue;
     if (whole) {
-      cache8_store<T, D / 16>(p, b, i, h * p.G + r % p.G, d0, o, m_all, l, (tid & 15) == 0);
+      cache8_store<T, N>(p, b, i, h * p.G + r % p.G, d0, o, m_all, l, d0 == 0);
     } else {
       const size_t part = (((size_t)b * p.Hk + h) * p.n_split + split) * p.part_rows + r;
 #pragma unroll
-      for (int e = 0; e < D / 16; e += 4)
-        *reinterpret_cast<f32x4*>(p.part_o + part * D + d0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
-      if ((tid & 15) == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_all, l};
+      for (int e = 0; e < N; ++e) p.part_o[part * D + d0 + e] = o[e];
+      if (d0 == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_all, l};
     }
   }
 }
 
-// Joins the pieces of a row whose tokens were split: a workgroup a row, each wave
-// every fourth piece, in an order that does not depend on the launch's timing.
+// Many query rows: 256 rows of one key head (four waves of 64) against a range of its
+// tokens, one workgroup a CU. Each 64-key tile is turned into bf16 once, on its way from
+// the registers that its codes arrived in to LDS, and read from there by all four waves;
+// a key or value operand serves two blocks of 32 queries.
+//
+// Products are transposed as in the page walk of the bf16 pool (S^T = K Q^T, O^T +=
+// V^T P^T, 32x32x16), with key rows in an order that makes a lane's scores the
+// weights' operand. A wave has its SIMD to itself, so the pipes overlap inside it: a step
+// does the softmax and the value product of tile t and the scores of tile t + 1,
+// matrix instructions between the exponentials.
+// Bound: the matrix pipe and, as close, the vector pipe (exponentials and conversions).
+template <int D>
+struct ManyLayout {
+  static constexpr int kRowK = 2 * D, kTileK = 64 * kRowK;  // bytes
+  static constexpr int kRowV = 128, kTileV = D * kRowV;
+  static constexpr int kVBase = 3 * kTileK;  // three key tiles, two value tiles
+  static constexpr int kBytes = kVBase + 2 * kTileV;
+  // 16-byte chunks of a row, permuted so that rows read together fall on their own banks
+  static __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int swz_v(int row) { return (row >> 1) & 7; }
+};
+
+constexpr int kManyRows = 256;  // query rows of a many-rows item
+
+template <int D, int kW, int QB>
+__global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnParams p) {
+  using L = ManyLayout<D>;
+  constexpr int KK = D / 16, NM = D / 32;
+  constexpr int kThreads = 64 * kW;
+  static_assert(32 * QB * kW == kManyRows, "rows of an item");
+  static_assert(4 * D == kThreads, "a thread converts 16 codes of keys and 16 of values a tile");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // workgroup i runs on XCD i % 8: an XCD takes consecutive items, which share their pages in
+  // its L2
+  const int n_wg = gridDim.x, x8 = blockIdx.x & 7;
+  const int id = x8 * (n_wg >> 3) + min(x8, n_wg & 7) + (blockIdx.x >> 3);
+  const int item = id / p.n_split, split = id - item * p.n_split, b = blockIdx.y;
+  const int h = item / p.n_rt, rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
+  const Cache8Walk w = cache8_walk(p, b, h, rt * kManyRows, kManyRows, lane);
+  if (w.rows <= 0) return;
+  const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
+  if (split > 0 && t_lo >= w.n_tiles) return;
+  const bool whole = w.n_tiles <= p.split_tiles;
+  const int n = t_hi - t_lo;
+
+  // queries
+  u32x4 qf[QB][KK];
+  int lim[QB];
+  const int row0 = rt * kManyRows + wave * 32 * QB;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int r = row0 + 32 * qb + l32, i = min(r / p.G, w.q_len - 1);
+    lim[qb] = cache8_limit(p, w, i);
+    const uint16_t* q =
+        static_cast<const uint16_t*>(p.q) + (((size_t)b * p.n_q + i) * p.H + h * p.G + r % p.G) * D + 8 * half;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[qb][kk] = ld_global16(q + 16 * kk);
+  }
+  const int lim_first = cache8_limit(p, w, min(row0 / p.G, w.q_len - 1));
+  const bool active = row0 < rt * kManyRows + w.rows;
+
+  // The tiles' stream: list position and tile within its page of the next keys to load. Slots
+  // are looked up with vector loads, a page ahead (logical page: two), so that
+  // they never wait and leave the LDS counter alone.
+  const int32_t* selrow = p.sel + ((size_t)b * p.Hk + h) * p.k_max;
+  const int32_t* ptrow = p.page_table + (size_t)b * p.max_pages;
+  const int last_li = max(w.n_list - 1, 0);
+  int zero = 0;
+  asm volatile("" : "+v"(zero));  // (keeps the lookups vector loads)
+  auto page_at = [&](int li) __attribute__((always_inline)) {
+    li = min(li, last_li);
+    return li < w.n_sel ? selrow[li + zero] : p.cur_first + li - w.n_sel + zero;
+  };
+  auto slot_at = [&](int lp) __attribute__((always_inline)) { return clampi(ptrow[clampi(lp, 0, p.max_pages - 1)], 0, p.num_slots - 1); };
+  int kbuf = 0;  // key buffer of tile t
+  int li = t_lo / p.tpp, kt = t_lo - li * p.tpp;
+  int lp_cur = page_at(li), lp_nxt = page_at(li + 1), lp_nx2 = page_at(li + 2);
+  int slot_cur = slot_at(lp_cur), slot_nxt = slot_at(lp_nxt);
+
+  u32x4 kc, vc;  // the codes of the next tiles, 16 a thread
+  uint32_t ke = 0, ve = 0;
+  size_t head_v = 0;   // the value tile one behind the keys
+  int kt_v = 0;
+  // logical token of each tile's first key and the tokens a tile at its page's
+  // end is shifted back by: of the tiles t, t + 1, .. t + 3
+  int tok[4], back[4];
+  auto load_k = [&]() __attribute__((always_inline)) {  // the next tile's keys; its place moves on
+    const int slot = __builtin_amdgcn_readfirstlane(slot_cur), lp = __builtin_amdgcn_readfirstlane(lp_cur);
+    const size_t head = (size_t)slot * p.Hk + h;
+    const int w0 = min(kt * 64, p.P - 64);
+    const uint8_t* kb = p.k + (head * p.P + w0) * D;
+    kc = ld_global16(kb + 16 * tid);
+    ke = p.k_exp[head * p.nb + kt];
+    tok[0] = tok[1];
+    tok[1] = tok[2];
+    tok[2] = tok[3];
+    back[0] = back[1];
+    back[1] = back[2];
+    back[2] = back[3];
+    tok[3] = lp * p.P + w0;
+    back[3] = kt * 64 - w0;
+    head_v = head;
+    kt_v = kt;
+    if (++kt == p.tpp) {
+      kt = 0;
+      ++li;
+      lp_cur = lp_nxt;
+      slot_cur = slot_nxt;
+      slot_nxt = slot_at(lp_nx2);
+      lp_nxt = lp_nx2;
+      lp_nx2 = page_at(li + 2);
+    }
+  };
+  auto load_v = [&](size_t head, int at) __attribute__((always_inline)) {
+    const uint8_t* vb = p.v + head * D * p.P + min(at * 64, p.P - 64);
+    const u32x4a8 y = *reinterpret_cast<const u32x4a8*>(vb + (size_t)(tid >> 2) * p.P + 16 * (tid & 3));
+    vc = u32x4{y[0], y[1], y[2], y[3]};
+    ve = p.v_exp[head * p.nb + at];
+  };
+  auto put_k = [&](int buf) __attribute__((always_inline)) {
+    const float s = scale_of(ke);
+    const int row = tid / (D / 16), c0 = 2 * (tid % (D / 16));
+    uint8_t* dst = smem + buf * L::kTileK + row * L::kRowK;
+    *reinterpret_cast<u32x4*>(dst + ((c0 ^ L::swz_k(row)) << 4)) = codes_to_bf16(kc[0], kc[1], s);
+    *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_k(row)) << 4)) = codes_to_bf16(kc[2], kc[3], s);
+  };
+  auto put_v = [&](int buf, int t0) __attribute__((always_inline)) {
+    const float s = scale_of(ve);
+    // codes past the last token any row sees may be anything
+    if (t0 + 64 > w.lim) vc = keep_codes(vc, clampi(w.lim - t0 - 16 * (tid & 3), 0, 16));
+    const int row = tid >> 2, c0 = 2 * (tid & 3);
+    uint8_t* dst = smem + L::kVBase + buf * L::kTileV + row * L::kRowV;
+    *reinterpret_cast<u32x4*>(dst + ((c0 ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[0], vc[1], s);
+    *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[2], vc[3], s);
+  };
+
+  f32x16 acc[QB][NM], sa[QB], sb[QB];
+  float m_run[QB], l_run[QB];
+  const float c2 = p.scale_log2;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m_run[qb] = softmax_floor(c2);
+    l_run[qb] = 0.f;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) acc[qb][m] = f32x16{0};
+  }
+  const int krow = (l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // bits 2 and 3 swapped
+  uint32_t offk[KK], offv[4];
+#pragma unroll
+  for (int j = 0; j < KK; ++j) offk[j] = krow * L::kRowK + (((2 * j + half) ^ L::swz_k(krow)) << 4);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) offv[ks] = l32 * L::kRowV + (((2 * ks + half) ^ L::swz_v(l32)) << 4);
+  // Operands: slice j of key half kh in key buffer buf; dim block m of 16-key group ks.
+  auto kop = [&](int buf, int kh, int j) __attribute__((always_inline)) {
+    return ld_lds16(smem + buf * L::kTileK + offk[j] + kh * 32 * L::kRowK);
+  };
+  auto vop = [&](int buf, int ks, int m) __attribute__((always_inline)) {
+    return ld_lds16(smem + L::kVBase + buf * L::kTileV + offv[ks] + m * 32 * L::kRowV);
+  };
+  // Two weights of 16-key group g of query block qb (score registers 8 g + 2 i, + 1), packed.
+  auto weigh = [&](const f32x16 (&s)[QB], const float (&mc)[QB], int g, int qb, int i) __attribute__((always_inline)) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[qb][8 * g + 2 * i], c2, -mc[qb]));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[qb][8 * g + 2 * i + 1], c2, -mc[qb]));
+    l_run[qb] += x + y;
+    return pack_bf16(x, y);
+  };
+  // keys of half kh that a query does not see, or that the tile repeats
+  auto mask = [&](int first, int skip, int kh, f32x16 (&s)[QB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = 32 * kh + 16 * (r >> 3) + 8 * half + (r & 7);
+        if (key < skip || first + key >= lim[qb]) s[qb][r] = -INFINITY;
+      }
+  };
+  // The largest of a half's scores, and the reference that follows it as in the few-rows kernel.
+  auto largest = [&](const f32x16 (&s)[QB], float (&mx)[QB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      mx[qb] = s[qb][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx[qb] = fmaxf(mx[qb], s[qb][r]);
+    }
+  };
+  auto raise = [&](const float (&mx)[QB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      if (__any(mx[qb] * c2 > m_run[qb] * c2 + 8.f)) {
+        const float top = fmaxf(mx[qb], __shfl_xor(mx[qb], 32));
+        const float m_new = top * c2 > m_run[qb] * c2 + 8.f ? top : m_run[qb];
+        const float alpha = __builtin_amdgcn_exp2f((m_run[qb] - m_new) * c2);
+        l_run[qb] *= alpha;
+#pragma unroll
+        for (int m = 0; m < NM; ++m) acc[qb][m] *= alpha;
+        m_run[qb] = m_new;
+      }
+    }
+  };
+  // Half a step: the softmax and value product of key half kh (scores s, value buffer vb), and
+  // the scores sn of the half after it: half nh of key buffer kb, of a tile that begins at token
+  // first and is shifted back by skip. It goes by pairs of matrix instructions, which share an
+  // operand that was read four pairs before; between the pairs go the weights (those of the
+  // first 16 keys two a pair and query block, so that their products can begin, those of the
+  // second one), the conversion of the tiles to come, and the maximum. The order is the source's:
+  // left to itself the compiler reads operands right before their use.
+  auto half_step = [&](int vb, int kh, const f32x16 (&s)[QB], int kb, int nh, int first, int skip, f32x16 (&sn)[QB],
+                       auto&& tail) __attribute__((always_inline)) {
+    constexpr int NP = KK + 2 * NM;                           // pairs
+    constexpr int kFirst = KK / 2;                            // pairs that the first 16 keys' weights take
+    constexpr int kSecond = KK + NM - kFirst;                 // pairs that the second 16 keys' take
+    float mc[QB], mx[QB];
+    u32x4 pk[2][QB];
+    u32x4 f[4];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      mc[qb] = m_run[qb] * c2;
+      mx[qb] = -INFINITY;
+      sn[qb] = f32x16{0};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = kop(kb, nh, i);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      // (what a pair computes from is opaque before it, and what it leaves is used in it)
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 a = f[i & 3];
+      asm volatile("" : "+v"(a));
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) asm volatile("" : "+v"(mc[qb]));
+      const int n = i + 4;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        if (i < KK) sn[qb] = mfma32(a, qf[qb][i], sn[qb]);
+        else acc[qb][(i - KK) % NM] = mfma32(a, pk[(i - KK) / NM][qb], acc[qb][(i - KK) % NM]);
+      }
+      if (n < KK) f[i & 3] = kop(kb, nh, n);
+      else if (n < NP) f[i & 3] = vop(vb, 2 * kh + (n - KK) / NM, (n - KK) % NM);
+      // packed weights: four a query block of each 16 keys
+#pragma unroll
+      for (int x = 0; x < 4 * QB; ++x) {
+        const int qb = x % QB, word = x / QB;
+        uint32_t e;
+        if (i < kFirst && x * kFirst / (4 * QB) == i) {
+          e = weigh(s, mc, 0, qb, word);
+          asm volatile("" : "+v"(e), "+v"(l_run[qb]));
+          pk[0][qb][word] = e;
+        }
+        if (i >= kFirst && i < kFirst + kSecond && x * kSecond / (4 * QB) == i - kFirst) {
+          e = weigh(s, mc, 1, qb, word);
+          asm volatile("" : "+v"(e), "+v"(l_run[qb]));
+          pk[1][qb][word] = e;
+        }
+      }
+      if (i >= KK + NM) {
+        // (they were complete KK pairs ago)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+          for (int r = (i - KK - NM) * 16 / NM; r < (i - KK - NM + 1) * 16 / NM; ++r) mx[qb] = fmaxf(mx[qb], sn[qb][r]);
+          asm volatile("" : "+v"(mx[qb]));
+        }
+      }
+      if (i == KK) tail();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (__builtin_expect(skip > 0 || first + 64 > lim_first, 0)) {
+      mask(first, skip, nh, sn);
+      largest(sn, mx);
+    }
+    raise(mx);
+  };
+  // One step: tile t (scores of its first half in sa on entry), with the first half of tile
+  // t + 1 at its end. par: t's parity, which buffers hold it.
+  auto step = [&](auto parity) __attribute__((always_inline)) {
+    constexpr int par = decltype(parity)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    // V(t + 1) goes over V(t - 1), K(t + 2) over K(t - 1), three key buffers on; the loads
+    // after them start as soon as their registers are free
+    const int k0 = kbuf, k1 = kbuf == 2 ? 0 : kbuf + 1, k2 = k1 == 2 ? 0 : k1 + 1;
+    kbuf = k1;
+    auto next_v = [&]() __attribute__((always_inline)) {
+      put_v(1 - par, tok[2]);
+      load_v(head_v, kt_v);
+    };
+    auto next_k = [&]() __attribute__((always_inline)) {
+      put_k(k2);
+      load_k();
+    };
+    if (!active) {
+      next_v();
+      next_k();
+      return;
+    }
+    // (tile t is tok[1] before load_k, tok[0] after it)
+    half_step(par, 0, sa, k0, 1, tok[1], back[1], sb, next_v);
+    half_step(par, 1, sb, k1, 0, tok[2], back[2], sa, next_k);
+  };
+
+  if (n > 0) {
+    // K(0), K(1) and V(0) to LDS; K(2) and V(1) on their way
+    load_k();
+    size_t hv = head_v;
+    int kv = kt_v;
+    load_v(hv, kv);
+    put_k(0);
+    load_k();
+    put_v(0, tok[2]);
+    hv = head_v;
+    kv = kt_v;
+    put_k(1);
+    load_v(hv, kv);
+    load_k();
+    // tok[1] is tile 0 now
+    lds_barrier();
+    if (active) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) sa[qb] = f32x16{0};
+#pragma unroll
+      for (int j = 0; j < KK; ++j)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) sa[qb] = mfma32(kop(0, 0, j), qf[qb][j], sa[qb]);
+      if (back[1] > 0 || tok[1] + 64 > lim_first) mask(tok[1], back[1], 0, sa);
+      float mx[QB];
+      largest(sa, mx);
+      raise(mx);
+    }
+    for (int t = 0; t < n; t += 2) {
+      step(std::integral_constant<int, 0>{});
+      if (t + 1 < n) step(std::integral_constant<int, 1>{});
+    }
+  }
+  if (!active) return;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int r = row0 + 32 * qb + l32, i = r / p.G;
+    const float l = l_run[qb] + __shfl_xor(l_run[qb], 32);
+    if (i >= w.q_len) continue;
+    if (whole) {
+      const int head = h * p.G + r % p.G;
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float o[4] = {acc[qb][m][4 * g], acc[qb][m][4 * g + 1], acc[qb][m][4 * g + 2], acc[qb][m][4 * g + 3]};
+          cache8_store<uint16_t, 4>(p, b, i, head, 32 * m + 8 * g + 4 * half, o, m_run[qb], l,
+                                    m == 0 && g == 0 && half == 0);
+        }
+    } else {
+      const size_t part = (((size_t)b * p.Hk + h) * p.n_split + split) * p.part_rows + r;
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(p.part_o + part * D + 32 * m + 8 * g + 4 * half) =
+              f32x4{acc[qb][m][4 * g], acc[qb][m][4 * g + 1], acc[qb][m][4 * g + 2], acc[qb][m][4 * g + 3]};
+      if (half == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_run[qb], l};
+    }
+  }
+}
+
+// Joins the pieces of a row whose tokens were split, in an order that does not depend on
+// the launch's timing. The pieces' maxima and sums are on their way before the row's
+// number of pieces is known (a piece that does not exist holds anything, and is
+// not used).
+// Few rows (of few-rows items): a workgroup of eight waves a row, each every eighth piece.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_kernel(Cache8AttnParams p) {
-  constexpr int E = D / 64;  // dims per lane
-  __shared__ float osm[4][D], lsm[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+__global__ __launch_bounds__(512) void join_row_kernel(Cache8AttnParams p) {
+  constexpr int E = D / 64, kW = 8;  // dims per lane, waves
+  __shared__ float osm[kW][D];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = blockIdx.x / p.Hk, h = blockIdx.x - r * p.Hk, b = blockIdx.y;
+  const size_t part0 = ((size_t)b * p.Hk + h) * p.n_split * p.part_rows + r;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml);
+  f32x2 x[kMaxSplit / 64];
+#pragma unroll
+  for (int k = 0; k < kMaxSplit / 64; ++k)
+    x[k] = 64 * k < p.n_split ? ml[part0 + (size_t)min(64 * k + lane, p.n_split - 1) * p.part_rows] : f32x2{0.f, 0.f};
   const Cache8Walk w = cache8_walk(p, b, h, r / p.rows_per_item * p.rows_per_item, p.rows_per_item, lane);
   const int i = r / p.G;
   if (w.rows <= 0 || i >= w.q_len || w.n_tiles <= p.split_tiles) return;
   const int n = (w.n_tiles + p.split_tiles - 1) / p.split_tiles;
-  const size_t part0 = ((size_t)b * p.Hk + h) * p.n_split * p.part_rows + r;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml);
   float m_all = -FLT_MAX;
-  for (int s = lane; s < n; s += 64) m_all = fmaxf(m_all, ml[part0 + (size_t)s * p.part_rows][0]);
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, x));
+  for (int k = 0; k < kMaxSplit / 64; ++k)
+    if (64 * k + lane < n) m_all = fmaxf(m_all, x[k][0]);
+#pragma unroll
+  for (int y = 1; y < 64; y <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, y));
   float l = 0.f, o[E] = {};
-#pragma unroll 4
-  for (int s = wave; s < n; s += 4) {
-    const size_t part = part0 + (size_t)s * p.part_rows;
-    const f32x2 x = ml[part];
-    const float wt = __builtin_amdgcn_exp2f((x[0] - m_all) * p.scale_log2);
-    l += wt * x[1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += wt * p.part_o[part * D + E * lane + e];
+  for (int k = 0; k < kMaxSplit / 64; ++k) {
+    if (64 * k >= n) break;
+    const bool in = 64 * k + lane < n;
+    const float wt = in ? __builtin_amdgcn_exp2f((x[k][0] - m_all) * p.scale_log2) : 0.f;
+    float sum = in ? wt * x[k][1] : 0.f;
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) sum += __shfl_xor(sum, y);
+    l += sum;
+    const int stop = min(64, n - 64 * k);
+#pragma unroll
+    for (int j = 0; j < 64 / kW; ++j) {
+      const int s = wave + kW * j;
+      if (s < stop) {
+        const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), s));
+        const float* src = p.part_o + (part0 + (size_t)(64 * k + s) * p.part_rows) * D + E * lane;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += ws * src[e];
+      }
+    }
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) osm[wave][E * lane + e] = o[e];
-  if (lane == 0) lsm[wave] = l;
   __syncthreads();
   if (wave) return;
-  l = (lsm[0] + lsm[1]) + (lsm[2] + lsm[3]);
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    o[e] = (osm[0][E * lane + e] + osm[1][E * lane + e]) + (osm[2][E * lane + e] + osm[3][E * lane + e]);
+  for (int e = 0; e < E; ++e) {
+    o[e] = osm[0][E * lane + e];
+#pragma unroll
+    for (int y = 1; y < kW; ++y) o[e] += osm[y][E * lane + e];
+  }
   cache8_store<T, E>(p, b, i, h * p.G + r % p.G, E * lane, o, m_all, l, lane == 0);
+}
+
+// Many rows: D / 4 lanes a row, four dims each, the pieces one after another.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void join_rows_kernel(Cache8AttnParams p) {
+  constexpr int kLanes = D / 4, kPerWg = 256 / kLanes;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int tiles = (p.part_rows + kPerWg - 1) / kPerWg;  // workgroups a key head
+  const int h = blockIdx.x / tiles, b = blockIdx.y;
+  const int row0 = (blockIdx.x - h * tiles) * kPerWg, r = row0 + tid / kLanes;
+  const size_t part0 = ((size_t)b * p.Hk + h) * p.n_split * p.part_rows + r;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml);
+  // (items are 16 rows or a multiple: a workgroup's are of one item)
+  const Cache8Walk w = cache8_walk(p, b, h, row0 / p.rows_per_item * p.rows_per_item, p.rows_per_item, lane);
+  const int i = r / p.G, d0 = 4 * (tid % kLanes);
+  if (w.rows <= 0 || i >= w.q_len || w.n_tiles <= p.split_tiles) return;
+  const int n = (w.n_tiles + p.split_tiles - 1) / p.split_tiles;
+  float m = -FLT_MAX, l = 0.f, o[4] = {};
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const f32x2 x = ml[part0 + (size_t)s * p.part_rows];
+    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_o + (part0 + (size_t)s * p.part_rows) * D + d0);
+    const float top = fmaxf(m, x[0]);
+    const float was = __builtin_amdgcn_exp2f((m - top) * p.scale_log2);
+    const float add = __builtin_amdgcn_exp2f((x[0] - top) * p.scale_log2);
+    l = l * was + add * x[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * was + add * y[e];
+    m = top;
+  }
+  cache8_store<T, 4>(p, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
 
 template <typename T, int D, int kCols, int kParts>
 void launch_rows(const Cache8AttnParams& p, int B, hipStream_t s) {
   const dim3 grid(p.n_split * p.Hk * p.n_rt, B);
-  if (p.P < 64) few_rows_kernel<T, D, kCols, kParts, true><<<grid, 64 * kWaves, 0, s>>>(p);
-  else few_rows_kernel<T, D, kCols, kParts, false><<<grid, 64 * kWaves, 0, s>>>(p);
+  const bool small = p.P < 64;
+  if (kCols == 1 && p.waves == 8) {
+    if (small) few_rows_kernel<T, D, 1, kParts, true, 8><<<grid, 512, 0, s>>>(p);
+    else few_rows_kernel<T, D, 1, kParts, false, 8><<<grid, 512, 0, s>>>(p);
+  } else {
+    if (small) few_rows_kernel<T, D, kCols, kParts, true, 4><<<grid, 256, 0, s>>>(p);
+    else few_rows_kernel<T, D, kCols, kParts, false, 4><<<grid, 256, 0, s>>>(p);
+  }
 }
 
 template <int D>
 hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s) {
   const int cols = p.rows_per_item / 16;
   if (dtype == HSA_DTYPE_BF16) {
-    if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
+    if (p.rows_per_item == kManyRows)
+      many_rows_kernel<D, D / 16, 128 / D><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
+    else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
     else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
     else launch_rows<uint16_t, D, 4, 1>(p, B, s);
   } else {
@@ -421,9 +877,17 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
     else launch_rows<float, D, 2, 3>(p, B, s);
   }
   if (p.n_split > 1) {
-    const dim3 grid(p.n_q * p.H, B);
-    if (dtype == HSA_DTYPE_BF16) join_kernel<uint16_t, D><<<grid, 256, 0, s>>>(p);
-    else join_kernel<float, D><<<grid, 256, 0, s>>>(p);
+    // a workgroup a row while the rows alone do not fill the chip
+    if ((int64_t)p.n_q * p.H * B <= 1024) {
+      const dim3 grid(p.n_q * p.H, B);
+      if (dtype == HSA_DTYPE_BF16) join_row_kernel<uint16_t, D><<<grid, 512, 0, s>>>(p);
+      else join_row_kernel<float, D><<<grid, 512, 0, s>>>(p);
+    } else {
+      const int per = 256 / (D / 4);
+      const dim3 grid((p.part_rows + per - 1) / per * p.Hk, B);
+      if (dtype == HSA_DTYPE_BF16) join_rows_kernel<uint16_t, D><<<grid, 256, 0, s>>>(p);
+      else join_rows_kernel<float, D><<<grid, 256, 0, s>>>(p);
+    }
   }
   return hipGetLastError();
 }
@@ -431,24 +895,48 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
 }  // namespace
 
 void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel) {
-  const int64_t rows = (int64_t)p.n_q * p.G;
-  const int most = dtype == HSA_DTYPE_BF16 ? 4 : 2;
-  p.rows_per_item = 16 * (rows <= 16 ? 1 : (rows <= 32 ? 2 : most));
-  p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
-  p.part_rows = p.n_rt * p.rows_per_item;
   p.nb = (p.P + 63) / 64;
   p.tpp = p.P < 64 ? 1 : p.nb;
   p.ppt = p.P < 64 && 64 % p.P == 0 ? 64 / p.P : 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
-  const int64_t tiles = p.ppt > 1 ? (list + p.ppt - 1) / p.ppt : list * p.tpp;
+  const int64_t tiles = std::max<int64_t>(1, p.ppt > 1 ? (list + p.ppt - 1) / p.ppt : list * p.tpp);
+  const int64_t rows = (int64_t)p.n_q * p.G;
+  const bool many = dtype == HSA_DTYPE_BF16 && rows > 64 && p.P >= 64;
+  // A list of up to 32 tiles is not split: eight waves take up to four tiles each, and one
+  // launch does it all.
+  const bool brief = !many && tiles <= 32 && (rows <= 16 || (int64_t)B * p.Hk * ((rows + 15) / 16) <= 256);
+  const int most = dtype == HSA_DTYPE_BF16 ? 64 : 32;
+  p.rows_per_item = many ? kManyRows : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
+  p.waves = brief ? 8 : 4;
+  p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
+  p.part_rows = p.n_rt * p.rows_per_item;
   const int64_t items = (int64_t)B * p.Hk * p.n_rt;
-  // about four workgroups a CU, pieces of at least eight tiles (two a wave)
-  int64_t n = (1024 + items - 1) / items;
-  n = std::max<int64_t>(1, std::min<int64_t>(n, (tiles + 7) / 8));
-  int64_t c = std::max<int64_t>(1, (tiles + n - 1) / n);
-  c = (c + kWaves - 1) / kWaves * kWaves;
+  int64_t n = 1;
+  if (many) {
+    // one workgroup a CU (two with d = 64): rounds of as many, each of its tiles and about
+    // six more for its start and end; pieces cost a partial output of 256 rows written
+    // and read again (four)
+    const int64_t slots = p.d == 128 ? 256 : 512;
+    double best = 1e300;
+    for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
+      const double t = (double)((items * k + slots - 1) / slots) * ((double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0));
+      if (t < 0.97 * best) {
+        best = t;
+        n = k;
+      }
+    }
+  } else if (!brief) {
+    // Two resident workgroups a CU: 512 of at least 16 tiles, or, so that sequences of
+    // different lengths balance, up to 2048 of at least 32 (shorter ones lose more
+    // to their start than they balance).
+    const int64_t some = std::min((512 + items - 1) / items, tiles / 16);
+    const int64_t more = std::min((2048 + items - 1) / items, tiles / 32);
+    n = std::max<int64_t>(1, std::min<int64_t>(std::max(some, more), kMaxSplit));
+  }
+  int64_t c = (tiles + n - 1) / n;
+  if (!many) c = (c + p.waves - 1) / p.waves * p.waves;
   p.split_tiles = (int)c;
-  p.n_split = (int)std::max<int64_t>(1, (tiles + c - 1) / c);
+  p.n_split = (int)((tiles + c - 1) / c);
 }
 
 size_t cache8_part_bytes(int64_t B, int64_t Hk, int64_t n_split, int64_t part_rows, int64_t d) {

@@ -242,6 +242,7 @@ struct Cache8AttnParams {
   int32_t nb;                 // scale blocks per page
   int32_t tpp, ppt;           // 64-key tiles per page; pages per tile
   int32_t rows_per_item, n_rt, part_rows;
+  int32_t waves;              // of a few-rows workgroup
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
 };
 

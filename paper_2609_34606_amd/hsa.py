@@ -64,11 +64,12 @@ class LibraryNotBuilt(RuntimeError):
 
 
 _lib = None
+_torch = None  # torch, once the library is loaded
 
 
 def lib():
     """The loaded libhsa.so; raises if it has not been built."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -77,7 +78,8 @@ def lib():
     # that copy (same soname). Loaded the other way round, torch loads its own
     # copy beside the system one, and memory and streams of one runtime are
     # not valid in the other (the library's launches then fail).
-    import torch  # noqa: F401
+    import torch
+    _torch = torch
     L = ctypes.CDLL(LIB_PATH)
     P = ctypes.POINTER
     L.hsa_status_string.restype = ctypes.c_char_p
@@ -633,54 +635,52 @@ def cache8_pool(k, v, k_exp, v_exp, page_table, cfg: HsaConfig) -> HsaCache8Pool
 
 
 # The calls below may serve a single token, where the host's time counts: their checks
-# compare types, shapes and devices without building strings or objects.
+# compare types, shapes and devices without building strings or objects. Each takes the
+# library first (lib()), which sets _torch.
 def _i32s(t, n: int, dev: int, what: str) -> Optional[int]:
     """Address of a contiguous int32 tensor of n elements on device dev, or None."""
     if t is None:
         return None
-    import torch
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not _torch.int32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must hold {n} contiguous int32 values, got {tuple(t.shape)} {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{what} is on {t.device}, not on the call's device")
     return t.data_ptr()
 
 
-def _strided(cfg, t, n: int, heads: int, dev: Optional[int], what: str):
-    """(address, batch stride, token stride, device) of a [B, n, heads, d] tensor whose
-    heads are contiguous within a token."""
-    import torch
-    d = cfg.head_dim
-    if t.dtype is not (torch.bfloat16 if cfg.dtype == HSA_DTYPE_BF16 else torch.float32) or \
-            t.shape != (cfg.batch, n, heads, d):
-        raise ValueError(f"{what} must be {_elem_dtype(cfg)} {(cfg.batch, n, heads, d)}, got "
-                         f"{t.dtype} {tuple(t.shape)}")
+def _strided(shape, dtype, t, what: str):
+    """(batch stride, token stride, device) of a [B, n, heads, d] tensor whose heads
+    are contiguous within a token."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     sb, st, sh, sd = t.stride()
-    if (sd != 1 or (sh != d and heads > 1)) and t.numel():
+    if (sd != 1 or sh != shape[3]) and (sd != 1 or shape[2] > 1) and t.numel():
         raise ValueError(f"{what}: the heads of a token must be contiguous, got strides {t.stride()}")
-    at = t.get_device()
-    if dev is not None and at != dev:
-        raise ValueError(f"{what} is on {t.device}, not on the call's device")
-    return t.data_ptr(), sb, st, at
+    return sb, st, t.get_device()
 
 
-def _contiguous(cfg, t, n: int, dev: Optional[int], what: str):
-    """(address, device) of a contiguous [B, n, num_heads, d] tensor."""
-    p, _, _, at = _strided(cfg, t, n, cfg.num_heads, dev, what)
-    if not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return p, at
+def _elem(cfg):
+    return _torch.bfloat16 if cfg.dtype == HSA_DTYPE_BF16 else _torch.float32
+
+
+def _apart(what: str, t):
+    return ValueError(f"{what} is on {t.device}, not on the call's device")
 
 
 def _call(fn, dev: int, stream, *args) -> int:
     """fn(*args, stream) with the tensors' device current (kernels launch there)."""
-    import torch
     if dev < 0:
         raise ValueError("the tensors must be on a GPU")
-    if dev != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            return _call(fn, dev, stream, *args)
-    return fn(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream))
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return fn(*args, _raw_stream(dev, stream))
+    return fn(*args, _raw_stream(dev, stream))
+
+
+def _raw_stream(dev: int, stream) -> int:
+    if stream is not None:
+        return int(getattr(stream, "cuda_stream", stream))
+    return _torch._C._cuda_getCurrentRawStream(dev)
 
 
 def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None,
@@ -688,25 +688,35 @@ def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stre
     """Turns x [B, n, heads, d] by its tokens' positions (pos int32 [B, n, axes], or
     first int32 [B] + the token's index) into o (x itself, or apart from it).
     inverse: by the opposite angles, the gradient's map."""
+    fn = lib().hsa_rope_apply
+    B = cfg.batch
     heads = x.shape[2] if x.dim() == 4 else 0
-    xp, xb, xt, dev = _strided(cfg, x, n, heads, None, "x")
-    op, ob, ot, _ = _strided(cfg, o, n, heads, dev, "o")
-    st = _call(lib().hsa_rope_apply, dev, stream, ctypes.byref(cfg), ctypes.byref(rope), xp, xb, xt, n, heads,
-               _i32s(pos, cfg.batch * n * rope.axes, dev, "pos"), _i32s(first, cfg.batch, dev, "first"),
-               1 if inverse else 0, op, ob, ot)
-    if check:
+    shape, dtype = (B, n, heads, cfg.head_dim), _elem(cfg)
+    xb, xt, dev = _strided(shape, dtype, x, "x")
+    ob, ot, at = _strided(shape, dtype, o, "o")
+    if at != dev:
+        raise _apart("o", o)
+    st = _call(fn, dev, stream, ctypes.byref(cfg), ctypes.byref(rope), x.data_ptr(), xb, xt, n, heads,
+               None if pos is None else _i32s(pos, B * n * rope.axes, dev, "pos"),
+               None if first is None else _i32s(first, B, dev, "first"), 1 if inverse else 0, o.data_ptr(), ob, ot)
+    if check and st:
         _check("hsa_rope_apply", st)
     return st
 
 
 def _token_write(name, fn, cfg, pool, heads, k_src, v_src, n, rope, pos, first, count, stream, check) -> int:
-    kp, kb, kt, dev = _strided(cfg, k_src, n, heads, None, "k_src")
-    vp, vb, vt, _ = _strided(cfg, v_src, n, heads, dev, "v_src")
+    B = cfg.batch
+    shape, dtype = (B, n, heads, cfg.head_dim), _elem(cfg)
+    kb, kt, dev = _strided(shape, dtype, k_src, "k_src")
+    vb, vt, at = _strided(shape, dtype, v_src, "v_src")
+    if at != dev:
+        raise _apart("v_src", v_src)
     st = _call(fn, dev, stream, ctypes.byref(cfg), ctypes.byref(pool),
-               None if rope is None else ctypes.byref(rope), kp, kb, kt, vp, vb, vt, n,
-               None if rope is None else _i32s(pos, cfg.batch * n * rope.axes, dev, "pos"),
-               _i32s(first, cfg.batch, dev, "first"), _i32s(count, cfg.batch, dev, "count"))
-    if check:
+               None if rope is None else ctypes.byref(rope), k_src.data_ptr(), kb, kt, v_src.data_ptr(), vb, vt, n,
+               None if rope is None or pos is None else _i32s(pos, B * n * rope.axes, dev, "pos"),
+               None if first is None else _i32s(first, B, dev, "first"),
+               None if count is None else _i32s(count, B, dev, "count"))
+    if check and st:
         _check(name, st)
     return st
 
@@ -734,38 +744,45 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
                     q_len=None, causal=False, ws=None, stream=None, check=True) -> int:
     """Attention of q [B, n_q, H, d] over the 8-bit cache's listed pages: sel int32 [B,
     kv_heads, k_max], then [cur_first_page, + n_cur_pages); tokens below kv_len[b]."""
-    import torch
-    B = cfg.batch
-    qp, dev = _contiguous(cfg, q, n_q, None, "q")
-    op, _ = _contiguous(cfg, o, n_q, dev, "o")
-    if lse is None:
-        lp = None
-    else:
-        if lse.dtype is not torch.float32 or lse.shape != (B, cfg.num_heads, n_q) or not lse.is_contiguous():
-            raise ValueError(f"lse must be contiguous float32 {(B, cfg.num_heads, n_q)}, got {lse.dtype} "
-                             f"{tuple(lse.shape)}")
+    L = lib()
+    B, H, dtype = cfg.batch, cfg.num_heads, _elem(cfg)
+    shape = (B, n_q, H, cfg.head_dim)
+    for t, what in ((q, "q"), (o, "o")):
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    dev = q.get_device()
+    if o.get_device() != dev:
+        raise _apart("o", o)
+    lp = kp = keep = None
+    if lse is not None:
+        if lse.dtype is not _torch.float32 or lse.shape != (B, H, n_q) or not lse.is_contiguous():
+            raise ValueError(f"lse must be contiguous float32 {(B, H, n_q)}, got {lse.dtype} {tuple(lse.shape)}")
         if lse.get_device() != dev:
-            raise ValueError(f"lse is on {lse.device}, not on the call's device")
+            raise _apart("lse", lse)
         lp = lse.data_ptr()
-    sp = _i32s(sel, B * cache.kv_heads * k_max, dev, "sel")
-    kvp, qlp = _i32s(kv_len, B, dev, "kv_len"), _i32s(q_len, B, dev, "q_len")
-    if k_h is not None and len(k_h) != cache.kv_heads:
-        raise ValueError(f"k_h must hold {cache.kv_heads} budgets, got {len(k_h)}")
-    _keep, kp = _budgets(k_h)
+    if k_h is not None:
+        if len(k_h) != cache.kv_heads:
+            raise ValueError(f"k_h must hold {cache.kv_heads} budgets, got {len(k_h)}")
+        keep = (c_i32 * len(k_h))(*[int(k) for k in k_h])
+        kp = ctypes.addressof(keep)
+    sp = None if sel is None else _i32s(sel, B * cache.kv_heads * k_max, dev, "sel")
+    kvp = None if kv_len is None else _i32s(kv_len, B, dev, "kv_len")
+    qlp = None if q_len is None else _i32s(q_len, B, dev, "q_len")
+    cp, hp = ctypes.byref(cfg), ctypes.byref(cache)
     if ws is None:
-        nbytes = lib().hsa_cache8_attn_workspace_size(ctypes.byref(cfg), n_q, cache.kv_heads, k_max, n_cur_pages)
-        wp = None
+        wp, nbytes = None, L.hsa_cache8_attn_workspace_size(cp, n_q, cache.kv_heads, k_max, n_cur_pages)
         if nbytes:
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            ws = _torch.empty(nbytes, dtype=_torch.uint8, device=q.device)
             wp = ws.data_ptr()
             if stream is not None and dev >= 0:  # not reused before that stream is done with it
-                ws.record_stream(stream if isinstance(stream, torch.cuda.Stream) else
-                                 torch.cuda.ExternalStream(int(stream), device=q.device))
+                ws.record_stream(stream if isinstance(stream, _torch.cuda.Stream) else
+                                 _torch.cuda.ExternalStream(int(stream), device=q.device))
     else:
         wp, nbytes = _ptr(ws), ws.numel() * ws.element_size()
-    st = _call(lib().hsa_cache8_attn, dev, stream, ctypes.byref(cfg), qp, n_q, ctypes.byref(cache), sp, k_max, kp,
-               cur_first_page, n_cur_pages, kvp, qlp, 1 if causal else 0, op, lp, wp, nbytes)
-    if check:
+    st = _call(L.hsa_cache8_attn, dev, stream, cp, q.data_ptr(), n_q, hp, sp, k_max, kp, cur_first_page, n_cur_pages, kvp,
+               qlp, 1 if causal else 0, o.data_ptr(), lp, wp, nbytes)
+    del keep
+    if check and st:
         _check("hsa_cache8_attn", st)
     return st
 

@@ -113,9 +113,11 @@ def test_attention_refusals():
     assert attn(cache=_cache(kv_heads=3)) == 1
     assert attn(cache=_cache(max_pages=1 << 23)) == 2
     assert attn(cfg=P.config(70000, 4, 64, 256, "bf16")) == 2
-    size = P.hsa_cache8_attn_workspace_size(cfg, 2, 2, 0, 4)
+    long = _cache(max_pages=400)
+    size = P.hsa_cache8_attn_workspace_size(cfg, 2, 2, 0, 400)
     assert size > 0 and size % 256 == 0
-    assert attn() == 4 and attn(ws=FAKE, nb=size - 1) == 4 and attn(ws=FAKE + 16, nb=size) == 4
+    for ws, nb in ((None, 0), (FAKE, size - 1), (FAKE + 16, size)):
+        assert attn(cache=long, n=400, ws=ws, nb=nb) == 4
     for bad in ((0, 2, 0, 4), (2, 3, 0, 4), (2, 2, -1, 4), (2, 2, 0, 0), (2, 0, 0, 4)):
         assert P.hsa_cache8_attn_workspace_size(cfg, *bad) == 0
     assert P.hsa_cache8_attn_workspace_size(P.config(1, 4, 96, 256, "bf16"), 2, 2, 0, 4) == 0
