@@ -717,7 +717,7 @@ typedef struct hsa_cache8 {
   void* v_exp;
   const int32_t* page_table; /* device [B, max_pages] */
   int32_t num_slots;
-  int32_t max_pages;         /* max_pages * P < 2^31 - 128 */
+  int32_t max_pages;         /* max_pages * P < 2^31 - 256, P <= 2^24 */
   int32_t kv_heads;          /* divides cfg->num_heads (the query heads) */
 } hsa_cache8_t;
 

@@ -1203,9 +1203,11 @@ hsa_status_t check_cache8(const hsa_config_t* c, const hsa_cache8_t* a) {
   return HSA_OK;
 }
 
-// A sequence's tokens are counted in 32 bits, with room for a tile past the end.
+// A sequence's tokens are counted in 32 bits, with room for a tile past the end, and a page's
+// value rows are addressed in 32.
 hsa_status_t check_table(const hsa_config_t* c, int32_t max_pages) {
-  return (int64_t)max_pages * c->page_size >= (1LL << 31) - 128 ? HSA_ERR_UNSUPPORTED : HSA_OK;
+  if (c->page_size > 1 << 24) return HSA_ERR_UNSUPPORTED;
+  return (int64_t)max_pages * c->page_size >= (1LL << 31) - 256 ? HSA_ERR_UNSUPPORTED : HSA_OK;
 }
 
 // With HSA_CHECK=1: n int32 values of device memory (`missing` where there are none).

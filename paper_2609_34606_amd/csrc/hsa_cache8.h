@@ -13,7 +13,8 @@ namespace hsa {
 // The list is n_sel selected pages, then pages [cur_first, ..); a page of 64 tokens or more is
 // tpp tiles (its last one shifted back to end at the page's end); of pages below 64
 // tokens, ppt whole ones share a tile where their size divides 64, and else each
-// has a tile of its own.
+// has a tile of its own. Many-rows items (stream) cut the listed tokens every 64 instead,
+// whatever pages they are in.
 struct Cache8Walk {
   int len, q_len;  // tokens and queries of the sequence
   int base;        // causal: query i sees tokens below base + i + 1
@@ -38,13 +39,16 @@ __device__ __forceinline__ Cache8Walk cache8_walk(const Cache8AttnParams& p, int
   w.base = w.len - w.q_len;
   const int last = min(row0 + rows, w.q_len * p.G);  // row past the last one
   w.rows = last - row0;
-  w.lim = cache8_limit(p, w, (last - 1) / p.G);
-  w.n_sel = min(count_selected(p.sel + ((size_t)b * p.Hk + h) * p.k_max, p.k_max, p.max_pages, lane),
-                (int)p.k_h[h]);
+  w.lim = cache8_limit(p, w, __builtin_amdgcn_readfirstlane((last - 1) / p.G));
+  w.n_sel = __builtin_amdgcn_readfirstlane(
+      min(count_selected(p.sel + ((size_t)b * p.Hk + h) * p.k_max, p.k_max, p.max_pages, lane), (int)p.k_h[h]));
   const int cur = clampi(w.lim - p.cur_first * p.P, 0, p.n_cur * p.P);  // tokens of the run of pages
-  w.n_list = w.n_sel + (cur + p.P - 1) / p.P;
-  w.n_tiles = p.ppt > 1 ? (w.n_list + p.ppt - 1) / p.ppt
-                        : w.n_sel * p.tpp + cur / p.P * p.tpp + (cur % p.P + 63) / 64;
+  // (quotients come from the vector unit: what follows from them is brought back)
+  const int full = __builtin_amdgcn_readfirstlane(cur / p.P), rest = cur - full * p.P;
+  w.n_list = w.n_sel + full + (rest > 0 ? 1 : 0);
+  if (p.stream) w.n_tiles = (int)(((int64_t)w.n_sel * p.P + cur + 63) >> 6);
+  else if (p.ppt > 1) w.n_tiles = __builtin_amdgcn_readfirstlane((w.n_list + p.ppt - 1) / p.ppt);
+  else w.n_tiles = w.n_sel * p.tpp + full * p.tpp + (rest + 63) / 64;
   return w;
 }
 

@@ -93,9 +93,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
   // sequences begin one apart, so that no XCD gets only last pieces, which short
   // sequences lack (32 sequences of 1 to 16384 tokens: %%% us, pieces together 154).
   const int n_items = p.Hk * p.n_rt, b = blockIdx.y;
-  const int x0 = (int)((blockIdx.x + blockIdx.y) % gridDim.x);
-  const int split = x0 / n_items, item = x0 - split * n_items;
-  const int rt = item / p.Hk, h = item - rt * p.Hk;
+  const int x0 = __builtin_amdgcn_readfirstlane((int)((blockIdx.x + blockIdx.y) % gridDim.x));
+  // (a quotient comes from the vector unit, and its uses would stay there)
+  const int split = __builtin_amdgcn_readfirstlane(x0 / n_items), item = x0 - split * n_items;
+  const int rt = __builtin_amdgcn_readfirstlane(item / p.Hk), h = item - rt * p.Hk;
   const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, lane);
   if (w.rows <= 0) return;
   const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
 #pragma unroll
       for (int u = 0; u < 2; ++u) split_row<T, kParts>(q + 64 * c + 16 * g + 8 * u, qf[n][c][u]);
   }
-  const int lim_first = cache8_limit(p, w, rt * kRows / p.G);  // the least of them
+  const int lim_first = cache8_limit(p, w, __builtin_amdgcn_readfirstlane(rt * kRows / p.G));  // the least of them
 
   f32x4 acc[kCols][M];
   float m_run[kCols], l_run[kCols];
@@ -144,13 +145,27 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
   const int rho = 4 * (c16 >> 2);  // key row of the lane in score block i: 4 rho + 4 i + c16 % 4
   int li = 0, kt = 0, li_next = 0, kt_next = 0;  // list position and tile within its page
   if constexpr (!kSmallP) {
-    li = (t_lo + wave) / p.tpp;
+    li = __builtin_amdgcn_readfirstlane((t_lo + wave) / p.tpp);
     kt = (t_lo + wave) - li * p.tpp;
   }
-  // The tile's page, and that of the wave's next tile: looked up a tile ahead.
+  // The tile's page, and that of the wave's next tile: looked up a tile ahead. Small pages: the
+  // slots of the lane's two key and two value granules (8 tokens), and the values' first tokens.
   int lp = 0, slot = 0, lp_next = 0, slot_next = 0;
+  int ks[2], vs[2], vt[2], ks_next[2], vs_next[2], vt_next[2];
+  auto look_up = [&](int t, int (&k)[2], int (&v)[2], int (&first)[2]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {  // keys 4 rho + 8 u + 0..7: score blocks 2 u and 2 u + 1
+      const Cache8Granule a = cache8_granule(p, w, t, (rho >> 1) + u), c = cache8_granule(p, w, t, 2 * g + u);
+      k[u] = slot_v(p, ptrow, page_v(p, w, selrow, a.li));
+      const int page = page_v(p, w, selrow, c.li);
+      v[u] = slot_v(p, ptrow, page);
+      first[u] = c.ok ? page * p.P + c.off : INT_MAX - 8;
+    }
+  };
   auto look_ahead = [&](int t) {
-    if constexpr (!kSmallP) {
+    if constexpr (kSmallP) {
+      if (t + kWaves < t_hi) look_up(t + kWaves, ks_next, vs_next, vt_next);
+    } else {
       kt_next = kt + kWaves;
       li_next = li;
       while (kt_next >= p.tpp) {
@@ -175,10 +190,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
       ksc[0] = ksc[1] = scale_of(p.k_exp[head * p.nb + kt]);
     } else {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {  // keys 4 rho + 8 u + 0..7: score blocks 2 u and 2 u + 1
-        const int gr = (rho >> 1) + u;
-        const Cache8Granule a = cache8_granule(p, w, t, gr);
-        const size_t head = (size_t)slot_v(p, ptrow, page_v(p, w, selrow, a.li)) * p.Hk + h;
+      for (int u = 0; u < 2; ++u) {
+        const Cache8Granule a = cache8_granule(p, w, t, (rho >> 1) + u);
+        const size_t head = (size_t)ks[u] * p.Hk + h;
         ksc[u] = scale_of(p.k_exp[head * p.nb]);
         const uint8_t* kb = p.k + (head * p.P + a.off + (c16 & 3)) * D + 16 * g;
 #pragma unroll
@@ -202,17 +216,26 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
       vsc[0] = vsc[1] = scale_of(p.v_exp[head * p.nb + kt]);
     } else {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const Cache8Granule a = cache8_granule(p, w, t, 2 * g + u);
-        const int page = page_v(p, w, selrow, a.li);
-        const size_t head = (size_t)slot_v(p, ptrow, page) * p.Hk + h;
-        vsc[u] = scale_of(p.v_exp[head * p.nb]);
-        const uint8_t* vb = p.v + (head * D + c16) * p.P + a.off;
+      for (int u = 0; u < 2; ++u) vsc[u] = scale_of(p.v_exp[((size_t)vs[u] * p.Hk + h) * p.nb]);
+      if (p.P % 16 == 0) {  // both granules are of one page
+        const Cache8Granule a = cache8_granule(p, w, t, 2 * g);
+        const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + a.off;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-          const u32x2a8 x = *reinterpret_cast<const u32x2a8*>(vb + (size_t)(16 * m) * p.P);
-          vc[m][2 * u] = x[0];
-          vc[m][2 * u + 1] = x[1];
+          const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(vb + (size_t)(16 * m) * p.P);
+          vc[m] = u32x4{x[0], x[1], x[2], x[3]};
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const Cache8Granule a = cache8_granule(p, w, t, 2 * g + u);
+          const uint8_t* vb = p.v + (((size_t)vs[u] * p.Hk + h) * D + c16) * p.P + a.off;
+#pragma unroll
+          for (int m = 0; m < M; ++m) {
+            const u32x2a8 x = *reinterpret_cast<const u32x2a8*>(vb + (size_t)(16 * m) * p.P);
+            vc[m][2 * u] = x[0];
+            vc[m][2 * u + 1] = x[1];
+          }
         }
       }
     }
@@ -226,17 +249,16 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
       tok[1] = w0 + 16 * g + 8 >= kt * 64 ? first + 8 : INT_MAX - 8;
       masked = kt * 64 > p.P - 64 || lp * p.P + kt * 64 + 64 > lim_first;
     } else {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const Cache8Granule a = cache8_granule(p, w, t, 2 * g + u);
-        tok[u] = a.ok ? page_v(p, w, selrow, a.li) * p.P + a.off : INT_MAX - 8;
-      }
+      tok[0] = vt[0];
+      tok[1] = vt[1];
       masked = true;
     }
   };
 
   if (t_lo + wave < t_hi) {
-    if constexpr (!kSmallP) {
+    if constexpr (kSmallP) {
+      look_up(t_lo + wave, ks, vs, vt);
+    } else {
       lp = page_of(li);
       slot = slot_of(lp);
     }
@@ -265,6 +287,14 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
             for (int k = 0; k < kParts; ++k) s[n][i] = mfma16(a, qf[n][c][u][k], s[n][i]);
         }
     // the next tile's keys take the registers of these
+    if constexpr (kSmallP) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        ks[u] = ks_next[u];
+        vs[u] = vs_next[u];
+        vt[u] = vt_next[u];
+      }
+    }
     lp = lp_next;
     slot = slot_next;
     li = li_next;
@@ -413,25 +443,33 @@ struct ManyLayout {
   static __device__ __forceinline__ int swz_v(int row) { return (row >> 1) & 7; }
 };
 
-constexpr int kManyRows = 256;  // query rows of a many-rows item
+constexpr int many_rows(int d) { return d == 128 ? 256 : 128; }  // query rows of a many-rows item
 
 template <int D, int kW, int QB>
-__global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnParams p) {
+__global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cache8AttnParams p) {
   using L = ManyLayout<D>;
   constexpr int KK = D / 16, NM = D / 32;
-  constexpr int kThreads = 64 * kW;
-  static_assert(32 * QB * kW == kManyRows, "rows of an item");
-  static_assert(4 * D == kThreads, "a thread converts 16 codes of keys and 16 of values a tile");
+  constexpr int kThreads = 64 * kW, kRows = many_rows(D);
+  static_assert(32 * QB * kW == kRows, "rows of an item");
+  constexpr int kLd = 4 * D;  // threads that convert: 16 codes of keys and 16 of values each
+  static_assert(kLd <= kThreads, "a tile's codes are 16 a thread");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // workgroup i runs on XCD i % 8: an XCD takes consecutive items, which share their pages in
-  // its L2
+  // workgroup i runs on XCD i % 8: an XCD takes an eighth of the items in a row, which share
+  // their pages in its L2, first pieces first (a causal item's last pieces may be empty: the
+  // workgroups of a CU, 32 apart, should not all be first pieces)
   const int n_wg = gridDim.x, x8 = blockIdx.x & 7;
   const int id = x8 * (n_wg >> 3) + min(x8, n_wg & 7) + (blockIdx.x >> 3);
-  const int item = id / p.n_split, split = id - item * p.n_split, b = blockIdx.y;
-  const int h = item / p.n_rt, rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
-  const Cache8Walk w = cache8_walk(p, b, h, rt * kManyRows, kManyRows, lane);
+  const int n_items = p.Hk * p.n_rt, share = (n_items + 7) >> 3;
+  // (a quotient comes from the vector unit, and its uses would stay there)
+  const int group = __builtin_amdgcn_readfirstlane(id / (share * p.n_split)), in = id - group * share * p.n_split;
+  const int members = min(share, n_items - group * share);
+  const int split = __builtin_amdgcn_readfirstlane(in / members), item = group * share + in - split * members;
+  const int b = blockIdx.y;
+  const int h = __builtin_amdgcn_readfirstlane(item / p.n_rt);
+  const int rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
+  const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, lane);
   if (w.rows <= 0) return;
   const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
   if (split > 0 && t_lo >= w.n_tiles) return;
@@ -441,7 +479,7 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
   // queries
   u32x4 qf[QB][KK];
   int lim[QB];
-  const int row0 = rt * kManyRows + wave * 32 * QB;
+  const int row0 = rt * kRows + wave * 32 * QB;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     const int r = row0 + 32 * qb + l32, i = min(r / p.G, w.q_len - 1);
@@ -451,53 +489,74 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qf[qb][kk] = ld_global16(q + 16 * kk);
   }
-  const int lim_first = cache8_limit(p, w, min(row0 / p.G, w.q_len - 1));
-  const bool active = row0 < rt * kManyRows + w.rows;
+  const int lim_first = cache8_limit(p, w, min(__builtin_amdgcn_readfirstlane(row0 / p.G), w.q_len - 1));
+  const bool active = row0 < rt * kRows + w.rows;
 
-  // The tiles' stream: list position and tile within its page of the next keys to load. Slots
-  // are looked up with vector loads, a page ahead (logical page: two), so that
+  // The listed pages are one stream of tokens, cut into tiles of 64; a tile lies in one page or
+  // in two (pages hold 64 tokens or more). off: the next tile's first token within its
+  // page. Slots are looked up with vector loads, a page ahead (logical pages: two), so that
   // they never wait and leave the LDS counter alone.
   const int32_t* selrow = p.sel + ((size_t)b * p.Hk + h) * p.k_max;
   const int32_t* ptrow = p.page_table + (size_t)b * p.max_pages;
-  const int last_li = max(w.n_list - 1, 0);
   int zero = 0;
   asm volatile("" : "+v"(zero));  // (keeps the lookups vector loads)
   auto page_at = [&](int li) __attribute__((always_inline)) {
-    li = min(li, last_li);
+    if (li >= w.n_list) return -1 + zero;  // past the end
     return li < w.n_sel ? selrow[li + zero] : p.cur_first + li - w.n_sel + zero;
   };
-  auto slot_at = [&](int lp) __attribute__((always_inline)) { return clampi(ptrow[clampi(lp, 0, p.max_pages - 1)], 0, p.num_slots - 1); };
+  auto slot_at = [&](int lp) __attribute__((always_inline)) {
+    return clampi(ptrow[clampi(lp, 0, p.max_pages - 1)], 0, p.num_slots - 1);
+  };
   int kbuf = 0;  // key buffer of tile t
-  int li = t_lo / p.tpp, kt = t_lo - li * p.tpp;
+  int li = __builtin_amdgcn_readfirstlane((int)((int64_t)t_lo * 64 / p.P));
+  int off = (int)((int64_t)t_lo * 64 - (int64_t)li * p.P);
   int lp_cur = page_at(li), lp_nxt = page_at(li + 1), lp_nx2 = page_at(li + 2);
   int slot_cur = slot_at(lp_cur), slot_nxt = slot_at(lp_nxt);
 
+  // What a tile is read and masked by: its first page's slot, the one after, its first token within
+  // the first; and the logical tokens: key j is token ta + j below cut, tb + j from there on.
+  struct Tile {
+    int slot_a, slot_b, off, ta, tb, cut;
+  };
+  // the tiles t, t + 1, .. t + 3, once load_k has moved on
+  Tile ring[4];
   u32x4 kc, vc;  // the codes of the next tiles, 16 a thread
-  uint32_t ke = 0, ve = 0;
-  size_t head_v = 0;   // the value tile one behind the keys
-  int kt_v = 0;
-  // logical token of each tile's first key and the tokens a tile at its page's
-  // end is shifted back by: of the tiles t, t + 1, .. t + 3
-  int tok[4], back[4];
-  auto load_k = [&]() __attribute__((always_inline)) {  // the next tile's keys; its place moves on
-    const int slot = __builtin_amdgcn_readfirstlane(slot_cur), lp = __builtin_amdgcn_readfirstlane(lp_cur);
-    const size_t head = (size_t)slot * p.Hk + h;
-    const int w0 = min(kt * 64, p.P - 64);
-    const uint8_t* kb = p.k + (head * p.P + w0) * D;
-    kc = ld_global16(kb + 16 * tid);
-    ke = p.k_exp[head * p.nb + kt];
-    tok[0] = tok[1];
-    tok[1] = tok[2];
-    tok[2] = tok[3];
-    back[0] = back[1];
-    back[1] = back[2];
-    back[2] = back[3];
-    tok[3] = lp * p.P + w0;
-    back[3] = kt * 64 - w0;
-    head_v = head;
-    kt_v = kt;
-    if (++kt == p.tpp) {
-      kt = 0;
+  uint32_t ke = 0, ve0 = 0, ve1 = 0;
+  const bool loads = kLd == kThreads || wave < kLd / 64;
+  const int krow_ld = tid / (D / 16), vtok_ld = 16 * (tid & 3);
+  const uint32_t vplace = (uint32_t)(tid >> 2) * (uint32_t)p.P + vtok_ld;
+  // the page's slot and token of the tile's token x
+  auto place = [&](const Tile& t, int x, int& at) __attribute__((always_inline)) {
+    const bool second = x >= t.cut;
+    at = second ? x - t.cut : t.off + x;
+    return (size_t)(second ? t.slot_b : t.slot_a) * p.Hk + h;
+  };
+  auto load_k = [&]() __attribute__((always_inline)) {  // the next tile's keys; the stream moves on
+    ring[0] = ring[1];
+    ring[1] = ring[2];
+    ring[2] = ring[3];
+    Tile& t = ring[3];
+    const int lp = __builtin_amdgcn_readfirstlane(lp_cur), lp2 = __builtin_amdgcn_readfirstlane(lp_nxt);
+    t.slot_a = __builtin_amdgcn_readfirstlane(slot_cur);
+    t.slot_b = __builtin_amdgcn_readfirstlane(slot_nxt);
+    t.off = off;
+    t.cut = p.P - off;
+    t.ta = lp >= 0 ? lp * p.P + off : INT_MAX - 128;
+    t.tb = lp2 >= 0 ? lp2 * p.P - t.cut : INT_MAX - 128;
+    if (!loads) {
+    } else if (t.cut >= 64) {  // one page: its place is scalar
+      const size_t head = (size_t)t.slot_a * p.Hk + h;
+      kc = ld_global16(p.k + (head * p.P + t.off) * D + 16 * tid);
+      ke = p.k_exp[head * p.nb + ((uint32_t)(t.off + krow_ld) >> 6)];
+    } else {
+      int at;
+      const size_t head = place(t, krow_ld, at);
+      kc = ld_global16(p.k + (head * p.P + at) * D + 16 * (tid % (D / 16)));
+      ke = p.k_exp[head * p.nb + (at >> 6)];
+    }
+    off += 64;
+    if (off >= p.P) {
+      off -= p.P;
       ++li;
       lp_cur = lp_nxt;
       slot_cur = slot_nxt;
@@ -506,27 +565,49 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
       lp_nx2 = page_at(li + 2);
     }
   };
-  auto load_v = [&](size_t head, int at) __attribute__((always_inline)) {
-    const uint8_t* vb = p.v + head * D * p.P + min(at * 64, p.P - 64);
-    const u32x4a8 y = *reinterpret_cast<const u32x4a8*>(vb + (size_t)(tid >> 2) * p.P + 16 * (tid & 3));
-    vc = u32x4{y[0], y[1], y[2], y[3]};
-    ve = p.v_exp[head * p.nb + at];
+  auto load_v = [&](const Tile& t) __attribute__((always_inline)) {
+    if (!loads) return;
+    if (t.cut >= 64) {
+      const size_t head = (size_t)t.slot_a * p.Hk + h;
+      const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(p.v + head * D * p.P + t.off + vplace);
+      vc = u32x4{x[0], x[1], x[2], x[3]};
+      ve0 = p.v_exp[head * p.nb + ((uint32_t)(t.off + vtok_ld) >> 6)];
+      ve1 = p.v_exp[head * p.nb + ((uint32_t)(t.off + vtok_ld + 8) >> 6)];
+      return;
+    }
+    int at0, at1;
+    const size_t h0 = place(t, vtok_ld, at0), h1 = place(t, vtok_ld + 8, at1);
+    const u32x2a8 x = *reinterpret_cast<const u32x2a8*>(p.v + (h0 * D + (tid >> 2)) * p.P + at0);
+    const u32x2a8 y = *reinterpret_cast<const u32x2a8*>(p.v + (h1 * D + (tid >> 2)) * p.P + at1);
+    vc = u32x4{x[0], x[1], y[0], y[1]};
+    ve0 = p.v_exp[h0 * p.nb + (at0 >> 6)];
+    ve1 = p.v_exp[h1 * p.nb + (at1 >> 6)];
   };
   auto put_k = [&](int buf) __attribute__((always_inline)) {
+    if (!loads) return;
     const float s = scale_of(ke);
-    const int row = tid / (D / 16), c0 = 2 * (tid % (D / 16));
+    const int row = krow_ld, c0 = 2 * (tid % (D / 16));
     uint8_t* dst = smem + buf * L::kTileK + row * L::kRowK;
     *reinterpret_cast<u32x4*>(dst + ((c0 ^ L::swz_k(row)) << 4)) = codes_to_bf16(kc[0], kc[1], s);
     *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_k(row)) << 4)) = codes_to_bf16(kc[2], kc[3], s);
   };
-  auto put_v = [&](int buf, int t0) __attribute__((always_inline)) {
-    const float s = scale_of(ve);
-    // codes past the last token any row sees may be anything
-    if (t0 + 64 > w.lim) vc = keep_codes(vc, clampi(w.lim - t0 - 16 * (tid & 3), 0, 16));
+  // whether some query of limit `most` does not see some token of a tile
+  auto beyond = [&](const Tile& t, int most) __attribute__((always_inline)) {
+    return t.ta + min(t.cut, 64) > most || (t.cut < 64 && t.tb + 64 > most);
+  };
+  auto put_v = [&](int buf, const Tile& t) __attribute__((always_inline)) {
+    if (!loads) return;
+    if (beyond(t, w.lim)) {
+      // codes past the last token any row sees may be anything
+      const int t0 = (vtok_ld < t.cut ? t.ta : t.tb) + vtok_ld, t1 = (vtok_ld + 8 < t.cut ? t.ta : t.tb) + vtok_ld + 8;
+      const u32x4 lo = keep_codes(vc, clampi(w.lim - min(t0, w.lim), 0, 8));
+      const u32x4 hi = keep_codes(u32x4{0, 0, vc[2], vc[3]}, 8 + clampi(w.lim - min(t1, w.lim), 0, 8));
+      vc = u32x4{lo[0], lo[1], hi[2], hi[3]};
+    }
     const int row = tid >> 2, c0 = 2 * (tid & 3);
     uint8_t* dst = smem + L::kVBase + buf * L::kTileV + row * L::kRowV;
-    *reinterpret_cast<u32x4*>(dst + ((c0 ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[0], vc[1], s);
-    *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[2], vc[3], s);
+    *reinterpret_cast<u32x4*>(dst + ((c0 ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[0], vc[1], scale_of(ve0));
+    *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[2], vc[3], scale_of(ve1));
   };
 
   f32x16 acc[QB][NM], sa[QB], sb[QB];
@@ -540,17 +621,15 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
     for (int m = 0; m < NM; ++m) acc[qb][m] = f32x16{0};
   }
   const int krow = (l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // bits 2 and 3 swapped
-  uint32_t offk[KK], offv[4];
-#pragma unroll
-  for (int j = 0; j < KK; ++j) offk[j] = krow * L::kRowK + (((2 * j + half) ^ L::swz_k(krow)) << 4);
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) offv[ks] = l32 * L::kRowV + (((2 * ks + half) ^ L::swz_v(l32)) << 4);
-  // Operands: slice j of key half kh in key buffer buf; dim block m of 16-key group ks.
-  auto kop = [&](int buf, int kh, int j) __attribute__((always_inline)) {
-    return ld_lds16(smem + buf * L::kTileK + offk[j] + kh * 32 * L::kRowK);
+  // Operands: slice j of key half kh in key buffer buf; dim block m of 16-key group ks. A
+  // lane's chunks of a row are its first one's place with bits 5 to 7 turned.
+  const uint32_t kfirst = krow * L::kRowK + ((half ^ L::swz_k(krow)) << 4);
+  const uint32_t vfirst = l32 * L::kRowV + ((half ^ L::swz_v(l32)) << 4);
+  auto kop = [&](uint32_t at, int kh, int j) __attribute__((always_inline)) {
+    return ld_lds16(smem + (at ^ (j << 5)) + kh * 32 * L::kRowK);
   };
-  auto vop = [&](int buf, int ks, int m) __attribute__((always_inline)) {
-    return ld_lds16(smem + L::kVBase + buf * L::kTileV + offv[ks] + m * 32 * L::kRowV);
+  auto vop = [&](uint32_t at, int ks, int m) __attribute__((always_inline)) {
+    return ld_lds16(smem + (at ^ (ks << 5)) + m * 32 * L::kRowV);
   };
   // Two weights of 16-key group g of query block qb (score registers 8 g + 2 i, + 1), packed.
   auto weigh = [&](const f32x16 (&s)[QB], const float (&mc)[QB], int g, int qb, int i) __attribute__((always_inline)) {
@@ -559,14 +638,19 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
     l_run[qb] += x + y;
     return pack_bf16(x, y);
   };
-  // keys of half kh that a query does not see, or that the tile repeats
-  auto mask = [&](int first, int skip, int kh, f32x16 (&s)[QB]) __attribute__((always_inline)) {
+  // keys of half kh that a query does not see (the eight keys of a group are of one page)
+  auto mask = [&](const Tile& t, int kh, f32x16 (&s)[QB]) __attribute__((always_inline)) {
+    int mine = 32 * kh + 8 * half;
+    asm volatile("" : "+v"(mine));  // (nothing of this is kept through the walk)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = 32 * kh + 16 * (r >> 3) + 8 * half + (r & 7);
-        if (key < skip || first + key >= lim[qb]) s[qb][r] = -INFINITY;
+      for (int g = 0; g < 2; ++g) {
+        const int key = mine + 16 * g;
+        const int sees = lim[qb] - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r >= sees) s[qb][8 * g + r] = -INFINITY;
       }
   };
   // The largest of a half's scores, and the reference that follows it as in the few-rows kernel.
@@ -593,13 +677,12 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
     }
   };
   // Half a step: the softmax and value product of key half kh (scores s, value buffer vb), and
-  // the scores sn of the half after it: half nh of key buffer kb, of a tile that begins at token
-  // first and is shifted back by skip. It goes by pairs of matrix instructions, which share an
+  // the scores sn of the half after it: half nh of tile nt, in key buffer kb. It goes by pairs of matrix instructions, which share an
   // operand that was read four pairs before; between the pairs go the weights (those of the
   // first 16 keys two a pair and query block, so that their products can begin, those of the
   // second one), the conversion of the tiles to come, and the maximum. The order is the source's:
   // left to itself the compiler reads operands right before their use.
-  auto half_step = [&](int vb, int kh, const f32x16 (&s)[QB], int kb, int nh, int first, int skip, f32x16 (&sn)[QB],
+  auto half_step = [&](int vb, int kh, const f32x16 (&s)[QB], int kb, int nh, const Tile& nt, f32x16 (&sn)[QB],
                        auto&& tail) __attribute__((always_inline)) {
     constexpr int NP = KK + 2 * NM;                           // pairs
     constexpr int kFirst = KK / 2;                            // pairs that the first 16 keys' weights take
@@ -613,8 +696,10 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
       mx[qb] = -INFINITY;
       sn[qb] = f32x16{0};
     }
+    uint32_t k_at = kfirst + kb * L::kTileK, v_at = L::kVBase + vfirst + vb * L::kTileV;
+    asm volatile("" : "+v"(k_at), "+v"(v_at));  // (a place each, not one for every operand)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = kop(kb, nh, i);
+    for (int i = 0; i < 4; ++i) f[i] = kop(k_at, nh, i);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       // (what a pair computes from is opaque before it, and what it leaves is used in it)
@@ -629,8 +714,8 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
         if (i < KK) sn[qb] = mfma32(a, qf[qb][i], sn[qb]);
         else acc[qb][(i - KK) % NM] = mfma32(a, pk[(i - KK) / NM][qb], acc[qb][(i - KK) % NM]);
       }
-      if (n < KK) f[i & 3] = kop(kb, nh, n);
-      else if (n < NP) f[i & 3] = vop(vb, 2 * kh + (n - KK) / NM, (n - KK) % NM);
+      if (n < KK) f[i & 3] = kop(k_at, nh, n);
+      else if (n < NP) f[i & 3] = vop(v_at, 2 * kh + (n - KK) / NM, (n - KK) % NM);
       // packed weights: four a query block of each 16 keys
 #pragma unroll
       for (int x = 0; x < 4 * QB; ++x) {
@@ -659,8 +744,8 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
       if (i == KK) tail();
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (__builtin_expect(skip > 0 || first + 64 > lim_first, 0)) {
-      mask(first, skip, nh, sn);
+    if (__builtin_expect(beyond(nt, lim_first), 0)) {
+      mask(nt, nh, sn);
       largest(sn, mx);
     }
     raise(mx);
@@ -677,8 +762,8 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
     const int k0 = kbuf, k1 = kbuf == 2 ? 0 : kbuf + 1, k2 = k1 == 2 ? 0 : k1 + 1;
     kbuf = k1;
     auto next_v = [&]() __attribute__((always_inline)) {
-      put_v(1 - par, tok[2]);
-      load_v(head_v, kt_v);
+      put_v(1 - par, ring[2]);
+      load_v(ring[3]);
     };
     auto next_k = [&]() __attribute__((always_inline)) {
       put_k(k2);
@@ -689,26 +774,23 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
       next_k();
       return;
     }
-    // (tile t is tok[1] before load_k, tok[0] after it)
-    half_step(par, 0, sa, k0, 1, tok[1], back[1], sb, next_v);
-    half_step(par, 1, sb, k1, 0, tok[2], back[2], sa, next_k);
+    // (tile t is ring[1] before load_k, ring[0] after it)
+    half_step(par, 0, sa, k0, 1, ring[1], sb, next_v);
+    const Tile ahead = ring[2];
+    half_step(par, 1, sb, k1, 0, ahead, sa, next_k);
   };
 
   if (n > 0) {
     // K(0), K(1) and V(0) to LDS; K(2) and V(1) on their way
     load_k();
-    size_t hv = head_v;
-    int kv = kt_v;
-    load_v(hv, kv);
+    load_v(ring[3]);
     put_k(0);
     load_k();
-    put_v(0, tok[2]);
-    hv = head_v;
-    kv = kt_v;
+    put_v(0, ring[2]);
     put_k(1);
-    load_v(hv, kv);
+    load_v(ring[3]);
     load_k();
-    // tok[1] is tile 0 now
+    // (ring[1] is tile 0 now)
     lds_barrier();
     if (active) {
 #pragma unroll
@@ -716,8 +798,8 @@ __global__ __launch_bounds__(64 * kW, 8 / kW) void many_rows_kernel(Cache8AttnPa
 #pragma unroll
       for (int j = 0; j < KK; ++j)
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) sa[qb] = mfma32(kop(0, 0, j), qf[qb][j], sa[qb]);
-      if (back[1] > 0 || tok[1] + 64 > lim_first) mask(tok[1], back[1], 0, sa);
+        for (int qb = 0; qb < QB; ++qb) sa[qb] = mfma32(kop(kfirst, 0, j), qf[qb][j], sa[qb]);
+      if (beyond(ring[1], lim_first)) mask(ring[1], 0, sa);
       float mx[QB];
       largest(sa, mx);
       raise(mx);
@@ -867,11 +949,11 @@ template <int D>
 hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s) {
   const int cols = p.rows_per_item / 16;
   if (dtype == HSA_DTYPE_BF16) {
-    if (p.rows_per_item == kManyRows)
-      many_rows_kernel<D, D / 16, 128 / D><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
+    if (p.stream)
+      many_rows_kernel<D, D / 16, 1><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
     else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
     else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
-    else launch_rows<uint16_t, D, 4, 1>(p, B, s);
+    else if constexpr (D == 64) launch_rows<uint16_t, D, 4, 1>(p, B, s);
   } else {
     if (cols == 1) launch_rows<float, D, 1, 3>(p, B, s);
     else launch_rows<float, D, 2, 3>(p, B, s);
@@ -899,14 +981,16 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel) {
   p.tpp = p.P < 64 ? 1 : p.nb;
   p.ppt = p.P < 64 && 64 % p.P == 0 ? 64 / p.P : 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
-  const int64_t tiles = std::max<int64_t>(1, p.ppt > 1 ? (list + p.ppt - 1) / p.ppt : list * p.tpp);
   const int64_t rows = (int64_t)p.n_q * p.G;
   const bool many = dtype == HSA_DTYPE_BF16 && rows > 64 && p.P >= 64;
+  p.stream = many;
+  const int64_t tiles = std::max<int64_t>(
+      1, many ? (list * p.P + 63) / 64 : (p.ppt > 1 ? (list + p.ppt - 1) / p.ppt : list * p.tpp));
   // A list of up to 32 tiles is not split: eight waves take up to four tiles each, and one
   // launch does it all.
   const bool brief = !many && tiles <= 32 && (rows <= 16 || (int64_t)B * p.Hk * ((rows + 15) / 16) <= 256);
-  const int most = dtype == HSA_DTYPE_BF16 ? 64 : 32;
-  p.rows_per_item = many ? kManyRows : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
+  const int most = dtype == HSA_DTYPE_BF16 && p.d == 64 ? 64 : 32;
+  p.rows_per_item = many ? many_rows(p.d) : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
   p.waves = brief ? 8 : 4;
   p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
   p.part_rows = p.n_rt * p.rows_per_item;
@@ -916,7 +1000,7 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel) {
     // one workgroup a CU (two with d = 64): rounds of as many, each of its tiles and about
     // six more for its start and end; pieces cost a partial output of 256 rows written
     // and read again (four)
-    const int64_t slots = p.d == 128 ? 256 : 512;
+    const int64_t slots = p.d == 128 ? 256 : 768;
     double best = 1e300;
     for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
       const double t = (double)((items * k + slots - 1) / slots) * ((double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0));

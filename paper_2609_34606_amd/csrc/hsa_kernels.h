@@ -241,6 +241,7 @@ struct Cache8AttnParams {
   // set by plan_cache8
   int32_t nb;                 // scale blocks per page
   int32_t tpp, ppt;           // 64-key tiles per page; pages per tile
+  int32_t stream;             // tiles of 64 listed tokens, across pages (many rows)
   int32_t rows_per_item, n_rt, part_rows;
   int32_t waves;              // of a few-rows workgroup
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
