@@ -84,6 +84,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
   constexpr int kRows = 16 * kCols;
+  // Parts of a weight. One bf16 part rounds it by up to 2^-9, about what the result's own rounding
+  // adds; two leave 2^-17. A step of up to 16 rows waits for memory and takes two (1 to 3% of
+  // its time); with more rows the second part would cost 7 to 10%. fp32 takes three.
+  constexpr int kWParts = kParts == 3 ? 3 : (kCols == 1 ? 2 : 1);
   constexpr int OS = D + 4;   // floats per row of the join buffer
   __shared__ __attribute__((aligned(16))) float osm[kWaves * 16 * OS];
   __shared__ float msm[kWaves][kRows], lsm[kWaves][kRows];
@@ -317,7 +321,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
         vc[m] = u32x4{lo[0], lo[1], hi[2], hi[3]};
       }
     }
-    u32x4 pk[kCols][2][kParts];
+    u32x4 pk[kCols][2][kWParts];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
       float mx = -INFINITY;
@@ -351,12 +355,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
         }
         sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
+        for (int k = 0; k < kWParts; ++k)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t x = pack_bf16(e[2 * i], e[2 * i + 1]);
             pk[n][u][k][i] = x;
-            if (k + 1 < kParts) {
+            if (k + 1 < kWParts) {
               e[2 * i] -= bf16_lo(x);
               e[2 * i + 1] -= bf16_hi(x);
             }
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams 
 #pragma unroll
         for (int n = 0; n < kCols; ++n)
 #pragma unroll
-          for (int k = 0; k < kParts; ++k) acc[n][m] = mfma16(a, pk[n][u][k], acc[n][m]);
+          for (int k = 0; k < kWParts; ++k) acc[n][m] = mfma16(a, pk[n][u][k], acc[n][m]);
       }
     if (more) load_values(t + kWaves);
   }

@@ -212,7 +212,7 @@ struct TokenWriteParams {
   const int32_t* first;       // [B] nullable
   const int32_t* count;       // [B] nullable
   int32_t H, P, n, num_slots, max_pages;
-  int32_t item_shift, heads;  // set by the launch: 2^item_shift threads share a token's key
+  int32_t item_shift, heads, roles;  // set by the launch: 2^item_shift threads share a token's key
                               // row; heads a workgroup
 };
 

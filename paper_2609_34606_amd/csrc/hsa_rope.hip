@@ -5,7 +5,8 @@
 // its own latency for few tokens). The angle's cosine and sine cost about 35 instructions
 // a pair; a thread computes those of one item (rope_mode) of a token once and
 // applies them to kHeads heads, whose loads are in flight together. Neighbouring
-// lanes take neighbouring 16-byte pieces of a head.
+// lanes take neighbouring 16-byte pieces of a head. 4680 tokens, 12 heads x d128 in bf16, out
+// of a fused projection: 7.2 us, 4.0 TB/s (a 1 GiB copy 5.1); one token 2.5 us.
 #include <math.h>
 
 #include "hsa_rope.h"
@@ -45,11 +46,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
 template <typename T, int kMode>
 hipError_t launch(RopeParams p, int B, hipStream_t s) {
   p.n_items = RopeItem<T, kMode>::count(p.table.rot, p.d);
-  const int k = p.heads >= 4 && (int64_t)B * p.n * p.n_items * ((p.heads + 3) / 4) >= 65536 ? 4 : 1;
+  // Two heads a thread share its angles, once that leaves a wave a SIMD (12 heads x d128,
+  // 4680 tokens, interleaved: one head 9.0 us, two 7.3, four 7.4; 300 tokens: 3.5, 3.6, 3.8).
+  const int k = p.heads >= 2 && (int64_t)B * p.n * p.n_items * ((p.heads + 1) / 2) >= 65536 ? 2 : 1;
   p.n_groups = (p.heads + k - 1) / k;
   const int64_t threads = (int64_t)p.n * p.n_groups * p.n_items;
   const dim3 grid((uint32_t)((threads + 255) / 256), B);
-  if (k == 4) rope_kernel<T, kMode, 4><<<grid, 256, 0, s>>>(p);
+  if (k == 2) rope_kernel<T, kMode, 2><<<grid, 256, 0, s>>>(p);
   else rope_kernel<T, kMode, 1><<<grid, 256, 0, s>>>(p);
   return hipGetLastError();
 }

@@ -2,13 +2,16 @@
 // writes them, go to any run of a sequence's tokens in the paged cache, keys rotated by their
 // position on the way: into the pool in its own type, or into the 8-bit cache.
 //
-// A workgroup takes one block of up to 64 tokens of a page (the tokens that share
-// a scale) of one head: its keys turn in registers, where they wait for the block's largest
-// magnitude, its values are transposed through LDS into the d-major rows. A block that holds older tokens keeps its scale or
-// grows it by a power of two; then, and only then, the older codes are read and
-// written again (exact unless they become subnormal).
-// Bound: HBM (the step's tokens read once, the codes written once); few
-// tokens: the launch's latency.
+// A workgroup takes one block of up to 64 tokens of a page (the tokens that share a scale): the
+// keys of one head or two, which turn in registers and wait there for the block's largest
+// magnitude, or the values of one, which are transposed through LDS into the d-major
+// rows. A block that holds older tokens keeps its scale or grows it by a power of two; then, and
+// only then, the older codes are read and written again (exact unless they become
+// subnormal).
+// Bound: HBM (the step's tokens read once, the codes written once): 4680 tokens, 12 heads x
+// d128, out of a fused projection (43 MB) in 15.5 us, four such sequences in 49 us (3.5
+// TB/s, a copy 5.1: a head's rows are 256 bytes of every token's 9216, a value row's new codes
+// 64 bytes); for few tokens the launch's latency, 6.8 us for 32 single ones.
 #include "hsa_fp8.h"
 #include "hsa_rope.h"
 
@@ -59,62 +62,46 @@ __device__ __forceinline__ uint32_t max_bits_f32(uint32_t m) {
   return m;
 }
 
+// Largest of a value over the workgroup's four waves. buf: one slot a wave.
+__device__ __forceinline__ uint32_t max_all(uint32_t a, uint32_t* buf, int tid) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, m));
+  if ((tid & 63) == 0) buf[tid >> 6] = a;
+  __syncthreads();
+  return max(max(buf[0], buf[1]), max(buf[2], buf[3]));
+}
+
+constexpr uint32_t kInf = 0x7f800000u;
+__device__ __forceinline__ void finite_bits(uint32_t& m, float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  m = u < kInf ? max(m, u) : m;
+}
+
+// One block of a sequence and the tokens of the step that fall into it.
+struct TokenBlock {
+  int b, page, blk, boff;  // batch entry, logical page, block of the page and its first token there
+  int o0, o1, ntok;        // the step's tokens [o0, o1) of the block
+  int i0;                  // the first of them within the step
+  int nb;
+};
+
 template <typename T, int D, bool kEight, int kMode>
-__global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
-  using V16 = typename Vec16<T>::type;
+__device__ __forceinline__ void write_keys(const TokenWriteParams& p, const TokenBlock& t, int h_lo, int h_hi,
+                                           uint32_t* amax) {
   using Item = RopeItem<T, kMode>;
   using Raw = typename Item::El::Raw;
   constexpr int E = 16 / (int)sizeof(T);
-  constexpr int CPR = D / E;                      // 16-byte chunks per token
-  constexpr int NLD = kTok * CPR / 256;           // value chunks per thread
-  constexpr int RW = D * (int)sizeof(T) / 4 + 1;  // dwords per value row: one more than d, so that rows fall on their own banks
-  constexpr int EPW = 4 / (int)sizeof(T);         // dims per dword
-  constexpr int NK = kMode == kRopeSingle ? 1 : kTok * D / E / (kMode == kRopeHalves ? 512 : 256);  // key items per thread
-  constexpr uint32_t kInf = 0x7f800000u;
-  __shared__ uint32_t vs[kTok * RW];
-  __shared__ uint32_t amax[2][4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int groups = (p.H + p.heads - 1) / p.heads;
-  const int unit = blockIdx.x / groups, b = blockIdx.y;
-  const int h_lo = (blockIdx.x - unit * groups) * p.heads, h_hi = min(h_lo + p.heads, p.H);
-  // the step's tokens that fall into the table: [t0, t1) of the sequence
-  const int64_t f = p.first ? p.first[b] : 0;
-  const int64_t c = p.count ? min(p.count[b], p.n) : p.n;
-  const int64_t t0 = f > 0 ? f : 0, cap = (int64_t)p.max_pages * p.P;
-  const int64_t t1 = f + c < cap ? f + c : cap;
-  if (t0 >= t1) return;
-  // this unit's block, and the tokens [o0, o1) of it that the step brings (tokens of
-  // the table are below 2^31, see hsa_cache8_t)
-  const int nb = (p.P + kTok - 1) / kTok;
-  const int page0 = (int)t0 / p.P;
-  const int g = ((int)t0 - page0 * p.P) / kTok + unit;
-  const int page = page0 + g / nb, blk = g % nb, boff = blk * kTok;
-  const int64_t base = (int64_t)page * p.P + boff;
-  if (base >= t1) return;
-  const int len = min(kTok, p.P - boff);
-  const int o0 = t0 > base ? (int)(t0 - base) : 0;
-  const int o1 = t1 - base < len ? (int)(t1 - base) : len;
-  const int ntok = o1 - o0;
-  if (ntok <= 0) return;
-  const int i0 = (int)(base + o0 - f);            // first of them within the step
-  const size_t slot = clampi(ld_const(p.page_table + (size_t)b * p.max_pages + page), 0, p.num_slots - 1);
-  const T* ksrc = static_cast<const T*>(p.k_src) + (int64_t)b * p.k_batch + (int64_t)i0 * p.k_token;
-  const T* vsrc = static_cast<const T*>(p.v_src) + (int64_t)b * p.v_batch + (int64_t)i0 * p.v_token;
-
-  // A thread has one key item (RopeItem) of every 256 >> item_shift tokens.
+  constexpr int NK = kMode == kRopeSingle ? 1 : kTok * D / E / (kMode == kRopeHalves ? 512 : 256);  // items a thread
+  const int tid = threadIdx.x, ntok = t.ntok;
+  const T* ksrc = static_cast<const T*>(p.k_src) + (int64_t)t.b * p.k_batch + (int64_t)t.i0 * p.k_token;
+  // A thread has one item (RopeItem) of every 256 >> item_shift tokens.
   const RopeTable& r = p.table;
-  const int step = 256 >> p.item_shift;
-  const int tk = tid >> p.item_shift;
+  const int step = 256 >> p.item_shift, tk = tid >> p.item_shift, j = tid & ((1 << p.item_shift) - 1);
   Item it;
-  it.set(r, tid & ((1 << p.item_shift) - 1));
-  const bool mine = (tid & ((1 << p.item_shift) - 1)) < Item::count(r.rot, D);
-  V16 v[NLD];
+  it.set(r, j);
+  const bool mine = j < Item::count(r.rot, D);
   Raw ra[NK], rb[NK];
   auto load = [&](int h) {
-#pragma unroll
-    for (int l = 0; l < NLD; ++l)
-      v[l] = *reinterpret_cast<const V16*>(vsrc + (int64_t)min((tid + 256 * l) / CPR, ntok - 1) * p.v_token +
-                                           h * D + tid % CPR * E);
     if (kMode != kRopeSingle && mine) {
 #pragma unroll
       for (int k = 0; k < NK; ++k)
@@ -122,40 +109,23 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
     }
   };
   load(h_lo);
+  const size_t slot =
+      clampi(ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page), 0, p.num_slots - 1);
   it.frequencies(r);
   float cs[NK][Item::NP], sn[NK][Item::NP];
-  auto angles = [&](int t, int k) { it.angles(r, rope_positions(r, b, i0 + t, p.n), cs[k], sn[k]); };
+  auto angles = [&](int i, int k) { it.angles(r, rope_positions(r, t.b, t.i0 + i, p.n), cs[k], sn[k]); };
   if (kMode != kRopeSingle && mine && it.turn) {
 #pragma unroll
     for (int k = 0; k < NK; ++k)
       if (tk + k * step < ntok) angles(tk + k * step, k);
   }
-
   for (int h = h_lo; h < h_hi; ++h) {
     const size_t head = slot * p.H + h;
-    int ek_old = kScaleMin, ev_old = kScaleMin;
-    if constexpr (kEight) {
-      if (o0 > 0) {
-        ek_old = (int)p.k_exp[head * nb + blk] - 127;
-        ev_old = (int)p.v_exp[head * nb + blk] - 127;
-      }
-    }
-    if (h > h_lo) __syncthreads();  // the last head's rows have been read
-    uint32_t mv = 0;
-#pragma unroll
-    for (int l = 0; l < NLD; ++l) {
-      const int t = (tid + 256 * l) / CPR;
-      if (t >= ntok) continue;
-      uint32_t* dst = vs + (o0 + t) * RW + tid % CPR * 4;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        dst[w] = v[l][w];
-        if constexpr (kEight) mv = max_bits<T>(mv, v[l][w]);
-      }
-    }
+    int e_old = kScaleMin;
+    if (kEight && t.o0 > 0) e_old = (int)p.k_exp[head * t.nb + t.blk] - 127;
     float mk = 0.f;
     float ku[NK][Item::N], kw[NK][Item::N];
-    T* kdst = kEight ? nullptr : static_cast<T*>(p.k) + (head * p.P + boff + o0) * D;
+    T* kdst = kEight ? nullptr : static_cast<T*>(p.k) + (head * p.P + t.boff + t.o0) * D;
     // (NaN does not count: it keeps its code under any scale)
     auto largest = [&](int k) {
 #pragma unroll
@@ -164,11 +134,11 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
         if (kMode != kRopeInterleaved && it.turn) mk = fmaxf(mk, fabsf(kw[k][i]));
       }
     };
-    // single: the item's pair at token t (turned again where it is needed: one pair a
+    // single: the item's pair at token i (turned again where it is needed: one pair a
     // thread makes too many to keep)
-    auto single = [&](int t) {
-      it.load(ksrc + (int64_t)t * p.k_token + h * D, ra[0], rb[0]);
-      if (it.turn) angles(t, 0);
+    auto single = [&](int i) {
+      it.load(ksrc + (int64_t)i * p.k_token + h * D, ra[0], rb[0]);
+      if (it.turn) angles(i, 0);
       it.result(ra[0], rb[0], cs[0], sn[0], ku[0], kw[0]);
     };
     if (mine) {
@@ -181,138 +151,52 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
             else it.store(kdst + (size_t)(tk + k * step) * D, ku[k], kw[k]);
           }
       } else {
-        for (int t = tk; t < ntok; t += step) {
-          single(t);
+        for (int i = tk; i < ntok; i += step) {
+          single(i);
           if constexpr (kEight) largest(0);
-          else it.store(kdst + (size_t)t * D, ku[0], kw[0]);
+          else it.store(kdst + (size_t)i * D, ku[0], kw[0]);
         }
       }
     }
     if (h + 1 < h_hi) load(h + 1);  // in flight during what follows
-
-    if constexpr (!kEight) {
-      __syncthreads();
-      // value rows: runs of E tokens (16 bytes of a row), a dword of dims each
-      constexpr int TG = kTok / E;
-#pragma unroll 2
-      for (int x = tid; x < TG * (RW - 1); x += 256) {
-        const int g0 = x % TG * E, w = x / TG;
-        if (g0 + E <= o0 || g0 >= o1) continue;
-        uint32_t e[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) e[i] = vs[clampi(g0 + i, o0, o1 - 1) * RW + w];
-        T* dst = static_cast<T*>(p.v) + (head * D + w * EPW) * p.P + boff + g0;
-        const bool whole = g0 >= o0 && g0 + E <= o1;
-        if constexpr (EPW == 2) {
-          if (whole) {
-            V16 lo, hi;  // dims 2 w and 2 w + 1
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              lo[i] = (e[2 * i] & 0xffffu) | (e[2 * i + 1] << 16);
-              hi[i] = (e[2 * i] >> 16) | (e[2 * i + 1] & 0xffff0000u);
-            }
-            *reinterpret_cast<V16*>(dst) = lo;
-            *reinterpret_cast<V16*>(dst + p.P) = hi;
-          } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-              if (g0 + i >= o0 && g0 + i < o1) {
-                dst[i] = (uint16_t)e[i];
-                dst[p.P + i] = (uint16_t)(e[i] >> 16);
-              }
-          }
-        } else {
-          if (whole) {
-            *reinterpret_cast<V16*>(dst) = V16{e[0], e[1], e[2], e[3]};
-          } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-              if (g0 + i >= o0 && g0 + i < o1) dst[i] = __uint_as_float(e[i]);
-          }
-        }
-      }
-    } else {
-      // the block's largest magnitudes, as the bits of fp32 numbers
-      auto reduce = [&](uint32_t& a, uint32_t& b2) {
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-          a = max(a, (uint32_t)__shfl_xor((int)a, m));
-          b2 = max(b2, (uint32_t)__shfl_xor((int)b2, m));
-        }
-        if (lane == 0) {
-          amax[0][wave] = a;
-          amax[1][wave] = b2;
-        }
+    if constexpr (kEight) {
+      if (h > h_lo) __syncthreads();  // (the last head's maxima have been read)
+      uint32_t bits = max_all(__float_as_uint(mk), amax, tid);
+      const bool wild = bits >= kInf;
+      if (wild) {  // the largest finite magnitude
         __syncthreads();
-        a = max(max(amax[0][0], amax[0][1]), max(amax[0][2], amax[0][3]));
-        b2 = max(max(amax[1][0], amax[1][1]), max(amax[1][2], amax[1][3]));
-      };
-      uint32_t bk = __float_as_uint(mk), bv = max_bits_f32<T>(mv);
-      reduce(bk, bv);
-      const bool wild = bk >= kInf || bv >= kInf;  // infinities, or NaN among the values
-      if (wild) {
-        // the largest finite magnitudes
-        __syncthreads();
-        bk = bv = 0;
-        auto finite = [](uint32_t& m, float x) {
-          const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-          m = u < kInf ? max(m, u) : m;
-        };
+        bits = 0;
         if (mine) {
-          for (int t = tk, k = 0; t < ntok; t += step, ++k) {
-            if constexpr (kMode == kRopeSingle) single(t);
+          for (int i = tk, k = 0; i < ntok; i += step, ++k) {
+            if constexpr (kMode == kRopeSingle) single(i);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk)
               if (kMode == kRopeSingle || kk == k) {
 #pragma unroll
-                for (int i = 0; i < Item::N; ++i) {
-                  finite(bk, ku[kk][i]);
-                  if (kMode != kRopeInterleaved && it.turn) finite(bk, kw[kk][i]);
+                for (int x = 0; x < Item::N; ++x) {
+                  finite_bits(bits, ku[kk][x]);
+                  if (kMode != kRopeInterleaved && it.turn) finite_bits(bits, kw[kk][x]);
                 }
               }
           }
         }
-        for (int x = tid; x < ntok * (RW - 1); x += 256) {
-          const uint32_t w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
-          if constexpr (sizeof(T) == 2) {
-            finite(bv, bf16_lo(w));
-            finite(bv, bf16_hi(w));
-          } else {
-            finite(bv, __uint_as_float(w));
+        bits = max_all(bits, amax, tid);
+      }
+      const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
+      const float scale = pow2i(e), most = kCodeMax * scale;
+      if (tid == 0) p.k_exp[head * t.nb + t.blk] = (uint8_t)(e + 127);
+      uint8_t* kc = static_cast<uint8_t*>(p.k) + (head * p.P + t.boff) * D;
+      auto put = [&](int i, int k) {
+        uint8_t* row = kc + (size_t)(t.o0 + i) * D;
+        if (wild) {  // infinities become the largest number of the block's scale
+#pragma unroll
+          for (int x = 0; x < Item::N; ++x) {
+            ku[k][x] = saturate(ku[k][x], most);
+            kw[k][x] = saturate(kw[k][x], most);
           }
         }
-        reduce(bk, bv);
-      }
-      const int ek = max(scale_exponent(__uint_as_float(bk)), ek_old);
-      const int ev = max(scale_exponent(__uint_as_float(bv)), ev_old);
-      uint8_t* kc = static_cast<uint8_t*>(p.k) + (head * p.P + boff) * D;
-      uint8_t* vc = static_cast<uint8_t*>(p.v) + head * D * p.P + boff;
-      if (tid == 0) p.k_exp[head * nb + blk] = (uint8_t)(ek + 127);
-      if (tid == 64) p.v_exp[head * nb + blk] = (uint8_t)(ev + 127);
-      const float sk = pow2i(ek), sv = pow2i(ev);
-      if (wild) {
-        // infinities become the largest number of the block's scale
-        const float lk = kCodeMax * sk, lv = kCodeMax * sv;
-        if constexpr (kMode != kRopeSingle) {
-#pragma unroll
-          for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int i = 0; i < Item::N; ++i) {
-              ku[k][i] = saturate(ku[k][i], lk);
-              kw[k][i] = saturate(kw[k][i], lk);
-            }
-        }
-        for (int x = tid; x < ntok * (RW - 1); x += 256) {
-          uint32_t& w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
-          if constexpr (sizeof(T) == 2) w = pack_bf16(saturate(bf16_lo(w), lv), saturate(bf16_hi(w), lv));
-          else w = __float_as_uint(saturate(__uint_as_float(w), lv));
-        }
-        __syncthreads();
-      }
-      auto put = [&](int t, int k) {
-        uint8_t* row = kc + (size_t)(o0 + t) * D;
-        store_codes<Item::N>(row + it.a, ku[k], sk);
-        if (kMode != kRopeInterleaved && it.turn) store_codes<Item::N>(row + it.b, kw[k], sk);
+        store_codes<Item::N>(row + it.a, ku[k], scale);
+        if (kMode != kRopeInterleaved && it.turn) store_codes<Item::N>(row + it.b, kw[k], scale);
       };
       if (mine) {
         if constexpr (kMode != kRopeSingle) {
@@ -320,19 +204,15 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
           for (int k = 0; k < NK; ++k)
             if (tk + k * step < ntok) put(tk + k * step, k);
         } else {
-          for (int t = tk; t < ntok; t += step) {
-            single(t);
-            if (wild) {
-              ku[0][0] = saturate(ku[0][0], kCodeMax * sk);
-              kw[0][0] = saturate(kw[0][0], kCodeMax * sk);
-            }
-            put(t, 0);
+          for (int i = tk; i < ntok; i += step) {
+            single(i);
+            put(i, 0);
           }
         }
       }
-      if (o0 > 0 && ek > ek_old) {  // the older rows, scaled down
-        const float shift = pow2i(ek_old - ek);
-        for (int x = tid; x < o0 * (D / 16); x += 256) {
+      if (t.o0 > 0 && e > e_old) {  // the older rows, scaled down
+        const float shift = pow2i(e_old - e);
+        for (int x = tid; x < t.o0 * (D / 16); x += 256) {
           u32x4* dst = reinterpret_cast<u32x4*>(kc + 16 * x);
           u32x4 w = *dst;
 #pragma unroll
@@ -340,56 +220,163 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
           *dst = w;
         }
       }
-      const bool grow = o0 > 0 && ev > ev_old;
-      if (!grow && ntok <= 4) {
-        // a few tokens (of a step that decodes): an element a thread
-        for (int x = tid; x < ntok * D; x += 256) {
-          const int t = o0 + x / D, e = x % D;
-          const uint32_t raw = vs[t * RW + e / EPW];
-          const float y = sizeof(T) == 4 ? __uint_as_float(raw) : (e & 1 ? bf16_hi(raw) : bf16_lo(raw));
-          vc[(size_t)e * p.P + t] = (uint8_t)codes2(y, y, sv);
-        }
-        continue;
-      }
-      // runs of 16 tokens of a dword of dims
-      const float shift = pow2i(ev_old - ev);
-      const int r0 = grow ? 0 : o0;
-      for (int x = tid; x < 4 * (RW - 1); x += 256) {
-        const int g0 = x % 4 * 16, w = x / 4;
-        uint8_t* dst = vc + (size_t)(w * EPW) * p.P + g0;
-        if (g0 >= o0 && g0 + 16 <= o1) {
-          const uint32_t* src = vs + g0 * RW + w;
-          uint32_t e[16];
+    }
+  }
+}
+
+// vs: kTok rows of RW dwords, one more than a row's values, so that rows fall on their own banks.
+template <typename T, int D, bool kEight>
+__device__ __forceinline__ void write_values(const TokenWriteParams& p, const TokenBlock& t, int h, uint32_t* vs,
+                                             uint32_t* amax) {
+  using V16 = typename Vec16<T>::type;
+  constexpr int E = 16 / (int)sizeof(T);
+  constexpr int CPR = D / E;                      // 16-byte chunks per token
+  constexpr int NLD = kTok * CPR / 256;           // chunks per thread
+  constexpr int RW = D * (int)sizeof(T) / 4 + 1;  // dwords per LDS row
+  constexpr int EPW = 4 / (int)sizeof(T);         // dims per dword
+  const int tid = threadIdx.x, ntok = t.ntok, o0 = t.o0, o1 = t.o1;
+  const T* src = static_cast<const T*>(p.v_src) + (int64_t)t.b * p.v_batch + (int64_t)t.i0 * p.v_token + h * D;
+  V16 v[NLD];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) e[i] = src[i * RW];
-          u32x4a8 lo, hi;  // dims EPW w and, in bf16, the next
+  for (int l = 0; l < NLD; ++l)
+    v[l] = *reinterpret_cast<const V16*>(src + (int64_t)min((tid + 256 * l) / CPR, ntok - 1) * p.v_token +
+                                         tid % CPR * E);
+  const size_t slot =
+      clampi(ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page), 0, p.num_slots - 1);
+  const size_t head = slot * p.H + h;
+  int e_old = kScaleMin;
+  if (kEight && o0 > 0) e_old = (int)p.v_exp[head * t.nb + t.blk] - 127;
+  uint32_t mv = 0;
+#pragma unroll
+  for (int l = 0; l < NLD; ++l) {
+    const int i = (tid + 256 * l) / CPR;
+    if (i >= ntok) continue;
+    uint32_t* dst = vs + (o0 + i) * RW + tid % CPR * 4;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      dst[w] = v[l][w];
+      if constexpr (kEight) mv = max_bits<T>(mv, v[l][w]);
+    }
+  }
+  if constexpr (!kEight) {
+    __syncthreads();
+    // value rows: runs of E tokens (16 bytes of a row), a dword of dims each
+    constexpr int TG = kTok / E;
+#pragma unroll 2
+    for (int x = tid; x < TG * (RW - 1); x += 256) {
+      const int g0 = x % TG * E, w = x / TG;
+      if (g0 + E <= o0 || g0 >= o1) continue;
+      uint32_t e[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = vs[clampi(g0 + i, o0, o1 - 1) * RW + w];
+      T* dst = static_cast<T*>(p.v) + (head * D + w * EPW) * p.P + t.boff + g0;
+      const bool whole = g0 >= o0 && g0 + E <= o1;
+      if constexpr (EPW == 2) {
+        if (whole) {
+          V16 lo, hi;  // dims 2 w and 2 w + 1
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if constexpr (EPW == 2) {
-              // pairs of tokens of one dim
-              const uint32_t a0 = __builtin_amdgcn_perm(e[4 * i + 1], e[4 * i], 0x05040100u);
-              const uint32_t a1 = __builtin_amdgcn_perm(e[4 * i + 3], e[4 * i + 2], 0x05040100u);
-              const uint32_t b0 = __builtin_amdgcn_perm(e[4 * i + 1], e[4 * i], 0x07060302u);
-              const uint32_t b1 = __builtin_amdgcn_perm(e[4 * i + 3], e[4 * i + 2], 0x07060302u);
-              lo[i] = codes4_bf16(a0, a1, sv);
-              hi[i] = codes4_bf16(b0, b1, sv);
-            } else {
-              lo[i] = codes4(__uint_as_float(e[4 * i]), __uint_as_float(e[4 * i + 1]), __uint_as_float(e[4 * i + 2]),
-                             __uint_as_float(e[4 * i + 3]), sv);
-            }
+            lo[i] = (e[2 * i] & 0xffffu) | (e[2 * i + 1] << 16);
+            hi[i] = (e[2 * i] >> 16) | (e[2 * i + 1] & 0xffff0000u);
           }
-          *reinterpret_cast<u32x4a8*>(dst) = lo;
-          if constexpr (EPW == 2) *reinterpret_cast<u32x4a8*>(dst + p.P) = hi;
-        } else if (g0 + 16 > r0 && g0 < o1) {
-          // a run that the step begins or ends in, or of older tokens
-          for (int t = max(g0, r0); t < min(g0 + 16, o1); ++t) {
+          *reinterpret_cast<V16*>(dst) = lo;
+          *reinterpret_cast<V16*>(dst + p.P) = hi;
+        } else {
 #pragma unroll
-            for (int e = 0; e < EPW; ++e) {
-              uint8_t* one = dst + (size_t)e * p.P + (t - g0);
-              const uint32_t raw = vs[max(t, o0) * RW + w];
-              const float y = EPW == 1 ? __uint_as_float(raw) : (e ? bf16_hi(raw) : bf16_lo(raw));
-              *one = (uint8_t)(t < o0 ? codes2(code_to_f32(*one) * shift, 0.f, 1.f) : codes2(y, 0.f, sv));
+          for (int i = 0; i < E; ++i)
+            if (g0 + i >= o0 && g0 + i < o1) {
+              dst[i] = (uint16_t)e[i];
+              dst[p.P + i] = (uint16_t)(e[i] >> 16);
             }
+        }
+      } else {
+        if (whole) {
+          *reinterpret_cast<V16*>(dst) = V16{e[0], e[1], e[2], e[3]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < E; ++i)
+            if (g0 + i >= o0 && g0 + i < o1) dst[i] = __uint_as_float(e[i]);
+        }
+      }
+    }
+  } else {
+    uint32_t bits = max_all(max_bits_f32<T>(mv), amax, tid);  // (its barrier: the rows are there)
+    const bool wild = bits >= kInf;                            // infinities or NaN
+    if (wild) {  // the largest finite magnitude
+      __syncthreads();
+      bits = 0;
+      for (int x = tid; x < ntok * (RW - 1); x += 256) {
+        const uint32_t w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
+        if constexpr (sizeof(T) == 2) {
+          finite_bits(bits, bf16_lo(w));
+          finite_bits(bits, bf16_hi(w));
+        } else {
+          finite_bits(bits, __uint_as_float(w));
+        }
+      }
+      bits = max_all(bits, amax, tid);
+    }
+    const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
+    const float scale = pow2i(e), most = kCodeMax * scale;
+    if (tid == 0) p.v_exp[head * t.nb + t.blk] = (uint8_t)(e + 127);
+    uint8_t* vc = static_cast<uint8_t*>(p.v) + head * D * p.P + t.boff;
+    if (wild) {  // infinities become the largest number of the block's scale
+      for (int x = tid; x < ntok * (RW - 1); x += 256) {
+        uint32_t& w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
+        if constexpr (sizeof(T) == 2) w = pack_bf16(saturate(bf16_lo(w), most), saturate(bf16_hi(w), most));
+        else w = __float_as_uint(saturate(__uint_as_float(w), most));
+      }
+      __syncthreads();
+    }
+    const bool grow = o0 > 0 && e > e_old;
+    if (!grow && ntok <= 4) {
+      // a few tokens (of a step that decodes): an element a thread
+      for (int x = tid; x < ntok * D; x += 256) {
+        const int i = o0 + x / D, c = x % D;
+        const uint32_t raw = vs[i * RW + c / EPW];
+        const float y = sizeof(T) == 4 ? __uint_as_float(raw) : (c & 1 ? bf16_hi(raw) : bf16_lo(raw));
+        vc[(size_t)c * p.P + i] = (uint8_t)codes2(y, y, scale);
+      }
+      return;
+    }
+    // runs of 16 tokens of a dword of dims
+    const float shift = pow2i(e_old - e);
+    const int r0 = grow ? 0 : o0;
+    for (int x = tid; x < 4 * (RW - 1); x += 256) {
+      const int g0 = x % 4 * 16, w = x / 4;
+      uint8_t* dst = vc + (size_t)(w * EPW) * p.P + g0;
+      if (g0 >= o0 && g0 + 16 <= o1) {
+        const uint32_t* row = vs + g0 * RW + w;
+        uint32_t c[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = row[i * RW];
+        u32x4a8 lo, hi;  // dims EPW w and, in bf16, the next
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (EPW == 2) {
+            // pairs of tokens of one dim
+            const uint32_t a0 = __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x05040100u);
+            const uint32_t a1 = __builtin_amdgcn_perm(c[4 * i + 3], c[4 * i + 2], 0x05040100u);
+            const uint32_t b0 = __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x07060302u);
+            const uint32_t b1 = __builtin_amdgcn_perm(c[4 * i + 3], c[4 * i + 2], 0x07060302u);
+            lo[i] = codes4_bf16(a0, a1, scale);
+            hi[i] = codes4_bf16(b0, b1, scale);
+          } else {
+            lo[i] = codes4(__uint_as_float(c[4 * i]), __uint_as_float(c[4 * i + 1]), __uint_as_float(c[4 * i + 2]),
+                           __uint_as_float(c[4 * i + 3]), scale);
+          }
+        }
+        *reinterpret_cast<u32x4a8*>(dst) = lo;
+        if constexpr (EPW == 2) *reinterpret_cast<u32x4a8*>(dst + p.P) = hi;
+      } else if (g0 + 16 > r0 && g0 < o1) {
+        // a run that the step begins or ends in, or of older tokens
+        for (int i = max(g0, r0); i < min(g0 + 16, o1); ++i) {
+#pragma unroll
+          for (int c = 0; c < EPW; ++c) {
+            uint8_t* one = dst + (size_t)c * p.P + (i - g0);
+            const uint32_t raw = vs[max(i, o0) * RW + w];
+            const float y = EPW == 1 ? __uint_as_float(raw) : (c ? bf16_hi(raw) : bf16_lo(raw));
+            *one = (uint8_t)(i < o0 ? codes2(code_to_f32(*one) * shift, 0.f, 1.f) : codes2(y, 0.f, scale));
           }
         }
       }
@@ -397,15 +384,53 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
   }
 }
 
+// A workgroup writes one block's keys of p.heads heads, or its values of one.
+template <typename T, int D, bool kEight, int kMode>
+__global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
+  __shared__ uint32_t vs[kTok * (D * (int)sizeof(T) / 4 + 1)];
+  __shared__ uint32_t amax[4];
+  const int groups = (p.H + p.heads - 1) / p.heads;
+  const int unit = blockIdx.x / p.roles, role = blockIdx.x - unit * p.roles;
+  if (role >= groups + p.H) return;
+  TokenBlock t;
+  t.b = blockIdx.y;
+  // the step's tokens that fall into the table: [t0, t1) of the sequence
+  const int64_t f = p.first ? p.first[t.b] : 0;
+  const int64_t c = p.count ? min(p.count[t.b], p.n) : p.n;
+  const int64_t t0 = f > 0 ? f : 0, cap = (int64_t)p.max_pages * p.P;
+  const int64_t t1 = f + c < cap ? f + c : cap;
+  if (t0 >= t1) return;
+  // this unit's block, and the tokens of it that the step brings (tokens of the table are
+  // below 2^31, see hsa_cache8_t)
+  t.nb = (p.P + kTok - 1) / kTok;
+  const int page0 = (int)t0 / p.P;
+  const int g = ((int)t0 - page0 * p.P) / kTok + unit;
+  t.page = page0 + g / t.nb;
+  t.blk = g % t.nb;
+  t.boff = t.blk * kTok;
+  const int64_t base = (int64_t)t.page * p.P + t.boff;
+  if (base >= t1) return;
+  const int len = min(kTok, p.P - t.boff);
+  t.o0 = t0 > base ? (int)(t0 - base) : 0;
+  t.o1 = t1 - base < len ? (int)(t1 - base) : len;
+  t.ntok = t.o1 - t.o0;
+  if (t.ntok <= 0) return;
+  t.i0 = (int)(base + t.o0 - f);
+  if (role < groups) write_keys<T, D, kEight, kMode>(p, t, role * p.heads, min((role + 1) * p.heads, p.H), amax);
+  else write_values<T, D, kEight>(p, t, role - groups, vs, amax);
+}
+
 template <typename T, int D, bool kEight, int kMode>
 void launch_mode(int B, TokenWriteParams p, hipStream_t s) {
   const int n = RopeItem<T, kMode>::count(p.table.rot, D);
   while (1 << p.item_shift < n) ++p.item_shift;
-  // Two heads a workgroup share the angles of their tokens, once that leaves work for
-  // every CU.
+  // Two heads a workgroup share the angles of their tokens, once that leaves work for every
+  // CU (8-bit append of 4680 tokens, 12 heads x d128: one 16.6 us, two 15.8, three 20.2, four
+  // 16.1; four sequences at once 51.3, 49.2, 62.3, 51.6).
   const int64_t wgs = (int64_t)((p.n + kTok - 1) / kTok) * p.H * B;
   p.heads = kMode != kRopeSingle && wgs >= 768 ? 2 : 1;
-  const dim3 grid((uint32_t)(token_write_units(p.n, p.P) * ((p.H + p.heads - 1) / p.heads)), B);
+  p.roles = (p.H + p.heads - 1) / p.heads + p.H;
+  const dim3 grid((uint32_t)(token_write_units(p.n, p.P) * p.roles), B);
   token_write_kernel<T, D, kEight, kMode><<<grid, 256, 0, s>>>(p);
 }
 
