@@ -1308,7 +1308,7 @@ hsa_status_t run_token_write(const hsa_config_t* cfg, TokenWriteParams& p, const
 
 // The parts of an attention call's parameters that its plan follows from.
 hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_most,
-                              int32_t n_cur_pages, Cache8AttnParams& p) {
+                              int32_t n_cur_pages, bool ragged, Cache8AttnParams& p) {
   p.H = cfg->num_heads;
   p.Hk = kv_heads;
   p.G = cfg->num_heads / kv_heads;
@@ -1317,7 +1317,7 @@ hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_h
   p.n_q = n_q;
   p.n_cur = n_cur_pages;
   if ((int64_t)n_q * p.G >= 1 << 30) return HSA_ERR_UNSUPPORTED;
-  plan_cache8(p, cfg->dtype, cfg->batch, k_most);
+  plan_cache8(p, cfg->dtype, cfg->batch, k_most, ragged);
   if (cfg->batch > kMaxGridY || (int64_t)p.n_split * p.n_rt * p.Hk > kMaxGrid || (int64_t)n_q * p.H > kMaxGrid)
     return HSA_ERR_UNSUPPORTED;
   return HSA_OK;
@@ -1404,9 +1404,13 @@ size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int3
                                       int32_t k_max, int32_t n_cur_pages) {
   if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return 0;
   if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return 0;
-  Cache8AttnParams p{};
-  if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, p) != HSA_OK) return 0;
-  return cache8_ws(cfg, p);
+  size_t need = 0;  // of either kind of call
+  for (const bool ragged : {false, true}) {
+    Cache8AttnParams p{};
+    if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged, p) != HSA_OK) return 0;
+    need = std::max(need, cache8_ws(cfg, p));
+  }
+  return need;
 }
 
 hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
@@ -1428,7 +1432,8 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
   if ((st = check_table(cfg, cache->max_pages)) != HSA_OK) return st;
   if (n_q == 0) return HSA_OK;
   Cache8AttnParams p{};
-  if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, p)) != HSA_OK) return st;
+  if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, kv_len != nullptr, p)) != HSA_OK)
+    return st;
   const size_t need = cache8_ws(cfg, p);
   if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);

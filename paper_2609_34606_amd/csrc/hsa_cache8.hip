@@ -80,7 +80,7 @@ __device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
 // score block's rows are read in 64-byte pieces, a value block's too.
 // Bound: HBM (2 d bytes a token and key head).
 template <typename T, int D, int kCols, int kParts, bool kSmallP, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(Cache8AttnParams p) {
+__global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kSmallP ? 3 : 1) void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
   constexpr int kRows = 16 * kCols;
@@ -880,15 +880,22 @@ __global__ __launch_bounds__(512) void join_row_kernel(Cache8AttnParams p) {
 #pragma unroll
     for (int y = 1; y < 64; y <<= 1) sum += __shfl_xor(sum, y);
     l += sum;
-    const int stop = min(64, n - 64 * k);
+    // (a piece past the last one repeats that with weight 0: no branch between the loads)
+    const int last = min(63, n - 64 * k - 1);
+    constexpr int kAtOnce = 4;
+    for (int s0 = wave; s0 <= last; s0 += kW * kAtOnce) {
+      float src[kAtOnce][E];
 #pragma unroll
-    for (int j = 0; j < 64 / kW; ++j) {
-      const int s = wave + kW * j;
-      if (s < stop) {
-        const float ws = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), s));
-        const float* src = p.part_o + (part0 + (size_t)(64 * k + s) * p.part_rows) * D + E * lane;
+      for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += ws * src[e];
+        for (int e = 0; e < E; ++e)
+          src[j][e] = p.part_o[(part0 + (size_t)(64 * k + min(s0 + kW * j, last)) * p.part_rows) * D + E * lane + e];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int s = s0 + kW * j;
+        const float ws = s <= last ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wt), s)) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += ws * src[j][e];
       }
     }
   }
@@ -980,7 +987,7 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
 
 }  // namespace
 
-void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel) {
+void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged) {
   p.nb = (p.P + 63) / 64;
   p.tpp = p.P < 64 ? 1 : p.nb;
   p.ppt = p.P < 64 && 64 % p.P == 0 ? 64 / p.P : 1;
@@ -1014,12 +1021,25 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel) {
       }
     }
   } else if (!brief) {
-    // Two resident workgroups a CU: 512 of at least 16 tiles, or, so that sequences of
-    // different lengths balance, up to 2048 of at least 32 (shorter ones lose more
-    // to their start than they balance).
-    const int64_t some = std::min((512 + items - 1) / items, tiles / 16);
-    const int64_t more = std::min((2048 + items - 1) / items, tiles / 32);
-    n = std::max<int64_t>(1, std::min<int64_t>(std::max(some, more), kMaxSplit));
+    const int64_t most_n = std::max<int64_t>(1, std::min<int64_t>(kMaxSplit, tiles / 16));
+    if (ragged) {
+      // Sequences of different lengths: short pieces balance (32 of 1 to 16384 tokens, 8 key
+      // heads: pieces of 16 tiles 124 us, of 32 128; 8 of them 42 and 49).
+      n = std::min((4096 + items - 1) / items, most_n);
+    } else {
+      // Equal pieces: at least two workgroups a CU, and as even a number on each as can be
+      // (8 sequences of 16384: 8 pieces, 512 workgroups, 57 us; 10 pieces 65, 12 61). A
+      // piece's start and end take about four tiles.
+      n = std::min((512 + items - 1) / items, most_n);
+      double best = 1e300;
+      for (int64_t k = n, stop = std::min((2048 + items - 1) / items, most_n); k <= stop; ++k) {
+        const double t = (double)((items * k + 255) / 256) * ((double)((tiles + k - 1) / k) + 4.0);
+        if (t < 0.99 * best) {
+          best = t;
+          n = k;
+        }
+      }
+    }
   }
   int64_t c = (tiles + n - 1) / n;
   if (!many) c = (c + p.waves - 1) / p.waves * p.waves;

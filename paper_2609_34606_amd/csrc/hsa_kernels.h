@@ -247,8 +247,9 @@ struct Cache8AttnParams {
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
 };
 
-// Plans the launch for lists of at most max_list_sel selected pages.
-void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel);
+// Plans the launch for lists of at most max_list_sel selected pages; ragged: the sequences'
+// lengths are on the device.
+void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged);
 size_t cache8_part_bytes(int64_t B, int64_t Hk, int64_t n_split, int64_t part_rows, int64_t d);
 hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s);
 
