@@ -222,8 +222,8 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
 #pragma unroll
       for (int u = 0; u < 2; ++u) vsc[u] = scale_of(p.v_exp[((size_t)vs[u] * p.Hk + h) * p.nb]);
       if (p.P % 16 == 0) {  // both granules are of one page
-        const Cache8Granule a = cache8_granule(p, w, t, 2 * g);
-        const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + a.off;
+        const int off = min(cache8_granule(p, w, t, 2 * g).off, p.P - 16);  // (past the page: masked)
+        const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + off;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
           const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(vb + (size_t)(16 * m) * p.P);
