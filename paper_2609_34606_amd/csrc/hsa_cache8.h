@@ -23,9 +23,10 @@ struct Cache8Walk {
   int n_sel, n_list, n_tiles;
 };
 
-// Tokens that query i of the sequence sees (an index below this).
+// Tokens that query i of the sequence sees (an index below this; 0 for a query before the first
+// token, so that differences with a place past the list's end fit 32 bits).
 __device__ __forceinline__ int cache8_limit(const Cache8AttnParams& p, const Cache8Walk& w, int i) {
-  return p.causal ? min(w.len, w.base + i + 1) : w.len;
+  return p.causal ? max(min(w.len, w.base + i + 1), 0) : w.len;
 }
 
 // Every lane of the wave must call it.
