@@ -673,6 +673,7 @@ typedef struct hsa_rope {
  * itself with the same strides, and must not overlap it otherwise. heads: 1 ..
  * HSA_MAX_HEADS (cfg->num_heads is not used). pos: device int32 [B, n, axes], or NULL: token i of
  * entry b is at first[b] + i (first: device int32 [B], NULL: 0; one axis only).
+ * No two tokens of o may lie in one place (INVALID_ARG).
  * inverse != 0 turns by the opposite angles. That is the transposed map:
  * given the gradient of o it gives the gradient of x. Errors: INVALID_ARG (NULL, a
  * bad rope or stride), UNSUPPORTED (sizes). n == 0 is a no-op.

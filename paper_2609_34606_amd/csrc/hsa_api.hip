@@ -1186,11 +1186,19 @@ hsa_status_t hsa_forward_noalloc(const hsa_config_t* cfg, const void* q, int32_t
 // ---------------------------------------------------------------- rotary positions, tokens, 8-bit cache
 namespace {
 
-// Largest grid of a launch in x (workgroups), and in y (batch entries).
-constexpr int64_t kMaxGrid = 0x7fffffff, kMaxGridY = 65535;
+// Largest grid of a launch in x (workgroups of up to 512 threads, 2^32 in all), and in y (batch
+// entries).
+constexpr int64_t kMaxGrid = (1 << 23) - 1, kMaxGridY = 65535;
 
 hsa_status_t check_strides(int64_t batch, int64_t token) {
   return batch < 0 || token < 0 ? HSA_ERR_INVALID_ARG : HSA_OK;
+}
+
+// Whether the rows of [B, n] tokens, `row` elements each, with these strides are apart.
+bool apart(int64_t batch, int64_t token, int64_t B, int64_t n, int64_t row) {
+  if (n == 1) return B == 1 || batch >= row;
+  if (B == 1) return token >= row;
+  return (token >= row && batch >= (n - 1) * token + row) || (batch >= row && token >= (B - 1) * batch + row);
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -1278,7 +1286,7 @@ hsa_status_t run_token_write(const hsa_config_t* cfg, TokenWriteParams& p, const
                              const void* k_src, int64_t k_batch, int64_t k_token, const void* v_src,
                              int64_t v_batch, int64_t v_token, int32_t n, const int32_t* pos,
                              const int32_t* first, const int32_t* count, bool eight, void* stream) {
-  if (!k_src || !v_src || n < 0) return HSA_ERR_INVALID_ARG;
+  if ((n != 0 && (!k_src || !v_src)) || n < 0) return HSA_ERR_INVALID_ARG;
   if (check_strides(k_batch, k_token) != HSA_OK || check_strides(v_batch, v_token) != HSA_OK)
     return HSA_ERR_INVALID_ARG;
   if (rope) {
@@ -1289,7 +1297,7 @@ hsa_status_t run_token_write(const hsa_config_t* cfg, TokenWriteParams& p, const
   }
   hsa_status_t st = check_table(cfg, p.max_pages);
   if (st != HSA_OK) return st;
-  if (cfg->batch > kMaxGridY || token_write_units(n, cfg->page_size) * p.H > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  if (cfg->batch > kMaxGridY || token_write_units(n, cfg->page_size) * 2 * p.H > kMaxGrid) return HSA_ERR_UNSUPPORTED;
   if (n == 0) return HSA_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if ((st = validate_tokens(cfg, p.page_table, p.num_slots, p.max_pages, first, count, n, s)) != HSA_OK) return st;
@@ -1318,7 +1326,8 @@ hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_h
   p.n_cur = n_cur_pages;
   if ((int64_t)n_q * p.G >= 1 << 30) return HSA_ERR_UNSUPPORTED;
   plan_cache8(p, cfg->dtype, cfg->batch, k_most, ragged);
-  if (cfg->batch > kMaxGridY || (int64_t)p.n_split * p.n_rt * p.Hk > kMaxGrid || (int64_t)n_q * p.H > kMaxGrid)
+  if (cfg->batch > kMaxGridY || (int64_t)p.n_split * p.n_rt * p.Hk > kMaxGrid ||
+      (int64_t)p.part_rows * p.Hk / 8 > kMaxGrid)
     return HSA_ERR_UNSUPPORTED;
   return HSA_OK;
 }
@@ -1338,15 +1347,17 @@ hsa_status_t hsa_rope_apply(const hsa_config_t* cfg, const hsa_rope_t* rope, con
                             int64_t o_token_stride, void* stream) {
   hsa_status_t st = check_cfg(cfg);
   if (st != HSA_OK) return st;
-  if (!rope || !x || !o || n < 0 || heads < 1) return HSA_ERR_INVALID_ARG;
+  if (!rope || (n != 0 && (!x || !o)) || n < 0 || heads < 1) return HSA_ERR_INVALID_ARG;
   if (check_strides(x_batch_stride, x_token_stride) != HSA_OK ||
       check_strides(o_batch_stride, o_token_stride) != HSA_OK)
     return HSA_ERR_INVALID_ARG;
   RopeParams p{};
   if (!rope_table(rope, cfg->head_dim, inverse != 0, pos, first, p.table)) return HSA_ERR_INVALID_ARG;
   if (heads > HSA_MAX_HEADS || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
-  if ((int64_t)n * heads * cfg->head_dim > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  if ((int64_t)n * heads * cfg->head_dim > 0x7fffffff) return HSA_ERR_UNSUPPORTED;
   if (n == 0) return HSA_OK;
+  if (!apart(o_batch_stride, o_token_stride, cfg->batch, n, (int64_t)heads * cfg->head_dim))
+    return HSA_ERR_INVALID_ARG;  // two tokens in one place
   p.x = x;
   p.o = o;
   p.x_batch = x_batch_stride;
@@ -1421,7 +1432,7 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
   hsa_status_t st = check_cfg(cfg);
   if (st != HSA_OK) return st;
   if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
-  if (!q || !o || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
+  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
   if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
   if ((int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
   if (k_h)

@@ -295,7 +295,7 @@ def kv_pool(k_pool, v_pool, page_table, cfg: Optional[HsaConfig] = None) -> HsaK
         slots = int(k_pool.shape[0])
         dt = _elem_dtype(cfg)
         for name, t, shape in (("k_pool", k_pool, (slots, H, P, d)), ("v_pool", v_pool, (slots, H, d, P))):
-            if tuple(t.shape) != shape or str(t.dtype) != dt:
+            if t.shape != shape or str(t.dtype) != dt:
                 raise ValueError(f"{name} must be {dt} {shape}, got {t.dtype} {tuple(t.shape)}")
         if page_table.dim() != 2 or page_table.shape[0] != cfg.batch or str(page_table.dtype) != "torch.int32":
             raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "

@@ -151,3 +151,30 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         P.HsaCache8(2, 4, 64, 72, torch.bfloat16, "cpu", kv_heads=4, k=c.k, v=c.v, k_exp=c.k_exp, v_exp=c.v_exp,
                     page_table=c.page_table)
+
+
+def test_empty_and_overlapping_calls():
+    """No tokens need no memory; an output whose tokens share a place is refused."""
+    cfg, rope = P.config(2, 2, 64, 64, "bf16"), P.rope(64)
+
+    def apply(n, ob, ot, x=FAKE, o=FAKE):
+        return P.lib().hsa_rope_apply(by(cfg), by(rope), x, 0, 0, n, 2, None, None, 0, o, ob, ot, None)
+    assert apply(0, 0, 0, x=None, o=None) == 0
+    for n, ob, ot in ((3, 384, 0), (3, 0, 128), (3, 300, 128), (3, 384, 100), (1, 100, 128), (3, 128, 200)):
+        assert apply(n, ob, ot) == 1, (n, ob, ot)
+    pool = H.HsaKvPool(FAKE, FAKE, FAKE, 4, 4)
+    for name, dst in (("hsa_token_write", pool), ("hsa_cache8_write", _cache())):
+        assert getattr(P.lib(), name)(by(cfg), by(dst), None, None, 0, 128, None, 0, 128, 0, None, None, None, None) == 0
+    assert P.lib().hsa_cache8_attn(by(cfg), None, 0, by(_cache()), None, 0, None, 0, 4, None, None, 0, None, None,
+                                   None, 0, None) == 0
+
+
+def test_sizes_past_a_launch_are_refused():
+    lib = P.lib()
+    cfg, pool = P.config(1, 64, 64, 64, "bf16"), H.HsaKvPool(FAKE, FAKE, FAKE, 4, 4)
+    assert lib.hsa_token_write(by(cfg), by(pool), None, FAKE, 0, 4096, FAKE, 0, 4096, 1 << 23, None, None, None,
+                               None) == 2
+    assert lib.hsa_cache8_attn(by(cfg), FAKE, 1 << 29, by(_cache()), None, 0, None, 0, 4, None, None, 0, FAKE, None,
+                               None, 0, None) == 2
+    assert lib.hsa_cache8_attn(by(P.config(1, 2, 64, (1 << 24) + 8, "bf16")), FAKE, 1, by(_cache()), None, 0, None,
+                               0, 4, None, None, 0, FAKE, None, None, 0, None) == 2
