@@ -730,7 +730,9 @@ typedef struct hsa_cache8 {
  * first tokens an earlier call wrote keeps the larger of its scale and the one the
  * new tokens need; if that grows, the older codes are scaled down by the power of two, which
  * rounds only those that become subnormal. A block written from its first
- * token on starts anew, whatever its memory held.
+ * token on starts anew, whatever its memory held. Codes of the block behind the new tokens stay as
+ * they are, and what they stand for is lost if the scale changes: a sequence is written forwards,
+ * and one that was cut back goes on from its new end.
  */
 hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache,
                               const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
@@ -750,14 +752,16 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  *   o[b][i][h] = sum_t softmax_t(scale * q_i . k_t) v_t     (cfg->dtype)
  *   lse[b][h][i] = log sum_t exp(scale * q_i . k_t)          (fp32, nullable)
  * A query that sees no token gets o = 0 and lse = -inf. What lies in a page at or past
- * kv_len is never used, whatever it holds.
+ * kv_len is never used, whatever it holds. (A NaN among the values of a token below kv_len can
+ * reach a query that the causal mask keeps from it: its weight is 0, and 0 times NaN is NaN.)
  * q, o: device [B, n_q, num_heads, d], 16-byte aligned. kv_len: device int32
  * [B], NULL: every token of the listed pages (causal: (cur_first_page +
  * n_cur_pages) * P). q_len: device int32 [B] in [0, n_q], NULL: n_q; rows of o and
  * lse at or past q_len[b] stay as they were. sel: device int32 [B, kv_heads, k_max], NULL
  * with k_max == 0. k_h: host int32 [kv_heads] in [0, k_max], NULL: k_max.
- * Products of bf16 operands (codes are exact in bf16) summed in fp32; bf16 rounds
- * the softmax weights to bf16; fp32 splits queries and weights into three bf16 parts,
+ * Products of bf16 operands (codes are exact in bf16) summed in fp32. A bf16 call rounds
+ * the softmax weights to bf16 (in two parts where a key head has up to 16 rows n_q *
+ * num_heads / kv_heads); an fp32 call splits queries and weights into three bf16 parts,
  * so that nothing but fp32 sums rounds. Sums are joined in a fixed order: the same
  * call gives the same bits. ws: hsa_cache8_attn_workspace_size(...) bytes, 256-byte aligned.
  * Errors: INVALID_ARG (NULL, sizes below 0, an empty list: k_max == 0 and

@@ -81,6 +81,7 @@ class HsaLayer:
     def write_tokens(self, k, v, first=None, count=None, rope=None, pos=None, stream=None):
         """Append tokens: k, v [B, n, H, d] become tokens first[b] + i, i < count[b],
         of each sequence (int32 [B]; default 0 and n), keys turned by rope."""
+        _same_device(k, self.k_pool)
         _h.hsa_token_write(self.cfg, self.pool, k, v, k.shape[1], first=first, count=count, rope=rope, pos=pos,
                            stream=stream)
 
@@ -142,6 +143,12 @@ class HsaLayer:
         return out
 
 
+def _same_device(t, pool):
+    """A call runs where its tokens are, and the cache has to be there too."""
+    if t.get_device() != pool.get_device():
+        raise ValueError(f"the tensors are on {t.device}, the cache on {pool.device}")
+
+
 class HsaCache8:
     """Paged 8-bit KV cache of one layer: e4m3 codes k [slots, Hk, P, d] and v
     [slots, Hk, d, P], exponent bytes of the scales of 64-token blocks k_exp, v_exp [slots,
@@ -186,6 +193,7 @@ class HsaCache8:
     def write(self, k, v, first=None, count=None, pos=None, stream=None):
         """Append tokens: k, v [B, n, kv_heads, d] become tokens first[b] + i, i <
         count[b], of each sequence (int32 [B]; default 0 and n)."""
+        _same_device(k, self.k)
         _h.hsa_cache8_write(self.cfg, self.pool, k, v, k.shape[1], first=first, count=count, rope=self.rope, pos=pos,
                             stream=stream)
 
@@ -193,6 +201,7 @@ class HsaCache8:
                q_len=None, causal: bool = False, out=None, lse=None, stream=None):
         """Attention of q [B, n_q, heads, d] over the selected pages (sel int32 [B,
         kv_heads, k_max], at most k_h of each head) and pages [first_page, + n_pages)."""
+        _same_device(q, self.k)
         if out is None:
             out = self.torch.empty_like(q)
         _h.hsa_cache8_attn(self.cfg, q, q.shape[1], self.pool, sel, 0 if sel is None else int(sel.shape[-1]), k_h,
