@@ -449,14 +449,11 @@ struct ManyLayout {
 
 constexpr int many_rows(int d) { return d == 128 ? 256 : 128; }  // query rows of a many-rows item
 
-template <int D, int kW, int QB>
-__global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cache8AttnParams p) {
+template <int D>
+__global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache8AttnParams p) {
   using L = ManyLayout<D>;
   constexpr int KK = D / 16, NM = D / 32;
-  constexpr int kThreads = 64 * kW, kRows = many_rows(D);
-  static_assert(32 * QB * kW == kRows, "rows of an item");
-  constexpr int kLd = 4 * D;  // threads that convert: 16 codes of keys and 16 of values each
-  static_assert(kLd <= kThreads, "a tile's codes are 16 a thread");
+  constexpr int kRows = many_rows(D);  // (32 a wave; 4 D threads: 16 codes of a tile's keys each, 16 of its values)
   __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -481,17 +478,16 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
   const int n = t_hi - t_lo;
 
   // queries
-  u32x4 qf[QB][KK];
-  int lim[QB];
-  const int row0 = rt * kRows + wave * 32 * QB;
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const int r = row0 + 32 * qb + l32, i = min(r / p.G, w.q_len - 1);
-    lim[qb] = cache8_limit(p, w, i);
+  u32x4 qf[KK];
+  int lim;
+  const int row0 = rt * kRows + wave * 32;
+  {
+    const int r = row0 + l32, i = min(r / p.G, w.q_len - 1);
+    lim = cache8_limit(p, w, i);
     const uint16_t* q =
         static_cast<const uint16_t*>(p.q) + (((size_t)b * p.n_q + i) * p.H + h * p.G + r % p.G) * D + 8 * half;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) qf[qb][kk] = ld_global16(q + 16 * kk);
+    for (int kk = 0; kk < KK; ++kk) qf[kk] = ld_global16(q + 16 * kk);
   }
   const int lim_first = cache8_limit(p, w, min(__builtin_amdgcn_readfirstlane(row0 / p.G), w.q_len - 1));
   const bool active = row0 < rt * kRows + w.rows;
@@ -526,7 +522,6 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
   Tile ring[4];
   u32x4 kc, vc;  // the codes of the next tiles, 16 a thread
   uint32_t ke = 0, ve0 = 0, ve1 = 0;
-  const bool loads = kLd == kThreads || wave < kLd / 64;
   const int krow_ld = tid / (D / 16), vtok_ld = 16 * (tid & 3);
   const uint32_t vplace = (uint32_t)(tid >> 2) * (uint32_t)p.P + vtok_ld;
   // the page's slot and token of the tile's token x
@@ -547,8 +542,7 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     t.cut = p.P - off;
     t.ta = lp >= 0 ? lp * p.P + off : INT_MAX - 128;
     t.tb = lp2 >= 0 ? lp2 * p.P - t.cut : INT_MAX - 128;
-    if (!loads) {
-    } else if (t.cut >= 64) {  // one page: its place is scalar
+    if (t.cut >= 64) {  // one page: its place is scalar
       const size_t head = (size_t)t.slot_a * p.Hk + h;
       kc = ld_global16(p.k + (head * p.P + t.off) * D + 16 * tid);
       ke = p.k_exp[head * p.nb + ((uint32_t)(t.off + krow_ld) >> 6)];
@@ -570,7 +564,6 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     }
   };
   auto load_v = [&](const Tile& t) __attribute__((always_inline)) {
-    if (!loads) return;
     if (t.cut >= 64) {
       const size_t head = (size_t)t.slot_a * p.Hk + h;
       const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(p.v + head * D * p.P + t.off + vplace);
@@ -588,7 +581,6 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     ve1 = p.v_exp[h1 * p.nb + (at1 >> 6)];
   };
   auto put_k = [&](int buf) __attribute__((always_inline)) {
-    if (!loads) return;
     const float s = scale_of(ke);
     const int row = krow_ld, c0 = 2 * (tid % (D / 16));
     uint8_t* dst = smem + buf * L::kTileK + row * L::kRowK;
@@ -600,7 +592,6 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     return t.ta + min(t.cut, 64) > most || (t.cut < 64 && t.tb + 64 > most);
   };
   auto put_v = [&](int buf, const Tile& t) __attribute__((always_inline)) {
-    if (!loads) return;
     if (beyond(t, w.lim)) {
       // codes past the last token any row sees may be anything
       const int t0 = (vtok_ld < t.cut ? t.ta : t.tb) + vtok_ld, t1 = (vtok_ld + 8 < t.cut ? t.ta : t.tb) + vtok_ld + 8;
@@ -614,16 +605,11 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     *reinterpret_cast<u32x4*>(dst + (((c0 + 1) ^ L::swz_v(row)) << 4)) = codes_to_bf16(vc[2], vc[3], scale_of(ve1));
   };
 
-  f32x16 acc[QB][NM], sa[QB], sb[QB];
-  float m_run[QB], l_run[QB];
+  f32x16 acc[NM], sa, sb;
   const float c2 = p.scale_log2;
+  float m_run = softmax_floor(c2), l_run = 0.f;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    m_run[qb] = softmax_floor(c2);
-    l_run[qb] = 0.f;
-#pragma unroll
-    for (int m = 0; m < NM; ++m) acc[qb][m] = f32x16{0};
-  }
+  for (int m = 0; m < NM; ++m) acc[m] = f32x16{0};
   const int krow = (l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // bits 2 and 3 swapped
   // Operands: slice j of key half kh in key buffer buf; dim block m of 16-key group ks. A
   // lane's chunks of a row are its first one's place with bits 5 to 7 turned.
@@ -635,122 +621,99 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
   auto vop = [&](uint32_t at, int ks, int m) __attribute__((always_inline)) {
     return ld_lds16(smem + (at ^ (ks << 5)) + m * 32 * L::kRowV);
   };
-  // Two weights of 16-key group g of query block qb (score registers 8 g + 2 i, + 1), packed.
-  auto weigh = [&](const f32x16 (&s)[QB], const float (&mc)[QB], int g, int qb, int i) __attribute__((always_inline)) {
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[qb][8 * g + 2 * i], c2, -mc[qb]));
-    const float y = __builtin_amdgcn_exp2f(fmaf(s[qb][8 * g + 2 * i + 1], c2, -mc[qb]));
-    l_run[qb] += x + y;
+  // Two weights of 16-key group g (score registers 8 g + 2 i, + 1), packed.
+  auto weigh = [&](const f32x16& s, float mc, int g, int i) __attribute__((always_inline)) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * g + 2 * i], c2, -mc));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * g + 2 * i + 1], c2, -mc));
+    l_run += x + y;
     return pack_bf16(x, y);
   };
   // keys of half kh that a query does not see (the eight keys of a group are of one page)
-  auto mask = [&](const Tile& t, int kh, f32x16 (&s)[QB]) __attribute__((always_inline)) {
+  auto mask = [&](const Tile& t, int kh, f32x16& s) __attribute__((always_inline)) {
     int mine = 32 * kh + 8 * half;
     asm volatile("" : "+v"(mine));  // (nothing of this is kept through the walk)
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
+    for (int g = 0; g < 2; ++g) {
+      const int key = mine + 16 * g;
+      const int sees = lim - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int key = mine + 16 * g;
-        const int sees = lim[qb] - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r >= sees) s[qb][8 * g + r] = -INFINITY;
-      }
-  };
-  // The largest of a half's scores, and the reference that follows it as in the few-rows kernel.
-  auto largest = [&](const f32x16 (&s)[QB], float (&mx)[QB]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      mx[qb] = s[qb][0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mx[qb] = fmaxf(mx[qb], s[qb][r]);
+      for (int x = 0; x < 8; ++x)
+        if (x >= sees) s[8 * g + x] = -INFINITY;
     }
   };
-  auto raise = [&](const float (&mx)[QB]) __attribute__((always_inline)) {
+  // The largest of a half's scores, and the reference that follows it as in the few-rows kernel.
+  auto largest = [&](const f32x16& s) __attribute__((always_inline)) {
+    float mx = s[0];
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      if (__any(mx[qb] * c2 > m_run[qb] * c2 + 8.f)) {
-        const float top = fmaxf(mx[qb], __shfl_xor(mx[qb], 32));
-        const float m_new = top * c2 > m_run[qb] * c2 + 8.f ? top : m_run[qb];
-        const float alpha = __builtin_amdgcn_exp2f((m_run[qb] - m_new) * c2);
-        l_run[qb] *= alpha;
+    for (int x = 1; x < 16; ++x) mx = fmaxf(mx, s[x]);
+    return mx;
+  };
+  auto raise = [&](float mx) __attribute__((always_inline)) {
+    if (__any(mx * c2 > m_run * c2 + 8.f)) {
+      const float top = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = top * c2 > m_run * c2 + 8.f ? top : m_run;
+      const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c2);
+      l_run *= alpha;
 #pragma unroll
-        for (int m = 0; m < NM; ++m) acc[qb][m] *= alpha;
-        m_run[qb] = m_new;
-      }
+      for (int m = 0; m < NM; ++m) acc[m] *= alpha;
+      m_run = m_new;
     }
   };
   // Half a step: the softmax and value product of key half kh (scores s, value buffer vb), and
-  // the scores sn of the half after it: half nh of tile nt, in key buffer kb. It goes by pairs of matrix instructions, which share an
-  // operand that was read four pairs before; between the pairs go the weights (those of the
-  // first 16 keys two a pair and query block, so that their products can begin, those of the
-  // second one), the conversion of the tiles to come, and the maximum. The order is the source's:
-  // left to itself the compiler reads operands right before their use.
-  auto half_step = [&](int vb, int kh, const f32x16 (&s)[QB], int kb, int nh, const Tile& nt, f32x16 (&sn)[QB],
+  // the scores sn of the half after it: half nh of tile nt, in key buffer kb. An operand is
+  // read four matrix instructions before its use; between them go the weights (those of the first 16 keys
+  // spread so that their products can begin, then those of the second), the conversion of
+  // the tiles to come, and the maximum. The order is the source's: left to itself the
+  // compiler reads operands right before their use.
+  auto half_step = [&](int vb, int kh, const f32x16& s, int kb, int nh, const Tile& nt, f32x16& sn,
                        auto&& tail) __attribute__((always_inline)) {
-    constexpr int NP = KK + 2 * NM;                           // pairs
-    constexpr int kFirst = KK / 2;                            // pairs that the first 16 keys' weights take
-    constexpr int kSecond = KK + NM - kFirst;                 // pairs that the second 16 keys' take
-    float mc[QB], mx[QB];
-    u32x4 pk[2][QB];
-    u32x4 f[4];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      mc[qb] = m_run[qb] * c2;
-      mx[qb] = -INFINITY;
-      sn[qb] = f32x16{0};
-    }
+    constexpr int NP = KK + 2 * NM;            // matrix instructions
+    constexpr int kFirst = KK / 2;             // of them, beside the weights of the first 16 keys
+    constexpr int kSecond = KK + NM - kFirst;  // and of the second
+    float mc = m_run * c2, mx = -INFINITY;
+    u32x4 pk[2], f[4];
+    sn = f32x16{0};
     uint32_t k_at = kfirst + kb * L::kTileK, v_at = L::kVBase + vfirst + vb * L::kTileV;
     asm volatile("" : "+v"(k_at), "+v"(v_at));  // (a place each, not one for every operand)
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = kop(k_at, nh, i);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      // (what a pair computes from is opaque before it, and what it leaves is used in it)
+      // (what an instruction computes from is opaque before it, and what it leaves is used in it)
       __builtin_amdgcn_sched_barrier(0);
       u32x4 a = f[i & 3];
       asm volatile("" : "+v"(a));
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) asm volatile("" : "+v"(mc[qb]));
+      asm volatile("" : "+v"(mc));
       const int n = i + 4;
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        if (i < KK) sn[qb] = mfma32(a, qf[qb][i], sn[qb]);
-        else acc[qb][(i - KK) % NM] = mfma32(a, pk[(i - KK) / NM][qb], acc[qb][(i - KK) % NM]);
-      }
+      if (i < KK) sn = mfma32(a, qf[i], sn);
+      else acc[(i - KK) % NM] = mfma32(a, pk[(i - KK) / NM], acc[(i - KK) % NM]);
       if (n < KK) f[i & 3] = kop(k_at, nh, n);
       else if (n < NP) f[i & 3] = vop(v_at, 2 * kh + (n - KK) / NM, (n - KK) % NM);
-      // packed weights: four a query block of each 16 keys
 #pragma unroll
-      for (int x = 0; x < 4 * QB; ++x) {
-        const int qb = x % QB, word = x / QB;
+      for (int x = 0; x < 4; ++x) {  // packed weights: four of each 16 keys
         uint32_t e;
-        if (i < kFirst && x * kFirst / (4 * QB) == i) {
-          e = weigh(s, mc, 0, qb, word);
-          asm volatile("" : "+v"(e), "+v"(l_run[qb]));
-          pk[0][qb][word] = e;
+        if (i < kFirst && x * kFirst / 4 == i) {
+          e = weigh(s, mc, 0, x);
+          asm volatile("" : "+v"(e), "+v"(l_run));
+          pk[0][x] = e;
         }
-        if (i >= kFirst && i < kFirst + kSecond && x * kSecond / (4 * QB) == i - kFirst) {
-          e = weigh(s, mc, 1, qb, word);
-          asm volatile("" : "+v"(e), "+v"(l_run[qb]));
-          pk[1][qb][word] = e;
+        if (i >= kFirst && i < kFirst + kSecond && x * kSecond / 4 == i - kFirst) {
+          e = weigh(s, mc, 1, x);
+          asm volatile("" : "+v"(e), "+v"(l_run));
+          pk[1][x] = e;
         }
       }
-      if (i >= KK + NM) {
-        // (they were complete KK pairs ago)
+      if (i >= KK + NM) {  // (the scores were complete NM instructions ago)
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-#pragma unroll
-          for (int r = (i - KK - NM) * 16 / NM; r < (i - KK - NM + 1) * 16 / NM; ++r) mx[qb] = fmaxf(mx[qb], sn[qb][r]);
-          asm volatile("" : "+v"(mx[qb]));
-        }
+        for (int x = (i - KK - NM) * 16 / NM; x < (i - KK - NM + 1) * 16 / NM; ++x) mx = fmaxf(mx, sn[x]);
+        asm volatile("" : "+v"(mx));
       }
       if (i == KK) tail();
     }
     __builtin_amdgcn_sched_barrier(0);
     if (__builtin_expect(beyond(nt, lim_first), 0)) {
       mask(nt, nh, sn);
-      largest(sn, mx);
+      mx = largest(sn);
     }
     raise(mx);
   };
@@ -797,16 +760,11 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     // (ring[1] is tile 0 now)
     lds_barrier();
     if (active) {
+      sa = f32x16{0};
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) sa[qb] = f32x16{0};
-#pragma unroll
-      for (int j = 0; j < KK; ++j)
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) sa[qb] = mfma32(kop(kfirst, 0, j), qf[qb][j], sa[qb]);
+      for (int j = 0; j < KK; ++j) sa = mfma32(kop(kfirst, 0, j), qf[j], sa);
       if (beyond(ring[1], lim_first)) mask(ring[1], 0, sa);
-      float mx[QB];
-      largest(sa, mx);
-      raise(mx);
+      raise(largest(sa));
     }
     for (int t = 0; t < n; t += 2) {
       step(std::integral_constant<int, 0>{});
@@ -814,31 +772,27 @@ __global__ __launch_bounds__(64 * kW, kW == 4 ? 3 : 1) void many_rows_kernel(Cac
     }
   }
   if (!active) return;
+  const int r = row0 + l32, i = r / p.G;
+  const float l = l_run + __shfl_xor(l_run, 32);
+  if (i >= w.q_len) return;
+  if (whole) {
+    const int head = h * p.G + r % p.G;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const int r = row0 + 32 * qb + l32, i = r / p.G;
-    const float l = l_run[qb] + __shfl_xor(l_run[qb], 32);
-    if (i >= w.q_len) continue;
-    if (whole) {
-      const int head = h * p.G + r % p.G;
+    for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int m = 0; m < NM; ++m)
+      for (int g = 0; g < 4; ++g) {
+        const float o[4] = {acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]};
+        cache8_store<uint16_t, 4>(p, b, i, head, 32 * m + 8 * g + 4 * half, o, m_run, l, m == 0 && g == 0 && half == 0);
+      }
+  } else {
+    const size_t part = (((size_t)b * p.Hk + h) * p.n_split + split) * p.part_rows + r;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float o[4] = {acc[qb][m][4 * g], acc[qb][m][4 * g + 1], acc[qb][m][4 * g + 2], acc[qb][m][4 * g + 3]};
-          cache8_store<uint16_t, 4>(p, b, i, head, 32 * m + 8 * g + 4 * half, o, m_run[qb], l,
-                                    m == 0 && g == 0 && half == 0);
-        }
-    } else {
-      const size_t part = (((size_t)b * p.Hk + h) * p.n_split + split) * p.part_rows + r;
+    for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int m = 0; m < NM; ++m)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4*>(p.part_o + part * D + 32 * m + 8 * g + 4 * half) =
-              f32x4{acc[qb][m][4 * g], acc[qb][m][4 * g + 1], acc[qb][m][4 * g + 2], acc[qb][m][4 * g + 3]};
-      if (half == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_run[qb], l};
-    }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(p.part_o + part * D + 32 * m + 8 * g + 4 * half) =
+            f32x4{acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]};
+    if (half == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_run, l};
   }
 }
 
@@ -961,7 +915,7 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
   const int cols = p.rows_per_item / 16;
   if (dtype == HSA_DTYPE_BF16) {
     if (p.stream)
-      many_rows_kernel<D, D / 16, 1><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
+      many_rows_kernel<D><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
     else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
     else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
     else if constexpr (D == 64) launch_rows<uint16_t, D, 4, 1>(p, B, s);
