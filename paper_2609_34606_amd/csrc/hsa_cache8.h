@@ -10,11 +10,9 @@
 namespace hsa {
 
 // One item (a tile of query rows of one key head): its queries and its 64-key tiles.
-// The list is n_sel selected pages, then pages [cur_first, ..); a page of 64 tokens or more is
-// tpp tiles (its last one shifted back to end at the page's end); of pages below 64
-// tokens, ppt whole ones share a tile where their size divides 64, and else each
-// has a tile of its own. Many-rows items (stream) cut the listed tokens every 64 instead,
-// whatever pages they are in.
+// The list is n_sel selected pages, then pages [cur_first, ..). Its tokens are one stream, cut every
+// 64 whatever pages they are in (stream), or a page is tpp tiles, its last one shifted back to
+// end at the page's end.
 struct Cache8Walk {
   int len, q_len;  // tokens and queries of the sequence
   int base;        // causal: query i sees tokens below base + i + 1
@@ -48,25 +46,25 @@ __device__ __forceinline__ Cache8Walk cache8_walk(const Cache8AttnParams& p, int
   const int full = __builtin_amdgcn_readfirstlane(cur / p.P), rest = cur - full * p.P;
   w.n_list = w.n_sel + full + (rest > 0 ? 1 : 0);
   if (p.stream) w.n_tiles = (int)(((int64_t)w.n_sel * p.P + cur + 63) >> 6);
-  else if (p.ppt > 1) w.n_tiles = __builtin_amdgcn_readfirstlane((w.n_list + p.ppt - 1) / p.ppt);
   else w.n_tiles = w.n_sel * p.tpp + full * p.tpp + (rest + 63) / 64;
   return w;
 }
 
-// Small pages: granule gr (8 keys) of tile t is in the page at list position li, from token off
-// of it on. ok: it is a token of a listed page (else it repeats one).
+// Granule gr (8 tokens) of a tile of the stream that begins in the page at list position li, at
+// the page's granule at: its list position and first token within the page. ok: it is a token of a
+// listed page (else it repeats one).
 struct Cache8Granule {
   int li, off;
   bool ok;
 };
-__device__ __forceinline__ Cache8Granule cache8_granule(const Cache8AttnParams& p, const Cache8Walk& w, int t, int gr) {
+__device__ __forceinline__ Cache8Granule cache8_granule(const Cache8AttnParams& p, const Cache8Walk& w, int li, int at,
+                                                        int gr) {
+  const int x = at + gr;                // below gpp + 8
+  const int pg = (x * p.gmul) >> 16;    // x / gpp: exact while (gpp + 8) gpp is below 2^16
   Cache8Granule a;
-  const int per = p.ppt > 1 ? p.P : 64;
-  const int pg = 8 * gr / per, li = t * p.ppt + pg;
-  a.off = 8 * gr - pg * per;
-  a.ok = li < w.n_list && a.off < p.P;
-  a.li = min(li, w.n_list - 1);
-  a.off = min(a.off, p.P - 8);
+  a.off = 8 * (x - pg * p.gpp);
+  a.ok = li + pg < w.n_list;
+  a.li = min(li + pg, w.n_list - 1);
   return a;
 }
 // Logical page of list position li and the slot of a page, per lane.

@@ -79,8 +79,8 @@ __device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
 // from HBM to the registers of the wave that uses them, 16 bytes a lane; a
 // score block's rows are read in 64-byte pieces, a value block's too.
 // Bound: HBM (2 d bytes a token and key head).
-template <typename T, int D, int kCols, int kParts, bool kSmallP, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kSmallP ? 3 : 1) void few_rows_kernel(Cache8AttnParams p) {
+template <typename T, int D, int kCols, int kParts, bool kStream, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kStream ? 3 : 1) void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
   constexpr int kRows = 16 * kCols;
@@ -147,19 +147,20 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
   bool masked;            // whether some query does not see all of the tile
 
   const int rho = 4 * (c16 >> 2);  // key row of the lane in score block i: 4 rho + 4 i + c16 % 4
-  int li = 0, kt = 0, li_next = 0, kt_next = 0;  // list position and tile within its page
-  if constexpr (!kSmallP) {
-    li = __builtin_amdgcn_readfirstlane((t_lo + wave) / p.tpp);
-    kt = (t_lo + wave) - li * p.tpp;
-  }
-  // The tile's page, and that of the wave's next tile: looked up a tile ahead. Small pages: the
-  // slots of the lane's two key and two value granules (8 tokens), and the values' first tokens.
+  // The tile's first page (list position) and tile, or granule of the stream, within it. A
+  // wave's next tile is kWaves on.
+  const int per_page = kStream ? p.gpp : p.tpp, on = kStream ? 8 * kWaves : kWaves;
+  int li = __builtin_amdgcn_readfirstlane((t_lo + wave) * (kStream ? 8 : 1) / per_page);
+  int kt = (t_lo + wave) * (kStream ? 8 : 1) - li * per_page, li_next = 0, kt_next = 0;
+  const int on_pages = __builtin_amdgcn_readfirstlane(on / per_page), on_rest = on - on_pages * per_page;
+  // The tile's page, and that of the wave's next tile: looked up a tile ahead. Stream: the
+  // slots of the lane's two key and two value granules, and the values' first tokens.
   int lp = 0, slot = 0, lp_next = 0, slot_next = 0;
   int ks[2], vs[2], vt[2], ks_next[2], vs_next[2], vt_next[2];
-  auto look_up = [&](int t, int (&k)[2], int (&v)[2], int (&first)[2]) {
+  auto look_up = [&](int l0, int at, int (&k)[2], int (&v)[2], int (&first)[2]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {  // keys 4 rho + 8 u + 0..7: score blocks 2 u and 2 u + 1
-      const Cache8Granule a = cache8_granule(p, w, t, (rho >> 1) + u), c = cache8_granule(p, w, t, 2 * g + u);
+      const Cache8Granule a = cache8_granule(p, w, l0, at, (rho >> 1) + u), c = cache8_granule(p, w, l0, at, 2 * g + u);
       k[u] = slot_v(p, ptrow, page_v(p, w, selrow, a.li));
       const int page = page_v(p, w, selrow, c.li);
       v[u] = slot_v(p, ptrow, page);
@@ -167,23 +168,23 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     }
   };
   auto look_ahead = [&](int t) {
-    if constexpr (kSmallP) {
-      if (t + kWaves < t_hi) look_up(t + kWaves, ks_next, vs_next, vt_next);
-    } else {
-      kt_next = kt + kWaves;
-      li_next = li;
-      while (kt_next >= p.tpp) {
-        kt_next -= p.tpp;
-        ++li_next;
-      }
-      if (t + kWaves < t_hi) {
+    kt_next = kt + on_rest;
+    li_next = li + on_pages;
+    if (kt_next >= per_page) {
+      kt_next -= per_page;
+      ++li_next;
+    }
+    if (t + kWaves < t_hi) {
+      if constexpr (kStream) {
+        look_up(li_next, kt_next, ks_next, vs_next, vt_next);
+      } else {
         lp_next = page_of(li_next);
         slot_next = slot_of(lp_next);
       }
     }
   };
-  auto load_keys = [&](int t) {
-    if constexpr (!kSmallP) {
+  auto load_keys = [&]() {
+    if constexpr (!kStream) {
       const size_t head = (size_t)slot * p.Hk + h;
       const int w0 = min(kt * 64, p.P - 64);
       const uint8_t* kb = p.k + (head * p.P + w0 + 4 * rho + (c16 & 3)) * D + 16 * g;
@@ -195,9 +196,9 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     } else {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const Cache8Granule a = cache8_granule(p, w, t, (rho >> 1) + u);
+        const Cache8Granule a = cache8_granule(p, w, li, kt, (rho >> 1) + u);
         const size_t head = (size_t)ks[u] * p.Hk + h;
-        ksc[u] = scale_of(p.k_exp[head * p.nb]);
+        ksc[u] = scale_of(p.k_exp[head * p.nb + (a.off >> 6)]);
         const uint8_t* kb = p.k + (head * p.P + a.off + (c16 & 3)) * D + 16 * g;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -207,8 +208,8 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
       }
     }
   };
-  auto load_values = [&](int t) {
-    if constexpr (!kSmallP) {
+  auto load_values = [&]() {
+    if constexpr (!kStream) {
       const size_t head = (size_t)slot * p.Hk + h;
       const int w0 = min(kt * 64, p.P - 64);
       const uint8_t* vb = p.v + (head * D + c16) * p.P + w0 + 16 * g;
@@ -220,10 +221,10 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
       vsc[0] = vsc[1] = scale_of(p.v_exp[head * p.nb + kt]);
     } else {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) vsc[u] = scale_of(p.v_exp[((size_t)vs[u] * p.Hk + h) * p.nb]);
+      for (int u = 0; u < 2; ++u)
+        vsc[u] = scale_of(p.v_exp[((size_t)vs[u] * p.Hk + h) * p.nb + (cache8_granule(p, w, li, kt, 2 * g + u).off >> 6)]);
       if (p.P % 16 == 0) {  // both granules are of one page
-        const int off = min(cache8_granule(p, w, t, 2 * g).off, p.P - 16);  // (past the page: masked)
-        const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + off;
+        const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + cache8_granule(p, w, li, kt, 2 * g).off;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
           const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(vb + (size_t)(16 * m) * p.P);
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
       } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const Cache8Granule a = cache8_granule(p, w, t, 2 * g + u);
+          const Cache8Granule a = cache8_granule(p, w, li, kt, 2 * g + u);
           const uint8_t* vb = p.v + (((size_t)vs[u] * p.Hk + h) * D + c16) * p.P + a.off;
 #pragma unroll
           for (int m = 0; m < M; ++m) {
@@ -245,8 +246,8 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     }
   };
   // what the mask of the tile needs, once its place is known
-  auto place = [&](int t) {
-    if constexpr (!kSmallP) {
+  auto place = [&]() {
+    if constexpr (!kStream) {
       const int w0 = min(kt * 64, p.P - 64), first = lp * p.P + w0 + 16 * g;
       // a tile that the page's end shifts back repeats keys of the one before
       tok[0] = w0 + 16 * g >= kt * 64 ? first : INT_MAX - 8;
@@ -255,23 +256,23 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     } else {
       tok[0] = vt[0];
       tok[1] = vt[1];
-      masked = true;
+      masked = __any(max(vt[0], vt[1]) + 8 > lim_first);
     }
   };
 
   if (t_lo + wave < t_hi) {
-    if constexpr (kSmallP) {
-      look_up(t_lo + wave, ks, vs, vt);
+    if constexpr (kStream) {
+      look_up(li, kt, ks, vs, vt);
     } else {
       lp = page_of(li);
       slot = slot_of(lp);
     }
-    load_keys(t_lo + wave);
-    load_values(t_lo + wave);
+    load_keys();
+    load_values();
   }
   for (int t = t_lo + wave; t < t_hi; t += kWaves) {
     look_ahead(t);
-    place(t);
+    place();
     const bool more = t + kWaves < t_hi;
     f32x4 s[kCols][4];
 #pragma unroll
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
             for (int k = 0; k < kParts; ++k) s[n][i] = mfma16(a, qf[n][c][u][k], s[n][i]);
         }
     // the next tile's keys take the registers of these
-    if constexpr (kSmallP) {
+    if constexpr (kStream) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         ks[u] = ks_next[u];
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     slot = slot_next;
     li = li_next;
     kt = kt_next;
-    if (more) load_keys(t + kWaves);
+    if (more) load_keys();
     if (masked) {
 #pragma unroll
       for (int n = 0; n < kCols; ++n)
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
 #pragma unroll
           for (int k = 0; k < kWParts; ++k) acc[n][m] = mfma16(a, pk[n][u][k], acc[n][m]);
       }
-    if (more) load_values(t + kWaves);
+    if (more) load_values();
   }
 
   // Join the waves: 16 rows at a time through LDS, then kShare threads a row.
@@ -900,12 +901,11 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Cache8AttnParams p) {
 template <typename T, int D, int kCols, int kParts>
 void launch_rows(const Cache8AttnParams& p, int B, hipStream_t s) {
   const dim3 grid(p.n_split * p.Hk * p.n_rt, B);
-  const bool small = p.P < 64;
   if (kCols == 1 && p.waves == 8) {
-    if (small) few_rows_kernel<T, D, 1, kParts, true, 8><<<grid, 512, 0, s>>>(p);
+    if (p.stream) few_rows_kernel<T, D, 1, kParts, true, 8><<<grid, 512, 0, s>>>(p);
     else few_rows_kernel<T, D, 1, kParts, false, 8><<<grid, 512, 0, s>>>(p);
   } else {
-    if (small) few_rows_kernel<T, D, kCols, kParts, true, 4><<<grid, 256, 0, s>>>(p);
+    if (p.stream) few_rows_kernel<T, D, kCols, kParts, true, 4><<<grid, 256, 0, s>>>(p);
     else few_rows_kernel<T, D, kCols, kParts, false, 4><<<grid, 256, 0, s>>>(p);
   }
 }
@@ -914,7 +914,7 @@ template <int D>
 hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s) {
   const int cols = p.rows_per_item / 16;
   if (dtype == HSA_DTYPE_BF16) {
-    if (p.stream)
+    if (p.many)
       many_rows_kernel<D><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
     else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
     else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
@@ -943,17 +943,23 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
 
 void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged) {
   p.nb = (p.P + 63) / 64;
-  p.tpp = p.P < 64 ? 1 : p.nb;
-  p.ppt = p.P < 64 && 64 % p.P == 0 ? 64 / p.P : 1;
+  p.tpp = p.nb;
+  p.gpp = p.P / 8;
+  p.gmul = 65536 / p.gpp + 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
   const int64_t rows = (int64_t)p.n_q * p.G;
   const bool many = dtype == HSA_DTYPE_BF16 && rows > 64 && p.P >= 64;
-  p.stream = many;
-  const int64_t tiles = std::max<int64_t>(
-      1, many ? (list * p.P + 63) / 64 : (p.ppt > 1 ? (list + p.ppt - 1) / p.ppt : list * p.tpp));
-  // A list of up to 32 tiles is not split: eight waves take up to four tiles each, and one
-  // launch does it all.
-  const bool brief = !many && tiles <= 32 && (rows <= 16 || (int64_t)B * p.Hk * ((rows + 15) / 16) <= 256);
+  p.many = many;
+  // Pages below 64 tokens are walked as a stream. Larger ones are not, though their last tile repeats
+  // tokens: the stream looks up two pages a lane (32 sequences of up to 16384 tokens, 8 key heads:
+  // pages of 72, 161 us as a stream and 143 by the page; of 200, 182 and 145; of 16, 140).
+  p.stream = many || p.P < 64;
+  const int64_t tiles = std::max<int64_t>(1, p.stream ? (list * p.P + 63) / 64 : list * p.tpp);
+  // Little work, up to two tiles for each of eight waves of every CU: eight waves a workgroup and
+  // 16 rows an item. What counts then is how many tiles a wave does after one another, and a second
+  // launch if they are cut.
+  const int64_t items16 = (int64_t)B * p.Hk * ((rows + 15) / 16);
+  const bool brief = !many && items16 <= 4096 && items16 * tiles <= 4096 && (rows <= 16 || items16 <= 256);
   const int most = dtype == HSA_DTYPE_BF16 && p.d == 64 ? 64 : 32;
   p.rows_per_item = many ? many_rows(p.d) : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
   p.waves = brief ? 8 : 4;
@@ -974,17 +980,30 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
         n = k;
       }
     }
-  } else if (!brief) {
-    const int64_t most_n = std::max<int64_t>(1, std::min<int64_t>(kMaxSplit, tiles / 16));
+  } else if (brief) {
+    // In us (12 key heads, one sequence): a tile after another 3.2, the join 3.5; 16 tiles whole
+    // 12.0, cut in two 12.4; 32 whole 19, cut in four 12.2; 128 cut in 16 13.0, in 8 16.4.
+    double best = 1e300;
+    for (int64_t k = 1; k == 1 || (k * items16 <= 256 && 8 * (k - 1) < tiles); ++k) {
+      const double t = 3.2 * (double)((tiles + 8 * k - 1) / (8 * k)) + (k > 1 ? 3.5 : 0.0);
+      if (t < best) {
+        best = t;
+        n = k;
+      }
+    }
+  } else {
+    const int64_t most_n = std::max<int64_t>(1, std::min<int64_t>(kMaxSplit, tiles / (ragged ? 16 : 8)));
     if (ragged) {
       // Sequences of different lengths: short pieces balance (32 of 1 to 16384 tokens, 8 key
       // heads: pieces of 16 tiles 124 us, of 32 128; 8 of them 42 and 49).
       n = std::min((4096 + items - 1) / items, most_n);
     } else {
-      // Equal pieces: at least two workgroups a CU, and as even a number on each as can be
-      // (8 sequences of 16384: 8 pieces, 512 workgroups, 57 us; 10 pieces 65, 12 61). A
-      // piece's start and end take about four tiles.
-      n = std::min((512 + items - 1) / items, most_n);
+      // Equal pieces: at least two workgroups a CU (one of more than 16 rows: its registers leave no
+      // room for another; 4 sequences of 8192, 32 rows: 8 pieces 25 us, 16 30), and as even a number on each as can be
+      // (8 sequences of 16384: 8 pieces, 512 workgroups, 57 us; 10 pieces 65, 12 61; 8 of 4096 and
+      // 12 key heads: 8 pieces of 8 tiles 26, 4 of 16 29). A piece's start and end take
+      // about four tiles.
+      n = std::min(((p.rows_per_item > 16 ? 256 : 512) + items - 1) / items, most_n);
       double best = 1e300;
       for (int64_t k = n, stop = std::min((2048 + items - 1) / items, most_n); k <= stop; ++k) {
         const double t = (double)((items * k + 255) / 256) * ((double)((tiles + k - 1) / k) + 4.0);

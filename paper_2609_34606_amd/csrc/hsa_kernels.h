@@ -240,8 +240,10 @@ struct Cache8AttnParams {
   int16_t k_h[HSA_MAX_HEADS]; // most pages of each key head's sel row
   // set by plan_cache8
   int32_t nb;                 // scale blocks per page
-  int32_t tpp, ppt;           // 64-key tiles per page; pages per tile
-  int32_t stream;             // tiles of 64 listed tokens, across pages (many rows)
+  int32_t many;               // the many-rows kernel
+  int32_t stream;             // tiles of 64 listed tokens, across pages; else tpp a page
+  int32_t tpp;
+  int32_t gpp, gmul;          // granules (8 tokens) per page, 65536 / gpp + 1
   int32_t rows_per_item, n_rt, part_rows;
   int32_t waves;              // of a few-rows workgroup
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
