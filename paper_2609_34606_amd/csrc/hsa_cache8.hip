@@ -450,12 +450,13 @@ struct ManyLayout {
 
 constexpr int many_rows(int d) { return d == 128 ? 256 : 128; }  // query rows of a many-rows item
 
-template <int D>
-__global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache8AttnParams p) {
+template <int D, bool kSmallP>
+__global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_rows_kernel(Cache8AttnParams p) {
   using L = ManyLayout<D>;
   constexpr int KK = D / 16, NM = D / 32;
   constexpr int kRows = many_rows(D);  // (32 a wave; 4 D threads: 16 codes of a tile's keys each, 16 of its values)
   __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
+  __shared__ int2 first_sm[kSmallP ? 8 : 1][4];  // first tokens of the granules of eight tiles
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // workgroup i runs on XCD i % 8: an XCD takes an eighth of the items in a row, which share
@@ -511,11 +512,16 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
   int kbuf = 0;  // key buffer of tile t
   int li = __builtin_amdgcn_readfirstlane((int)((int64_t)t_lo * 64 / p.P));
   int off = (int)((int64_t)t_lo * 64 - (int64_t)li * p.P);
-  int lp_cur = page_at(li), lp_nxt = page_at(li + 1), lp_nx2 = page_at(li + 2);
-  int slot_cur = slot_at(lp_cur), slot_nxt = slot_at(lp_nxt);
+  int lp_cur = 0, lp_nxt = 0, lp_nx2 = 0, slot_cur = 0, slot_nxt = 0;
+  if constexpr (!kSmallP) {
+    lp_cur = page_at(li), lp_nxt = page_at(li + 1), lp_nx2 = page_at(li + 2);
+    slot_cur = slot_at(lp_cur), slot_nxt = slot_at(lp_nxt);
+  }
 
   // What a tile is read and masked by: its first page's slot, the one after, its first token within
   // the first; and the logical tokens: key j is token ta + j below cut, tb + j from there on.
+  // Small pages: off is in granules, ta and tb say whether the wave's first query, or the item's last, does not
+  // see all of it, and cut is its place in first_sm.
   struct Tile {
     int slot_a, slot_b, off, ta, tb, cut;
   };
@@ -531,11 +537,67 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
     at = second ? x - t.cut : t.off + x;
     return (size_t)(second ? t.slot_b : t.slot_a) * p.Hk + h;
   };
+  // Small pages: a thread looks up the pages of its key row and of its two runs of values, slots
+  // a tile ahead and pages two.
+  int pages[3], slots[3], v_slots[2], next_at = 0, next_first = 0, next_lim = 0, staged = 0;
+  int at = off >> 3;  // of the tile whose pages are looked up next
+  const int on_pages = kSmallP ? __builtin_amdgcn_readfirstlane(8 / p.gpp) : 0, on_rest = 8 - on_pages * p.gpp;
+  auto within = [&](int x, int& pg) __attribute__((always_inline)) {  // token of a granule x in its page, pg on
+    pg = (x * p.gmul) >> 16;
+    return 8 * (x - pg * p.gpp);
+  };
+  const int granules[3] = {krow_ld >> 3, 2 * (tid & 3), 2 * (tid & 3) + 1};
+  auto stage_pages = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int pg;
+      within(at + granules[i], pg);
+      pages[i] = page_at(li + pg);
+    }
+  };
+  auto stage = [&]() __attribute__((always_inline)) {
+    int first[2];
+    next_at = at;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int pg;
+      const int x = within(at + granules[i], pg);
+      slots[i] = slot_at(pages[i]);
+      if (i > 0) first[i - 1] = pages[i] < 0 ? INT_MAX - 8 : pages[i] * p.P + x;
+    }
+    if (tid < 4) first_sm[staged & 7][tid] = int2{first[0], first[1]};
+    const int end = max(first[0], first[1]) + 8;
+    next_first = __any(end > lim_first);
+    next_lim = __any(end > w.lim);
+    ++staged;
+    at += on_rest;
+    li += on_pages;
+    if (at >= p.gpp) {
+      at -= p.gpp;
+      ++li;
+    }
+    stage_pages();
+  };
   auto load_k = [&]() __attribute__((always_inline)) {  // the next tile's keys; the stream moves on
     ring[0] = ring[1];
     ring[1] = ring[2];
     ring[2] = ring[3];
     Tile& t = ring[3];
+    if constexpr (kSmallP) {
+      t.off = next_at;
+      t.ta = next_first;
+      t.tb = next_lim;
+      t.cut = (staged - 1) & 7;
+      int pg;
+      const int x = within(next_at + granules[0], pg);
+      const size_t head = (size_t)slots[0] * p.Hk + h;
+      kc = ld_global16(p.k + (head * p.P + x + (krow_ld & 7)) * D + 16 * (tid % (D / 16)));
+      ke = p.k_exp[head];
+      v_slots[0] = slots[1];
+      v_slots[1] = slots[2];
+      stage();
+      return;
+    }
     const int lp = __builtin_amdgcn_readfirstlane(lp_cur), lp2 = __builtin_amdgcn_readfirstlane(lp_nxt);
     t.slot_a = __builtin_amdgcn_readfirstlane(slot_cur);
     t.slot_b = __builtin_amdgcn_readfirstlane(slot_nxt);
@@ -565,6 +627,17 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
     }
   };
   auto load_v = [&](const Tile& t) __attribute__((always_inline)) {
+    if constexpr (kSmallP) {
+      int pg;
+      const int x0 = within(t.off + granules[1], pg), x1 = within(t.off + granules[2], pg);
+      const size_t h0 = (size_t)v_slots[0] * p.Hk + h, h1 = (size_t)v_slots[1] * p.Hk + h;
+      const u32x2a8 x = *reinterpret_cast<const u32x2a8*>(p.v + (h0 * D + (tid >> 2)) * p.P + x0);
+      const u32x2a8 y = *reinterpret_cast<const u32x2a8*>(p.v + (h1 * D + (tid >> 2)) * p.P + x1);
+      vc = u32x4{x[0], x[1], y[0], y[1]};
+      ve0 = p.v_exp[h0];
+      ve1 = p.v_exp[h1];
+      return;
+    }
     if (t.cut >= 64) {
       const size_t head = (size_t)t.slot_a * p.Hk + h;
       const u32x4a8 x = *reinterpret_cast<const u32x4a8*>(p.v + head * D * p.P + t.off + vplace);
@@ -590,12 +663,17 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
   };
   // whether some query of limit `most` does not see some token of a tile
   auto beyond = [&](const Tile& t, int most) __attribute__((always_inline)) {
+    if constexpr (kSmallP) return (most == w.lim ? t.tb : t.ta) != 0;
     return t.ta + min(t.cut, 64) > most || (t.cut < 64 && t.tb + 64 > most);
   };
   auto put_v = [&](int buf, const Tile& t) __attribute__((always_inline)) {
     if (beyond(t, w.lim)) {
       // codes past the last token any row sees may be anything
-      const int t0 = (vtok_ld < t.cut ? t.ta : t.tb) + vtok_ld, t1 = (vtok_ld + 8 < t.cut ? t.ta : t.tb) + vtok_ld + 8;
+      int t0 = (vtok_ld < t.cut ? t.ta : t.tb) + vtok_ld, t1 = (vtok_ld + 8 < t.cut ? t.ta : t.tb) + vtok_ld + 8;
+      if constexpr (kSmallP) {
+        t0 = first_sm[t.cut][tid & 3].x;
+        t1 = first_sm[t.cut][tid & 3].y;
+      }
       const u32x4 lo = keep_codes(vc, clampi(w.lim - min(t0, w.lim), 0, 8));
       const u32x4 hi = keep_codes(u32x4{0, 0, vc[2], vc[3]}, 8 + clampi(w.lim - min(t1, w.lim), 0, 8));
       vc = u32x4{lo[0], lo[1], hi[2], hi[3]};
@@ -636,7 +714,8 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int key = mine + 16 * g;
-      const int sees = lim - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
+      int sees = lim - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
+      if constexpr (kSmallP) sees = lim - (half ? first_sm[t.cut][2 * kh + g].y : first_sm[t.cut][2 * kh + g].x);
 #pragma unroll
       for (int x = 0; x < 8; ++x)
         if (x >= sees) s[8 * g + x] = -INFINITY;
@@ -749,6 +828,11 @@ __global__ __launch_bounds__(4 * D, D == 64 ? 3 : 1) void many_rows_kernel(Cache
   };
 
   if (n > 0) {
+    if constexpr (kSmallP) {
+      stage_pages();
+      stage();
+      lds_barrier();  // (first_sm of tile 0, which every wave may read below)
+    }
     // K(0), K(1) and V(0) to LDS; K(2) and V(1) on their way
     load_k();
     load_v(ring[3]);
@@ -915,7 +999,8 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
   const int cols = p.rows_per_item / 16;
   if (dtype == HSA_DTYPE_BF16) {
     if (p.many)
-      many_rows_kernel<D><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
+      p.P < 64 ? many_rows_kernel<D, true><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p)
+               : many_rows_kernel<D, false><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
     else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
     else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
     else if constexpr (D == 64) launch_rows<uint16_t, D, 4, 1>(p, B, s);
@@ -948,7 +1033,7 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.gmul = 65536 / p.gpp + 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
   const int64_t rows = (int64_t)p.n_q * p.G;
-  const bool many = dtype == HSA_DTYPE_BF16 && rows > 64 && p.P >= 64;
+  const bool many = dtype == HSA_DTYPE_BF16 && rows > 64;
   p.many = many;
   // Pages below 64 tokens are walked as a stream. Larger ones are not, though their last tile repeats
   // tokens: the stream looks up two pages a lane (32 sequences of up to 16384 tokens, 8 key heads:
@@ -971,7 +1056,7 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
     // one workgroup a CU (two with d = 64): rounds of as many, each of its tiles and about
     // six more for its start and end; pieces cost a partial output of 256 rows written
     // and read again (four)
-    const int64_t slots = p.d == 128 ? 256 : 768;
+    const int64_t slots = p.d == 128 ? 256 : (p.P < 64 ? 512 : 768);
     double best = 1e300;
     for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
       const double t = (double)((items * k + slots - 1) / slots) * ((double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0));

@@ -104,3 +104,16 @@ def test_rotation_strides_past_32_bits():
     P.hsa_rope_apply(cfg, rope, far, 3, apart, first=i32([5, 9]))
     P.hsa_rope_apply(cfg, rope, far, 3, far, first=i32([5, 9]))
     assert torch.equal(apart, want) and torch.equal(far, want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P_", [8, 16, 24, 40, 56])
+def test_many_rows_over_small_pages(P_, d):
+    """Tiles of two to eight pages: in pieces, over selected pages, with lengths that end
+    inside a page, queries that see nothing, a head without pages."""
+    pages = 2000 // P_
+    print(P_, d, flush=True)
+    run_case(P_, 1, 2, 1, d, P_, 90, BF, pages, first=pages - 2, k_max=pages - 4, k_h=[pages - 5])
+    run_case(P_ + 1, 2, 6, 3, d, P_, 200, BF, 30, first=20, k_max=17, k_h=[17, 0, 3], sel_valid=[17, 5, 1],
+             kv_len=[30 * P_ - 3, 20 * P_ + 1], q_len=[200, 111], causal=True)
+    run_case(P_ + 2, 3, 2, 2, d, P_, 130, BF, pages, kv_len=[pages * P_ - 9, 70, 0], q_len=[130, 129, 3], causal=True)
