@@ -92,7 +92,8 @@ __device__ __forceinline__ void cache8_store(const Cache8AttnParams& p, int b, i
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
   }
-  if (lse && p.lse) p.lse[((size_t)b * p.H + head) * p.n_q + i] = l > 0.f ? m * p.sm_scale + logf(l) : (l == l ? -INFINITY : l);
+  if (lse && p.lse)
+    p.lse[((size_t)b * p.H + head) * p.n_q + i] = l > 0.f ? m * p.sm_scale + logf(l) : (l == l ? -INFINITY : l);
 }
 
 }  // namespace hsa

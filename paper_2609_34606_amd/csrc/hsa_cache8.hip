@@ -67,9 +67,9 @@ __device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
   }
 }
 
-// Few query rows: 16 kCols rows of one key head against a range of its tokens. Each
-// of the four waves takes every fourth 64-key tile and keeps an online softmax
-// of its own; the workgroup joins them at the end.
+// Few query rows: 16 kCols rows of one key head against a range of its tokens. A wave takes
+// every kWaves-th 64-key tile and keeps an online softmax of its own; the workgroup
+// joins them at the end. Four waves, or eight where the whole call is little work (plan_cache8).
 //
 // Products are transposed (keys are the rows of S^T = K Q^T, dims those of O^T = V^T P^T),
 // so a lane holds scores of one query and the 16 keys of its quarter. Row m of
@@ -77,16 +77,23 @@ __device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
 // holds 16 consecutive keys, in the order in which the value operand, 16 consecutive codes
 // of a d-major row, has them, and the weights need no exchange between lanes. Codes go
 // from HBM to the registers of the wave that uses them, 16 bytes a lane; a
-// score block's rows are read in 64-byte pieces, a value block's too.
-// Bound: HBM (2 d bytes a token and key head).
+// score block's rows are read in 64-byte pieces, a value block's too. The keys of a wave's next
+// tile are asked for once this one's scores are done with their registers, the values after its
+// output; other waves of the CU (three workgroups of 168 registers) cover the rest.
+// Bound: HBM (2 d bytes a token and key head): 32 sequences of 1 to 16384 tokens, 32 query and 8 key
+// heads, 560 MB in 124 us, 4.6 TB/s; one token over 187200 of 12 heads, 575 MB in 127 us.
+// A kernel that only reads a cache in this pattern takes 115 to 126 us for the latter: value
+// rows of pages of 1560 tokens begin at any multiple of 8 bytes (a copy's reads: 6.1 TB/s). For short
+// lists, latency: 3.2 us a tile that a wave does after another, 9 us for a whole call of one.
 template <typename T, int D, int kCols, int kParts, bool kStream, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kStream ? 3 : 1) void few_rows_kernel(Cache8AttnParams p) {
+__global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kStream ? 3 : 1)
+void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
   constexpr int kRows = 16 * kCols;
   // Parts of a weight. One bf16 part rounds it by up to 2^-9, about what the result's own rounding
-  // adds; two leave 2^-17. A step of up to 16 rows waits for memory and takes two (1 to 3% of
-  // its time); with more rows the second part would cost 7 to 10%. fp32 takes three.
+  // adds; two leave 2^-17. Items of 16 rows wait for memory and take two (1 to 3% of
+  // their time); with more rows the second part would cost 7 to 10%. fp32 takes three.
   constexpr int kWParts = kParts == 3 ? 3 : (kCols == 1 ? 2 : 1);
   constexpr int OS = D + 4;   // floats per row of the join buffer
   __shared__ __attribute__((aligned(16))) float osm[kWaves * 16 * OS];
@@ -95,7 +102,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroup i runs on XCD i % 8. Pieces of one sequence and head come n_items apart, and
   // sequences begin one apart, so that no XCD gets only last pieces, which short
-  // sequences lack (32 sequences of 1 to 16384 tokens: %%% us, pieces together 154).
+  // sequences lack (32 sequences of 1 to 16384 tokens, 8 pieces each: 129 us, pieces together 164).
   const int n_items = p.Hk * p.n_rt, b = blockIdx.y;
   const int x0 = __builtin_amdgcn_readfirstlane((int)((blockIdx.x + blockIdx.y) % gridDim.x));
   // (a quotient comes from the vector unit, and its uses would stay there)
@@ -198,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
       for (int u = 0; u < 2; ++u) {
         const Cache8Granule a = cache8_granule(p, w, li, kt, (rho >> 1) + u);
         const size_t head = (size_t)ks[u] * p.Hk + h;
-        ksc[u] = scale_of(p.k_exp[head * p.nb + (a.off >> 6)]);
+        ksc[u] = scale_of(p.k_exp[head]);
         const uint8_t* kb = p.k + (head * p.P + a.off + (c16 & 3)) * D + 16 * g;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -222,7 +229,7 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
     } else {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        vsc[u] = scale_of(p.v_exp[((size_t)vs[u] * p.Hk + h) * p.nb + (cache8_granule(p, w, li, kt, 2 * g + u).off >> 6)]);
+        vsc[u] = scale_of(p.v_exp[(size_t)vs[u] * p.Hk + h]);  // (a page below 64 tokens is one block)
       if (p.P % 16 == 0) {  // both granules are of one page
         const uint8_t* vb = p.v + (((size_t)vs[0] * p.Hk + h) * D + c16) * p.P + cache8_granule(p, w, li, kt, 2 * g).off;
 #pragma unroll
@@ -426,17 +433,22 @@ __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves ==
   }
 }
 
-// Many query rows: 256 rows of one key head (four waves of 64) against a range of its
-// tokens, one workgroup a CU. Each 64-key tile is turned into bf16 once, on its way from
-// the registers that its codes arrived in to LDS, and read from there by all four waves;
-// a key or value operand serves two blocks of 32 queries.
+// Many query rows: 256 rows of one key head with d = 128 (eight waves of 32, a workgroup a CU), 128
+// with d = 64 (four waves, three workgroups), against a range of its tokens. Each 64-key tile is
+// turned into bf16 once, on its way from the registers that its codes arrived in
+// to LDS, and read from there by all waves.
 //
 // Products are transposed as in the page walk of the bf16 pool (S^T = K Q^T, O^T +=
 // V^T P^T, 32x32x16), with key rows in an order that makes a lane's scores the
-// weights' operand. A wave has its SIMD to itself, so the pipes overlap inside it: a step
-// does the softmax and the value product of tile t and the scores of tile t + 1,
-// matrix instructions between the exponentials.
-// Bound: the matrix pipe and, as close, the vector pipe (exponentials and conversions).
+// weights' operand. A step does the softmax and the value product of half a tile and the scores
+// of the next half, matrix instructions between the exponentials.
+// Bound: the matrix and the vector pipe one after the other. 4680 queries over 10920 tokens, 12 heads
+// (314 GFLOP): 340 us, 924 TFLOP/s; the matrix pipe is busy 44% of the time and the vector pipe
+// (exponentials, their packing, the maximum; 16 codes of each operand a thread and tile) 49%, and the two
+// hardly overlap, neither within a wave nor between the two of a SIMD. A large library product
+// reaches 1322 TFLOP/s (238 us). Waves of 64 rows need more registers than a wave has (spills);
+// 512 rows a workgroup was no faster, and d = 64 with 256 rows slower (55.9 us and 49.5 for causal
+// prompts of up to 1001 tokens; 45 now).
 template <int D>
 struct ManyLayout {
   static constexpr int kRowK = 2 * D, kTileK = 64 * kRowK;  // bytes
@@ -885,7 +897,8 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
 // the launch's timing. The pieces' maxima and sums are on their way before the row's
 // number of pieces is known (a piece that does not exist holds anything, and is
 // not used).
-// Few rows (of few-rows items): a workgroup of eight waves a row, each every eighth piece.
+// Up to 1024 rows: a workgroup of eight waves a row, each every eighth piece (1024 rows of up to 16
+// pieces: 7.0 us).
 template <typename T, int D>
 __global__ __launch_bounds__(512) void join_row_kernel(Cache8AttnParams p) {
   constexpr int E = D / 64, kW = 8;  // dims per lane, waves
@@ -1033,6 +1046,9 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.gmul = 65536 / p.gpp + 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
   const int64_t rows = (int64_t)p.n_q * p.G;
+  // More than 64 rows of bf16 (8 sequences of 8192 tokens, 8 heads, d = 128: 96 rows 66 us, in items of
+  // 32 rows 86; d = 64, 64 rows: 39 us, in one item of 64 rows 30). fp32 has three parts of
+  // everything, and its registers hold 32 rows.
   const bool many = dtype == HSA_DTYPE_BF16 && rows > 64;
   p.many = many;
   // Pages below 64 tokens are walked as a stream. Larger ones are not, though their last tile repeats
@@ -1053,13 +1069,15 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   const int64_t items = (int64_t)B * p.Hk * p.n_rt;
   int64_t n = 1;
   if (many) {
-    // one workgroup a CU (two with d = 64): rounds of as many, each of its tiles and about
-    // six more for its start and end; pieces cost a partial output of 256 rows written
-    // and read again (four)
+    // Rounds of as many workgroups as are resident (one a CU, with d = 64 three, of small pages
+    // two), each of its tiles and about six more for its start and end; pieces cost a
+    // partial output written and read again (four). 8 causal sequences of 8192 tokens,
+    // d = 128, 128 queries: 74 us in four pieces.
     const int64_t slots = p.d == 128 ? 256 : (p.P < 64 ? 512 : 768);
     double best = 1e300;
     for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
-      const double t = (double)((items * k + slots - 1) / slots) * ((double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0));
+      const double each = (double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0);
+      const double t = (double)((items * k + slots - 1) / slots) * each;
       if (t < 0.97 * best) {
         best = t;
         n = k;
@@ -1084,7 +1102,8 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
       n = std::min((4096 + items - 1) / items, most_n);
     } else {
       // Equal pieces: at least two workgroups a CU (one of more than 16 rows: its registers leave no
-      // room for another; 4 sequences of 8192, 32 rows: 8 pieces 25 us, 16 30), and as even a number on each as can be
+      // room for another; 4 sequences of 8192, 32 rows: 8 pieces 25 us, 16 30), and as even a
+      // number on each as can be
       // (8 sequences of 16384: 8 pieces, 512 workgroups, 57 us; 10 pieces 65, 12 61; 8 of 4096 and
       // 12 key heads: 8 pieces of 8 tiles 26, 4 of 16 29). A piece's start and end take
       // about four tiles.
