@@ -1046,21 +1046,23 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.gmul = 65536 / p.gpp + 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
   const int64_t rows = (int64_t)p.n_q * p.G;
-  // More than 64 rows of bf16 (8 sequences of 8192 tokens, 8 heads, d = 128: 96 rows 66 us, in items of
-  // 32 rows 86; d = 64, 64 rows: 39 us, in one item of 64 rows 30). fp32 has three parts of
-  // everything, and its registers hold 32 rows.
-  const bool many = dtype == HSA_DTYPE_BF16 && rows > 64;
+  // Little work, up to two tiles for each of eight waves of every CU: eight waves a workgroup and
+  // 16 rows an item. What counts then is how many tiles a wave does after one another, and a second
+  // launch if they are cut (4 query and 2 key heads, d = 128: 64 queries over 1024 tokens 13 us, in 256
+  // rows a workgroup 19; 512 over 2048 18 and 26).
+  const int64_t items16 = (int64_t)B * p.Hk * ((rows + 15) / 16);
+  const int64_t by_page = p.P < 64 ? (list * p.P + 63) / 64 : list * p.tpp;
+  const bool brief = items16 <= (rows <= 16 ? 4096 : 256) && items16 * by_page <= 4096;
+  // More than 64 rows of bf16 otherwise (8 sequences of 8192 tokens, 8 heads, d = 128: 96 rows 66 us,
+  // in items of 32 rows 86; d = 64, 64 rows: 39 us, in one item of 64 rows 30). fp32 has three
+  // parts of everything, and its registers hold 32 rows.
+  const bool many = !brief && dtype == HSA_DTYPE_BF16 && rows > 64;
   p.many = many;
   // Pages below 64 tokens are walked as a stream. Larger ones are not, though their last tile repeats
   // tokens: the stream looks up two pages a lane (32 sequences of up to 16384 tokens, 8 key heads:
   // pages of 72, 161 us as a stream and 143 by the page; of 200, 182 and 145; of 16, 140).
   p.stream = many || p.P < 64;
-  const int64_t tiles = std::max<int64_t>(1, p.stream ? (list * p.P + 63) / 64 : list * p.tpp);
-  // Little work, up to two tiles for each of eight waves of every CU: eight waves a workgroup and
-  // 16 rows an item. What counts then is how many tiles a wave does after one another, and a second
-  // launch if they are cut.
-  const int64_t items16 = (int64_t)B * p.Hk * ((rows + 15) / 16);
-  const bool brief = !many && items16 <= 4096 && items16 * tiles <= 4096 && (rows <= 16 || items16 <= 256);
+  const int64_t tiles = std::max<int64_t>(1, many ? (list * p.P + 63) / 64 : by_page);
   const int most = dtype == HSA_DTYPE_BF16 && p.d == 64 ? 64 : 32;
   p.rows_per_item = many ? many_rows(p.d) : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
   p.waves = brief ? 8 : 4;
