@@ -1046,17 +1046,21 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.gmul = 65536 / p.gpp + 1;
   const int64_t list = (int64_t)max_list_sel + p.n_cur;
   const int64_t rows = (int64_t)p.n_q * p.G;
-  // Little work, up to two tiles for each of eight waves of every CU: eight waves a workgroup and
-  // 16 rows an item. What counts then is how many tiles a wave does after one another, and a second
-  // launch if they are cut (4 query and 2 key heads, d = 128: 64 queries over 1024 tokens 13 us, in 256
-  // rows a workgroup 19; 512 over 2048 18 and 26).
+  // Little work: eight waves a workgroup and 16 rows an item. Up to two tiles for each wave of every CU,
+  // what counts is how many tiles a wave does after one another, and a second launch if they are
+  // cut. The many-rows kernel starts slower still, so calls of more than 64 bf16 rows come here up to
+  // four tiles a wave (d = 128: 2048 queries of 4 heads, 2 key heads, over 1024 tokens 25 us and 31;
+  // twice the tokens 38 and 36) or sixteen (d = 64: 4096 over 2048 31 us and 35; three ragged
+  // prompts, 2.3 times the work, 50 and 46).
   const int64_t items16 = (int64_t)B * p.Hk * ((rows + 15) / 16);
   const int64_t by_page = p.P < 64 ? (list * p.P + 63) / 64 : list * p.tpp;
-  const bool brief = items16 <= (rows <= 16 ? 4096 : 256) && items16 * by_page <= 4096;
+  const bool large = dtype == HSA_DTYPE_BF16 && rows > 64;
+  const int64_t little = large ? (p.d == 64 ? 32768 : 8192) : 4096;
+  const bool brief = items16 <= (large || rows <= 16 ? 4096 : 256) && items16 * by_page <= little;
   // More than 64 rows of bf16 otherwise (8 sequences of 8192 tokens, 8 heads, d = 128: 96 rows 66 us,
   // in items of 32 rows 86; d = 64, 64 rows: 39 us, in one item of 64 rows 30). fp32 has three
   // parts of everything, and its registers hold 32 rows.
-  const bool many = !brief && dtype == HSA_DTYPE_BF16 && rows > 64;
+  const bool many = !brief && large;
   p.many = many;
   // Pages below 64 tokens are walked as a stream. Larger ones are not, though their last tile repeats
   // tokens: the stream looks up two pages a lane (32 sequences of up to 16384 tokens, 8 key heads:
