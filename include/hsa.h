@@ -761,7 +761,7 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  * with k_max == 0. k_h: host int32 [kv_heads] in [0, k_max], NULL: k_max.
  * Products of bf16 operands (codes are exact in bf16) summed in fp32. A bf16 call rounds
  * the softmax weights to bf16 (in two parts where a key head has up to 16 rows n_q *
- * num_heads / kv_heads); an fp32 call splits queries and weights into three bf16 parts,
+ * num_heads / kv_heads, and in other small calls); an fp32 call splits queries and weights into three bf16 parts,
  * so that nothing but fp32 sums rounds. Sums are joined in a fixed order: the same
  * call gives the same bits. ws: hsa_cache8_attn_workspace_size(...) bytes, 256-byte aligned.
  * Errors: INVALID_ARG (NULL, sizes below 0, an empty list: k_max == 0 and

@@ -184,6 +184,8 @@ class HsaCache8:
 
     def rotate(self, q, pos=None, first=None, out=None, inverse: bool = False, stream=None):
         """q [B, n, heads, d] turned by its tokens' positions."""
+        if self.rope is None:
+            raise ValueError("the cache has no rope")
         if out is None:
             out = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
         _h.hsa_rope_apply(self.cfg, self.rope, q, q.shape[1], out, pos=pos, first=first, inverse=inverse,

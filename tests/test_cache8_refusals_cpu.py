@@ -178,3 +178,9 @@ def test_sizes_past_a_launch_are_refused():
                                None, 0, None) == 2
     assert lib.hsa_cache8_attn(by(P.config(1, 2, 64, (1 << 24) + 8, "bf16")), FAKE, 1, by(_cache()), None, 0, None,
                                0, 4, None, None, 0, FAKE, None, None, 0, None) == 2
+
+
+def test_a_cache_without_rope_does_not_rotate():
+    c = P.HsaCache8(1, 2, 64, 64, torch.bfloat16, "cpu", num_slots=2, max_pages=2)
+    with pytest.raises(ValueError):
+        c.rotate(torch.zeros((1, 3, 2, 64), dtype=torch.bfloat16))
