@@ -25,7 +25,6 @@ int64_t token_write_units(int64_t n, int P) {
 
 namespace {
 
-constexpr int kTok = kScaleTok;  // tokens per block
 
 // N codes of x / 2^e (scale = 2^e).
 template <int N>
@@ -62,13 +61,18 @@ __device__ __forceinline__ uint32_t max_bits_f32(uint32_t m) {
   return m;
 }
 
-// Largest of a value over the workgroup's four waves. buf: one slot a wave.
+// Largest of a value over the workgroup's kW waves. buf: one slot a wave. What the workgroup has
+// put into shared memory is there afterwards.
+template <int kW>
 __device__ __forceinline__ uint32_t max_all(uint32_t a, uint32_t* buf, int tid) {
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, m));
   if ((tid & 63) == 0) buf[tid >> 6] = a;
   __syncthreads();
-  return max(max(buf[0], buf[1]), max(buf[2], buf[3]));
+  uint32_t most = buf[0];
+#pragma unroll
+  for (int w = 1; w < kW; ++w) most = max(most, buf[w]);
+  return most;
 }
 
 constexpr uint32_t kInf = 0x7f800000u;
@@ -85,18 +89,20 @@ struct TokenBlock {
   int nb;
 };
 
-template <typename T, int D, bool kEight, int kMode>
+// kTok: most tokens of a block; four threads each.
+template <typename T, int D, bool kEight, int kMode, int kTok>
 __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const TokenBlock& t, int h_lo, int h_hi,
                                            uint32_t* amax) {
   using Item = RopeItem<T, kMode>;
   using Raw = typename Item::El::Raw;
   constexpr int E = 16 / (int)sizeof(T);
-  constexpr int NK = kMode == kRopeSingle ? 1 : kTok * D / E / (kMode == kRopeHalves ? 512 : 256);  // items a thread
+  constexpr int kThreads = 4 * kTok;
+  constexpr int NK = kMode == kRopeSingle ? 1 : D / E / (kMode == kRopeHalves ? 8 : 4);  // items a thread
   const int tid = threadIdx.x, ntok = t.ntok;
   const T* ksrc = static_cast<const T*>(p.k_src) + (int64_t)t.b * p.k_batch + (int64_t)t.i0 * p.k_token;
-  // A thread has one item (RopeItem) of every 256 >> item_shift tokens.
+  // A thread has one item (RopeItem) of every kThreads >> item_shift tokens.
   const RopeTable& r = p.table;
-  const int step = 256 >> p.item_shift, tk = tid >> p.item_shift, j = tid & ((1 << p.item_shift) - 1);
+  const int step = kThreads >> p.item_shift, tk = tid >> p.item_shift, j = tid & ((1 << p.item_shift) - 1);
   Item it;
   it.set(r, j);
   const bool mine = j < Item::count(r.rot, D);
@@ -161,7 +167,7 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
     if (h + 1 < h_hi) load(h + 1);  // in flight during what follows
     if constexpr (kEight) {
       if (h > h_lo) __syncthreads();  // (the last head's maxima have been read)
-      uint32_t bits = max_all(__float_as_uint(mk), amax, tid);
+      uint32_t bits = max_all<kThreads / 64>(__float_as_uint(mk), amax, tid);
       const bool wild = bits >= kInf;
       if (wild) {  // the largest finite magnitude
         __syncthreads();
@@ -180,7 +186,7 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
               }
           }
         }
-        bits = max_all(bits, amax, tid);
+        bits = max_all<kThreads / 64>(bits, amax, tid);
       }
       const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
       const float scale = pow2i(e), most = kCodeMax * scale;
@@ -212,7 +218,7 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
       }
       if (t.o0 > 0 && e > e_old) {  // the older rows, scaled down
         const float shift = pow2i(e_old - e);
-        for (int x = tid; x < t.o0 * (D / 16); x += 256) {
+        for (int x = tid; x < t.o0 * (D / 16); x += kThreads) {
           u32x4* dst = reinterpret_cast<u32x4*>(kc + 16 * x);
           u32x4 w = *dst;
 #pragma unroll
@@ -225,13 +231,14 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
 }
 
 // vs: kTok rows of RW dwords, one more than a row's values, so that rows fall on their own banks.
-template <typename T, int D, bool kEight>
+template <typename T, int D, bool kEight, int kTok>
 __device__ __forceinline__ void write_values(const TokenWriteParams& p, const TokenBlock& t, int h, uint32_t* vs,
                                              uint32_t* amax) {
   using V16 = typename Vec16<T>::type;
   constexpr int E = 16 / (int)sizeof(T);
   constexpr int CPR = D / E;                      // 16-byte chunks per token
-  constexpr int NLD = kTok * CPR / 256;           // chunks per thread
+  constexpr int kThreads = 4 * kTok;
+  constexpr int NLD = CPR / 4;                    // chunks per thread
   constexpr int RW = D * (int)sizeof(T) / 4 + 1;  // dwords per LDS row
   constexpr int EPW = 4 / (int)sizeof(T);         // dims per dword
   const int tid = threadIdx.x, ntok = t.ntok, o0 = t.o0, o1 = t.o1;
@@ -239,7 +246,7 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
   V16 v[NLD];
 #pragma unroll
   for (int l = 0; l < NLD; ++l)
-    v[l] = *reinterpret_cast<const V16*>(src + (int64_t)min((tid + 256 * l) / CPR, ntok - 1) * p.v_token +
+    v[l] = *reinterpret_cast<const V16*>(src + (int64_t)min((tid + kThreads * l) / CPR, ntok - 1) * p.v_token +
                                          tid % CPR * E);
   const size_t slot =
       clampi(ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page), 0, p.num_slots - 1);
@@ -249,7 +256,7 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
   uint32_t mv = 0;
 #pragma unroll
   for (int l = 0; l < NLD; ++l) {
-    const int i = (tid + 256 * l) / CPR;
+    const int i = (tid + kThreads * l) / CPR;
     if (i >= ntok) continue;
     uint32_t* dst = vs + (o0 + i) * RW + tid % CPR * 4;
 #pragma unroll
@@ -263,7 +270,7 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
     // value rows: runs of E tokens (16 bytes of a row), a dword of dims each
     constexpr int TG = kTok / E;
 #pragma unroll 2
-    for (int x = tid; x < TG * (RW - 1); x += 256) {
+    for (int x = tid; x < TG * (RW - 1); x += kThreads) {
       const int g0 = x % TG * E, w = x / TG;
       if (g0 + E <= o0 || g0 >= o1) continue;
       uint32_t e[E];
@@ -300,12 +307,12 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
       }
     }
   } else {
-    uint32_t bits = max_all(max_bits_f32<T>(mv), amax, tid);  // (its barrier: the rows are there)
+    uint32_t bits = max_all<kThreads / 64>(max_bits_f32<T>(mv), amax, tid);  // (its barrier: the rows are there)
     const bool wild = bits >= kInf;                            // infinities or NaN
     if (wild) {  // the largest finite magnitude
       __syncthreads();
       bits = 0;
-      for (int x = tid; x < ntok * (RW - 1); x += 256) {
+      for (int x = tid; x < ntok * (RW - 1); x += kThreads) {
         const uint32_t w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
         if constexpr (sizeof(T) == 2) {
           finite_bits(bits, bf16_lo(w));
@@ -314,14 +321,14 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
           finite_bits(bits, __uint_as_float(w));
         }
       }
-      bits = max_all(bits, amax, tid);
+      bits = max_all<kThreads / 64>(bits, amax, tid);
     }
     const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
     const float scale = pow2i(e), most = kCodeMax * scale;
     if (tid == 0) p.v_exp[head * t.nb + t.blk] = (uint8_t)(e + 127);
     uint8_t* vc = static_cast<uint8_t*>(p.v) + head * D * p.P + t.boff;
     if (wild) {  // infinities become the largest number of the block's scale
-      for (int x = tid; x < ntok * (RW - 1); x += 256) {
+      for (int x = tid; x < ntok * (RW - 1); x += kThreads) {
         uint32_t& w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
         if constexpr (sizeof(T) == 2) w = pack_bf16(saturate(bf16_lo(w), most), saturate(bf16_hi(w), most));
         else w = __float_as_uint(saturate(__uint_as_float(w), most));
@@ -331,7 +338,7 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
     const bool grow = o0 > 0 && e > e_old;
     if (!grow && ntok <= 4) {
       // a few tokens (of a step that decodes): an element a thread
-      for (int x = tid; x < ntok * D; x += 256) {
+      for (int x = tid; x < ntok * D; x += kThreads) {
         const int i = o0 + x / D, c = x % D;
         const uint32_t raw = vs[i * RW + c / EPW];
         const float y = sizeof(T) == 4 ? __uint_as_float(raw) : (c & 1 ? bf16_hi(raw) : bf16_lo(raw));
@@ -339,20 +346,22 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
       }
       return;
     }
-    // runs of 16 tokens of a dword of dims
+    // runs of 16 tokens (of small pages: 8) of a dword of dims
+    constexpr int R = kTok >= 64 ? 16 : 8, kRuns = kTok / R;
+    typedef uint32_t Run __attribute__((ext_vector_type(R / 4), aligned(8)));
     const float shift = pow2i(e_old - e);
     const int r0 = grow ? 0 : o0;
-    for (int x = tid; x < 4 * (RW - 1); x += 256) {
-      const int g0 = x % 4 * 16, w = x / 4;
+    for (int x = tid; x < kRuns * (RW - 1); x += kThreads) {
+      const int g0 = x % kRuns * R, w = x / kRuns;
       uint8_t* dst = vc + (size_t)(w * EPW) * p.P + g0;
-      if (g0 >= o0 && g0 + 16 <= o1) {
+      if (g0 >= o0 && g0 + R <= o1) {
         const uint32_t* row = vs + g0 * RW + w;
-        uint32_t c[16];
+        uint32_t c[R];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) c[i] = row[i * RW];
-        u32x4a8 lo, hi;  // dims EPW w and, in bf16, the next
+        for (int i = 0; i < R; ++i) c[i] = row[i * RW];
+        Run lo, hi;  // dims EPW w and, in bf16, the next
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R / 4; ++i) {
           if constexpr (EPW == 2) {
             // pairs of tokens of one dim
             const uint32_t a0 = __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x05040100u);
@@ -366,11 +375,11 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
                            __uint_as_float(c[4 * i + 3]), scale);
           }
         }
-        *reinterpret_cast<u32x4a8*>(dst) = lo;
-        if constexpr (EPW == 2) *reinterpret_cast<u32x4a8*>(dst + p.P) = hi;
-      } else if (g0 + 16 > r0 && g0 < o1) {
+        *reinterpret_cast<Run*>(dst) = lo;
+        if constexpr (EPW == 2) *reinterpret_cast<Run*>(dst + p.P) = hi;
+      } else if (g0 + R > r0 && g0 < o1) {
         // a run that the step begins or ends in, or of older tokens
-        for (int i = max(g0, r0); i < min(g0 + 16, o1); ++i) {
+        for (int i = max(g0, r0); i < min(g0 + R, o1); ++i) {
 #pragma unroll
           for (int c = 0; c < EPW; ++c) {
             uint8_t* one = dst + (size_t)c * p.P + (i - g0);
@@ -385,10 +394,10 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
 }
 
 // A workgroup writes one block's keys of p.heads heads, or its values of one.
-template <typename T, int D, bool kEight, int kMode>
-__global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
+template <typename T, int D, bool kEight, int kMode, int kTok>
+__global__ __launch_bounds__(4 * kTok) void token_write_kernel(TokenWriteParams p) {
   __shared__ uint32_t vs[kTok * (D * (int)sizeof(T) / 4 + 1)];
-  __shared__ uint32_t amax[4];
+  __shared__ uint32_t amax[kTok / 16];
   const int groups = (p.H + p.heads - 1) / p.heads;
   const int unit = blockIdx.x / p.roles, role = blockIdx.x - unit * p.roles;
   if (role >= groups + p.H) return;
@@ -402,45 +411,54 @@ __global__ __launch_bounds__(256) void token_write_kernel(TokenWriteParams p) {
   if (t0 >= t1) return;
   // this unit's block, and the tokens of it that the step brings (tokens of the table are
   // below 2^31, see hsa_cache8_t)
-  t.nb = (p.P + kTok - 1) / kTok;
+  t.nb = (p.P + kScaleTok - 1) / kScaleTok;
   const int page0 = (int)t0 / p.P;
-  const int g = ((int)t0 - page0 * p.P) / kTok + unit;
+  const int g = ((int)t0 - page0 * p.P) / kScaleTok + unit;
   t.page = page0 + g / t.nb;
   t.blk = g % t.nb;
-  t.boff = t.blk * kTok;
+  t.boff = t.blk * kScaleTok;
   const int64_t base = (int64_t)t.page * p.P + t.boff;
   if (base >= t1) return;
-  const int len = min(kTok, p.P - t.boff);
+  const int len = min(kScaleTok, p.P - t.boff);  // (at most kTok)
   t.o0 = t0 > base ? (int)(t0 - base) : 0;
   t.o1 = t1 - base < len ? (int)(t1 - base) : len;
   t.ntok = t.o1 - t.o0;
   if (t.ntok <= 0) return;
   t.i0 = (int)(base + t.o0 - f);
-  if (role < groups) write_keys<T, D, kEight, kMode>(p, t, role * p.heads, min((role + 1) * p.heads, p.H), amax);
-  else write_values<T, D, kEight>(p, t, role - groups, vs, amax);
+  if (role < groups) write_keys<T, D, kEight, kMode, kTok>(p, t, role * p.heads, min((role + 1) * p.heads, p.H), amax);
+  else write_values<T, D, kEight, kTok>(p, t, role - groups, vs, amax);
 }
 
-template <typename T, int D, bool kEight, int kMode>
+template <typename T, int D, bool kEight, int kMode, int kTok>
 void launch_mode(int B, TokenWriteParams p, hipStream_t s) {
   const int n = RopeItem<T, kMode>::count(p.table.rot, D);
   while (1 << p.item_shift < n) ++p.item_shift;
   // Two heads a workgroup share the angles of their tokens, once that leaves work for every
   // CU (8-bit append of 4680 tokens, 12 heads x d128: one 16.6 us, two 15.8, three 20.2, four
   // 16.1; four sequences at once 51.3, 49.2, 62.3, 51.6).
-  const int64_t wgs = (int64_t)((p.n + kTok - 1) / kTok) * p.H * B;
+  const int64_t wgs = (int64_t)((p.n + kScaleTok - 1) / kScaleTok) * p.H * B;
   p.heads = kMode != kRopeSingle && wgs >= 768 ? 2 : 1;
   p.roles = (p.H + p.heads - 1) / p.heads + p.H;
   const dim3 grid((uint32_t)(token_write_units(p.n, p.P) * p.roles), B);
-  token_write_kernel<T, D, kEight, kMode><<<grid, 256, 0, s>>>(p);
+  token_write_kernel<T, D, kEight, kMode, kTok><<<grid, 4 * kTok, 0, s>>>(p);
+}
+
+// Pages of up to 16 tokens are blocks of a wave each, so that a CU holds more of them (8-bit append
+// of 4680 tokens, 12 heads x d128, pages of 8: 16.7 us, by four waves 44.5; of 16: 15.1 and 22.6). A
+// token's items have to fit its threads: single pairs of d = 128 do not.
+template <typename T, int D, bool kEight, int kMode>
+void launch_blocks(int B, const TokenWriteParams& p, hipStream_t s) {
+  if (p.P <= 16 && RopeItem<T, kMode>::count(p.table.rot, D) <= 64) launch_mode<T, D, kEight, kMode, 16>(B, p, s);
+  else launch_mode<T, D, kEight, kMode, kScaleTok>(B, p, s);
 }
 
 template <typename T, int D, bool kEight>
 void launch_as(int B, const TokenWriteParams& p, hipStream_t s) {
   switch (rope_mode<T>(p.table, D)) {
-    case kRopeHalves: return launch_mode<T, D, kEight, kRopeHalves>(B, p, s);
-    case kRopePart: return launch_mode<T, D, kEight, kRopePart>(B, p, s);
-    case kRopeInterleaved: return launch_mode<T, D, kEight, kRopeInterleaved>(B, p, s);
-    default: return launch_mode<T, D, kEight, kRopeSingle>(B, p, s);
+    case kRopeHalves: return launch_blocks<T, D, kEight, kRopeHalves>(B, p, s);
+    case kRopePart: return launch_blocks<T, D, kEight, kRopePart>(B, p, s);
+    case kRopeInterleaved: return launch_blocks<T, D, kEight, kRopeInterleaved>(B, p, s);
+    default: return launch_blocks<T, D, kEight, kRopeSingle>(B, p, s);
   }
 }
 

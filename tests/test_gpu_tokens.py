@@ -265,3 +265,38 @@ def test_captured_appends_follow_their_lengths():
         torch.cuda.synchronize()
         same(c, arrays(e))
         assert torch.equal(layer.k_pool, eager.k_pool) and torch.equal(layer.v_pool, eager.v_pool)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P_", [8, 16, 24])
+@pytest.mark.parametrize("layout,rot", [("half", 64), ("interleaved", 32), ("half", 16), ("half", 10)])
+def test_small_pages_rotated(P_, layout, rot, d, dt):
+    """Pages of a block each: runs that begin and end inside one, a scale that an earlier
+    call set, infinities and NaN in one of the blocks; the pool's own type beside it."""
+    B, H, n = 2, 5, 90
+    first, count = [5, 0], [90, 61]
+    rope = P.rope(rot, layout=layout)
+    pages = 100 // P_ + 1
+    c, pt = cache(P_, B, H, d, P_, dt, pages, rope=rope)
+    k, v = source(1, B, 5, H, d, dt, False)
+    c.write(k, v, count=i32([5, 0]))
+    want = arrays(c)
+    k, v = source(2, B, n, H, d, dt, True)
+    k, v = k * 3.0, v.clone()
+    k[1, 20, 1, 60], v[1, 20, 0, 3], v[0, 40, 2, 5] = float("inf"), float("-inf"), float("nan")
+    c.write(k, v, i32(first), count=i32(count))
+    turned = O.rope(host(k), O.places(first, n), rot, layout)
+    exact = O.write8(want, pt, turned, host(v), first, count)
+    exact["k"][:] = np.where(np.isfinite(exact["k"]), exact["k"], np.nan)  # (an infinity has its code)
+    same(c, want, keys_too=False)
+    check_keys(c, want, exact, 448.0 * 2)
+    layer = P.HsaLayer(B, H, d, P_, dt, DEV, num_slots=c.k.shape[0], max_pages=pages, page_table=c.page_table)
+    layer.k_pool.zero_(), layer.v_pool.zero_()
+    wk, wv = host(layer.k_pool), host(layer.v_pool)
+    k = torch.where(torch.isfinite(k), k, torch.ones_like(k))
+    layer.write_tokens(k, v, i32(first), count=i32(count), rope=rope)
+    O.write_tokens(wk, wv, pt, O.rope(host(k), O.places(first, n), rot, layout), host(v), first, count)
+    eps = 2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -24
+    assert (np.abs(host(layer.k_pool) - wk) <= eps * np.abs(wk) + 16 * 2.0 ** -24 * float(k.abs().max())).all()
+    assert np.array_equal(host(layer.v_pool), wv, equal_nan=True)
