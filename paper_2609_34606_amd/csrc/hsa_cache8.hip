@@ -448,7 +448,7 @@ void few_rows_kernel(Cache8AttnParams p) {
 // hardly overlap, neither within a wave nor between the two of a SIMD. A large library product
 // reaches 1322 TFLOP/s (238 us). Waves of 64 rows need more registers than a wave has (spills);
 // 512 rows a workgroup was no faster, and d = 64 with 256 rows slower (55.9 us and 49.5 for causal
-// prompts of up to 1001 tokens; 45 now).
+// prompts of up to 1001 tokens; 42 now).
 template <int D>
 struct ManyLayout {
   static constexpr int kRowK = 2 * D, kTileK = 64 * kRowK;  // bytes
@@ -1078,8 +1078,10 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
     // Rounds of as many workgroups as are resident (one a CU, with d = 64 three, of small pages
     // two), each of its tiles and about six more for its start and end; pieces cost a
     // partial output written and read again (four). 8 causal sequences of 8192 tokens,
-    // d = 128, 128 queries: 74 us in four pieces.
-    const int64_t slots = p.d == 128 ? 256 : (p.P < 64 ? 512 : 768);
+    // d = 128, 128 queries: 74 us in four pieces. Of ragged sequences, d = 64, some slots
+    // are idle anyway (three prompts of up to 1001 tokens: whole items 43 us, in two 46; one causal
+    // call of 4096 queries over 8192 tokens: with 512 slots 66 us, with 768 63).
+    const int64_t slots = p.d == 128 ? 256 : (ragged || p.P < 64 ? 512 : 768);
     double best = 1e300;
     for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
       const double each = (double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0);
