@@ -683,6 +683,29 @@ def _raw_stream(dev: int, stream) -> int:
     return _torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _empty(shape, dtype, device, stream):
+    """An uninitialised tensor that a launch on stream (None: the current one) may write at
+    once. It comes from that stream's memory: a block of the current stream's may still be in use by
+    what is queued there, and the launch does not wait for that."""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, _torch.cuda.Stream):
+        stream = _torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+    with _torch.cuda.stream(stream):
+        return _torch.empty(shape, dtype=dtype, device=device)
+
+
+def out_like(t, stream=None):
+    """A contiguous output of t's shape, type and device for a call on stream, to be read on the
+    current stream (once that waits for the call)."""
+    lib()
+    if stream is None or not t.is_cuda:
+        return _torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    o = _empty(t.shape, t.dtype, t.device, stream)
+    o.record_stream(_torch.cuda.current_stream(t.device))  # not written anew before its reader is done
+    return o
+
+
 def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None,
                    check=True) -> int:
     """Turns x [B, n, heads, d] by its tokens' positions (pos int32 [B, n, axes], or
@@ -772,11 +795,8 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
     if ws is None:
         wp, nbytes = None, L.hsa_cache8_attn_workspace_size(cp, n_q, cache.kv_heads, k_max, n_cur_pages)
         if nbytes:
-            ws = _torch.empty(nbytes, dtype=_torch.uint8, device=q.device)
+            ws = _empty(nbytes, _torch.uint8, q.device, stream if dev >= 0 else None)
             wp = ws.data_ptr()
-            if stream is not None and dev >= 0:  # not reused before that stream is done with it
-                ws.record_stream(stream if isinstance(stream, _torch.cuda.Stream) else
-                                 _torch.cuda.ExternalStream(int(stream), device=q.device))
     else:
         wp, nbytes = _ptr(ws), ws.numel() * ws.element_size()
     st = _call(L.hsa_cache8_attn, dev, stream, cp, q.data_ptr(), n_q, hp, sp, k_max, kp, cur_first_page, n_cur_pages, kvp,

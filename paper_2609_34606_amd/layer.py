@@ -187,7 +187,7 @@ class HsaCache8:
         if self.rope is None:
             raise ValueError("the cache has no rope")
         if out is None:
-            out = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = _h.out_like(q, stream)
         _h.hsa_rope_apply(self.cfg, self.rope, q, q.shape[1], out, pos=pos, first=first, inverse=inverse,
                           stream=stream)
         return out
@@ -205,7 +205,7 @@ class HsaCache8:
         kv_heads, k_max], at most k_h of each head) and pages [first_page, + n_pages)."""
         _same_device(q, self.k)
         if out is None:
-            out = self.torch.empty_like(q)
+            out = _h.out_like(q, stream)
         _h.hsa_cache8_attn(self.cfg, q, q.shape[1], self.pool, sel, 0 if sel is None else int(sel.shape[-1]), k_h,
                            first_page, n_pages, out, lse=lse, kv_len=kv_len, q_len=q_len, causal=causal,
                            stream=stream)
