@@ -798,6 +798,8 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
             ws = _empty(nbytes, _torch.uint8, q.device, stream if dev >= 0 else None)
             wp = ws.data_ptr()
     else:
+        if ws.get_device() != dev:
+            raise _apart("ws", ws)
         wp, nbytes = _ptr(ws), ws.numel() * ws.element_size()
     st = _call(L.hsa_cache8_attn, dev, stream, cp, q.data_ptr(), n_q, hp, sp, k_max, kp, cur_first_page, n_cur_pages, kvp,
                qlp, 1 if causal else 0, o.data_ptr(), lp, wp, nbytes)
