@@ -643,7 +643,8 @@ hsa_status_t hsa_forward_linformer(const hsa_config_t* cfg, const void* q, int32
  * the slow ones only: with r = orig_len f / (2 pi) turns over the original length and
  * w = (r - low) / (high - low) clamped to [0, 1], f becomes w f + (1 - w) f /
  * factor. Angles are fp64 up to their reduction, cosines, sines and products
- * fp32, and the result is rounded once to the type of the call.
+ * fp32, and the result is rounded once to the type of the call. A rope is invalid if an f
+ * exceeds 2^18 pi (theta below 1 or a small factor) or A is no finite fp32 number.
  */
 #define HSA_ROPE_HALF 0
 #define HSA_ROPE_INTERLEAVED 1

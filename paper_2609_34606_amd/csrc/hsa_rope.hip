@@ -75,6 +75,9 @@ hipError_t launch_rope(int dtype, int B, const RopeParams& p, hipStream_t s) {
 
 bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, const int32_t* first, RopeTable& t) {
   constexpr double kTau = 6.28318530717958647692;
+  // Quarter turns a position: 2^31 positions then stay below 2^50, where fp64 still holds the
+  // fraction of a quarter that cos_sin_quarters takes off.
+  constexpr double kMostQuarters = 524288.0;
   if (r->rot_dim < 2 || r->rot_dim > d || r->rot_dim % 2) return false;
   if (r->layout != HSA_ROPE_HALF && r->layout != HSA_ROPE_INTERLEAVED) return false;
   if (r->axes < 1 || r->axes > 3 || (r->axes > 1 && !pos)) return false;
@@ -86,7 +89,7 @@ bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, co
       sum += dims[a];
     }
   if (r->axes > 1 && sum != r->rot_dim) return false;
-  if (!(r->theta > 0.0) || isinf(r->theta) || !isfinite(r->amplitude)) return false;
+  if (!(r->theta > 0.0) || isinf(r->theta) || !isfinite((float)r->amplitude)) return false;
   if (r->scaling != HSA_ROPE_UNSCALED && (!(r->factor > 0.0) || isinf(r->factor))) return false;
   if (r->scaling == HSA_ROPE_PARTS) {
     if (!(r->low >= 0.0) || !(r->high > r->low) || isinf(r->high) || r->orig_len < 1) return false;
@@ -109,8 +112,8 @@ bool rope_table(const hsa_rope_t* r, int d, bool inverse, const int32_t* pos, co
         w = w < 0.0 ? 0.0 : (w > 1.0 ? 1.0 : w);
         f = w * f + (1.0 - w) * f / r->factor;
       }
-      if (!isfinite(f)) return false;
       t.quarters[i] = 4.0 * (inverse ? -f : f) / kTau;
+      if (!(fabs(t.quarters[i]) <= kMostQuarters)) return false;
       t.axis[i] = (int8_t)a;
     }
   }

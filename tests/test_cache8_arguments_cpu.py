@@ -1,5 +1,8 @@
 """Arguments of the 8-bit cache's and the rotation's calls that the binding or the library
 settles before any launch; none of these needs a GPU."""
+import ctypes
+import math
+
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -19,3 +22,30 @@ def test_a_workspace_on_another_device_is_refused():
             ws = torch.empty(256, dtype=torch.uint8, device=where)
             with pytest.raises(ValueError, match="ws is on"):
                 P.hsa_cache8_attn(cfg, q, 3, cache, None, 0, None, 0, 2, o, ws=ws)
+
+
+def _apply(rope, pos=None, n=1):
+    """Status of a call that reads no memory where it is refused (without a GPU the launch of a
+    valid one fails: 5)."""
+    cfg = P.config(1, 1, 64, 64, BF)
+    return P.lib().hsa_rope_apply(ctypes.byref(cfg), ctypes.byref(rope), 0x10000, 64, 64, n, 1, pos, None, 0, 0x10000,
+                                  64, 64, None)
+
+
+def test_ropes_out_of_the_kernels_range_are_refused():
+    """An amplitude beyond fp32, and frequencies whose angle at a far position no longer has its
+    fraction of a quarter turn in fp64: 2^18 pi radians a position are 2^19 quarters."""
+    most = 2.0 ** 18 * math.pi
+    f32_max = float(torch.finfo(torch.float32).max)
+    for kw in (dict(amplitude=1e39), dict(amplitude=-1e39), dict(amplitude=f32_max * (1 + 2.0 ** -24)),
+               dict(scaling="linear", factor=1 / (most * 1.001)), dict(scaling="linear", factor=1e-300),
+               dict(scaling="parts", factor=1e-9, low=10.0, high=11.0, orig_len=10), dict(theta=1e-12),
+               dict(theta=1e-300)):
+        assert _apply(P.rope(64, **kw), n=1) == 1, kw
+        # 8-bit and pool appends take the same table
+        cfg, pool = P.config(1, 2, 64, 64, BF), P.HsaKvPool(*[0x10000] * 3, 4, 4)
+        assert P.lib().hsa_token_write(ctypes.byref(cfg), ctypes.byref(pool), ctypes.byref(P.rope(64, **kw)), 0x10000, 0,
+                                       128, 0x10000, 0, 128, 0, None, None, None, None) == 1, kw
+    for kw in (dict(amplitude=f32_max), dict(scaling="linear", factor=1.001 / most), dict(theta=1e-4),
+               dict(theta=0.5), dict(amplitude=1e-60)):
+        assert _apply(P.rope(64, **kw), n=0) == 0, kw
