@@ -731,7 +731,8 @@ typedef struct hsa_cache8 {
  * first tokens an earlier call wrote keeps the larger of its scale and the one the
  * new tokens need; if that grows, the older codes are scaled down by the power of two, which
  * rounds only those that become subnormal. A block written from its first
- * token on starts anew, whatever its memory held. Codes of the block behind the new tokens stay as
+ * token on starts anew, whatever its memory held; one that an append enters further on, with nothing
+ * written before, needs an exponent byte of 0 (any other is taken for an earlier call's). Codes of the block behind the new tokens stay as
  * they are, and what they stand for is lost if the scale changes: a sequence is written forwards,
  * and one that was cut back goes on from its new end.
  */

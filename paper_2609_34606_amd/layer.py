@@ -152,7 +152,8 @@ def _same_device(t, pool):
 class HsaCache8:
     """Paged 8-bit KV cache of one layer: e4m3 codes k [slots, Hk, P, d] and v
     [slots, Hk, d, P], exponent bytes of the scales of 64-token blocks k_exp, v_exp [slots,
-    Hk, ceil(P / 64)], page_table [B, max_pages]; tensors not given are allocated. The tensors stay
+    Hk, ceil(P / 64)], page_table [B, max_pages]; tensors not given are allocated (exponent
+    bytes as 0, for appends that begin inside a block that nothing was written to). The tensors stay
     the same over the cache's life (fill the page table in place). ``heads`` are the query heads,
     kv_heads (default: as many) the cached ones. rope turns the keys that are
     written and the queries given to ``rotate``.
@@ -171,7 +172,8 @@ class HsaCache8:
         if k is None:
             k = torch.empty((num_slots, kv, page_size, head_dim), **u8)
             v = torch.empty((num_slots, kv, head_dim, page_size), **u8)
-            k_exp, v_exp = torch.empty((num_slots, kv, nb), **u8), torch.empty((num_slots, kv, nb), **u8)
+            # (an append that begins inside a block keeps a larger exponent than its own)
+            k_exp, v_exp = torch.zeros((num_slots, kv, nb), **u8), torch.zeros((num_slots, kv, nb), **u8)
         if page_table is None:
             page_table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
         if int(k.shape[1]) != kv:

@@ -49,3 +49,19 @@ def test_ropes_out_of_the_kernels_range_are_refused():
     for kw in (dict(amplitude=f32_max), dict(scaling="linear", factor=1.001 / most), dict(theta=1e-4),
                dict(theta=0.5), dict(amplitude=1e-60)):
         assert _apply(P.rope(64, **kw), n=0) == 0, kw
+
+
+def test_a_new_cache_has_zero_exponents():
+    """Whatever its memory held: a first append that begins inside a block keeps the larger of its own
+    exponent and the byte there, and 255 would make every code 0."""
+    held = torch.are_deterministic_algorithms_enabled(), torch.utils.deterministic.fill_uninitialized_memory
+    torch.use_deterministic_algorithms(True)
+    torch.utils.deterministic.fill_uninitialized_memory = True  # (new memory: 255 in every byte)
+    try:
+        assert (torch.empty(4, dtype=torch.uint8) == 255).all()
+        c = P.HsaCache8(1, 2, 64, 72, BF, "cpu", num_slots=3, max_pages=2)
+    finally:
+        torch.use_deterministic_algorithms(held[0])
+        torch.utils.deterministic.fill_uninitialized_memory = held[1]
+    for e in (c.k_exp, c.v_exp):
+        assert e.shape == (3, 2, 2) and (e == 0).all()
