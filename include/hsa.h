@@ -774,6 +774,13 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  */
 size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
                                       int32_t k_max, int32_t n_cur_pages);
+/* How such a call is launched (host-only inspection: it launches nothing and needs no device):
+ * whether it takes the kernel for many query rows (1) or few (0), the query rows (queries times query
+ * heads of a key head) of a work item, and the pieces that the longest item's list is cut into. ragged:
+ * the call has kv_len. Each output pointer is nullable. Errors: INVALID_ARG, UNSUPPORTED. */
+hsa_status_t hsa_cache8_attn_plan(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                  int32_t k_max, int32_t n_cur_pages, int32_t ragged,
+                                  int32_t* many_rows, int32_t* rows_per_item, int32_t* n_pieces);
 hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
                              const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
                              const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,

@@ -1424,6 +1424,21 @@ size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int3
   return need;
 }
 
+hsa_status_t hsa_cache8_attn_plan(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                  int32_t k_max, int32_t n_cur_pages, int32_t ragged,
+                                  int32_t* many_rows, int32_t* rows_per_item, int32_t* n_pieces) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if (n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
+  if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
+  Cache8AttnParams p{};
+  if ((st = plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged != 0, p)) != HSA_OK) return st;
+  if (many_rows) *many_rows = p.many;
+  if (rows_per_item) *rows_per_item = p.rows_per_item;
+  if (n_pieces) *n_pieces = p.n_split;
+  return HSA_OK;
+}
+
 hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
                              const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
                              const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,

@@ -185,6 +185,8 @@ def lib():
                       c_vp, c_vp, c_vp, c_vp]
     L.hsa_cache8_attn_workspace_size.restype = c_sz
     L.hsa_cache8_attn_workspace_size.argtypes = [P(HsaConfig), c_i32, c_i32, c_i32, c_i32]
+    L.hsa_cache8_attn_plan.restype = ctypes.c_int
+    L.hsa_cache8_attn_plan.argtypes = [P(HsaConfig), c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp]
     L.hsa_cache8_attn.restype = ctypes.c_int
     L.hsa_cache8_attn.argtypes = [P(HsaConfig), c_vp, c_i32, P(HsaCache8Pool), c_vp, c_i32, c_vp, c_i32,
                                   c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
@@ -761,6 +763,15 @@ def hsa_cache8_write(cfg, cache, k_src, v_src, n, first=None, count=None, rope=N
 
 def hsa_cache8_attn_workspace_size(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int) -> int:
     return lib().hsa_cache8_attn_workspace_size(ctypes.byref(cfg), n_q, kv_heads, k_max, n_cur_pages)
+
+
+def hsa_cache8_attn_plan(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int, ragged: bool = False):
+    """(many_rows, rows_per_item, n_pieces) of such a call's launch, without making it; ragged: it has kv_len."""
+    out = (c_i32 * 3)()
+    at = ctypes.addressof(out)
+    _check("hsa_cache8_attn_plan", lib().hsa_cache8_attn_plan(ctypes.byref(cfg), n_q, kv_heads, k_max, n_cur_pages,
+                                                              1 if ragged else 0, at, at + 4, at + 8))
+    return bool(out[0]), out[1], out[2]
 
 
 def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, kv_len=None,
