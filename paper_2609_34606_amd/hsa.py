@@ -712,7 +712,8 @@ def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stre
                    check=True) -> int:
     """Turns x [B, n, heads, d] by its tokens' positions (pos int32 [B, n, axes], or
     first int32 [B] + the token's index) into o (x itself, or apart from it).
-    inverse: by the opposite angles, the gradient's map."""
+    inverse: by the opposite angles, the gradient's map. No autograd graph is
+    recorded (HsaCache8.rotate records one)."""
     fn = lib().hsa_rope_apply
     B = cfg.batch
     heads = x.shape[2] if x.dim() == 4 else 0

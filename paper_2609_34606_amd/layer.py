@@ -1,6 +1,7 @@
 """Device buffers of one HSA attention layer, driven through the C ABI."""
 from __future__ import annotations
 
+import functools
 from typing import Optional, Sequence
 
 from . import hsa as _h
@@ -149,6 +150,33 @@ def _same_device(t, pool):
         raise ValueError(f"the tensors are on {t.device}, the cache on {pool.device}")
 
 
+@functools.lru_cache(None)
+def _rotation():
+    """The rotation as a node of an autograd graph: its gradient is the opposite rotation (with the
+    same amplitude), which has a gradient of its own."""
+    import torch
+
+    class Rotation(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, cfg, rope, pos, first, inverse, stream):
+            ctx.call = cfg, rope, inverse
+            ctx.save_for_backward(pos, first)
+            out = _h.out_like(q, stream)
+            _h.hsa_rope_apply(cfg, rope, q, q.shape[1], out, pos=pos, first=first, inverse=inverse, stream=stream)
+            return out
+
+        @staticmethod
+        def backward(ctx, g):
+            # on the stream that was current in the forward pass, where autograd keeps the gradient
+            cfg, rope, inverse = ctx.call
+            pos, first = ctx.saved_tensors
+            if g.stride(3) != 1 or g.stride(2) != g.shape[3]:  # (of a sum: expanded)
+                g = g.contiguous()
+            return Rotation.apply(g, cfg, rope, pos, first, not inverse, None), None, None, None, None, None, None
+
+    return Rotation
+
+
 class HsaCache8:
     """Paged 8-bit KV cache of one layer: e4m3 codes k [slots, Hk, P, d] and v
     [slots, Hk, d, P], exponent bytes of the scales of 64-token blocks k_exp, v_exp [slots,
@@ -185,9 +213,13 @@ class HsaCache8:
         self.pool = _h.cache8_pool(k, v, k_exp, v_exp, page_table, self.cfg)
 
     def rotate(self, q, pos=None, first=None, out=None, inverse: bool = False, stream=None):
-        """q [B, n, heads, d] turned by its tokens' positions."""
+        """q [B, n, heads, d] turned by its tokens' positions, with its gradient if q needs one."""
         if self.rope is None:
             raise ValueError("the cache has no rope")
+        if q.requires_grad and self.torch.is_grad_enabled():
+            if out is not None:
+                raise ValueError("an out of the caller's does not keep the gradient that q needs")
+            return _rotation().apply(q, self.cfg, self.rope, pos, first, inverse, stream)
         if out is None:
             out = _h.out_like(q, stream)
         _h.hsa_rope_apply(self.cfg, self.rope, q, q.shape[1], out, pos=pos, first=first, inverse=inverse,

@@ -65,3 +65,46 @@ def test_a_new_cache_has_zero_exponents():
         torch.utils.deterministic.fill_uninitialized_memory = held[1]
     for e in (c.k_exp, c.v_exp):
         assert e.shape == (3, 2, 2) and (e == 0).all()
+
+
+def test_rotate_keeps_the_gradient(monkeypatch):
+    """The rotated queries of a tensor that needs a gradient have one: the opposite rotation's,
+    twice differentiable. (The kernel is replaced by the same map, quarter turns here, on the CPU.)"""
+    calls = []
+
+    def turn(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None):
+        half = rope.rot_dim // 2
+        a, b = x[..., :half], x[..., half:]
+        assert x.stride(3) == 1 and x.stride(2) == x.shape[3]
+        o.copy_(torch.cat([b, -a] if inverse else [-b, a], -1) * first.view(-1, 1, 1, 1))
+        calls.append((inverse, stream))
+    monkeypatch.setattr(P.hsa, "hsa_rope_apply", turn)
+    c = P.HsaCache8(2, 3, 64, 64, torch.float32, "cpu", num_slots=2, max_pages=2, rope=P.rope(64))
+    g = torch.Generator().manual_seed(1)
+    q = torch.randn((2, 4, 3, 64), generator=g, requires_grad=True)
+    up = torch.randn((2, 4, 3, 64), generator=g)
+    first = torch.tensor([2, 3], dtype=torch.int32)
+    out = c.rotate(q, first=first)
+    assert out.requires_grad
+    out.backward(up)
+    by = first.view(-1, 1, 1, 1)
+    assert torch.equal(q.grad, torch.cat([up[..., 32:], -up[..., :32]], -1) * by)
+    assert [x[0] for x in calls] == [False, True]
+    # through a sum (an expanded gradient), and twice
+    grad, = torch.autograd.grad((c.rotate(q, first=first) ** 2).sum(), q, create_graph=True)
+    want = 2 * q * by ** 2  # (this product rounds once, the two by 3 of the other side once each: half a step, 2^-24)
+    assert ((grad - want).abs() <= 3 * 2.0 ** -24 * want.abs()).all()
+    twice, = torch.autograd.grad(grad.sum(), q)
+    assert torch.equal(twice, (2 * by ** 2).expand_as(q))
+    c.rotate(q, first=first).sum().backward()
+    # no graph where none is asked for
+    with torch.no_grad():
+        assert not c.rotate(q, first=first, out=torch.empty_like(q)).requires_grad
+    assert not c.rotate(q.detach(), first=first).requires_grad
+    with pytest.raises(ValueError, match="gradient"):
+        c.rotate(q, first=first, out=torch.empty_like(q))
+    # positions changed before the backward pass are noticed
+    out = c.rotate(q, first=first)
+    first += 1
+    with pytest.raises(RuntimeError, match="modified"):
+        out.sum().backward()

@@ -1,11 +1,14 @@
 """Single calls of the 8-bit cache and the rotation that a program makes and the other tests do
-not: a first append inside a block."""
+not: a first append inside a block, the gradient of rotated queries."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2609_34606_amd as P
+from oracle import hsa_cache8_oracle as O
 from test_gpu_cache8 import BF, F32
-from test_gpu_tokens import i32, source
+from test_gpu_rope import EPS, check
+from test_gpu_tokens import host, i32, source
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -36,3 +39,78 @@ def test_first_append_inside_a_block(P_, dt):
             assert torch.equal(new.v[s, ..., first:last], old.v[s, ..., first:last])
             assert torch.equal(new.k_exp[s, :, :blocks], old.k_exp[s, :, :blocks])
             assert torch.equal(new.v_exp[s, :, :blocks], old.v_exp[s, :, :blocks])
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_gradient_through_rotate(layout, dt):
+    """The gradient of rotated queries against the oracle's opposite rotation (bound:
+    test_gpu_rope.py), of a fused projection's part, with a stream of its own, captured and replayed."""
+    kw = dict(rot=48, layout=layout, amplitude=1.5)
+    c = P.HsaCache8(2, 3, 64, 64, dt, DEV, num_slots=2, max_pages=2, rope=P.rope(48, layout=layout, amplitude=1.5))
+    first = i32([7, 9001])
+    where = O.places(first.cpu().numpy(), 33)
+    g = torch.Generator().manual_seed(3)
+    qkv = torch.randn((2, 33, 3, 3, 64), generator=g).to(dt).to(DEV).requires_grad_()
+    up = torch.randn((2, 33, 3, 64), generator=g).to(dt).to(DEV)
+    s = torch.cuda.Stream()
+    for stream in (None, s):
+        qkv.grad = None
+        out = c.rotate(qkv[:, :, 1], first=first, stream=stream)
+        torch.cuda.current_stream().wait_stream(s)
+        check(host(qkv[:, :, 1].detach()), host(out.detach()), where, kw, EPS[dt])
+        out.backward(up)
+        check(host(up), host(qkv.grad[:, :, 1]), where, dict(kw, inverse=True), EPS[dt])
+        assert (qkv.grad[:, :, 0] == 0).all() and (qkv.grad[:, :, 2] == 0).all()
+    # captured: the forward and the backward pass, replayed on other positions
+    q = qkv.detach()[:, :, 1].contiguous().requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):  # (a first pass outside, as captured training needs)
+        torch.autograd.grad(c.rotate(q, first=first), q, up)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = c.rotate(q, first=first)
+        grad, = torch.autograd.grad(out, q, up)
+    out = out.detach()
+    for at in ([7, 9001], [0, 70000], [123, 5]):
+        first.copy_(torch.tensor(at))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = c.rotate(q, first=first)
+        assert torch.equal(out, eager)
+        assert torch.equal(grad, torch.autograd.grad(eager, q, up)[0])
+        del eager
+
+
+def test_rotated_attention_trains():
+    """Rotated queries and keys in a plain attention: the gradient of the projections against
+    differences of the loss in fp64 of the oracle's rotation."""
+    B, n, heads, d = 1, 5, 2, 64
+    c = P.HsaCache8(B, heads, d, 64, F32, DEV, num_slots=1, max_pages=1, rope=P.rope(d))
+    g = torch.Generator().manual_seed(4)
+    q, k = (torch.randn((B, n, heads, d), generator=g) for _ in range(2))
+    where = O.places([11], n)
+
+    def loss64(a, b):
+        x, y = (O.rope(t, where, d) for t in (a, b))
+        s = np.einsum("bihd,bjhd->bhij", x, y) / d ** 0.5
+        return np.log(np.exp(s).sum(-1)).sum()
+    ql, kl = (t.to(DEV).requires_grad_() for t in (q, k))
+    first = i32([11])
+    x, y = c.rotate(ql, first=first), c.rotate(kl, first=first)
+    s = (x[:, :, None] * y[:, None]).sum(-1) / d ** 0.5  # [B, i, j, heads]
+    torch.logsumexp(s, 2).sum().backward()
+    # Differences of fp64 with a step of 2^-13 are off by about 2^-26 of the third derivative, and
+    # fp32 by some 100 roundings of numbers of the gradient's size (below 3): 2^-14 covers both.
+    r = np.random.default_rng(5)
+    a, b = q.double().numpy(), k.double().numpy()
+    for _ in range(3):
+        da, db = r.standard_normal(a.shape), r.standard_normal(b.shape)
+        size = np.sqrt((da ** 2).sum() + (db ** 2).sum())
+        da, db = da / size, db / size
+        h = 2.0 ** -13
+        num = (loss64(a + h * da, b + h * db) - loss64(a - h * da, b - h * db)) / (2 * h)
+        got = (host(ql.grad) * da).sum() + (host(kl.grad) * db).sum()
+        assert abs(num - got) < 2.0 ** -14 * max(1.0, np.sqrt((host(ql.grad) ** 2).sum() + (host(kl.grad) ** 2).sum()))
