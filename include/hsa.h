@@ -770,7 +770,10 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  * n_cur_pages == 0), OUT_OF_RANGE (pages beyond max_pages), UNSUPPORTED
  * (sizes, alignment), WORKSPACE. n_q == 0 is a no-op. Kernels read kv_len and q_len,
  * so a captured call follows them. k_max is at most HSA_MAX_LIST; a size of 0 means that no
- * workspace is needed (or invalid input).
+ * workspace is needed (or invalid input). The size grows with the list (k_max + n_cur_pages): the one for a
+ * program's longest list serves every shorter one of the same cfg, n_q and kv_heads, with or without
+ * kv_len. It does not grow with n_q (a step of one token may be cut into pieces where a prompt is
+ * not): a program that calls with several takes the largest of their sizes.
  */
 size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
                                       int32_t k_max, int32_t n_cur_pages);

@@ -1332,8 +1332,12 @@ hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_h
   return HSA_OK;
 }
 
-size_t cache8_ws(const hsa_config_t* cfg, const Cache8AttnParams& p) {
-  return align_up(cache8_part_bytes(cfg->batch, p.Hk, p.n_split, p.part_rows, p.d));
+// Outputs, maxima and sums of the pieces of any call of these sizes with up to `list` pages: not
+// those of this list's plan, which cuts some longer lists into fewer pieces than shorter ones.
+size_t cache8_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int64_t list) {
+  const int64_t rows = (int64_t)n_q * (cfg->num_heads / kv_heads);
+  const int64_t parts = cache8_most_part_rows(cfg->dtype, cfg->head_dim, cfg->page_size, cfg->batch, kv_heads, rows, list);
+  return align_up((size_t)(parts * cfg->batch * kv_heads * (cfg->head_dim + 2)) * 4);
 }
 
 }  // namespace
@@ -1415,13 +1419,10 @@ size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int3
                                       int32_t k_max, int32_t n_cur_pages) {
   if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return 0;
   if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return 0;
-  size_t need = 0;  // of either kind of call
-  for (const bool ragged : {false, true}) {
-    Cache8AttnParams p{};
+  Cache8AttnParams p{};
+  for (const bool ragged : {false, true})
     if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged, p) != HSA_OK) return 0;
-    need = std::max(need, cache8_ws(cfg, p));
-  }
-  return need;
+  return cache8_ws(cfg, n_q, kv_heads, (int64_t)k_max + n_cur_pages);
 }
 
 hsa_status_t hsa_cache8_attn_plan(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
@@ -1460,7 +1461,7 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
   Cache8AttnParams p{};
   if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, kv_len != nullptr, p)) != HSA_OK)
     return st;
-  const size_t need = cache8_ws(cfg, p);
+  const size_t need = cache8_ws(cfg, n_q, cache->kv_heads, (int64_t)k_max + n_cur_pages);
   if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if ((st = validate_cache8(cfg, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK)

@@ -1037,6 +1037,25 @@ hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s
   return hipGetLastError();
 }
 
+// 64-token tiles of a list, walked by the page or, of small pages, as a stream.
+int64_t cache8_tiles(int64_t list, int P) { return P < 64 ? (list * P + 63) / 64 : list * ((P + 63) / 64); }
+// Calls that the many-rows kernel may take, and the work (items of 16 rows times tiles) up to which a
+// call is little.
+bool cache8_large(int dtype, int64_t rows) { return dtype == HSA_DTYPE_BF16 && rows > 64; }
+int64_t cache8_little(bool large, int d) { return large ? (d == 64 ? 32768 : 8192) : 4096; }
+bool cache8_brief(int64_t items16, int64_t tiles, int64_t rows, bool large, int d) {
+  return items16 <= (large || rows <= 16 ? 4096 : 256) && items16 * tiles <= cache8_little(large, d);
+}
+// Rows of an item of the four-wave workgroups.
+int cache8_few_rows(int dtype, int d, int64_t rows) {
+  return rows <= 16 ? 16 : (rows > 32 && dtype == HSA_DTYPE_BF16 && d == 64 ? 64 : 32);
+}
+// Workgroups of the many-rows kernel that a call is planned for.
+int64_t cache8_slots(int d, int P, bool ragged) { return d == 128 ? 256 : (ragged || P < 64 ? 512 : 768); }
+// Most pieces of such a call, their ends counted (see plan_cache8).
+constexpr int kManyPieces = 16;
+constexpr double kManyEnds = 6.0, kManyJoin = 4.0, kManyGain = 0.97;
+
 }  // namespace
 
 void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged) {
@@ -1053,10 +1072,9 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   // twice the tokens 38 and 36) or sixteen (d = 64: 4096 over 2048 31 us and 35; three ragged
   // prompts, 2.3 times the work, 50 and 46).
   const int64_t items16 = (int64_t)B * p.Hk * ((rows + 15) / 16);
-  const int64_t by_page = p.P < 64 ? (list * p.P + 63) / 64 : list * p.tpp;
-  const bool large = dtype == HSA_DTYPE_BF16 && rows > 64;
-  const int64_t little = large ? (p.d == 64 ? 32768 : 8192) : 4096;
-  const bool brief = items16 <= (large || rows <= 16 ? 4096 : 256) && items16 * by_page <= little;
+  const int64_t by_page = cache8_tiles(list, p.P);
+  const bool large = cache8_large(dtype, rows);
+  const bool brief = cache8_brief(items16, by_page, rows, large, p.d);
   // More than 64 rows of bf16 otherwise (8 sequences of 8192 tokens, 8 heads, d = 128: 96 rows 66 us,
   // in items of 32 rows 86; d = 64, 64 rows: 39 us, in one item of 64 rows 30). fp32 has three
   // parts of everything, and its registers hold 32 rows.
@@ -1067,8 +1085,7 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   // pages of 72, 161 us as a stream and 143 by the page; of 200, 182 and 145; of 16, 140).
   p.stream = many || p.P < 64;
   const int64_t tiles = std::max<int64_t>(1, many ? (list * p.P + 63) / 64 : by_page);
-  const int most = dtype == HSA_DTYPE_BF16 && p.d == 64 ? 64 : 32;
-  p.rows_per_item = many ? many_rows(p.d) : (brief || rows <= 16 ? 16 : (rows <= 32 ? 32 : most));
+  p.rows_per_item = many ? many_rows(p.d) : (brief ? 16 : cache8_few_rows(dtype, p.d, rows));
   p.waves = brief ? 8 : 4;
   p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
   p.part_rows = p.n_rt * p.rows_per_item;
@@ -1081,12 +1098,12 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
     // d = 128, 128 queries: 74 us in four pieces. Of ragged sequences, d = 64, some slots
     // are idle anyway (three prompts of up to 1001 tokens: whole items 43 us, in two 46; one causal
     // call of 4096 queries over 8192 tokens: with 512 slots 66 us, with 768 63).
-    const int64_t slots = p.d == 128 ? 256 : (ragged || p.P < 64 ? 512 : 768);
+    const int64_t slots = cache8_slots(p.d, p.P, ragged);
     double best = 1e300;
-    for (int64_t k = 1; k <= 16 && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
-      const double each = (double)((tiles + k - 1) / k) + 6.0 + (k > 1 ? 4.0 : 0.0);
+    for (int64_t k = 1; k <= kManyPieces && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
+      const double each = (double)((tiles + k - 1) / k) + kManyEnds + (k > 1 ? kManyJoin : 0.0);
       const double t = (double)((items * k + slots - 1) / slots) * each;
-      if (t < 0.97 * best) {
+      if (t < kManyGain * best) {
         best = t;
         n = k;
       }
@@ -1132,8 +1149,50 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.n_split = (int)((tiles + c - 1) / c);
 }
 
-size_t cache8_part_bytes(int64_t B, int64_t Hk, int64_t n_split, int64_t part_rows, int64_t d) {
-  return n_split > 1 ? (size_t)(B * Hk * n_split * part_rows * (d + 2)) * 4 : 0;
+int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list) {
+  const int64_t tiles = cache8_tiles(list, P), items16 = (int64_t)B * Hk * ((rows + 15) / 16);
+  const bool large = cache8_large(dtype, rows);
+  int64_t most = 0;
+  auto take = [&](int64_t pieces, int64_t per_item) {
+    if (pieces > 1) most = std::max(most, pieces * ((rows + per_item - 1) / per_item * per_item));
+  };
+  // Lists up to some length are little work: as many pieces as workgroups, of at least a tile a wave.
+  if (cache8_brief(items16, cache8_tiles(1, P), rows, large, d)) {
+    const int64_t longest = std::min(tiles, cache8_little(large, d) / items16);
+    take(std::min(256 / items16, (longest - 1) / 8 + 1), 16);
+  }
+  if (cache8_brief(items16, tiles, rows, large, d)) return most;
+  if (large) {
+    // k pieces of T tiles (4 k or more) have to be faster than any fewer. With r the rounds of workgroups
+    // and e their ends and the join: r(k) (ceil(T / k) + e) < r(j) (ceil(T / j) + e), 1 < j < k (a j that did not
+    // gain enough itself leaves no less to beat), and below the gain times r(1) (T + ends). With T / k for the
+    // left side and T / j + 1 for the right one, both are linear in T: a range [lo, hi] of it.
+    const int64_t all = (list * P + 63) / 64, per = many_rows(d), items = (int64_t)B * Hk * ((rows + per - 1) / per);
+    constexpr double e = kManyEnds + kManyJoin, kSlack = 1.0 + 1e-9;
+    for (const bool ragged : {false, true}) {
+      const int64_t slots = cache8_slots(d, P, ragged);
+      auto rounds = [&](int64_t k) { return (double)((items * k + slots - 1) / slots); };
+      for (int64_t k = kManyPieces; k > 1; --k) {
+        double lo = 4.0 * (double)k, hi = (double)all;
+        for (int64_t j = 1; j < k; ++j) {
+          const double r = rounds(j) * kSlack * (j > 1 ? 1.0 : kManyGain);
+          const double slope = rounds(k) / (double)k - r / (double)j;  // slope T <= room
+          const double room = r * (j > 1 ? e + 1.0 : kManyEnds) - rounds(k) * e;
+          if (slope > 0.0) hi = std::min(hi, room / slope);
+          else if (slope < 0.0) lo = std::max(lo, room / slope);
+          else if (room < 0.0) hi = -1.0;
+        }
+        if (lo > hi) continue;
+        take(k, per);
+        break;
+      }
+    }
+  } else {
+    const int64_t per = cache8_few_rows(dtype, d, rows), items = (int64_t)B * Hk * ((rows + per - 1) / per);
+    take(std::min((4096 + items - 1) / items, std::min<int64_t>(kMaxSplit, tiles / 16)), per);  // ragged
+    take(std::min((2048 + items - 1) / items, std::min<int64_t>(kMaxSplit, tiles / 8)), per);
+  }
+  return most;
 }
 
 hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s) {

@@ -252,7 +252,9 @@ struct Cache8AttnParams {
 // Plans the launch for lists of at most max_list_sel selected pages; ragged: the sequences'
 // lengths are on the device.
 void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged);
-size_t cache8_part_bytes(int64_t B, int64_t Hk, int64_t n_split, int64_t part_rows, int64_t d);
+// Most rows of partial outputs (n_split * part_rows) that plan_cache8 gives a key head for any list up to
+// `list` pages, of either kind of call. rows: n_q * G.
+int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list);
 hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s);
 
 // ------------------------------------------------------------ attention

@@ -1,5 +1,6 @@
 """Single calls of the 8-bit cache and the rotation that a program makes and the other tests do
-not: a first append inside a block, the gradient of rotated queries."""
+not: a first append inside a block, the gradient of rotated queries, one
+workspace for lists of many lengths."""
 import numpy as np
 import pytest
 import torch
@@ -8,7 +9,7 @@ import paper_2609_34606_amd as P
 from oracle import hsa_cache8_oracle as O
 from test_gpu_cache8 import BF, F32
 from test_gpu_rope import EPS, check
-from test_gpu_tokens import host, i32, source
+from test_gpu_tokens import cache, host, i32, source
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -114,3 +115,24 @@ def test_rotated_attention_trains():
         num = (loss64(a + h * da, b + h * db) - loss64(a - h * da, b - h * db)) / (2 * h)
         got = (host(ql.grad) * da).sum() + (host(kl.grad) * db).sum()
         assert abs(num - got) < 2.0 ** -14 * max(1.0, np.sqrt((host(ql.grad) ** 2).sum() + (host(kl.grad) ** 2).sum()))
+
+
+@pytest.mark.parametrize("B,H,kv,d,P_,n_q,pages", [(1, 12, 12, 128, 256, 1, 64), (2, 4, 2, 64, 40, 5, 150),
+                                                   (1, 12, 12, 128, 200, 700, 40), (8, 8, 8, 128, 64, 128, 60)])
+def test_one_workspace_for_every_list_up_to_the_longest(B, H, kv, d, P_, n_q, pages):
+    """A program's own workspace, as large as its longest list asks for: the bits of calls that take
+    their own."""
+    c, _ = cache(5, B, H, d, P_, BF, pages, kv=kv)
+    c.write(*source(5, B, pages * P_, kv, d, BF, False))
+    q = source(6, B, n_q, H, d, BF, False)[0]
+    ws = torch.empty(P.hsa_cache8_attn_workspace_size(c.cfg, n_q, kv, 0, pages), dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+    cut = 0
+    for n in list(range(1, pages, 3)) + [pages]:
+        for ragged in (False, True):
+            lens = i32([n * P_ - 5 * b for b in range(B)]) if ragged else None
+            cut += P.hsa_cache8_attn_plan(c.cfg, n_q, kv, 0, n, ragged)[2] > 1
+            out = torch.full_like(q, 3.0)
+            P.hsa_cache8_attn(c.cfg, q, n_q, c.pool, None, 0, None, 0, n, out, kv_len=lens, ws=ws)
+            assert torch.equal(out, c.attend(q, n, kv_len=lens)), n
+    assert cut > 4
