@@ -91,8 +91,8 @@ void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
   constexpr int M = D / 16;   // 16-dim blocks of the output
   constexpr int kRows = 16 * kCols;
-  // Parts of a weight. One bf16 part rounds it by up to 2^-9, about what the result's own rounding
-  // adds; two leave 2^-17. Items of 16 rows wait for memory and take two (1 to 3% of
+  // Parts of a weight. One bf16 part rounds it by up to 2^-8, what the result's own rounding
+  // adds too; two leave 2^-16. Items of 16 rows wait for memory and take two (1 to 3% of
   // their time); with more rows the second part would cost 7 to 10%. fp32 takes three.
   constexpr int kWParts = kParts == 3 ? 3 : (kCols == 1 ? 2 : 1);
   constexpr int OS = D + 4;   // floats per row of the join buffer
