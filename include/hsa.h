@@ -748,9 +748,9 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
  * calls): per batch entry and key head the listed pages are sel[b][hk][0..) (up to the first
  * entry outside [0, max_pages), at most k_h[hk]) followed by pages
  * [cur_first_page, cur_first_page + n_cur_pages). Query head h reads key head
- * h / (num_heads / kv_heads). Query i of entry b sees the tokens t of the listed
- * pages with t < kv_len[b] and, with causal != 0, t <= kv_len[b] - q_len[b] + i
- * (query i is the sequence's token at that place):
+ * h / (num_heads / kv_heads). A page listed twice counts twice. Query i of entry b sees
+ * the tokens t of the listed pages with t < kv_len[b] and, with causal != 0, t <=
+ * kv_len[b] - q_len[b] + i (query i is the sequence's token at that place):
  *   o[b][i][h] = sum_t softmax_t(scale * q_i . k_t) v_t     (cfg->dtype)
  *   lse[b][h][i] = log sum_t exp(scale * q_i . k_t)          (fp32, nullable)
  * A query that sees no token gets o = 0 and lse = -inf. What lies in a page at or past

@@ -1,6 +1,6 @@
 """Single calls of the 8-bit cache and the rotation that a program makes and the other tests do
 not: a first append inside a block, the gradient of rotated queries, one
-workspace for lists of many lengths."""
+workspace for lists of many lengths, pages listed twice."""
 import numpy as np
 import pytest
 import torch
@@ -8,8 +8,9 @@ import torch
 import paper_2609_34606_amd as P
 from oracle import hsa_cache8_oracle as O
 from test_gpu_cache8 import BF, F32
+from test_gpu_cache8 import check as attended
 from test_gpu_rope import EPS, check
-from test_gpu_tokens import cache, host, i32, source
+from test_gpu_tokens import arrays, cache, host, i32, source
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -136,3 +137,23 @@ def test_one_workspace_for_every_list_up_to_the_longest(B, H, kv, d, P_, n_q, pa
             P.hsa_cache8_attn(c.cfg, q, n_q, c.pool, None, 0, None, 0, n, out, kv_len=lens, ws=ws)
             assert torch.equal(out, c.attend(q, n, kv_len=lens)), n
     assert cut > 4
+
+
+@pytest.mark.parametrize("d,P_,n_q,dt", [(128, 200, 1, BF), (64, 40, 3, F32), (64, 72, 30, BF), (128, 136, 1024, BF),
+                                         (64, 24, 1024, BF)])
+def test_a_page_listed_twice_counts_twice(d, P_, n_q, dt):
+    """Among the selected pages, and as a selected one and one of the run."""
+    B, H, kv, times = 2, 4, 2, 1 if n_q < 1024 else -(-4400 // P_ // 4)
+    c, pt = cache(8, B, H, d, P_, dt, 4, kv=kv)
+    w = P.HsaCache8(B, H, d, P_, F32, DEV, kv_heads=kv, k=c.k, v=c.v, k_exp=c.k_exp, v_exp=c.v_exp, page_table=c.page_table)
+    w.write(*source(8, B, 4 * P_, kv, d, F32, False, 0.3))
+    rows = [[3, 3, 0, 2] * times, [1, 1, 1, 1] * times]
+    sel = i32([rows] * B)
+    if n_q == 1024:
+        assert P.hsa_cache8_attn_plan(c.cfg, n_q, kv, 4 * times, 2, True)[0]
+    q = source(9, B, n_q, H, d, dt, False)[0]
+    out, lse = torch.full_like(q, 3.0), torch.full((B, H, n_q), 5.0, device=DEV)
+    lens, q_len = [4 * P_ - 3, 3 * P_ + 1], [min(n_q, 20), min(n_q, 7)]
+    c.attend(q, 2, first_page=2, sel=sel, kv_len=i32(lens), q_len=i32(q_len), causal=True, out=out, lse=lse)
+    kd, vd = O.dequantise(arrays(c))
+    attended(q, out, lse, kd, vd, pt, [[r + [2, 3] for r in rows]] * B, lens, q_len, True, d ** -0.5)
