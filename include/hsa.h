@@ -727,7 +727,8 @@ typedef struct hsa_cache8 {
  * hsa_cache8_write -- hsa_token_write into the 8-bit cache: k_src, v_src are
  * [B, n, kv_heads, d]. A block's scale 2^e has the smallest e in [-100, 120] with 448 *
  * 2^e >= its largest finite magnitude (keys after the rotation, in fp32); codes are rounded to
- * nearest even, infinities to the largest code, NaN to a NaN code (0x7f or 0xff). A block whose
+ * nearest even, infinities to the largest code, NaN to a NaN code (0x7f or 0xff). (Magnitudes from
+ * 1.9375 * 2^127 on, which only e = 120 holds, round to 2^128: an infinity to the attention.) A block whose
  * first tokens an earlier call wrote keeps the larger of its scale and the one the
  * new tokens need; if that grows, the older codes are scaled down by the power of two, which
  * rounds only those that become subnormal. A block written from its first

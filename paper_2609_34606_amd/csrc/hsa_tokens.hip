@@ -189,16 +189,17 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
         bits = max_all<kThreads / 64>(bits, amax, tid);
       }
       const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
-      const float scale = pow2i(e), most = kCodeMax * scale;
+      const float scale = wild ? 1.f : pow2i(e);
       if (tid == 0) p.k_exp[head * t.nb + t.blk] = (uint8_t)(e + 127);
       uint8_t* kc = static_cast<uint8_t*>(p.k) + (head * p.P + t.boff) * D;
       auto put = [&](int i, int k) {
         uint8_t* row = kc + (size_t)(t.o0 + i) * D;
-        if (wild) {  // infinities become the largest number of the block's scale
+        if (wild) {  // infinities become the largest code (in units of the scale: 448 * 2^120 is no fp32 number)
+          const float unit = pow2i(-e);
 #pragma unroll
           for (int x = 0; x < Item::N; ++x) {
-            ku[k][x] = saturate(ku[k][x], most);
-            kw[k][x] = saturate(kw[k][x], most);
+            ku[k][x] = saturate(ku[k][x] * unit, kCodeMax);
+            kw[k][x] = saturate(kw[k][x] * unit, kCodeMax);
           }
         }
         store_codes<Item::N>(row + it.a, ku[k], scale);
@@ -324,14 +325,17 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
       bits = max_all<kThreads / 64>(bits, amax, tid);
     }
     const int e = max(scale_exponent(__uint_as_float(bits)), e_old);
-    const float scale = pow2i(e), most = kCodeMax * scale;
+    const float scale = wild ? 1.f : pow2i(e);
     if (tid == 0) p.v_exp[head * t.nb + t.blk] = (uint8_t)(e + 127);
     uint8_t* vc = static_cast<uint8_t*>(p.v) + head * D * p.P + t.boff;
-    if (wild) {  // infinities become the largest number of the block's scale
+    if (wild) {  // infinities become the largest code, as in write_keys (exact in bf16 too)
+      const float unit = pow2i(-e);
       for (int x = tid; x < ntok * (RW - 1); x += kThreads) {
         uint32_t& w = vs[(o0 + x / (RW - 1)) * RW + x % (RW - 1)];
-        if constexpr (sizeof(T) == 2) w = pack_bf16(saturate(bf16_lo(w), most), saturate(bf16_hi(w), most));
-        else w = __float_as_uint(saturate(__uint_as_float(w), most));
+        if constexpr (sizeof(T) == 2)
+          w = pack_bf16(saturate(bf16_lo(w) * unit, kCodeMax), saturate(bf16_hi(w) * unit, kCodeMax));
+        else
+          w = __float_as_uint(saturate(__uint_as_float(w) * unit, kCodeMax));
       }
       __syncthreads();
     }

@@ -1,6 +1,6 @@
 """Single calls of the 8-bit cache and the rotation that a program makes and the other tests do
 not: a first append inside a block, the gradient of rotated queries, one
-workspace for lists of many lengths, pages listed twice."""
+workspace for lists of many lengths, pages listed twice, infinities beside the largest numbers."""
 import numpy as np
 import pytest
 import torch
@@ -10,7 +10,7 @@ from oracle import hsa_cache8_oracle as O
 from test_gpu_cache8 import BF, F32
 from test_gpu_cache8 import check as attended
 from test_gpu_rope import EPS, check
-from test_gpu_tokens import arrays, cache, host, i32, source
+from test_gpu_tokens import arrays, cache, host, i32, one_nan, source
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -157,3 +157,36 @@ def test_a_page_listed_twice_counts_twice(d, P_, n_q, dt):
     c.attend(q, 2, first_page=2, sel=sel, kv_len=i32(lens), q_len=i32(q_len), causal=True, out=out, lse=lse)
     kd, vd = O.dequantise(arrays(c))
     attended(q, out, lse, kd, vd, pt, [[r + [2, 3] for r in rows]] * B, lens, q_len, True, d ** -0.5)
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("P_,at,n", [(16, 0, 5), (16, 3, 40), (200, 0, 200), (200, 70, 3), (72, 5, 100)])
+@pytest.mark.parametrize("rot", [0, 2])
+def test_infinities_beside_the_largest_numbers(rot, P_, at, n, dt):
+    """A block whose scale is the largest, 2^120, of which 448 is no fp32 number: infinities still become
+    the largest code and NaN a NaN code, in a block of their own and in one that holds older tokens."""
+    H, d = 3, 64
+    c, pt = cache(7, 1, H, d, P_, dt, (at + n) // P_ + 1, rope=P.rope(rot) if rot else None)
+    top = torch.finfo(dt).max
+    g = np.random.default_rng(n)
+    some = np.array([top, -top, np.inf, -np.inf, np.nan, 1e38, -2.0 ** 120, 1.0, 0.0])
+    where = []
+    for first, count in ((0, at), (at, n)):
+        if not count:
+            continue
+        x = torch.from_numpy(g.choice(some, (2, 1, count, H, d))).to(dt).to(DEV)
+        x[:, 0, 0, :, 5] = top  # (each block's scale is 2^120 from its first token on)
+        x[0, ..., :rot] = 0.0   # (so that the rotated keys are exact)
+        want = arrays(c)
+        c.write(x[0], x[1], i32([first]))
+        O.write8(want, pt, host(x[0]), host(x[1]), [first], [count])
+        got = arrays(c)
+        # the sign of the rotated zeros is the angle's
+        for name in ("k", "v"):
+            a, b = got[name], want[name]
+            if name == "k":
+                a, b = a[..., rot:], b[..., rot:]
+            assert np.array_equal(one_nan(a), one_nan(b)), name
+            assert np.array_equal(got[name + "_exp"], want[name + "_exp"])
+        where.append(int((got["v"] == 0x7e).sum() + (got["k"] == 0x7e).sum()))
+    assert min(where) > 0
