@@ -442,13 +442,18 @@ void few_rows_kernel(Cache8AttnParams p) {
 // V^T P^T, 32x32x16), with key rows in an order that makes a lane's scores the
 // weights' operand. A step does the softmax and the value product of half a tile and the scores
 // of the next half, matrix instructions between the exponentials.
+// A weight is one bf16 part, rounded by up to 2^-8 of it, as in that walk (their sum is of the fp32 ones):
+// the result is off by 1.9e-3 of its norm, its own rounding alone by 1.7e-3. A second part would be half
+// as many matrix instructions again.
 // Bound: the matrix and the vector pipe one after the other. 4680 queries over 10920 tokens, 12 heads
-// (314 GFLOP): 340 us, 924 TFLOP/s; the matrix pipe is busy 44% of the time and the vector pipe
-// (exponentials, their packing, the maximum; 16 codes of each operand a thread and tile) 49%, and the two
-// hardly overlap, neither within a wave nor between the two of a SIMD. A large library product
-// reaches 1322 TFLOP/s (238 us). Waves of 64 rows need more registers than a wave has (spills);
-// 512 rows a workgroup was no faster, and d = 64 with 256 rows slower (55.9 us and 49.5 for causal
-// prompts of up to 1001 tokens; 42 now).
+// (314 GFLOP): 334 to 340 us, 924 to 940 TFLOP/s, once 100 to 150 launches in a row have brought the clock
+// from 1.8 to 2.3 GHz (the first ten 425 to 450 us, one every 20 ms 420 to 440). Of the cycles of a CU that
+// has a workgroup the matrix pipe is busy in 44%, and vector instructions (exponentials, their packing, the
+// maximum; 16 codes of each operand a thread and tile) issue in 51%, matrix instructions' own issue among
+// them; the two hardly overlap, neither within a wave nor between the two of a SIMD. A large library product
+// goes from 1140 to 1430 TFLOP/s over the same launches (275 to 220 us). Waves of 64 rows need more
+// registers than a wave has (spills); 512 rows a workgroup was no faster, and d = 64 with 256 rows slower
+// (55.9 us and 49.5 for causal prompts of up to 1001 tokens; 42 now).
 template <int D>
 struct ManyLayout {
   static constexpr int kRowK = 2 * D, kTileK = 64 * kRowK;  // bytes
@@ -1095,9 +1100,12 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
     // Rounds of as many workgroups as are resident (one a CU, with d = 64 three, of small pages
     // two), each of its tiles and about six more for its start and end; pieces cost a
     // partial output written and read again (four). 8 causal sequences of 8192 tokens,
-    // d = 128, 128 queries: 74 us in four pieces. Of ragged sequences, d = 64, some slots
-    // are idle anyway (three prompts of up to 1001 tokens: whole items 43 us, in two 46; one causal
-    // call of 4096 queries over 8192 tokens: with 512 slots 66 us, with 768 63).
+    // d = 128, 128 queries: 74 us in four pieces. Calls with kv_len, d = 64, are planned for two workgroups a
+    // CU, which leaves more items whole: right for prompts (three of up to 1001 tokens, 16 query and 4 key
+    // heads, of drawn, nearly equal and equal lengths 28, 34 and 35 us, for three a CU 34, 40 and 40; two of 3000
+    // tokens 117 and 127), not for queries over a longer history (4096 of 4 heads over 8192 tokens 67 us and 63;
+    // 4680 of 12 heads over 10920, 265 and 254) or short ones over small pages (four of 900 tokens, pages
+    // of 136, 29 and 28).
     const int64_t slots = cache8_slots(p.d, p.P, ragged);
     double best = 1e300;
     for (int64_t k = 1; k <= kManyPieces && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
