@@ -733,9 +733,9 @@ typedef struct hsa_cache8 {
  * new tokens need; if that grows, the older codes are scaled down by the power of two, which
  * rounds only those that become subnormal. A block written from its first
  * token on starts anew, whatever its memory held; one that an append enters further on, with nothing
- * written before, needs an exponent byte of 0 (any other is taken for an earlier call's). Codes of the block behind the new tokens stay as
- * they are, and what they stand for is lost if the scale changes: a sequence is written forwards,
- * and one that was cut back goes on from its new end.
+ * written before, needs an exponent byte of 0 (any other is taken for an earlier call's). Codes of
+ * the block behind the new tokens stay as they are, and what they stand for is lost if the scale
+ * changes: a sequence is written forwards, and one that was cut back goes on from its new end.
  */
 hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache,
                               const hsa_rope_t* rope, const void* k_src, int64_t k_batch_stride,
