@@ -791,6 +791,170 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
                              const int32_t* kv_len, const int32_t* q_len, int32_t causal,
                              void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Drafted trees. A step that drafts several continuations at once brings a tree of up to
+ * HSA_MAX_TREE nodes per sequence, appended behind it as its last tokens in an order that has
+ * every parent before its children. Then: hsa_tree_mask (once a step), hsa_token_write or
+ * hsa_cache8_write and hsa_tree_attn or hsa_cache8_tree_attn (each layer), and, once a path is
+ * accepted, hsa_token_keep or hsa_cache8_keep (each layer). A tree without branches is a
+ * causal run of tokens, one of a single node an ordinary decoded token.
+ */
+#define HSA_MAX_TREE 256
+
+/*
+ * hsa_tree_mask -- the ancestors of every node, as bits: bit j % 32 of mask[b][i][j / 32] is set
+ * if node j lies on the path from node i's root to node i (i itself included). parent: device
+ * int32 [B, n], in [0, i) for node i; any other value: a root (which sees the sequence alone).
+ * count: device int32 [B] in [0, n], NULL: n; rows of mask and pos at or past count[b] stay as they were. pos[b][i]
+ * = first[b] + the node's depth (0 for a root), the position that hsa_rope_apply takes (device int32 [B, n],
+ * nullable; first: device int32 [B], NULL: 0). mask: device uint32 [B, n, ceil(n / 32)]. n in
+ * [0, HSA_MAX_TREE] (UNSUPPORTED above); n == 0 is a no-op.
+ */
+hsa_status_t hsa_tree_mask(const hsa_config_t* cfg, const int32_t* parent, int32_t n, const int32_t* count,
+                           const int32_t* first, uint32_t* mask, int32_t* pos, void* stream);
+
+/*
+ * hsa_tree_attn -- exact softmax attention of a step's nodes over the pool. Per batch entry and key
+ * head the listed pages are those of hsa_cache8_attn (sel[b][hk], at most k_h[hk], then
+ * [cur_first_page, cur_first_page + n_cur_pages)). Query head h reads key head h / (num_heads /
+ * kv_heads); the pool is [num_slots, kv_heads, ..]. With base = kv_len[b] - q_len[b], query i sees the
+ * tokens t < kv_len[b] of the listed pages with t < base, or with bit (t - base) of mask row i set:
+ *   o[b][i][h] = sum_t softmax_t(scale * q_i . k_t) v_t     (cfg->dtype)
+ *   lse[b][h][i] = log sum_t exp(scale * q_i . k_t)          (fp32, nullable)
+ * A query that sees no token gets o = 0 and lse = -inf. What a query does not see never reaches it,
+ * whatever it holds. q, o: device [B, n_q, num_heads, d], n_q in [0, HSA_MAX_TREE]. mask: device uint32 [B,
+ * n_q, ceil(n_q / 32)] (any bits, not only those of a tree), NULL: query i sees base + j for j <= i.
+ * kv_len: device int32 [B], NULL: (cur_first_page + n_cur_pages) * P. q_len: device int32 [B] in
+ * [0, n_q], NULL: n_q; rows of o and lse at or past q_len[b] stay as they were.
+ * Products of bf16 operands summed in fp32; a bf16 call rounds the softmax weights to bf16 (in two parts
+ * where a key head has up to 16 rows n_q * num_heads / kv_heads); an fp32 call's products are of fp32. Sums are
+ * joined in a fixed order: the same call gives the same bits. ws: hsa_tree_attn_workspace_size(...)
+ * bytes, 256-byte aligned; the size for a program's longest list serves every shorter one of the same cfg,
+ * n_q and kv_heads. It does not grow with n_q (see hsa_cache8_attn). Errors as hsa_cache8_attn; q, o, pool->k and
+ * pool->v are 16-byte aligned, and the listed pages hold fewer than 2^31 - 256 tokens (UNSUPPORTED).
+ * Kernels read kv_len, q_len and mask, so a captured call follows them.
+ */
+size_t hsa_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                    int32_t k_max, int32_t n_cur_pages);
+hsa_status_t hsa_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
+                           const hsa_kv_pool_t* pool, int32_t kv_heads, const int32_t* sel, int32_t k_max,
+                           const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
+                           const int32_t* kv_len, const int32_t* q_len, const uint32_t* mask, void* o,
+                           float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * hsa_cache8_tree_attn -- hsa_tree_attn over the 8-bit cache. An fp32 call splits queries and
+ * weights into three bf16 parts, as hsa_cache8_attn does. ws:
+ * hsa_cache8_tree_attn_workspace_size(...) bytes.
+ */
+size_t hsa_cache8_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
+                                           int32_t k_max, int32_t n_cur_pages);
+hsa_status_t hsa_cache8_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
+                                  const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
+                                  const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
+                                  const int32_t* kv_len, const int32_t* q_len, const uint32_t* mask,
+                                  void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * hsa_token_keep -- tokens of a sequence move to others of its places in the pool: token first[b] + i takes
+ * the key and value of token first[b] + index[b][i], i < count[b], all read before any is written (an
+ * index may occur twice). With first the base of a tree and index the nodes of the accepted path, the path becomes
+ * the sequence's next tokens. Keys are moved as they are: a node's position is that of its depth already. first:
+ * device int32 [B], NULL: 0. index: device int32 [B, n]. count: device int32 [B] in [0, n], NULL: n. n in
+ * [0, HSA_MAX_TREE] (UNSUPPORTED above). Tokens outside [0, max_pages * P) are neither read nor written (nor is
+ * what they would have gone to). No two entries may write to the same page. cfg->num_heads are
+ * the pool's heads. pool->k and pool->v 16-byte aligned (UNSUPPORTED). n == 0 is a no-op. Kernels read
+ * first, index and count, so a captured call follows them.
+ */
+hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* first,
+                            const int32_t* index, int32_t n, const int32_t* count, void* stream);
+
+/*
+ * hsa_cache8_keep -- the same in the 8-bit cache. The result is that of appending the kept tokens'
+ * numbers (code * 2^(exponent byte - 127)) at first[b] with hsa_cache8_write: a block that begins with
+ * kept tokens takes the smallest scale that holds them, one with older tokens before them keeps the larger of
+ * its own and that (older codes scaled down). A number changes only if its code becomes subnormal. Codes of a block
+ * behind the kept tokens stay as they are, and what they stand for is lost if the scale changes.
+ */
+hsa_status_t hsa_cache8_keep(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* first,
+                             const int32_t* index, int32_t n, const int32_t* count, void* stream);
+
+/*
+ * Slots. A page table whose rows may share slots, and the count of its entries that hold each slot
+ * (0: the slot is free), both on the device: no call waits for the host, and all of them can be
+ * captured. The layers of a model can share one table, each with a pool of its own of the same
+ * num_slots; hsa_page_copy then does each layer's part of the moves. Everything is decided in a fixed order, so
+ * the same tables give the same tables. A pool whose table a tier keeps (hsa_tier_*) is not for these calls.
+ * Calls on one table are ordered by the caller (one stream). Of cfg, batch and page_size count. Entries
+ * at or past num_slots are left alone. Errors: INVALID_ARG (NULL, sizes below 1), UNSUPPORTED (B above 8192 for
+ * take and above 65535, B * max_pages or num_slots above 2^30, max_pages * P above 2^31 - 257), WORKSPACE. ws (256-byte aligned) is
+ * hsa_slots_workspace_size(...) bytes for every call that takes one; its contents do not matter.
+ */
+typedef struct hsa_slots {
+  int32_t* page_table; /* device [B, max_pages]; -1: no page */
+  int32_t* refs;       /* device [num_slots] */
+  int32_t num_slots;
+  int32_t max_pages;
+} hsa_slots_t;
+
+size_t hsa_slots_workspace_size(const hsa_config_t* cfg, int32_t num_slots, int32_t max_pages);
+
+/*
+ * hsa_slots_take -- makes the pages of row b that hold tokens [first[b], end[b]) its own, before
+ * they are written: an entry without a slot takes a free one; an entry whose slot is shared takes a
+ * free one too, except that the last entry that holds a slot keeps it (in order of rows and pages, if every
+ * other holder takes part in this call and comes before it). Entries take the lowest free slots, in order of rows and
+ * pages. Where the first page was shared and holds tokens before first[b], moves[b] = {old
+ * slot, new slot, first[b] % P} for hsa_page_copy, {-1, -1, -1} otherwise (device int32 [B, 3], nullable: such
+ * tokens are then lost). If the free slots do not suffice, the entries that come last stay as they were and
+ * *missing (device int32, nullable) is their number, else 0: a program that can run out of slots
+ * reads it before it writes. Pages past max_pages are not taken. first: device int32 [B], NULL: 0.
+ * end: device int32 [B]; end[b] <= first[b] takes nothing.
+ */
+hsa_status_t hsa_slots_take(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* first,
+                            const int32_t* end, int32_t* moves, int32_t* missing, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/*
+ * hsa_slots_fork -- row b becomes what row parent[b] was before the call (all rows at once: a beam
+ * search's step), sharing its slots. parent: device int32 [B]; a value outside [0, B) keeps the row.
+ * Before a row's shared last page is written, hsa_slots_take gives it one of its own. (What a layer holds
+ * by batch entry, kv_state, k_state and page_kmean, is the caller's to index by parent.)
+ */
+hsa_status_t hsa_slots_fork(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* parent, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
+ * hsa_slots_free -- row b lets go of its pages behind its first keep[b] tokens (0: of all, the
+ * sequence has ended; below 0: of none). keep: device int32 [B].
+ */
+hsa_status_t hsa_slots_free(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* keep,
+                            void* stream);
+
+/*
+ * hsa_slots_compact -- moves the slots in use to the front of the pool: with n slots in use, the i-th one
+ * at or behind slot n goes to the i-th free one before it, for at most n_moves of them (a program may spread
+ * the copies over several calls). moves[i] = {from, to, P}, {-1, -1, -1} past the last (device int32 [n_moves, 3]).
+ * table_out [B, max_pages], refs_out [num_slots]: device, the new table and counts; NULL or slots' own
+ * arrays: in place. The pages hold their tokens after hsa_page_copy(moves).
+ */
+hsa_status_t hsa_slots_compact(const hsa_config_t* cfg, const hsa_slots_t* slots, int32_t* moves, int32_t n_moves,
+                               int32_t* table_out, int32_t* refs_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * hsa_page_copy -- copies pages between slots of the pool, every head's keys and values: moves[i] = {from, to,
+ * tokens} (device int32 [n, 3]), the first `tokens` tokens of a page rounded up to a multiple of 8 (P or more: the whole
+ * page); the rest of the page at `to` stays as it was. A move with a slot outside [0, num_slots) or no tokens
+ * copies nothing. No slot may be written by two moves, or written by one and read by another.
+ * cfg->num_heads are the pool's heads. pool->k and pool->v 16-byte aligned. A compressed pool is copied
+ * with cfg->page_size = rank. n == 0 is a no-op. pool->page_table is not used.
+ */
+hsa_status_t hsa_page_copy(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* moves, int32_t n,
+                           void* stream);
+/* The same in the 8-bit cache: codes and the scales of the blocks that the tokens are in. */
+hsa_status_t hsa_cache8_page_copy(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* moves,
+                                  int32_t n, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1340,6 +1340,196 @@ size_t cache8_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int64_t
   return align_up((size_t)(parts * cfg->batch * kv_heads * (cfg->head_dim + 2)) * 4);
 }
 
+// With HSA_CHECK=1: as validate_tokens, and the page of every token of the table that is read must map to
+// a slot.
+hsa_status_t validate_kept(const hsa_config_t* c, const int32_t* page_table, int num_slots, int max_pages,
+                           const int32_t* first, const int32_t* index, const int32_t* count, int n, hipStream_t s) {
+  if (!check_env()) return HSA_OK;
+  const hsa_status_t st = validate_tokens(c, page_table, num_slots, max_pages, first, count, n, s);
+  if (st != HSA_OK) return st;
+  try {
+    std::vector<int32_t> pt, f, k, x;
+    if (fetch(page_table, (size_t)c->batch * max_pages, 0, pt) != HSA_OK || fetch(first, c->batch, 0, f) != HSA_OK ||
+        fetch(count, c->batch, n, k) != HSA_OK || fetch(index, (size_t)c->batch * n, 0, x) != HSA_OK)
+      return HSA_ERR_DEVICE;
+    for (int b = 0; b < c->batch; ++b)
+      for (int i = 0; i < k[b]; ++i) {
+        const int64_t t = (int64_t)f[b] + x[(size_t)b * n + i];
+        if (t < 0 || t >= (int64_t)max_pages * c->page_size) continue;
+        const int32_t slot = pt[(size_t)b * max_pages + t / c->page_size];
+        if (slot < 0 || slot >= num_slots) return HSA_ERR_OUT_OF_RANGE;
+      }
+  } catch (const std::exception&) {
+    return HSA_ERR_DEVICE;
+  }
+  return HSA_OK;
+}
+
+// What the calls of a drafted tree over either cache share.
+hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur,
+                            bool eight, TreeAttnParams& p, size_t& ws) {
+  if (n_q > HSA_MAX_TREE || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
+  if (((int64_t)k_max + n_cur) * cfg->page_size >= (1LL << 31) - 256) return HSA_ERR_UNSUPPORTED;
+  p.B = cfg->batch;
+  p.H = cfg->num_heads;
+  p.Hk = kv_heads;
+  p.G = cfg->num_heads / kv_heads;
+  p.P = cfg->page_size;
+  p.n_q = n_q;
+  p.words = (n_q + 31) / 32;
+  p.k_max = k_max;
+  p.n_cur = n_cur;
+  const int64_t parts = plan_tree(p, cfg->dtype, eight, (int64_t)k_max + n_cur);
+  const int64_t heads = (int64_t)cfg->batch * kv_heads;
+  if (heads * p.n_split * p.n_rt + 8 * p.n_rt > kMaxGrid || heads * p.part_rows > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  ws = parts > p.part_rows ? align_up((size_t)(parts * heads * (cfg->head_dim + 2)) * 4) : 0;
+  return HSA_OK;
+}
+
+size_t tree_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur, bool eight) {
+  if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur < 0) return 0;
+  if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur < 1) return 0;
+  TreeAttnParams p{};
+  size_t ws = 0;
+  return plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur, eight, p, ws) == HSA_OK ? ws : 0;
+}
+
+// cache: the descriptor of either cache's pages (of the pool: without exponent bytes).
+hsa_status_t run_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_cache8_t& cache, bool eight,
+                           const int32_t* sel, int32_t k_max, const int32_t* k_h, int32_t cur_first, int32_t n_cur,
+                           const int32_t* kv_len, const int32_t* q_len, const uint32_t* mask, void* o, float* lse,
+                           void* ws, size_t ws_bytes, void* stream) {
+  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first < 0 || n_cur < 0) return HSA_ERR_INVALID_ARG;
+  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)k_max + n_cur < 1) return HSA_ERR_INVALID_ARG;
+  if (k_h)
+    for (int h = 0; h < cache.kv_heads; ++h)
+      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)cur_first + n_cur > cache.max_pages) return HSA_ERR_OUT_OF_RANGE;
+  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
+  hsa_status_t st = check_table(cfg, cache.max_pages);
+  if (st != HSA_OK) return st;
+  if (n_q == 0) return HSA_OK;
+  TreeAttnParams p{};
+  size_t need = 0;
+  if ((st = plan_tree_call(cfg, n_q, cache.kv_heads, k_max, n_cur, eight, p, need)) != HSA_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_cache8(cfg, &cache, sel, k_max, k_h, cur_first, n_cur, kv_len, s)) != HSA_OK) return st;
+  p.q = q;
+  p.k = cache.k;
+  p.v = cache.v;
+  p.k_exp = static_cast<const uint8_t*>(cache.k_exp);
+  p.v_exp = static_cast<const uint8_t*>(cache.v_exp);
+  p.page_table = cache.page_table;
+  p.sel = sel;
+  p.kv_len = kv_len;
+  p.q_len = q_len;
+  p.mask = mask;
+  p.o = o;
+  p.lse = lse;
+  p.num_slots = cache.num_slots;
+  p.max_pages = cache.max_pages;
+  p.cur_first = cur_first;
+  p.sm_scale = softmax_scale(cfg);
+  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
+  for (int h = 0; h < cache.kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * cfg->head_dim;
+  return from_hip(launch_tree_attention(cfg->dtype, cfg->head_dim, eight, p, s));
+}
+
+// The pool's pages as the descriptor that the calls over either cache take.
+hsa_status_t pool_pages(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, int32_t kv_heads, hsa_cache8_t& c) {
+  hsa_status_t st = check_pool(pool);
+  if (st != HSA_OK) return st;
+  if (kv_heads < 1 || cfg->num_heads % kv_heads != 0) return HSA_ERR_INVALID_ARG;
+  if (!aligned16(pool->k) || !aligned16(pool->v)) return HSA_ERR_UNSUPPORTED;
+  // the pool is the caller's device memory; some of these calls are among those that write it
+  c.k = const_cast<void*>(pool->k);
+  c.v = const_cast<void*>(pool->v);
+  c.page_table = pool->page_table;
+  c.num_slots = pool->num_slots;
+  c.max_pages = pool->max_pages;
+  c.kv_heads = kv_heads;
+  return HSA_OK;
+}
+
+hsa_status_t run_keep(const hsa_config_t* cfg, const hsa_cache8_t& cache, bool eight, const int32_t* first,
+                      const int32_t* index, int32_t n, const int32_t* count, void* stream) {
+  if (n < 0 || (n != 0 && !index)) return HSA_ERR_INVALID_ARG;
+  hsa_status_t st = check_table(cfg, cache.max_pages);
+  if (st != HSA_OK) return st;
+  if (n > HSA_MAX_TREE || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
+  if (n == 0) return HSA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_kept(cfg, cache.page_table, cache.num_slots, cache.max_pages, first, index, count, n, s)) != HSA_OK)
+    return st;
+  TokenKeepParams p{};
+  p.k = cache.k;
+  p.v = cache.v;
+  p.k_exp = static_cast<uint8_t*>(cache.k_exp);
+  p.v_exp = static_cast<uint8_t*>(cache.v_exp);
+  p.page_table = cache.page_table;
+  p.first = first;
+  p.index = index;
+  p.count = count;
+  p.H = cache.kv_heads;
+  p.P = cfg->page_size;
+  p.n = n;
+  p.num_slots = cache.num_slots;
+  p.max_pages = cache.max_pages;
+  return from_hip(launch_token_keep(cfg->dtype, cfg->head_dim, cfg->batch, eight, p, s));
+}
+
+hsa_status_t run_page_copy(const hsa_config_t* cfg, const hsa_cache8_t& cache, int size, const int32_t* moves,
+                           int32_t n, void* stream) {
+  if (n < 0 || (n != 0 && !moves)) return HSA_ERR_INVALID_ARG;
+  if (cfg->page_size > 1 << 24) return HSA_ERR_UNSUPPORTED;
+  PageCopyParams p{};
+  p.k = cache.k;
+  p.v = cache.v;
+  p.k_exp = static_cast<uint8_t*>(cache.k_exp);
+  p.v_exp = static_cast<uint8_t*>(cache.v_exp);
+  p.moves = moves;
+  p.H = cache.kv_heads;
+  p.P = cfg->page_size;
+  p.d = cfg->head_dim;
+  p.size = size;
+  p.n = n;
+  p.num_slots = cache.num_slots;
+  if (page_copy_parts(p) * n > kMaxGrid) return HSA_ERR_UNSUPPORTED;
+  return n == 0 ? HSA_OK : from_hip(launch_page_copy(p, static_cast<hipStream_t>(stream)));
+}
+
+int size_of(const hsa_config_t* cfg) { return cfg->dtype == HSA_DTYPE_BF16 ? 2 : 4; }
+
+// Sizes of the slot calls; fills in what they share.
+hsa_status_t check_slots(const hsa_config_t* cfg, int32_t num_slots, int32_t max_pages, SlotsParams& p) {
+  if (num_slots < 1 || max_pages < 1) return HSA_ERR_INVALID_ARG;
+  const hsa_status_t st = check_table(cfg, max_pages);
+  if (st != HSA_OK) return st;
+  if (cfg->batch > kMaxGridY || num_slots > 1 << 30 || (int64_t)cfg->batch * max_pages > 1 << 30) return HSA_ERR_UNSUPPORTED;
+  p.B = cfg->batch;
+  p.P = cfg->page_size;
+  p.num_slots = num_slots;
+  p.max_pages = max_pages;
+  return HSA_OK;
+}
+
+size_t slots_ws(const SlotsParams& p) {
+  return align_up(4 * std::max({slots_take_ints(p), slots_fork_ints(p), slots_compact_ints(p)}));
+}
+
+hsa_status_t slots_call(const hsa_config_t* cfg, const hsa_slots_t* slots, SlotsParams& p) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if (!slots || !slots->page_table || !slots->refs) return HSA_ERR_INVALID_ARG;
+  p.page_table = slots->page_table;
+  p.refs = slots->refs;
+  return check_slots(cfg, slots->num_slots, slots->max_pages, p);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1488,6 +1678,153 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * p.d;
   return from_hip(launch_cache8_attention(cfg->dtype, cfg->head_dim, cfg->batch, p, s));
+}
+
+hsa_status_t hsa_tree_mask(const hsa_config_t* cfg, const int32_t* parent, int32_t n, const int32_t* count,
+                           const int32_t* first, uint32_t* mask, int32_t* pos, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if (n < 0 || (n != 0 && (!parent || !mask))) return HSA_ERR_INVALID_ARG;
+  if (n > HSA_MAX_TREE) return HSA_ERR_UNSUPPORTED;
+  if (n == 0) return HSA_OK;
+  TreeMaskParams p{};
+  p.parent = parent;
+  p.count = count;
+  p.first = first;
+  p.mask = mask;
+  p.pos = pos;
+  p.n = n;
+  p.words = (n + 31) / 32;
+  return from_hip(launch_tree_mask(cfg->batch, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t hsa_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max,
+                                    int32_t n_cur_pages) {
+  return tree_ws(cfg, n_q, kv_heads, k_max, n_cur_pages, false);
+}
+
+size_t hsa_cache8_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max,
+                                           int32_t n_cur_pages) {
+  return tree_ws(cfg, n_q, kv_heads, k_max, n_cur_pages, true);
+}
+
+hsa_status_t hsa_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_kv_pool_t* pool,
+                           int32_t kv_heads, const int32_t* sel, int32_t k_max, const int32_t* k_h,
+                           int32_t cur_first_page, int32_t n_cur_pages, const int32_t* kv_len,
+                           const int32_t* q_len, const uint32_t* mask, void* o, float* lse, void* ws,
+                           size_t ws_bytes, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  hsa_cache8_t pages{};
+  if ((st = pool_pages(cfg, pool, kv_heads, pages)) != HSA_OK) return st;
+  return run_tree_attn(cfg, q, n_q, pages, false, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, mask,
+                       o, lse, ws, ws_bytes, stream);
+}
+
+hsa_status_t hsa_cache8_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_cache8_t* cache,
+                                  const int32_t* sel, int32_t k_max, const int32_t* k_h, int32_t cur_first_page,
+                                  int32_t n_cur_pages, const int32_t* kv_len, const int32_t* q_len,
+                                  const uint32_t* mask, void* o, float* lse, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  return run_tree_attn(cfg, q, n_q, *cache, true, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, mask,
+                       o, lse, ws, ws_bytes, stream);
+}
+
+hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* first,
+                            const int32_t* index, int32_t n, const int32_t* count, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  hsa_cache8_t pages{};
+  if ((st = pool_pages(cfg, pool, cfg->num_heads, pages)) != HSA_OK) return st;
+  return run_keep(cfg, pages, false, first, index, n, count, stream);
+}
+
+hsa_status_t hsa_cache8_keep(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* first,
+                             const int32_t* index, int32_t n, const int32_t* count, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  return run_keep(cfg, *cache, true, first, index, n, count, stream);
+}
+
+hsa_status_t hsa_page_copy(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* moves, int32_t n,
+                           void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  hsa_cache8_t pages{};
+  if ((st = pool_pages(cfg, pool, cfg->num_heads, pages)) != HSA_OK) return st;
+  return run_page_copy(cfg, pages, size_of(cfg), moves, n, stream);
+}
+
+hsa_status_t hsa_cache8_page_copy(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* moves, int32_t n,
+                                  void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  return run_page_copy(cfg, *cache, 1, moves, n, stream);
+}
+
+size_t hsa_slots_workspace_size(const hsa_config_t* cfg, int32_t num_slots, int32_t max_pages) {
+  SlotsParams p{};
+  if (check_cfg(cfg) != HSA_OK || check_slots(cfg, num_slots, max_pages, p) != HSA_OK) return 0;
+  return slots_ws(p);
+}
+
+hsa_status_t hsa_slots_take(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* first,
+                            const int32_t* end, int32_t* moves, int32_t* missing, void* ws, size_t ws_bytes,
+                            void* stream) {
+  SlotsParams p{};
+  hsa_status_t st = slots_call(cfg, slots, p);
+  if (st != HSA_OK) return st;
+  if (!end) return HSA_ERR_INVALID_ARG;
+  if (p.B > kSlotsMaxBatch) return HSA_ERR_UNSUPPORTED;
+  if ((st = check_ws(ws, ws_bytes, slots_ws(p))) != HSA_OK) return st;
+  p.first = first;
+  p.end = end;
+  p.moves = moves;
+  p.missing = missing;
+  p.ws = static_cast<int32_t*>(ws);
+  return from_hip(launch_slots_take(p, static_cast<hipStream_t>(stream)));
+}
+
+hsa_status_t hsa_slots_fork(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* parent, void* ws,
+                            size_t ws_bytes, void* stream) {
+  SlotsParams p{};
+  hsa_status_t st = slots_call(cfg, slots, p);
+  if (st != HSA_OK) return st;
+  if (!parent) return HSA_ERR_INVALID_ARG;
+  if ((st = check_ws(ws, ws_bytes, slots_ws(p))) != HSA_OK) return st;
+  p.parent = parent;
+  p.ws = static_cast<int32_t*>(ws);
+  return from_hip(launch_slots_fork(p, static_cast<hipStream_t>(stream)));
+}
+
+hsa_status_t hsa_slots_free(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* keep, void* stream) {
+  SlotsParams p{};
+  hsa_status_t st = slots_call(cfg, slots, p);
+  if (st != HSA_OK) return st;
+  if (!keep) return HSA_ERR_INVALID_ARG;
+  p.end = keep;
+  return from_hip(launch_slots_free(p, static_cast<hipStream_t>(stream)));
+}
+
+hsa_status_t hsa_slots_compact(const hsa_config_t* cfg, const hsa_slots_t* slots, int32_t* moves, int32_t n_moves,
+                               int32_t* table_out, int32_t* refs_out, void* ws, size_t ws_bytes, void* stream) {
+  SlotsParams p{};
+  hsa_status_t st = slots_call(cfg, slots, p);
+  if (st != HSA_OK) return st;
+  if (n_moves < 0 || (n_moves != 0 && !moves)) return HSA_ERR_INVALID_ARG;
+  if (n_moves > 1 << 29) return HSA_ERR_UNSUPPORTED;
+  if ((st = check_ws(ws, ws_bytes, slots_ws(p))) != HSA_OK) return st;
+  p.moves = moves;
+  p.n_moves = n_moves;
+  p.table_out = table_out ? table_out : slots->page_table;
+  p.refs_out = refs_out ? refs_out : slots->refs;
+  p.ws = static_cast<int32_t*>(ws);
+  return from_hip(launch_slots_compact(p, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

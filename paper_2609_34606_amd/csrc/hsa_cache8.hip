@@ -21,13 +21,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxSplit = 256;  // pieces of one item
 
-// D[16x16] += A[16x32] * B[32x16]. Lane l supplies A row (l % 16), k =
-// 8*(l/16)..+8, and B column (l % 16), same k range. Result register r of
-// lane l holds row 4*(l/16) + r, column l % 16.
-__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
-}
-
 // Byte masks that keep the first n (0..16) of 16 codes.
 __device__ __forceinline__ u32x4 keep_codes(u32x4 v, int n) {
 #pragma unroll
@@ -36,35 +29,6 @@ __device__ __forceinline__ u32x4 keep_codes(u32x4 v, int n) {
     v[i] = m == 4 ? v[i] : v[i] & ((1u << (8 * m)) - 1u);
   }
   return v;
-}
-
-// Eight elements of T in kParts bf16 operands whose sum is the element: one for
-// bf16, three for fp32 (3 x 8 significant bits).
-template <typename T, int kParts>
-__device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
-  if constexpr (kParts == 1) {
-    f[0] = ld_global16(p);
-  } else {
-    float x[8];
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[k][i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        x[2 * i] -= bf16_lo(f[k][i]);
-        x[2 * i + 1] -= bf16_hi(f[k][i]);
-      }
-      // an infinity is its first part alone
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? x[i] : 0.f;
-    }
-  }
 }
 
 // Few query rows: 16 kCols rows of one key head against a range of its tokens. A wave takes

@@ -39,6 +39,13 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
+// D[16x16] += A[16x32] * B[32x16]. Lane l supplies A row (l % 16), k =
+// 8*(l/16)..+8, and B column (l % 16), same k range. Result register r of
+// lane l holds row 4*(l/16) + r, column l % 16.
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+
 // ---------------------------------------------------------------- feature map
 // elu(x) + 1
 __device__ __forceinline__ float phi(float x) { return x > 0.f ? x + 1.f : __expf(x); }
@@ -136,5 +143,34 @@ __device__ __forceinline__ int count_selected(const int32_t* row, int k_max, int
 __device__ __forceinline__ float softmax_floor(float c2) { return c2 > 1.f ? -0.5f * FLT_MAX / c2 : -FLT_MAX; }
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Eight elements of T in kParts bf16 operands whose sum is the element: one for
+// bf16, three for fp32 (3 x 8 significant bits).
+template <typename T, int kParts>
+__device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
+  if constexpr (kParts == 1) {
+    f[0] = ld_global16(p);
+  } else {
+    float x[8];
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[k][i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        x[2 * i] -= bf16_lo(f[k][i]);
+        x[2 * i + 1] -= bf16_hi(f[k][i]);
+      }
+      // an infinity is its first part alone
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? x[i] : 0.f;
+    }
+  }
+}
 
 }  // namespace hsa

@@ -257,6 +257,99 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
 int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list);
 hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s);
 
+// ------------------------------------------------------------ drafted trees
+struct TreeMaskParams {
+  const int32_t* parent;      // [B, n]
+  const int32_t* count;       // [B] nullable
+  const int32_t* first;       // [B] nullable
+  uint32_t* mask;             // [B, n, words]
+  int32_t* pos;               // [B, n] nullable
+  int32_t n, words;
+};
+hipError_t launch_tree_mask(int B, const TreeMaskParams& p, hipStream_t s);
+
+constexpr int kTreePages = 512;     // listed pages that a workgroup looks up at once
+constexpr int kTreeMaxSplit = 128;  // pieces of one item
+
+struct TreeAttnParams {
+  const void* q;              // [B, n_q, H, d]
+  const void* k;              // [num_slots, Hk, P, d] numbers or codes
+  const void* v;              // [num_slots, Hk, d, P]
+  const uint8_t* k_exp;       // [num_slots, Hk, nb] (8-bit cache)
+  const uint8_t* v_exp;
+  const int32_t* page_table;  // [B, max_pages]
+  const int32_t* sel;         // [B, Hk, k_max]
+  const int32_t* kv_len;      // [B] nullable
+  const int32_t* q_len;       // [B] nullable
+  const uint32_t* mask;       // [B, n_q, words] nullable
+  void* o;                    // [B, n_q, H, d]
+  float* lse;                 // [B, H, n_q] nullable
+  float* part_o;              // [B, Hk, n_split, part_rows, d] (n_split > 1)
+  float* part_ml;             // [B, Hk, n_split, part_rows, 2] reference maximum and sum
+  int32_t B, H, Hk, G, P, n_q, words, num_slots, max_pages, k_max, cur_first, n_cur;
+  float sm_scale, scale_log2;
+  int16_t k_h[HSA_MAX_HEADS]; // most pages of each key head's sel row
+  // set by plan_tree
+  int32_t nb;                 // scale blocks per page
+  int32_t gpp, gmul;          // granules (8 tokens) per page, 65536 / gpp + 1
+  int32_t rows_per_item, n_rt, part_rows;
+  int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
+};
+
+// Plans the launch for lists of at most `list` pages. Returns rows of partial outputs that a key head
+// needs at most, for this list or a shorter one.
+int64_t plan_tree(TreeAttnParams& p, int dtype, bool eight, int64_t list);
+hipError_t launch_tree_attention(int dtype, int d, bool eight, const TreeAttnParams& p, hipStream_t s);
+
+// ------------------------------------------------------------ kept tokens
+struct TokenKeepParams {
+  void* k;                    // [num_slots, H, P, d] pool keys, or codes
+  void* v;                    // [num_slots, H, d, P]
+  uint8_t* k_exp;             // [num_slots, H, ceil(P / 64)] (8-bit cache)
+  uint8_t* v_exp;
+  const int32_t* page_table;  // [B, max_pages]
+  const int32_t* first;       // [B] nullable
+  const int32_t* index;       // [B, n]
+  const int32_t* count;       // [B] nullable
+  int32_t H, P, n, num_slots, max_pages;
+};
+hipError_t launch_token_keep(int dtype, int d, int B, bool eight, const TokenKeepParams& p, hipStream_t s);
+
+// ------------------------------------------------------------ pages
+struct PageCopyParams {
+  void* k;                    // [num_slots, H, P, d] numbers or codes
+  void* v;                    // [num_slots, H, d, P]
+  uint8_t* k_exp;             // nullable
+  uint8_t* v_exp;
+  const int32_t* moves;       // [n, 3]
+  int32_t H, P, d, size, n, num_slots;  // size: bytes of a number
+};
+int64_t page_copy_parts(const PageCopyParams& p);  // workgroups of a move
+hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s);
+
+struct SlotsParams {
+  int32_t* page_table;        // [B, max_pages]
+  int32_t* refs;              // [num_slots]
+  int32_t B, max_pages, num_slots, P;
+  const int32_t* parent;      // [B] (fork)
+  const int32_t* first;       // [B] nullable (take)
+  const int32_t* end;         // [B] (take; free: the tokens kept)
+  int32_t* moves;             // [B, 3] nullable (take), [n_moves, 3] (compact)
+  int32_t* missing;           // [1] nullable (take)
+  int32_t n_moves;
+  int32_t* table_out;         // (compact)
+  int32_t* refs_out;
+  int32_t* ws;
+};
+constexpr int kSlotsMaxBatch = 8192;
+size_t slots_take_ints(const SlotsParams& p);
+size_t slots_fork_ints(const SlotsParams& p);
+size_t slots_compact_ints(const SlotsParams& p);
+hipError_t launch_slots_take(const SlotsParams& p, hipStream_t s);
+hipError_t launch_slots_fork(const SlotsParams& p, hipStream_t s);
+hipError_t launch_slots_free(const SlotsParams& p, hipStream_t s);
+hipError_t launch_slots_compact(const SlotsParams& p, hipStream_t s);
+
 // ------------------------------------------------------------ attention
 enum AttnMode : int32_t {
   ATTN_FINAL = 0,   // fused linear branch + gated merge, write o (dtype)

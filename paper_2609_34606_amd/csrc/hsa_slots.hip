@@ -1,0 +1,344 @@
+// Page tables on the device: which slots of a pool are free, which are shared, and the copies of pages
+// that follow from it. refs[s] counts the table's entries that hold slot s; 0: free. Everything is whole
+// numbers, and the order of choices is fixed (rows in order, pages in order, the lowest free slot
+// first), so the same tables give the same tables.
+#include "hsa_device.h"
+#include "hsa_kernels.h"
+
+namespace hsa {
+namespace {
+
+constexpr int kPlan = 1024;  // threads of a planning workgroup
+
+// What a workgroup's atomics left in memory (its plain loads may have older copies).
+__device__ __forceinline__ int ld_fresh(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Exclusive sum over the workgroup, in thread order; total: the sum of all. Every thread must call it.
+__device__ __forceinline__ int scan_all(int x, int* buf, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int sum = x;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int y = __shfl_up(sum, m);
+    if (lane >= m) sum += y;
+  }
+  if (lane == 63) buf[wave] = sum;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlan / 64; ++w) {
+    const int y = buf[w];
+    before += w < wave ? y : 0;
+    total += y;
+  }
+  __syncthreads();
+  return before + sum - x;
+}
+
+// The first `most` slots s with test(refs[s]), ascending, in out; returns how many there are (up to
+// `most`). Each thread takes kEach consecutive slots a round.
+template <typename Test>
+__device__ __forceinline__ int list_slots(const int32_t* refs, int lo, int hi, int most, int32_t* out, int* buf, Test test) {
+  constexpr int kEach = 16;
+  int found = 0;
+  for (int s0 = lo; s0 < hi && found < most; s0 += kPlan * kEach) {
+    const int mine = s0 + (int)threadIdx.x * kEach;
+    uint32_t on = 0;
+    int r[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) r[i] = mine + i < hi ? refs[mine + i] : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) on |= (uint32_t)(mine + i < hi && test(r[i])) << i;
+    int total;
+    int at = found + scan_all(__popc(on), buf, total);
+    for (; on; on &= on - 1, ++at)
+      if (at < most) out[at] = mine + __builtin_ctz(on);
+    found += total;
+  }
+  return min(found, most);
+}
+
+// ---------------------------------------------------------------- take
+// Pages of a row that hold its tokens [first, end).
+struct RowPages {
+  int lo, n, inside;  // inside: tokens of the first page before `first`
+};
+__device__ __forceinline__ RowPages row_pages(const SlotsParams& p, int b) {
+  RowPages r;
+  const int first = p.first ? max(p.first[b], 0) : 0, end = p.end[b];
+  r.lo = first / p.P;
+  r.inside = first - r.lo * p.P;
+  const int hi = min((int)(((int64_t)end + p.P - 1) / p.P), p.max_pages);
+  r.n = end > first ? max(hi - r.lo, 0) : 0;
+  return r;
+}
+
+// One workgroup: the wanted entries of all rows are numbered in order; what is shared is counted before
+// anything changes. ws: wanting entries and the last of them for each slot, an entry's rank among those
+// that get a slot, the free slots.
+__global__ __launch_bounds__(kPlan) void slots_take_kernel(SlotsParams p) {
+  __shared__ int starts[kSlotsMaxBatch + 1];  // number of a row's first wanted entry
+  __shared__ int buf[kPlan / 64];
+  const int tid = threadIdx.x;
+  int32_t* wants = p.ws;
+  int32_t* last = wants + p.num_slots;
+  int32_t* ranks = last + p.num_slots;
+  int32_t* free_slots = ranks + (size_t)p.B * p.max_pages;
+  int n = 0;  // wanted entries
+  for (int b0 = 0; b0 < p.B; b0 += kPlan) {
+    int total;
+    const int b = b0 + tid;
+    const int at = n + scan_all(b < p.B ? row_pages(p, b).n : 0, buf, total);
+    if (b < p.B) starts[b] = at;
+    n += total;
+  }
+  if (tid == 0) starts[p.B] = n;
+  __syncthreads();
+  // row and table entry of wanted entry x
+  auto entry = [&](int x, int& b, int& page) {
+    int lo = 0, hi = p.B;  // the last row that starts at or before x
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (starts[mid] <= x) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    page = (p.first ? max(p.first[b], 0) : 0) / p.P + x - starts[b];
+    return (size_t)b * p.max_pages + page;
+  };
+  // whether a slot that an entry holds is held by others too
+  auto shared = [&](int slot) { return slot >= 0 && slot < p.num_slots && p.refs[slot] > 1; };
+  for (int x = tid; x < n; x += kPlan) {
+    int b, page;
+    const int slot = p.page_table[entry(x, b, page)];
+    if (shared(slot)) {
+      wants[slot] = 0;
+      last[slot] = -1;
+    }
+  }
+  __syncthreads();
+  for (int x = tid; x < n; x += kPlan) {
+    int b, page;
+    const int slot = p.page_table[entry(x, b, page)];
+    if (shared(slot)) {
+      atomicAdd(wants + slot, 1);
+      atomicMax(last + slot, x);
+    }
+  }
+  __syncthreads();
+  // An entry needs a slot if it has none, or shares one: but the last of the entries that hold it, if
+  // all of them want it, keeps it.
+  int needs = 0;
+  for (int x0 = 0; x0 < n; x0 += kPlan) {
+    const int x = x0 + tid;
+    bool need = false;
+    if (x < n) {
+      int b, page;
+      const int slot = p.page_table[entry(x, b, page)];
+      need = slot < 0;
+      if (shared(slot)) need = !(ld_fresh(wants + slot) == p.refs[slot] && ld_fresh(last + slot) == x);
+    }
+    int total;
+    const int rank = needs + scan_all(need ? 1 : 0, buf, total);
+    if (x < n) ranks[x] = need ? rank : -1;
+    needs += total;
+  }
+  const int n_free = list_slots(p.refs, 0, p.num_slots, needs, free_slots, buf, [](int r) { return r == 0; });
+  if (p.moves)
+    for (int x = tid; x < 3 * p.B; x += kPlan) p.moves[x] = -1;
+  __syncthreads();
+  for (int x = tid; x < n; x += kPlan) {
+    const int rank = ranks[x];
+    if (rank < 0 || rank >= n_free) continue;
+    int b, page;
+    const size_t at = entry(x, b, page);
+    const int was = p.page_table[at], now = free_slots[rank];
+    p.page_table[at] = now;
+    p.refs[now] = 1;
+    if (was < 0) continue;
+    atomicSub(p.refs + was, 1);
+    const RowPages r = row_pages(p, b);
+    if (p.moves && page == r.lo && r.inside > 0) {
+      p.moves[3 * b] = was;
+      p.moves[3 * b + 1] = now;
+      p.moves[3 * b + 2] = r.inside;
+    }
+  }
+  if (p.missing && tid == 0) *p.missing = needs - n_free;
+}
+
+// ---------------------------------------------------------------- fork, free
+__device__ __forceinline__ int parent_of(const SlotsParams& p, int b) {
+  const int x = p.parent[b];
+  return x >= 0 && x < p.B ? x : b;
+}
+
+// The new rows go to ws first: a row may be the parent of one and the child of another.
+__global__ __launch_bounds__(256) void slots_fork_kernel(SlotsParams p) {
+  const int b = blockIdx.y, page = blockIdx.x * 256 + threadIdx.x;
+  const int from = parent_of(p, b);
+  if (page >= p.max_pages || from == b) return;
+  const int was = p.page_table[(size_t)b * p.max_pages + page], now = p.page_table[(size_t)from * p.max_pages + page];
+  p.ws[(size_t)b * p.max_pages + page] = now;
+  if (was == now) return;
+  if (was >= 0 && was < p.num_slots) atomicSub(p.refs + was, 1);
+  if (now >= 0 && now < p.num_slots) atomicAdd(p.refs + now, 1);
+}
+__global__ __launch_bounds__(256) void slots_forked_kernel(SlotsParams p) {
+  const int b = blockIdx.y, page = blockIdx.x * 256 + threadIdx.x;
+  if (page >= p.max_pages || parent_of(p, b) == b) return;
+  p.page_table[(size_t)b * p.max_pages + page] = p.ws[(size_t)b * p.max_pages + page];
+}
+
+__global__ __launch_bounds__(256) void slots_free_kernel(SlotsParams p) {
+  const int b = blockIdx.y, page = blockIdx.x * 256 + threadIdx.x;
+  const int keep = p.end[b];
+  if (page >= p.max_pages || keep < 0 || (int64_t)page * p.P < keep) return;
+  int32_t* at = p.page_table + (size_t)b * p.max_pages + page;
+  const int slot = *at;
+  if (slot >= 0 && slot < p.num_slots) atomicSub(p.refs + slot, 1);
+  *at = -1;
+}
+
+// ---------------------------------------------------------------- compact
+// One workgroup: the slots in use behind the n-th (n: slots in use), in order, go to the free ones before
+// it, in order. ws: where each slot goes, its count then, the holes, the slots that move.
+__global__ __launch_bounds__(kPlan) void slots_compact_kernel(SlotsParams p) {
+  __shared__ int buf[kPlan / 64];
+  const int tid = threadIdx.x;
+  int32_t* to = p.ws;
+  int32_t* refs = to + p.num_slots;
+  int32_t* holes = refs + p.num_slots;
+  int32_t* movers = holes + p.num_slots;
+  int mine = 0, live;
+  for (int s = tid; s < p.num_slots; s += kPlan) {
+    const int r = p.refs[s];
+    to[s] = s;
+    refs[s] = r;
+    mine += r > 0;
+  }
+  scan_all(mine, buf, live);
+  const int n = list_slots(p.refs, 0, live, p.n_moves, holes, buf, [](int r) { return r <= 0; });
+  list_slots(p.refs, live, p.num_slots, p.n_moves, movers, buf, [](int r) { return r > 0; });
+  __syncthreads();
+  for (int i = tid; i < p.n_moves; i += kPlan) {
+    const bool is = i < n;
+    const int src = is ? movers[i] : -1, dst = is ? holes[i] : -1;
+    p.moves[3 * i] = src;
+    p.moves[3 * i + 1] = dst;
+    p.moves[3 * i + 2] = is ? p.P : -1;
+    if (is) {
+      to[src] = dst;
+      refs[dst] = p.refs[src];
+      refs[src] = 0;
+    }
+  }
+}
+__global__ __launch_bounds__(256) void slots_compacted_kernel(SlotsParams p) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, entries = (int64_t)p.B * p.max_pages;
+  if (x < entries) {
+    const int slot = p.page_table[x];
+    p.table_out[x] = slot >= 0 && slot < p.num_slots ? p.ws[slot] : slot;
+  }
+  if (x < p.num_slots) p.refs_out[x] = p.ws[p.num_slots + x];
+}
+
+// ---------------------------------------------------------------- copies
+constexpr int kCopyBytes = 32768;  // of a workgroup
+
+// Pages slot to slot: moves[i] = {from, to, tokens}. A whole page is one run of bytes for its keys and one for
+// its values; of a part, the rows of its first tokens (up to eight more than asked for, whole granules).
+// Bound: HBM.
+__global__ __launch_bounds__(256) void page_copy_kernel(PageCopyParams p, int parts) {
+  const int move = blockIdx.x / parts, part = blockIdx.x - move * parts, tid = threadIdx.x;
+  const int src = p.moves[3 * move], dst = p.moves[3 * move + 1];
+  const int tokens = (clampi(p.moves[3 * move + 2], 0, p.P) + 7) & ~7;  // (P is a multiple of 8)
+  if (src < 0 || dst < 0 || src >= p.num_slots || dst >= p.num_slots || src == dst || tokens == 0) return;
+  const size_t slot = (size_t)p.H * p.P * p.d * p.size;  // bytes
+  const uint8_t* ks = static_cast<const uint8_t*>(p.k) + src * slot;
+  const uint8_t* vs = static_cast<const uint8_t*>(p.v) + src * slot;
+  uint8_t* kd = static_cast<uint8_t*>(p.k) + dst * slot;
+  uint8_t* vd = static_cast<uint8_t*>(p.v) + dst * slot;
+  const int half = parts / 2;
+  const bool values = part >= half;
+  const int at = values ? part - half : part;
+  const int64_t lo = (int64_t)at * kCopyBytes;
+  if (tokens == p.P) {
+    const int64_t hi = lo + kCopyBytes < (int64_t)slot ? lo + kCopyBytes : (int64_t)slot;
+    const uint8_t* s = values ? vs : ks;
+    uint8_t* d = values ? vd : kd;
+    for (int64_t x = lo + 16 * tid; x < hi; x += 16 * 256) *reinterpret_cast<u32x4*>(d + x) = ld_global16(s + x);
+  } else if (!values) {
+    const int64_t row = (int64_t)tokens * p.d * p.size, all = row * p.H, page = (int64_t)p.P * p.d * p.size;
+    const int64_t hi = lo + kCopyBytes < all ? lo + kCopyBytes : all;
+    for (int64_t x = lo + 16 * tid; x < hi; x += 16 * 256) {
+      const int64_t o = x / row * page + x % row;
+      *reinterpret_cast<u32x4*>(kd + o) = ld_global16(ks + o);
+    }
+  } else {
+    // eight tokens of a value row: 8, 16 or 32 bytes
+    const int64_t row = (int64_t)tokens * p.size, all = row * p.d * p.H, page = (int64_t)p.P * p.size;
+    const int64_t hi = lo + kCopyBytes < all ? lo + kCopyBytes : all;
+    for (int64_t x = lo + 8 * tid; x < hi; x += 8 * 256) {
+      const int64_t o = x / row * page + x % row;
+      *reinterpret_cast<u32x2*>(vd + o) = *reinterpret_cast<const u32x2*>(vs + o);
+    }
+  }
+  if (part == 0 && p.k_exp) {
+    const int nb = (p.P + HSA_CACHE8_BLOCK - 1) / HSA_CACHE8_BLOCK, n = (tokens + HSA_CACHE8_BLOCK - 1) / HSA_CACHE8_BLOCK;
+    for (int x = tid; x < p.H * n; x += 256) {
+      const size_t o = (size_t)(x / n) * nb + x % n, a = (size_t)src * p.H * nb + o, c = (size_t)dst * p.H * nb + o;
+      p.k_exp[c] = p.k_exp[a];
+      p.v_exp[c] = p.v_exp[a];
+    }
+  }
+}
+
+}  // namespace
+
+size_t slots_take_ints(const SlotsParams& p) {
+  const size_t entries = (size_t)p.B * p.max_pages;
+  return 2 * (size_t)p.num_slots + entries + (entries < (size_t)p.num_slots ? entries : (size_t)p.num_slots);
+}
+size_t slots_fork_ints(const SlotsParams& p) { return (size_t)p.B * p.max_pages; }
+size_t slots_compact_ints(const SlotsParams& p) { return 4 * (size_t)p.num_slots; }
+
+hipError_t launch_slots_take(const SlotsParams& p, hipStream_t s) {
+  slots_take_kernel<<<1, kPlan, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_slots_fork(const SlotsParams& p, hipStream_t s) {
+  const dim3 grid((p.max_pages + 255) / 256, p.B);
+  slots_fork_kernel<<<grid, 256, 0, s>>>(p);
+  slots_forked_kernel<<<grid, 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_slots_free(const SlotsParams& p, hipStream_t s) {
+  slots_free_kernel<<<dim3((p.max_pages + 255) / 256, p.B), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_slots_compact(const SlotsParams& p, hipStream_t s) {
+  slots_compact_kernel<<<1, kPlan, 0, s>>>(p);
+  const int64_t entries = (int64_t)p.B * p.max_pages, n = entries > p.num_slots ? entries : p.num_slots;
+  slots_compacted_kernel<<<(uint32_t)((n + 255) / 256), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+int64_t page_copy_parts(const PageCopyParams& p) {
+  const int64_t slot = (int64_t)p.H * p.P * p.d * p.size;
+  return 2 * ((slot + kCopyBytes - 1) / kCopyBytes);
+}
+
+hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s) {
+  const int64_t parts = page_copy_parts(p);
+  page_copy_kernel<<<(uint32_t)(parts * p.n), 256, 0, s>>>(p, (int)parts);
+  return hipGetLastError();
+}
+
+}  // namespace hsa

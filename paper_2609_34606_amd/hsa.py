@@ -53,6 +53,10 @@ class HsaCache8Pool(ctypes.Structure):
                 ("num_slots", c_i32), ("max_pages", c_i32), ("kv_heads", c_i32)]
 
 
+class HsaSlotTable(ctypes.Structure):
+    _fields_ = [("page_table", c_vp), ("refs", c_vp), ("num_slots", c_i32), ("max_pages", c_i32)]
+
+
 class HsaError(RuntimeError):
     def __init__(self, fn: str, status: int):
         super().__init__(f"{fn} failed: {STATUS.get(status, status)}")
@@ -190,6 +194,25 @@ def lib():
     L.hsa_cache8_attn.restype = ctypes.c_int
     L.hsa_cache8_attn.argtypes = [P(HsaConfig), c_vp, c_i32, P(HsaCache8Pool), c_vp, c_i32, c_vp, c_i32,
                                   c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
+    i = ctypes.c_int
+    cfg, tree = P(HsaConfig), [c_vp, c_i32, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    for n, res, args in (
+            ("hsa_tree_mask", i, [c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]),
+            ("hsa_tree_attn_workspace_size", c_sz, [c_i32, c_i32, c_i32, c_i32]),
+            ("hsa_cache8_tree_attn_workspace_size", c_sz, [c_i32, c_i32, c_i32, c_i32]),
+            ("hsa_tree_attn", i, [c_vp, c_i32, P(HsaKvPool), c_i32] + tree),
+            ("hsa_cache8_tree_attn", i, [c_vp, c_i32, P(HsaCache8Pool)] + tree),
+            ("hsa_token_keep", i, [P(HsaKvPool), c_vp, c_vp, c_i32, c_vp, c_vp]),
+            ("hsa_cache8_keep", i, [P(HsaCache8Pool), c_vp, c_vp, c_i32, c_vp, c_vp]),
+            ("hsa_page_copy", i, [P(HsaKvPool), c_vp, c_i32, c_vp]),
+            ("hsa_cache8_page_copy", i, [P(HsaCache8Pool), c_vp, c_i32, c_vp]),
+            ("hsa_slots_workspace_size", c_sz, [c_i32, c_i32]),
+            ("hsa_slots_take", i, [P(HsaSlotTable), c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
+            ("hsa_slots_fork", i, [P(HsaSlotTable), c_vp, c_vp, c_sz, c_vp]),
+            ("hsa_slots_free", i, [P(HsaSlotTable), c_vp, c_vp]),
+            ("hsa_slots_compact", i, [P(HsaSlotTable), c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp])):
+        f = getattr(L, n)
+        f.restype, f.argtypes = res, [cfg] + args
     _lib = L
     return L
 
@@ -697,15 +720,21 @@ def _empty(shape, dtype, device, stream):
         return _torch.empty(shape, dtype=dtype, device=device)
 
 
+def empty_on(shape, dtype, device, stream=None):
+    """An uninitialised tensor that a call on stream writes, to be read on the current stream (once that waits
+    for the call)."""
+    lib()
+    if stream is None or _torch.device(device).type != "cuda":
+        return _torch.empty(shape, dtype=dtype, device=device)
+    t = _empty(shape, dtype, device, stream)
+    t.record_stream(_torch.cuda.current_stream(device))  # not written anew before its reader is done
+    return t
+
+
 def out_like(t, stream=None):
     """A contiguous output of t's shape, type and device for a call on stream, to be read on the
     current stream (once that waits for the call)."""
-    lib()
-    if stream is None or not t.is_cuda:
-        return _torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    o = _empty(t.shape, t.dtype, t.device, stream)
-    o.record_stream(_torch.cuda.current_stream(t.device))  # not written anew before its reader is done
-    return o
+    return empty_on(t.shape, t.dtype, t.device, stream)
 
 
 def hsa_rope_apply(cfg, rope, x, n, o, pos=None, first=None, inverse=False, stream=None,
@@ -775,11 +804,10 @@ def hsa_cache8_attn_plan(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_
     return bool(out[0]), out[1], out[2]
 
 
-def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, kv_len=None,
-                    q_len=None, causal=False, ws=None, stream=None, check=True) -> int:
-    """Attention of q [B, n_q, H, d] over the 8-bit cache's listed pages: sel int32 [B,
-    kv_heads, k_max], then [cur_first_page, + n_cur_pages); tokens below kv_len[b]."""
-    L = lib()
+def _paged_attn(name, fn, size, cfg, q, n_q, pages, kv_heads, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse,
+                kv_len, q_len, how, how_name, ws, stream, check, lead=()) -> int:
+    """What the attention calls over paged tokens share; how: the last argument before the outputs, a
+    flag or (how_name) an int32 tensor or None."""
     B, H, dtype = cfg.batch, cfg.num_heads, _elem(cfg)
     shape = (B, n_q, H, cfg.head_dim)
     for t, what in ((q, "q"), (o, "o")):
@@ -796,16 +824,18 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
             raise _apart("lse", lse)
         lp = lse.data_ptr()
     if k_h is not None:
-        if len(k_h) != cache.kv_heads:
-            raise ValueError(f"k_h must hold {cache.kv_heads} budgets, got {len(k_h)}")
+        if len(k_h) != kv_heads:
+            raise ValueError(f"k_h must hold {kv_heads} budgets, got {len(k_h)}")
         keep = (c_i32 * len(k_h))(*[int(k) for k in k_h])
         kp = ctypes.addressof(keep)
-    sp = None if sel is None else _i32s(sel, B * cache.kv_heads * k_max, dev, "sel")
+    sp = None if sel is None else _i32s(sel, B * kv_heads * k_max, dev, "sel")
     kvp = None if kv_len is None else _i32s(kv_len, B, dev, "kv_len")
     qlp = None if q_len is None else _i32s(q_len, B, dev, "q_len")
-    cp, hp = ctypes.byref(cfg), ctypes.byref(cache)
+    if how_name is not None and how is not None:
+        how = _i32s(how, B * n_q * -(-n_q // 32), dev, how_name)
+    cp, hp = ctypes.byref(cfg), ctypes.byref(pages)
     if ws is None:
-        wp, nbytes = None, L.hsa_cache8_attn_workspace_size(cp, n_q, cache.kv_heads, k_max, n_cur_pages)
+        wp, nbytes = None, size(cp, n_q, kv_heads, k_max, n_cur_pages)
         if nbytes:
             ws = _empty(nbytes, _torch.uint8, q.device, stream if dev >= 0 else None)
             wp = ws.data_ptr()
@@ -813,12 +843,165 @@ def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_p
         if ws.get_device() != dev:
             raise _apart("ws", ws)
         wp, nbytes = _ptr(ws), ws.numel() * ws.element_size()
-    st = _call(L.hsa_cache8_attn, dev, stream, cp, q.data_ptr(), n_q, hp, sp, k_max, kp, cur_first_page, n_cur_pages, kvp,
-               qlp, 1 if causal else 0, o.data_ptr(), lp, wp, nbytes)
+    st = _call(fn, dev, stream, cp, q.data_ptr(), n_q, hp, *lead, sp, k_max, kp, cur_first_page, n_cur_pages, kvp, qlp,
+               how, o.data_ptr(), lp, wp, nbytes)
     del keep
     if check and st:
-        _check("hsa_cache8_attn", st)
+        _check(name, st)
     return st
+
+
+def hsa_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, kv_len=None,
+                    q_len=None, causal=False, ws=None, stream=None, check=True) -> int:
+    """Attention of q [B, n_q, H, d] over the 8-bit cache's listed pages: sel int32 [B,
+    kv_heads, k_max], then [cur_first_page, + n_cur_pages); tokens below kv_len[b]."""
+    L = lib()
+    return _paged_attn("hsa_cache8_attn", L.hsa_cache8_attn, L.hsa_cache8_attn_workspace_size, cfg, q, n_q, cache,
+                       cache.kv_heads, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse, kv_len, q_len,
+                       1 if causal else 0, None, ws, stream, check)
+
+
+# ------------------------------------------------------------------ drafted trees
+def hsa_tree_mask(cfg, parent, n, mask, pos=None, count=None, first=None, stream=None, check=True) -> int:
+    """The ancestors of every node as bits, mask int32 [B, n, ceil(n / 32)], from parent int32 [B, n] (a
+    smaller node, or -1 for a root), and pos int32 [B, n] = first[b] + depth; nodes at or past
+    count[b] are left out."""
+    L = lib()
+    B, dev = cfg.batch, parent.get_device()
+    st = _call(L.hsa_tree_mask, dev, stream, ctypes.byref(cfg), _i32s(parent, B * n, dev, "parent"), n,
+               _i32s(count, B, dev, "count"), _i32s(first, B, dev, "first"),
+               _i32s(mask, B * n * -(-n // 32), dev, "mask"), _i32s(pos, B * n, dev, "pos"))
+    if check and st:
+        _check("hsa_tree_mask", st)
+    return st
+
+
+def hsa_tree_attn_workspace_size(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int) -> int:
+    return lib().hsa_tree_attn_workspace_size(ctypes.byref(cfg), n_q, kv_heads, k_max, n_cur_pages)
+
+
+def hsa_cache8_tree_attn_workspace_size(cfg: HsaConfig, n_q: int, kv_heads: int, k_max: int, n_cur_pages: int) -> int:
+    return lib().hsa_cache8_tree_attn_workspace_size(ctypes.byref(cfg), n_q, kv_heads, k_max, n_cur_pages)
+
+
+def hsa_tree_attn(cfg, q, n_q, pool, kv_heads, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, mask=None,
+                  kv_len=None, q_len=None, ws=None, stream=None, check=True) -> int:
+    """Attention of a step's nodes q [B, n_q, H, d] over the pool's listed pages (kv_heads heads): tokens
+    before kv_len[b] - q_len[b], and of the q_len[b] after them those of the node's mask bits (mask
+    None: those up to the node itself)."""
+    L = lib()
+    return _paged_attn("hsa_tree_attn", L.hsa_tree_attn, L.hsa_tree_attn_workspace_size, cfg, q, n_q, pool, kv_heads,
+                       sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse, kv_len, q_len, mask, "mask", ws, stream,
+                       check, (kv_heads,))
+
+
+def hsa_cache8_tree_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse=None, mask=None,
+                         kv_len=None, q_len=None, ws=None, stream=None, check=True) -> int:
+    """hsa_tree_attn over the 8-bit cache."""
+    L = lib()
+    return _paged_attn("hsa_cache8_tree_attn", L.hsa_cache8_tree_attn, L.hsa_cache8_tree_attn_workspace_size, cfg, q,
+                       n_q, cache, cache.kv_heads, sel, k_max, k_h, cur_first_page, n_cur_pages, o, lse, kv_len,
+                       q_len, mask, "mask", ws, stream, check)
+
+
+def _pages_call(name, fn, cfg, pages, stream, check, *args) -> int:
+    st = _call(fn, args[0].get_device(), stream, ctypes.byref(cfg), ctypes.byref(pages), *args[1:])
+    if check and st:
+        _check(name, st)
+    return st
+
+
+def _keep(name, fn, cfg, pages, first, index, n, count, stream, check) -> int:
+    B, dev = cfg.batch, index.get_device()
+    return _pages_call(name, fn, cfg, pages, stream, check, index, _i32s(first, B, dev, "first"),
+                       _i32s(index, B * n, dev, "index"), n, _i32s(count, B, dev, "count"))
+
+
+def hsa_token_keep(cfg, pool, first, index, n, count=None, stream=None, check=True) -> int:
+    """Token first[b] + i of the pool takes what token first[b] + index[b][i] holds, i < count[b], all
+    read before any is written (index int32 [B, n])."""
+    return _keep("hsa_token_keep", lib().hsa_token_keep, cfg, pool, first, index, n, count, stream, check)
+
+
+def hsa_cache8_keep(cfg, cache, first, index, n, count=None, stream=None, check=True) -> int:
+    """hsa_token_keep in the 8-bit cache."""
+    return _keep("hsa_cache8_keep", lib().hsa_cache8_keep, cfg, cache, first, index, n, count, stream, check)
+
+
+# ------------------------------------------------------------------ pages
+def hsa_page_copy(cfg, pool, moves, n, stream=None, check=True) -> int:
+    """Copies pages between the pool's slots: moves int32 [n, 3], rows {from, to, tokens}."""
+    L = lib()
+    return _pages_call("hsa_page_copy", L.hsa_page_copy, cfg, pool, stream, check, moves,
+                       _i32s(moves, 3 * n, moves.get_device(), "moves"), n)
+
+
+def hsa_cache8_page_copy(cfg, cache, moves, n, stream=None, check=True) -> int:
+    """hsa_page_copy in the 8-bit cache."""
+    L = lib()
+    return _pages_call("hsa_cache8_page_copy", L.hsa_cache8_page_copy, cfg, cache, stream, check, moves,
+                       _i32s(moves, 3 * n, moves.get_device(), "moves"), n)
+
+
+def slot_table(page_table, refs, cfg: HsaConfig) -> HsaSlotTable:
+    """The descriptor of a page table (int32 [B, max_pages]) and its slots' counts (int32 [num_slots])."""
+    if page_table.dim() != 2 or page_table.shape[0] != cfg.batch or str(page_table.dtype) != "torch.int32":
+        raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "
+                         f"{page_table.dtype} {tuple(page_table.shape)}")
+    if refs.dim() != 1 or str(refs.dtype) != "torch.int32":
+        raise ValueError(f"refs must be int32 [num_slots], got {refs.dtype} {tuple(refs.shape)}")
+    return HsaSlotTable(_ptr(page_table), _ptr(refs), int(refs.shape[0]), int(page_table.shape[1]))
+
+
+def hsa_slots_workspace_size(cfg: HsaConfig, num_slots: int, max_pages: int) -> int:
+    return lib().hsa_slots_workspace_size(ctypes.byref(cfg), num_slots, max_pages)
+
+
+def _slots_ws(cfg, slots, ws, like, stream):
+    """Address and size of the workspace of a slot call (one of its own where ws is None), and its tensor."""
+    if ws is None:
+        n = hsa_slots_workspace_size(cfg, slots.num_slots, slots.max_pages)
+        ws = _empty(n, _torch.uint8, like.device, stream if like.is_cuda else None)
+    elif ws.get_device() != like.get_device():
+        raise _apart("ws", ws)
+    return _ptr(ws), ws.numel() * ws.element_size(), ws
+
+
+def hsa_slots_take(cfg, slots, first, end, moves=None, missing=None, ws=None, stream=None, check=True) -> int:
+    """Makes the pages of tokens [first[b], end[b]) the rows' own; moves int32 [B, 3] for hsa_page_copy,
+    missing int32 [1]: entries that found no free slot."""
+    L = lib()
+    B, dev = cfg.batch, end.get_device()
+    f, e = _i32s(first, B, dev, "first"), _i32s(end, B, dev, "end")
+    m, x = _i32s(moves, 3 * B, dev, "moves"), _i32s(missing, 1, dev, "missing")
+    wp, nbytes, ws = _slots_ws(cfg, slots, ws, end, stream)
+    return _pages_call("hsa_slots_take", L.hsa_slots_take, cfg, slots, stream, check, end, f, e, m, x, wp, nbytes)
+
+
+def hsa_slots_fork(cfg, slots, parent, ws=None, stream=None, check=True) -> int:
+    """Row b of the page table becomes what row parent[b] was, sharing its slots."""
+    L = lib()
+    at = _i32s(parent, cfg.batch, parent.get_device(), "parent")
+    wp, nbytes, ws = _slots_ws(cfg, slots, ws, parent, stream)
+    return _pages_call("hsa_slots_fork", L.hsa_slots_fork, cfg, slots, stream, check, parent, at, wp, nbytes)
+
+
+def hsa_slots_free(cfg, slots, keep, stream=None, check=True) -> int:
+    """Row b lets go of its pages behind its first keep[b] tokens."""
+    return _pages_call("hsa_slots_free", lib().hsa_slots_free, cfg, slots, stream, check, keep,
+                       _i32s(keep, cfg.batch, keep.get_device(), "keep"))
+
+
+def hsa_slots_compact(cfg, slots, moves, n_moves, table_out=None, refs_out=None, ws=None, stream=None,
+                      check=True) -> int:
+    """Moves the slots in use to the front of the pool (moves int32 [n_moves, 3] for hsa_page_copy)."""
+    L = lib()
+    dev = moves.get_device()
+    m = _i32s(moves, 3 * n_moves, dev, "moves")
+    t = _i32s(table_out, cfg.batch * slots.max_pages, dev, "table_out")
+    r = _i32s(refs_out, slots.num_slots, dev, "refs_out")
+    wp, nbytes, ws = _slots_ws(cfg, slots, ws, moves, stream)
+    return _pages_call("hsa_slots_compact", L.hsa_slots_compact, cfg, slots, stream, check, moves, m, n_moves, t, r, wp, nbytes)
 
 
 class HsaTier:

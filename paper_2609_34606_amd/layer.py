@@ -86,6 +86,39 @@ class HsaLayer:
         _h.hsa_token_write(self.cfg, self.pool, k, v, k.shape[1], first=first, count=count, rope=rope, pos=pos,
                            stream=stream)
 
+    def attend_tree(self, q, n_pages: int, mask=None, first_page: int = 0, sel=None,
+                    k_h: Optional[Sequence[int]] = None, kv_len=None, q_len=None, out=None, lse=None, stream=None):
+        """Attention of a step's nodes q [B, n_q, heads, d] (heads: the layer's, or a multiple) over the
+        selected pages (sel int32 [B, H, k_max], at most k_h of each head) and pages [first_page, + n_pages):
+        tokens before kv_len[b] - q_len[b], and those of the node's mask bits after (hsa_tree_mask; None: up
+        to the node itself, as for a single token)."""
+        _same_device(q, self.k_pool)
+        heads = self.cfg.num_heads
+        cfg = self.cfg if q.shape[2] == heads else _h.HsaConfig(self.cfg.batch, q.shape[2], self.cfg.head_dim,
+                                                                self.cfg.page_size, self.cfg.dtype,
+                                                                self.cfg.sm_scale, 0)
+        if out is None:
+            out = _h.out_like(q, stream)
+        _h.hsa_tree_attn(cfg, q, q.shape[1], self.pool, heads, sel, 0 if sel is None else int(sel.shape[-1]), k_h,
+                         first_page, n_pages, out, lse=lse, mask=mask, kv_len=kv_len, q_len=q_len, stream=stream)
+        return out
+
+    def keep_tokens(self, first, index, count=None, stream=None):
+        """Token first[b] + i takes what token first[b] + index[b][i] holds, i < count[b] (index int32
+        [B, n]): the accepted path of a tree becomes the sequence's next tokens."""
+        _same_device(index, self.k_pool)
+        _h.hsa_token_keep(self.cfg, self.pool, first, index, index.shape[1], count=count, stream=stream)
+
+    def copy_pages(self, moves, stream=None):
+        """Copies pages between slots (moves int32 [n, 3] of HsaSlots), compressed pages as well."""
+        _same_device(moves, self.k_pool)
+        _h.hsa_page_copy(self.cfg, self.pool, moves, moves.shape[0], stream=stream)
+        if getattr(self, "ck", None) is not None:
+            c = self.cfg
+            whole = _h.HsaConfig(c.batch, c.num_heads, c.head_dim, self.rank, c.dtype, c.sm_scale, 0)
+            _h.hsa_page_copy(whole, _h.kv_pool(self.ck, self.cv, self.page_table), moves, moves.shape[0],
+                             stream=stream)
+
     def forward(self, q, n_cand: int, n_cur: int, k_h: Sequence[int], k_max: Optional[int] = None,
                 g_lin=None, g_sp=None, out=None, sel_out=None, stream=None):
         B, n_q = q.shape[0], q.shape[1]
@@ -244,3 +277,78 @@ class HsaCache8:
                            first_page, n_pages, out, lse=lse, kv_len=kv_len, q_len=q_len, causal=causal,
                            stream=stream)
         return out
+
+    def attend_tree(self, q, n_pages: int, mask=None, first_page: int = 0, sel=None,
+                    k_h: Optional[Sequence[int]] = None, kv_len=None, q_len=None, out=None, lse=None, stream=None):
+        """Attention of a step's nodes q [B, n_q, heads, d] over the selected pages and pages [first_page, +
+        n_pages): tokens before kv_len[b] - q_len[b], and those of the node's mask bits after
+        (hsa_tree_mask; None: up to the node itself)."""
+        _same_device(q, self.k)
+        if out is None:
+            out = _h.out_like(q, stream)
+        _h.hsa_cache8_tree_attn(self.cfg, q, q.shape[1], self.pool, sel, 0 if sel is None else int(sel.shape[-1]), k_h,
+                                first_page, n_pages, out, lse=lse, mask=mask, kv_len=kv_len, q_len=q_len,
+                                stream=stream)
+        return out
+
+    def keep_tokens(self, first, index, count=None, stream=None):
+        """Token first[b] + i takes what token first[b] + index[b][i] holds, i < count[b] (index int32
+        [B, n]), as ``write`` appends its numbers."""
+        _same_device(index, self.k)
+        _h.hsa_cache8_keep(self.cfg, self.pool, first, index, index.shape[1], count=count, stream=stream)
+
+    def copy_pages(self, moves, stream=None):
+        """Copies pages between slots (moves int32 [n, 3] of HsaSlots)."""
+        _same_device(moves, self.k)
+        _h.hsa_cache8_page_copy(self.cfg, self.pool, moves, moves.shape[0], stream=stream)
+
+
+class HsaSlots:
+    """A page table [B, max_pages] whose rows may share slots, and the count of its entries that hold each
+    slot, refs [num_slots], on the device (tensors not given are made, with no page and every slot
+    free). Layers and caches that are given its page_table follow it; their ``copy_pages`` carries out the
+    moves. missing int32 [1]: the entries that found no free slot in the last ``take``.
+    """
+
+    def __init__(self, batch: int, page_size: int, device, num_slots: int = 0, max_pages: int = 0, page_table=None,
+                 refs=None, missing=None):
+        import torch
+        self.torch = torch
+        i32 = dict(dtype=torch.int32, device=device)
+        if (page_table is None) != (refs is None):
+            raise ValueError("a page table and its slots' counts are given together")
+        if page_table is None:
+            page_table, refs = torch.full((batch, max_pages), -1, **i32), torch.zeros(num_slots, **i32)
+        self.page_table, self.refs = page_table, refs
+        self.missing = torch.zeros(1, **i32) if missing is None else missing
+        if len({t.device for t in (self.page_table, self.refs, self.missing)}) > 1:
+            raise ValueError("the table's tensors must be on one device")
+        self.cfg = _h.config(batch, 1, 64, page_size, _h.HSA_DTYPE_BF16)
+        self.table = _h.slot_table(page_table, refs, self.cfg)
+
+    def take(self, first, end, moves=None, stream=None):
+        """Makes the pages that hold tokens [first[b], end[b]) of each row (int32 [B]) its own before they are
+        written; returns the moves (int32 [B, 3]) that carry over what a shared first page holds."""
+        _same_device(end, self.refs)
+        if moves is None:
+            moves = _h.empty_on((self.cfg.batch, 3), self.torch.int32, end.device, stream)
+        _h.hsa_slots_take(self.cfg, self.table, first, end, moves=moves, missing=self.missing, stream=stream)
+        return moves
+
+    def fork(self, parent, stream=None):
+        """Row b becomes what row parent[b] (int32 [B]; outside [0, B): itself) was, sharing its slots."""
+        _same_device(parent, self.refs)
+        _h.hsa_slots_fork(self.cfg, self.table, parent, stream=stream)
+
+    def free(self, keep, stream=None):
+        """Row b lets go of its pages behind its first keep[b] tokens (int32 [B]; 0: all, below 0: none)."""
+        _same_device(keep, self.refs)
+        _h.hsa_slots_free(self.cfg, self.table, keep, stream=stream)
+
+    def compact(self, moves, table_out=None, refs_out=None, stream=None):
+        """Moves the slots in use to the front of the pool, at most as many as moves (int32 [n, 3]) has rows; the
+        new table and counts go to table_out and refs_out, or in place."""
+        _same_device(moves, self.refs)
+        _h.hsa_slots_compact(self.cfg, self.table, moves, moves.shape[0], table_out=table_out, refs_out=refs_out,
+                             stream=stream)
+        return moves
