@@ -1316,7 +1316,8 @@ hsa_status_t run_token_write(const hsa_config_t* cfg, TokenWriteParams& p, const
 
 // The parts of an attention call's parameters that its plan follows from.
 hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_most,
-                              int32_t n_cur_pages, bool ragged, Cache8AttnParams& p) {
+                              int32_t n_cur_pages, bool ragged, bool tree, Cache8AttnParams& p) {
+  p.tree = tree;
   p.H = cfg->num_heads;
   p.Hk = kv_heads;
   p.G = cfg->num_heads / kv_heads;
@@ -1334,10 +1335,76 @@ hsa_status_t plan_cache8_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_h
 
 // Outputs, maxima and sums of the pieces of any call of these sizes with up to `list` pages: not
 // those of this list's plan, which cuts some longer lists into fewer pieces than shorter ones.
-size_t cache8_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int64_t list) {
+size_t cache8_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int64_t list, bool tree) {
   const int64_t rows = (int64_t)n_q * (cfg->num_heads / kv_heads);
-  const int64_t parts = cache8_most_part_rows(cfg->dtype, cfg->head_dim, cfg->page_size, cfg->batch, kv_heads, rows, list);
+  const int64_t parts = cache8_most_part_rows(cfg->dtype, cfg->head_dim, cfg->page_size, cfg->batch, kv_heads, rows, list, tree);
   return align_up((size_t)(parts * cfg->batch * kv_heads * (cfg->head_dim + 2)) * 4);
+}
+
+size_t cache8_ws_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur_pages,
+                      bool tree) {
+  if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return 0;
+  if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return 0;
+  Cache8AttnParams p{};
+  for (const bool ragged : {false, true})
+    if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged, tree, p) != HSA_OK) return 0;
+  return cache8_ws(cfg, n_q, kv_heads, (int64_t)k_max + n_cur_pages, tree);
+}
+
+// The attention calls over the 8-bit cache: tokens up to each query's own (causal), all of them, or those of a
+// drafted tree's mask (tree).
+hsa_status_t run_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q,
+                             const hsa_cache8_t* cache, const int32_t* sel, int32_t k_max,
+                             const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
+                             const int32_t* kv_len, const int32_t* q_len, int32_t causal,
+                             bool tree, const uint32_t* mask, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  hsa_status_t st = check_cfg(cfg);
+  if (st != HSA_OK) return st;
+  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
+  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
+  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
+  if (k_h)
+    for (int h = 0; h < cache->kv_heads; ++h)
+      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)cur_first_page + n_cur_pages > cache->max_pages) return HSA_ERR_OUT_OF_RANGE;
+  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
+  if ((st = check_table(cfg, cache->max_pages)) != HSA_OK) return st;
+  if (tree && (n_q > HSA_MAX_TREE || ((int64_t)k_max + n_cur_pages) * cfg->page_size >= (1LL << 31) - 256))
+    return HSA_ERR_UNSUPPORTED;
+  if (n_q == 0) return HSA_OK;
+  Cache8AttnParams p{};
+  if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, kv_len != nullptr, tree, p)) != HSA_OK)
+    return st;
+  const size_t need = cache8_ws(cfg, n_q, cache->kv_heads, (int64_t)k_max + n_cur_pages, tree);
+  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_cache8(cfg, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK)
+    return st;
+  p.q = q;
+  p.k = static_cast<const uint8_t*>(cache->k);
+  p.v = static_cast<const uint8_t*>(cache->v);
+  p.k_exp = static_cast<const uint8_t*>(cache->k_exp);
+  p.v_exp = static_cast<const uint8_t*>(cache->v_exp);
+  p.page_table = cache->page_table;
+  p.sel = sel;
+  p.kv_len = kv_len;
+  p.q_len = q_len;
+  p.o = o;
+  p.lse = lse;
+  p.num_slots = cache->num_slots;
+  p.max_pages = cache->max_pages;
+  p.k_max = k_max;
+  p.cur_first = cur_first_page;
+  p.causal = causal != 0;
+  p.mask = mask;
+  p.words = (n_q + 31) / 32;
+  p.sm_scale = softmax_scale(cfg);
+  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
+  for (int h = 0; h < cache->kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * p.d;
+  return from_hip(launch_cache8_attention(cfg->dtype, cfg->head_dim, cfg->batch, p, s));
 }
 
 // With HSA_CHECK=1: as validate_tokens, and the page of every token of the table that is read must map to
@@ -1365,9 +1432,8 @@ hsa_status_t validate_kept(const hsa_config_t* c, const int32_t* page_table, int
   return HSA_OK;
 }
 
-// What the calls of a drafted tree over either cache share.
 hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur,
-                            bool eight, TreeAttnParams& p, size_t& ws) {
+                            TreeAttnParams& p, size_t& ws) {
   if (n_q > HSA_MAX_TREE || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
   if (((int64_t)k_max + n_cur) * cfg->page_size >= (1LL << 31) - 256) return HSA_ERR_UNSUPPORTED;
   p.B = cfg->batch;
@@ -1379,64 +1445,19 @@ hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_hea
   p.words = (n_q + 31) / 32;
   p.k_max = k_max;
   p.n_cur = n_cur;
-  const int64_t parts = plan_tree(p, cfg->dtype, eight, (int64_t)k_max + n_cur);
+  const int64_t parts = plan_tree(p, cfg->dtype, (int64_t)k_max + n_cur);
   const int64_t heads = (int64_t)cfg->batch * kv_heads;
   if (heads * p.n_split * p.n_rt + 8 * p.n_rt > kMaxGrid || heads * p.part_rows > kMaxGrid) return HSA_ERR_UNSUPPORTED;
   ws = parts > p.part_rows ? align_up((size_t)(parts * heads * (cfg->head_dim + 2)) * 4) : 0;
   return HSA_OK;
 }
 
-size_t tree_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur, bool eight) {
+size_t tree_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur) {
   if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur < 0) return 0;
   if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur < 1) return 0;
   TreeAttnParams p{};
   size_t ws = 0;
-  return plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur, eight, p, ws) == HSA_OK ? ws : 0;
-}
-
-// cache: the descriptor of either cache's pages (of the pool: without exponent bytes).
-hsa_status_t run_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_cache8_t& cache, bool eight,
-                           const int32_t* sel, int32_t k_max, const int32_t* k_h, int32_t cur_first, int32_t n_cur,
-                           const int32_t* kv_len, const int32_t* q_len, const uint32_t* mask, void* o, float* lse,
-                           void* ws, size_t ws_bytes, void* stream) {
-  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first < 0 || n_cur < 0) return HSA_ERR_INVALID_ARG;
-  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
-  if ((int64_t)k_max + n_cur < 1) return HSA_ERR_INVALID_ARG;
-  if (k_h)
-    for (int h = 0; h < cache.kv_heads; ++h)
-      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
-  if ((int64_t)cur_first + n_cur > cache.max_pages) return HSA_ERR_OUT_OF_RANGE;
-  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
-  hsa_status_t st = check_table(cfg, cache.max_pages);
-  if (st != HSA_OK) return st;
-  if (n_q == 0) return HSA_OK;
-  TreeAttnParams p{};
-  size_t need = 0;
-  if ((st = plan_tree_call(cfg, n_q, cache.kv_heads, k_max, n_cur, eight, p, need)) != HSA_OK) return st;
-  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = validate_cache8(cfg, &cache, sel, k_max, k_h, cur_first, n_cur, kv_len, s)) != HSA_OK) return st;
-  p.q = q;
-  p.k = cache.k;
-  p.v = cache.v;
-  p.k_exp = static_cast<const uint8_t*>(cache.k_exp);
-  p.v_exp = static_cast<const uint8_t*>(cache.v_exp);
-  p.page_table = cache.page_table;
-  p.sel = sel;
-  p.kv_len = kv_len;
-  p.q_len = q_len;
-  p.mask = mask;
-  p.o = o;
-  p.lse = lse;
-  p.num_slots = cache.num_slots;
-  p.max_pages = cache.max_pages;
-  p.cur_first = cur_first;
-  p.sm_scale = softmax_scale(cfg);
-  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
-  for (int h = 0; h < cache.kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
-  p.part_o = static_cast<float*>(ws);
-  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * cfg->head_dim;
-  return from_hip(launch_tree_attention(cfg->dtype, cfg->head_dim, eight, p, s));
+  return plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur, p, ws) == HSA_OK ? ws : 0;
 }
 
 // The pool's pages as the descriptor that the calls over either cache take.
@@ -1607,12 +1628,7 @@ hsa_status_t hsa_cache8_write(const hsa_config_t* cfg, const hsa_cache8_t* cache
 
 size_t hsa_cache8_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
                                       int32_t k_max, int32_t n_cur_pages) {
-  if (check_cfg(cfg) != HSA_OK || n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return 0;
-  if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return 0;
-  Cache8AttnParams p{};
-  for (const bool ragged : {false, true})
-    if (plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged, p) != HSA_OK) return 0;
-  return cache8_ws(cfg, n_q, kv_heads, (int64_t)k_max + n_cur_pages);
+  return cache8_ws_size(cfg, n_q, kv_heads, k_max, n_cur_pages, false);
 }
 
 hsa_status_t hsa_cache8_attn_plan(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads,
@@ -1623,7 +1639,7 @@ hsa_status_t hsa_cache8_attn_plan(const hsa_config_t* cfg, int32_t n_q, int32_t 
   if (n_q < 1 || kv_heads < 1 || k_max < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
   if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
   Cache8AttnParams p{};
-  if ((st = plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged != 0, p)) != HSA_OK) return st;
+  if ((st = plan_cache8_call(cfg, n_q, kv_heads, k_max, n_cur_pages, ragged != 0, false, p)) != HSA_OK) return st;
   if (many_rows) *many_rows = p.many;
   if (rows_per_item) *rows_per_item = p.rows_per_item;
   if (n_pieces) *n_pieces = p.n_split;
@@ -1635,49 +1651,8 @@ hsa_status_t hsa_cache8_attn(const hsa_config_t* cfg, const void* q, int32_t n_q
                              const int32_t* k_h, int32_t cur_first_page, int32_t n_cur_pages,
                              const int32_t* kv_len, const int32_t* q_len, int32_t causal,
                              void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
-  hsa_status_t st = check_cfg(cfg);
-  if (st != HSA_OK) return st;
-  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
-  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
-  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
-  if ((int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
-  if (k_h)
-    for (int h = 0; h < cache->kv_heads; ++h)
-      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
-  if ((int64_t)cur_first_page + n_cur_pages > cache->max_pages) return HSA_ERR_OUT_OF_RANGE;
-  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
-  if ((st = check_table(cfg, cache->max_pages)) != HSA_OK) return st;
-  if (n_q == 0) return HSA_OK;
-  Cache8AttnParams p{};
-  if ((st = plan_cache8_call(cfg, n_q, cache->kv_heads, k_max, n_cur_pages, kv_len != nullptr, p)) != HSA_OK)
-    return st;
-  const size_t need = cache8_ws(cfg, n_q, cache->kv_heads, (int64_t)k_max + n_cur_pages);
-  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if ((st = validate_cache8(cfg, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK)
-    return st;
-  p.q = q;
-  p.k = static_cast<const uint8_t*>(cache->k);
-  p.v = static_cast<const uint8_t*>(cache->v);
-  p.k_exp = static_cast<const uint8_t*>(cache->k_exp);
-  p.v_exp = static_cast<const uint8_t*>(cache->v_exp);
-  p.page_table = cache->page_table;
-  p.sel = sel;
-  p.kv_len = kv_len;
-  p.q_len = q_len;
-  p.o = o;
-  p.lse = lse;
-  p.num_slots = cache->num_slots;
-  p.max_pages = cache->max_pages;
-  p.k_max = k_max;
-  p.cur_first = cur_first_page;
-  p.causal = causal != 0;
-  p.sm_scale = softmax_scale(cfg);
-  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
-  for (int h = 0; h < cache->kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
-  p.part_o = static_cast<float*>(ws);
-  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * p.d;
-  return from_hip(launch_cache8_attention(cfg->dtype, cfg->head_dim, cfg->batch, p, s));
+  return run_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, causal,
+                         false, nullptr, o, lse, ws, ws_bytes, stream);
 }
 
 hsa_status_t hsa_tree_mask(const hsa_config_t* cfg, const int32_t* parent, int32_t n, const int32_t* count,
@@ -1700,12 +1675,12 @@ hsa_status_t hsa_tree_mask(const hsa_config_t* cfg, const int32_t* parent, int32
 
 size_t hsa_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max,
                                     int32_t n_cur_pages) {
-  return tree_ws(cfg, n_q, kv_heads, k_max, n_cur_pages, false);
+  return tree_ws(cfg, n_q, kv_heads, k_max, n_cur_pages);
 }
 
 size_t hsa_cache8_tree_attn_workspace_size(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max,
                                            int32_t n_cur_pages) {
-  return tree_ws(cfg, n_q, kv_heads, k_max, n_cur_pages, true);
+  return n_q > HSA_MAX_TREE ? 0 : cache8_ws_size(cfg, n_q, kv_heads, k_max, n_cur_pages, true);
 }
 
 hsa_status_t hsa_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_kv_pool_t* pool,
@@ -1717,8 +1692,41 @@ hsa_status_t hsa_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, 
   if (st != HSA_OK) return st;
   hsa_cache8_t pages{};
   if ((st = pool_pages(cfg, pool, kv_heads, pages)) != HSA_OK) return st;
-  return run_tree_attn(cfg, q, n_q, pages, false, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, mask,
-                       o, lse, ws, ws_bytes, stream);
+  if ((n_q != 0 && (!q || !o)) || n_q < 0 || k_max < 0 || cur_first_page < 0 || n_cur_pages < 0) return HSA_ERR_INVALID_ARG;
+  if (k_max > 0 && !sel) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)k_max + n_cur_pages < 1) return HSA_ERR_INVALID_ARG;
+  if (k_h)
+    for (int h = 0; h < kv_heads; ++h)
+      if (k_h[h] < 0 || k_h[h] > k_max) return HSA_ERR_INVALID_ARG;
+  if ((int64_t)cur_first_page + n_cur_pages > pool->max_pages) return HSA_ERR_OUT_OF_RANGE;
+  if (k_max > HSA_MAX_LIST || !aligned16(q) || !aligned16(o)) return HSA_ERR_UNSUPPORTED;
+  if ((st = check_table(cfg, pool->max_pages)) != HSA_OK) return st;
+  if (n_q == 0) return HSA_OK;
+  TreeAttnParams p{};
+  size_t need = 0;
+  if ((st = plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur_pages, p, need)) != HSA_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = validate_cache8(cfg, &pages, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK) return st;
+  p.q = q;
+  p.k = pool->k;
+  p.v = pool->v;
+  p.page_table = pool->page_table;
+  p.sel = sel;
+  p.kv_len = kv_len;
+  p.q_len = q_len;
+  p.mask = mask;
+  p.o = o;
+  p.lse = lse;
+  p.num_slots = pool->num_slots;
+  p.max_pages = pool->max_pages;
+  p.cur_first = cur_first_page;
+  p.sm_scale = softmax_scale(cfg);
+  p.scale_log2 = p.sm_scale * 1.4426950408889634f;
+  for (int h = 0; h < kv_heads; ++h) p.k_h[h] = (int16_t)(k_h ? k_h[h] : k_max);
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = p.part_o + (size_t)cfg->batch * p.Hk * p.n_split * p.part_rows * cfg->head_dim;
+  return from_hip(launch_tree_attention(cfg->dtype, cfg->head_dim, p, s));
 }
 
 hsa_status_t hsa_cache8_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, const hsa_cache8_t* cache,
@@ -1726,11 +1734,8 @@ hsa_status_t hsa_cache8_tree_attn(const hsa_config_t* cfg, const void* q, int32_
                                   int32_t n_cur_pages, const int32_t* kv_len, const int32_t* q_len,
                                   const uint32_t* mask, void* o, float* lse, void* ws, size_t ws_bytes,
                                   void* stream) {
-  hsa_status_t st = check_cfg(cfg);
-  if (st != HSA_OK) return st;
-  if ((st = check_cache8(cfg, cache)) != HSA_OK) return st;
-  return run_tree_attn(cfg, q, n_q, *cache, true, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, mask,
-                       o, lse, ws, ws_bytes, stream);
+  return run_cache8_attn(cfg, q, n_q, cache, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, q_len, 0, true,
+                         mask, o, lse, ws, ws_bytes, stream);
 }
 
 hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* first,

@@ -33,7 +33,7 @@ __device__ __forceinline__ Cache8Walk cache8_walk(const Cache8AttnParams& p, int
   Cache8Walk w;
   const int cap = p.max_pages * p.P;
   const int end = (p.cur_first + p.n_cur) * p.P;
-  w.len = p.kv_len ? clampi(ld_const(p.kv_len + b), 0, cap) : (p.causal ? end : cap);
+  w.len = p.kv_len ? clampi(ld_const(p.kv_len + b), 0, cap) : (p.causal || p.tree ? end : cap);
   w.q_len = p.q_len ? clampi(ld_const(p.q_len + b), 0, p.n_q) : p.n_q;
   w.base = w.len - w.q_len;
   const int last = min(row0 + rows, w.q_len * p.G);  // row past the last one

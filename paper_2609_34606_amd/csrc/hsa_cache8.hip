@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "hsa_cache8.h"
+#include "hsa_tree.h"
 
 namespace hsa {
 namespace {
@@ -29,6 +30,22 @@ __device__ __forceinline__ u32x4 keep_codes(u32x4 v, int n) {
     v[i] = m == 4 ? v[i] : v[i] & ((1u << (8 * m)) - 1u);
   }
   return v;
+}
+
+// Eight codes of which the tokens that are not in `in_len` become 0, and those of `nodes` that are no finite numbers
+// (a code above 2^8 at the largest scale, 2^120, is none), whose bits are returned.
+__device__ __forceinline__ uint32_t clean_codes(uint32_t& lo, uint32_t& hi, uint32_t in_len, uint32_t nodes, uint32_t exp) {
+  const uint32_t over = exp >= 120 + 127 ? 0x08080808u : 0x01010101u;
+  const uint32_t bad0 = ((lo & 0x7f7f7f7fu) + over) & bytes4(nodes), bad1 = ((hi & 0x7f7f7f7fu) + over) & bytes4(nodes >> 4);
+  lo &= fill8(bytes4(in_len)) & ~fill8(bad0);
+  hi &= fill8(bytes4(in_len >> 4)) & ~fill8(bad1);
+  return bad0 | bad1;
+}
+// Bits of a granule's tokens t0 .. t0 + 7 below `end`.
+__device__ __forceinline__ uint32_t below(int t0, int end) { return low_bits(clampi(end - min(t0, end), 0, 8)); }
+// A code as a number, as the matrix operand has it.
+__device__ __forceinline__ float code_value(const Cache8AttnParams& p, size_t head, size_t at, int off) {
+  return bf16_lo(codes_to_bf16(p.v[at], 0, scale_of(p.v_exp[head * p.nb + (off >> 6)]))[0]);
 }
 
 // Few query rows: 16 kCols rows of one key head against a range of its tokens. A wave takes
@@ -49,7 +66,8 @@ __device__ __forceinline__ u32x4 keep_codes(u32x4 v, int n) {
 // A kernel that only reads a cache in this pattern takes 115 to 126 us for the latter: value
 // rows of pages of 1560 tokens begin at any multiple of 8 bytes (a copy's reads: 6.1 TB/s). For short
 // lists, latency: 3.2 us a tile that a wave does after another, 9 us for a whole call of one.
-template <typename T, int D, int kCols, int kParts, bool kStream, int kWaves>
+// kTree: the queries are a drafted tree's nodes, and each sees the tokens before them and those of its mask.
+template <typename T, int D, int kCols, int kParts, bool kStream, int kWaves, bool kTree>
 __global__ __launch_bounds__(64 * kWaves, kCols == 1 && kParts == 1 && kWaves == 4 && !kStream ? 3 : 1)
 void few_rows_kernel(Cache8AttnParams p) {
   constexpr int C = D / 64;   // 64-dim groups of a key row
@@ -62,6 +80,7 @@ void few_rows_kernel(Cache8AttnParams p) {
   constexpr int OS = D + 4;   // floats per row of the join buffer
   __shared__ __attribute__((aligned(16))) float osm[kWaves * 16 * OS];
   __shared__ float msm[kWaves][kRows], lsm[kWaves][kRows];
+  __shared__ uint32_t bits[kTree ? kRows : 1][kMaskWords + 1];  // mask rows of the item's nodes
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Workgroup i runs on XCD i % 8. Pieces of one sequence and head come n_items apart, and
@@ -83,14 +102,23 @@ void few_rows_kernel(Cache8AttnParams p) {
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
     const int r = rt * kRows + 16 * n + c16, i = min(r / p.G, w.q_len - 1);
-    lim[n] = cache8_limit(p, w, i);
+    lim[n] = kTree ? i : cache8_limit(p, w, i);  // (a tree: the column's node)
     const T* q = static_cast<const T*>(p.q) + (((size_t)b * p.n_q + i) * p.H + h * p.G + r % p.G) * D;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int u = 0; u < 2; ++u) split_row<T, kParts>(q + 64 * c + 16 * g + 8 * u, qf[n][c][u]);
   }
-  const int lim_first = cache8_limit(p, w, __builtin_amdgcn_readfirstlane(rt * kRows / p.G));  // the least of them
+  const int i0 = __builtin_amdgcn_readfirstlane(rt * kRows / p.G);
+  const int lim_first = kTree ? w.base : cache8_limit(p, w, i0);  // the least of them
+  uint32_t wild = 0;  // whether a node's value is no finite number
+  if (kTree && p.mask) {
+    const int nodes = min((rt * kRows + kRows - 1) / p.G, w.q_len - 1) - i0 + 1;
+    const uint32_t* src = p.mask + ((size_t)b * p.n_q + i0) * p.words;
+    for (int x = tid; x < nodes * p.words; x += 64 * kWaves) bits[x / p.words][x % p.words] = src[x];
+  }
+  if constexpr (kTree) __syncthreads();
+  auto sees = [&](int n, int t0) { return tree_sees(p, w, bits[kTree && p.mask ? lim[n] - i0 : 0], lim[n], t0); };
 
   f32x4 acc[kCols][M];
   float m_run[kCols], l_run[kCols];
@@ -277,20 +305,42 @@ void few_rows_kernel(Cache8AttnParams p) {
     kt = kt_next;
     if (more) load_keys();
     if (masked) {
+      if constexpr (kTree) {
 #pragma unroll
-      for (int n = 0; n < kCols; ++n)
+        for (int n = 0; n < kCols; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t on = sees(n, tok[u]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (tok[i >> 1] >= lim[n] - (4 * (i & 1) + r)) s[n][i][r] = -INFINITY;
-      // Codes past the last token any row sees may be anything; a weight of 0 would
-      // not take a NaN out.
+            for (int x = 0; x < 8; ++x) s[n][2 * u + (x >> 2)][x & 3] = hidden(on, x, s[n][2 * u + (x >> 2)][x & 3]);
+          }
+        // (a node's value that is no finite number reaches the rows that see it at the end)
 #pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const int n0 = clampi(w.lim - min(tok[0], w.lim), 0, 8), n1 = clampi(w.lim - min(tok[1], w.lim), 0, 8);
-        const u32x4 lo = keep_codes(vc[m], n0), hi = keep_codes(u32x4{0, 0, vc[m][2], vc[m][3]}, 8 + n1);
-        vc[m] = u32x4{lo[0], lo[1], hi[2], hi[3]};
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            uint32_t lo = vc[m][2 * u], hi = vc[m][2 * u + 1];
+            const uint32_t in_len = below(tok[u], w.lim);
+            wild |= clean_codes(lo, hi, in_len, in_len & ~below(tok[u], w.base), __float_as_uint(vsc[u]) >> 23);
+            vc[m][2 * u] = lo;
+            vc[m][2 * u + 1] = hi;
+          }
+      } else {
+#pragma unroll
+        for (int n = 0; n < kCols; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (tok[i >> 1] >= lim[n] - (4 * (i & 1) + r)) s[n][i][r] = -INFINITY;
+        // Codes past the last token any row sees may be anything; a weight of 0 would
+        // not take a NaN out.
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const int n0 = clampi(w.lim - min(tok[0], w.lim), 0, 8), n1 = clampi(w.lim - min(tok[1], w.lim), 0, 8);
+          const u32x4 lo = keep_codes(vc[m], n0), hi = keep_codes(u32x4{0, 0, vc[m][2], vc[m][3]}, 8 + n1);
+          vc[m] = u32x4{lo[0], lo[1], hi[2], hi[3]};
+        }
       }
     }
     u32x4 pk[kCols][2][kWParts];
@@ -353,6 +403,27 @@ void few_rows_kernel(Cache8AttnParams p) {
     if (more) load_values();
   }
 
+  if constexpr (kTree) {
+    // a piece's tiles as granules of its list
+    auto granule = [&](int t) {
+      if (kStream) return 8 * t;
+      const int page = t / p.tpp;
+      return page * p.gpp + min(8 * (t - page * p.tpp), p.gpp);
+    };
+    if (__syncthreads_or(wild != 0) && wave == 0)
+      tree_wild(p, w, b, h, D, granule(t_lo), granule(t_hi),
+                [&](size_t head, size_t at, int off) { return code_value(p, head, at, off); },
+                [&](int t0, int j, auto&& value) {
+#pragma unroll
+                  for (int n = 0; n < kCols; ++n)
+                    if (sees(n, t0) >> j & 1u) {
+#pragma unroll
+                      for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[n][m][r] += value(16 * m + 4 * g + r);
+                    }
+                });
+  }
   // Join the waves: 16 rows at a time through LDS, then kShare threads a row.
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
@@ -431,13 +502,15 @@ struct ManyLayout {
 
 constexpr int many_rows(int d) { return d == 128 ? 256 : 128; }  // query rows of a many-rows item
 
-template <int D, bool kSmallP>
+template <int D, bool kSmallP, bool kTree>
 __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_rows_kernel(Cache8AttnParams p) {
   using L = ManyLayout<D>;
   constexpr int KK = D / 16, NM = D / 32;
   constexpr int kRows = many_rows(D);  // (32 a wave; 4 D threads: 16 codes of a tile's keys each, 16 of its values)
   __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
   __shared__ int2 first_sm[kSmallP ? 8 : 1][4];  // first tokens of the granules of eight tiles
+  __shared__ uint32_t bits[kTree ? kRows : 1][kMaskWords + 1];  // mask rows of the item's nodes
+  __shared__ int wild;                                          // whether a node's value is no finite number
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // workgroup i runs on XCD i % 8: an XCD takes an eighth of the items in a row, which share
@@ -460,19 +533,32 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
   const bool whole = w.n_tiles <= p.split_tiles;
   const int n = t_hi - t_lo;
 
+  const int i0 = __builtin_amdgcn_readfirstlane(rt * kRows / p.G);
+  if constexpr (kTree) {
+    if (p.mask) {
+      const int nodes = min((rt * kRows + kRows - 1) / p.G, w.q_len - 1) - i0 + 1;
+      const uint32_t* src = p.mask + ((size_t)b * p.n_q + i0) * p.words;
+      for (int x = tid; x < nodes * p.words; x += 4 * D) bits[x / p.words][x % p.words] = src[x];
+    }
+    if (tid == 0) wild = 0;
+    __syncthreads();
+  }
   // queries
   u32x4 qf[KK];
   int lim;
   const int row0 = rt * kRows + wave * 32;
   {
     const int r = row0 + l32, i = min(r / p.G, w.q_len - 1);
-    lim = cache8_limit(p, w, i);
+    lim = kTree ? i : cache8_limit(p, w, i);  // (a tree: the row's node)
     const uint16_t* q =
         static_cast<const uint16_t*>(p.q) + (((size_t)b * p.n_q + i) * p.H + h * p.G + r % p.G) * D + 8 * half;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qf[kk] = ld_global16(q + 16 * kk);
   }
-  const int lim_first = cache8_limit(p, w, min(__builtin_amdgcn_readfirstlane(row0 / p.G), w.q_len - 1));
+  const int lim_first = kTree ? w.base : cache8_limit(p, w, min(__builtin_amdgcn_readfirstlane(row0 / p.G), w.q_len - 1));
+  auto sees = [&](int t0) __attribute__((always_inline)) {
+    return tree_sees(p, w, bits[kTree && p.mask ? lim - i0 : 0], lim, t0);
+  };
   const bool active = row0 < rt * kRows + w.rows;
 
   // The listed pages are one stream of tokens, cut into tiles of 64; a tile lies in one page or
@@ -648,16 +734,24 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
     return t.ta + min(t.cut, 64) > most || (t.cut < 64 && t.tb + 64 > most);
   };
   auto put_v = [&](int buf, const Tile& t) __attribute__((always_inline)) {
-    if (beyond(t, w.lim)) {
+    if (beyond(t, kTree ? lim_first : w.lim)) {
       // codes past the last token any row sees may be anything
       int t0 = (vtok_ld < t.cut ? t.ta : t.tb) + vtok_ld, t1 = (vtok_ld + 8 < t.cut ? t.ta : t.tb) + vtok_ld + 8;
       if constexpr (kSmallP) {
         t0 = first_sm[t.cut][tid & 3].x;
         t1 = first_sm[t.cut][tid & 3].y;
       }
-      const u32x4 lo = keep_codes(vc, clampi(w.lim - min(t0, w.lim), 0, 8));
-      const u32x4 hi = keep_codes(u32x4{0, 0, vc[2], vc[3]}, 8 + clampi(w.lim - min(t1, w.lim), 0, 8));
-      vc = u32x4{lo[0], lo[1], hi[2], hi[3]};
+      if constexpr (kTree) {
+        uint32_t a = vc[0], x = vc[1], y = vc[2], z = vc[3];
+        const uint32_t in0 = below(t0, w.lim), in1 = below(t1, w.lim);
+        // (a node's value that is no finite number reaches the rows that see it at the end)
+        if (clean_codes(a, x, in0, in0 & ~below(t0, w.base), ve0) | clean_codes(y, z, in1, in1 & ~below(t1, w.base), ve1)) wild = 1;
+        vc = u32x4{a, x, y, z};
+      } else {
+        const u32x4 lo = keep_codes(vc, clampi(w.lim - min(t0, w.lim), 0, 8));
+        const u32x4 hi = keep_codes(u32x4{0, 0, vc[2], vc[3]}, 8 + clampi(w.lim - min(t1, w.lim), 0, 8));
+        vc = u32x4{lo[0], lo[1], hi[2], hi[3]};
+      }
     }
     const int row = tid >> 2, c0 = 2 * (tid & 3);
     uint8_t* dst = smem + L::kVBase + buf * L::kTileV + row * L::kRowV;
@@ -695,11 +789,19 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int key = mine + 16 * g;
-      int sees = lim - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
-      if constexpr (kSmallP) sees = lim - (half ? first_sm[t.cut][2 * kh + g].y : first_sm[t.cut][2 * kh + g].x);
+      if constexpr (kTree) {
+        const int t0 = kSmallP ? (half ? first_sm[t.cut][2 * kh + g].y : first_sm[t.cut][2 * kh + g].x)
+                               : key + (key < t.cut ? t.ta : t.tb);
+        const uint32_t on = sees(t0);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) s[8 * g + x] = hidden(on, x, s[8 * g + x]);
+        continue;
+      }
+      int seen = lim - (key + (key < t.cut ? t.ta : t.tb));  // of the group's keys
+      if constexpr (kSmallP) seen = lim - (half ? first_sm[t.cut][2 * kh + g].y : first_sm[t.cut][2 * kh + g].x);
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        if (x >= sees) s[8 * g + x] = -INFINITY;
+        if (x >= seen) s[8 * g + x] = -INFINITY;
     }
   };
   // The largest of a half's scores, and the reference that follows it as in the few-rows kernel.
@@ -837,6 +939,20 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
       if (t + 1 < n) step(std::integral_constant<int, 1>{});
     }
   }
+  if constexpr (kTree) {
+    __syncthreads();
+    if (wild && active)
+      tree_wild(p, w, b, h, D, t_lo * 8, t_hi * 8,
+                [&](size_t head, size_t at, int off) { return code_value(p, head, at, off); },
+                [&](int t0, int j, auto&& value) {
+                  if (sees(t0) >> j & 1u) {
+#pragma unroll
+                    for (int m = 0; m < NM; ++m)
+#pragma unroll
+                      for (int x = 0; x < 16; ++x) acc[m][x] += value(32 * m + 8 * (x >> 2) + 4 * half + (x & 3));
+                  }
+                });
+  }
   if (!active) return;
   const int r = row0 + l32, i = r / p.G;
   const float l = l_run + __shfl_xor(l_run, 32);
@@ -964,32 +1080,38 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Cache8AttnParams p) {
   cache8_store<T, 4>(p, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
 
-template <typename T, int D, int kCols, int kParts>
+template <typename T, int D, int kCols, int kParts, bool kTree>
 void launch_rows(const Cache8AttnParams& p, int B, hipStream_t s) {
   const dim3 grid(p.n_split * p.Hk * p.n_rt, B);
   if (kCols == 1 && p.waves == 8) {
-    if (p.stream) few_rows_kernel<T, D, 1, kParts, true, 8><<<grid, 512, 0, s>>>(p);
-    else few_rows_kernel<T, D, 1, kParts, false, 8><<<grid, 512, 0, s>>>(p);
+    if (p.stream) few_rows_kernel<T, D, 1, kParts, true, 8, kTree><<<grid, 512, 0, s>>>(p);
+    else few_rows_kernel<T, D, 1, kParts, false, 8, kTree><<<grid, 512, 0, s>>>(p);
   } else {
-    if (p.stream) few_rows_kernel<T, D, kCols, kParts, true, 4><<<grid, 256, 0, s>>>(p);
-    else few_rows_kernel<T, D, kCols, kParts, false, 4><<<grid, 256, 0, s>>>(p);
+    if (p.stream) few_rows_kernel<T, D, kCols, kParts, true, 4, kTree><<<grid, 256, 0, s>>>(p);
+    else few_rows_kernel<T, D, kCols, kParts, false, 4, kTree><<<grid, 256, 0, s>>>(p);
+  }
+}
+
+template <int D, bool kTree>
+void launch_items(int dtype, int B, const Cache8AttnParams& p, hipStream_t s) {
+  const int cols = p.rows_per_item / 16;
+  if (dtype == HSA_DTYPE_BF16) {
+    if (p.many)
+      p.P < 64 ? many_rows_kernel<D, true, kTree><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p)
+               : many_rows_kernel<D, false, kTree><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
+    else if (cols == 1) launch_rows<uint16_t, D, 1, 1, kTree>(p, B, s);
+    else if (cols == 2) launch_rows<uint16_t, D, 2, 1, kTree>(p, B, s);
+    else if constexpr (D == 64) launch_rows<uint16_t, D, 4, 1, kTree>(p, B, s);
+  } else {
+    if (cols == 1) launch_rows<float, D, 1, 3, kTree>(p, B, s);
+    else launch_rows<float, D, 2, 3, kTree>(p, B, s);
   }
 }
 
 template <int D>
 hipError_t launch_for(int dtype, int B, const Cache8AttnParams& p, hipStream_t s) {
-  const int cols = p.rows_per_item / 16;
-  if (dtype == HSA_DTYPE_BF16) {
-    if (p.many)
-      p.P < 64 ? many_rows_kernel<D, true><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p)
-               : many_rows_kernel<D, false><<<dim3(p.n_split * p.Hk * p.n_rt, B), 4 * D, 0, s>>>(p);
-    else if (cols == 1) launch_rows<uint16_t, D, 1, 1>(p, B, s);
-    else if (cols == 2) launch_rows<uint16_t, D, 2, 1>(p, B, s);
-    else if constexpr (D == 64) launch_rows<uint16_t, D, 4, 1>(p, B, s);
-  } else {
-    if (cols == 1) launch_rows<float, D, 1, 3>(p, B, s);
-    else launch_rows<float, D, 2, 3>(p, B, s);
-  }
+  if (p.tree) launch_items<D, true>(dtype, B, p, s);
+  else launch_items<D, false>(dtype, B, p, s);
   if (p.n_split > 1) {
     // a workgroup a row while the rows alone do not fill the chip
     if ((int64_t)p.n_q * p.H * B <= 1024) {
@@ -1024,6 +1146,11 @@ int64_t cache8_slots(int d, int P, bool ragged) { return d == 128 ? 256 : (ragge
 // Most pieces of such a call, their ends counted (see plan_cache8).
 constexpr int kManyPieces = 16;
 constexpr double kManyEnds = 6.0, kManyJoin = 4.0, kManyGain = 0.97;
+// Pieces of a ragged batch's trees.
+constexpr int kTreeTiles = 32, kTreeItems = 2048;
+int64_t cache8_tree_pieces(int64_t items, int64_t tiles) {
+  return std::max<int64_t>(1, std::min<int64_t>({kManyPieces, tiles / kTreeTiles, (kTreeItems + items - 1) / items}));
+}
 
 }  // namespace
 
@@ -1072,7 +1199,8 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
     // of 136, 29 and 28).
     const int64_t slots = cache8_slots(p.d, p.P, ragged);
     double best = 1e300;
-    for (int64_t k = 1; k <= kManyPieces && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
+    if (p.tree && ragged) n = cache8_tree_pieces(items, tiles);
+    else for (int64_t k = 1; k <= kManyPieces && k * 4 <= std::max<int64_t>(tiles, 4); ++k) {
       const double each = (double)((tiles + k - 1) / k) + kManyEnds + (k > 1 ? kManyJoin : 0.0);
       const double t = (double)((items * k + slots - 1) / slots) * each;
       if (t < kManyGain * best) {
@@ -1121,7 +1249,7 @@ void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool r
   p.n_split = (int)((tiles + c - 1) / c);
 }
 
-int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list) {
+int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list, bool tree) {
   const int64_t tiles = cache8_tiles(list, P), items16 = (int64_t)B * Hk * ((rows + 15) / 16);
   const bool large = cache8_large(dtype, rows);
   int64_t most = 0;
@@ -1141,6 +1269,7 @@ int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t ro
     // left side and T / j + 1 for the right one, both are linear in T: a range [lo, hi] of it.
     const int64_t all = (list * P + 63) / 64, per = many_rows(d), items = (int64_t)B * Hk * ((rows + per - 1) / per);
     constexpr double e = kManyEnds + kManyJoin, kSlack = 1.0 + 1e-9;
+    if (tree) take(cache8_tree_pieces(items, all), per);
     for (const bool ragged : {false, true}) {
       const int64_t slots = cache8_slots(d, P, ragged);
       auto rounds = [&](int64_t k) { return (double)((items * k + slots - 1) / slots); };

@@ -231,11 +231,13 @@ struct Cache8AttnParams {
   const int32_t* sel;         // [B, Hk, k_max]
   const int32_t* kv_len;      // [B] nullable
   const int32_t* q_len;       // [B] nullable
+  const uint32_t* mask;       // [B, n_q, words] nullable (tree)
   void* o;                    // [B, n_q, H, d]
   float* lse;                 // [B, H, n_q] nullable
   float* part_o;              // [B, Hk, n_split, part_rows, d] (n_split > 1)
   float* part_ml;             // [B, Hk, n_split, part_rows, 2] reference maximum and sum
   int32_t H, Hk, G, P, d, n_q, num_slots, max_pages, k_max, cur_first, n_cur, causal;
+  int32_t tree, words;        // a drafted tree's queries (and not causal)
   float sm_scale, scale_log2;
   int16_t k_h[HSA_MAX_HEADS]; // most pages of each key head's sel row
   // set by plan_cache8
@@ -254,7 +256,7 @@ struct Cache8AttnParams {
 void plan_cache8(Cache8AttnParams& p, int dtype, int B, int max_list_sel, bool ragged);
 // Most rows of partial outputs (n_split * part_rows) that plan_cache8 gives a key head for any list up to
 // `list` pages, of either kind of call. rows: n_q * G.
-int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list);
+int64_t cache8_most_part_rows(int dtype, int d, int P, int B, int Hk, int64_t rows, int64_t list, bool tree);
 hipError_t launch_cache8_attention(int dtype, int d, int B, const Cache8AttnParams& p, hipStream_t s);
 
 // ------------------------------------------------------------ drafted trees
@@ -273,10 +275,8 @@ constexpr int kTreeMaxSplit = 128;  // pieces of one item
 
 struct TreeAttnParams {
   const void* q;              // [B, n_q, H, d]
-  const void* k;              // [num_slots, Hk, P, d] numbers or codes
+  const void* k;              // [num_slots, Hk, P, d]
   const void* v;              // [num_slots, Hk, d, P]
-  const uint8_t* k_exp;       // [num_slots, Hk, nb] (8-bit cache)
-  const uint8_t* v_exp;
   const int32_t* page_table;  // [B, max_pages]
   const int32_t* sel;         // [B, Hk, k_max]
   const int32_t* kv_len;      // [B] nullable
@@ -290,16 +290,16 @@ struct TreeAttnParams {
   float sm_scale, scale_log2;
   int16_t k_h[HSA_MAX_HEADS]; // most pages of each key head's sel row
   // set by plan_tree
-  int32_t nb;                 // scale blocks per page
   int32_t gpp, gmul;          // granules (8 tokens) per page, 65536 / gpp + 1
   int32_t rows_per_item, n_rt, part_rows;
+  int32_t tile;               // tokens of a tile
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
 };
 
 // Plans the launch for lists of at most `list` pages. Returns rows of partial outputs that a key head
 // needs at most, for this list or a shorter one.
-int64_t plan_tree(TreeAttnParams& p, int dtype, bool eight, int64_t list);
-hipError_t launch_tree_attention(int dtype, int d, bool eight, const TreeAttnParams& p, hipStream_t s);
+int64_t plan_tree(TreeAttnParams& p, int dtype, int64_t list);
+hipError_t launch_tree_attention(int dtype, int d, const TreeAttnParams& p, hipStream_t s);
 
 // ------------------------------------------------------------ kept tokens
 struct TokenKeepParams {

@@ -13,15 +13,14 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "hsa_fp8.h"
+#include "hsa_device.h"
 #include "hsa_kernels.h"
+#include "hsa_tree.h"
 
 namespace hsa {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kMaskWords = HSA_MAX_TREE / 32;
 
 // ---------------------------------------------------------------- ancestors
 // A node's row is its own bit and its parent's row. Rows double the path they hold with every
@@ -64,29 +63,10 @@ __global__ __launch_bounds__(HSA_MAX_TREE) void tree_mask_kernel(TreeMaskParams 
 }
 
 // ---------------------------------------------------------------- attention
-// What a cache holds, and the type of queries and outputs: e4m3 codes (bf16 or fp32 queries), or numbers
-// in the type of the call.
-enum Held { kCodes, kCodesF32, kBf16, kF32 };
-
 // The same of fp32 numbers, A[16x4] * B[4x16], k = l/16.
 __device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
-
-// Two bf16 numbers of a word where bits 0 and 1 of `on` are set.
-__device__ __forceinline__ uint32_t keep2(uint32_t w, uint32_t on) {
-  return w & (((on & 1u) ? 0xffffu : 0u) | ((on & 2u) ? 0xffff0000u : 0u));
-}
-__device__ __forceinline__ u32x4 keep8(u32x4 v, uint32_t on) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = keep2(v[i], on >> (2 * i));
-  return v;
-}
-__device__ __forceinline__ bool wild2(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
-// The low n bits.
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
 // A sequence's tokens as an item's key head lists them: n_sel selected pages, then pages
 // [cur_first, ..), one stream cut into tiles whatever pages they are in.
@@ -96,7 +76,6 @@ struct TreeWalk {
 };
 
 // Every lane of the wave must call it.
-template <int kTile>
 __device__ __forceinline__ TreeWalk tree_walk(const TreeAttnParams& p, int b, int h, int lane) {
   TreeWalk w;
   const int end = (p.cur_first + p.n_cur) * p.P;
@@ -107,12 +86,61 @@ __device__ __forceinline__ TreeWalk tree_walk(const TreeAttnParams& p, int b, in
       min(count_selected(p.sel + ((size_t)b * p.Hk + h) * p.k_max, p.k_max, p.max_pages, lane), (int)p.k_h[h]));
   const int cur = clampi(w.len - p.cur_first * p.P, 0, p.n_cur * p.P);
   w.n_list = w.n_sel + __builtin_amdgcn_readfirstlane((cur + p.P - 1) / p.P);
-  w.n_tiles = (w.n_sel * p.P + cur + kTile - 1) / kTile;
+  w.n_tiles = (w.n_sel * p.P + cur + p.tile - 1) / p.tile;
   return w;
 }
 
-template <int H>
-using QType = typename std::conditional<H == kCodes || H == kBf16, uint16_t, float>::type;
+// A listed page: where its numbers of the key head begin (of keys and values alike), the head's index in the
+// cache, the page's first token (-1 past the list, where it repeats the last page).
+struct TreePage {
+  int64_t at;
+  int head, first;
+};
+__device__ __forceinline__ void tree_pages(const TreeAttnParams& p, const TreeWalk& w, int b, int h, int li0, int n,
+                                           int D, int tid, int threads, TreePage* pages) {
+  for (int x = tid; x < n; x += threads) {
+    const int li = min(li0 + x, w.n_list - 1);
+    const int page = li < w.n_sel ? p.sel[((size_t)b * p.Hk + h) * p.k_max + li] : p.cur_first + li - w.n_sel;
+    const int slot = clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1);
+    const int64_t head = (int64_t)slot * p.Hk + h;
+    pages[x] = TreePage{head * p.P * D, (int)head, li0 + x < w.n_list ? page * p.P : -1};
+  }
+}
+
+// A tile's place in the table: list position and granule within the page. Most tiles lie in one page, which is then
+// a scalar, as is all that follows from it.
+struct TreePlace {
+  int li, at;
+  bool one;       // the whole tile is in one page
+  int64_t base;   // (one) its first token's place among the page's tokens, and the page's
+  int head, off, first;
+};
+__device__ __forceinline__ void tree_place(const TreeAttnParams& p, const TreePage* pages, int grans, TreePlace& t) {
+  t.one = t.at + grans <= p.gpp;
+  if (t.one) {
+    const TreePage e = pages[t.li];
+    t.base = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)e.at) |
+             (int64_t)__builtin_amdgcn_readfirstlane((int)(e.at >> 32)) << 32;
+    t.head = __builtin_amdgcn_readfirstlane(e.head);
+    t.off = 8 * t.at;
+    t.first = __builtin_amdgcn_readfirstlane(e.first) + t.off;
+  }
+}
+// Granule gr of a tile: its page and token within it.
+__device__ __forceinline__ TreePage tree_granule(const TreeAttnParams& p, const TreePage* pages, const TreePlace& t, int gr,
+                                                 int& off) {
+  const int x = t.at + gr, pg = p.gpp >= 8 ? (x >= p.gpp) : (x * p.gmul) >> 16;
+  off = 8 * (x - pg * p.gpp);
+  return pages[t.li + pg];
+}
+__device__ __forceinline__ int tree_token(const TreeAttnParams& p, const TreePage* pages, const TreePlace& t, int gr) {
+  if (t.one) return t.first + 8 * gr;
+  int off;
+  const int first = tree_granule(p, pages, t, gr, off).first;
+  return first < 0 ? INT_MAX - 8 : first + off;
+}
+// 16 bytes at a uniform place plus a thread's own offset (bytes).
+__device__ __forceinline__ u32x4 ld_at(const uint8_t* base, uint32_t off) { return ld_global16(base + off); }
 
 // N dims of a finished row: o / l, and the log-sum-exp once a row. A row that sees no token is
 // 0 with a log-sum-exp of -inf.
@@ -134,32 +162,44 @@ __device__ __forceinline__ void tree_store(const TreeAttnParams& p, int D, int b
     p.lse[((size_t)b * p.H + head) * p.n_q + i] = l > 0.f ? m * p.sm_scale + logf(l) : (l == l ? -INFINITY : l);
 }
 
-// Up to 16 kCols rows of one key head against a range of its tiles. A wave takes every kWaves-th tile (64
-// tokens, fp32 32) and keeps an online softmax of its own; the workgroup joins them at the end.
+// A number of the pool.
+template <typename T>
+__device__ __forceinline__ float pool_value(const TreeAttnParams& p, size_t at) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f32(static_cast<const uint16_t*>(p.v)[at]);
+  else return static_cast<const float*>(p.v)[at];
+}
+
+constexpr int kTreeTile = 32;  // tokens of a tile of up to 32 rows
+
+// Up to 16 kCols rows of one key head against a range of its tiles. A wave takes every kWaves-th tile and
+// keeps an online softmax of its own; the workgroup joins them at the end.
 //
 // Products are transposed (keys are the rows of S^T = K Q^T, dims those of O^T = V^T P^T), so a lane
 // holds scores of one row r = l % 16. Keys take the places in S^T that give a lane the scores of the
-// keys whose values it loads, a granule of eight tokens (which never crosses a page) for each half u
+// keys whose values it loads, a granule of eight tokens (which never crosses a page) for each part u
 // of the tile: weights become the second product's operand without an exchange between lanes. Tiles go
 // from memory to the registers of the wave that uses them; the next tile's keys are asked for once this
 // one's scores are done with their registers, the values after its output.
-template <int H, int D, int kCols, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_kernel(TreeAttnParams p) {
-  using T = QType<H>;
-  constexpr bool kEight = H == kCodes || H == kCodesF32, kMat32 = H == kF32;
-  constexpr int kTile = kMat32 ? 32 : 64, kGran = kTile / 8;  // tokens, granules of a tile
-  constexpr int NI = kTile / 16;                              // score blocks
-  constexpr int M = D / 16;                                   // blocks of output dims
-  constexpr int kParts = H == kCodesF32 ? 3 : 1;              // bf16 parts of a query
+template <typename T, int D, int kCols, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kCols == 1 ? (sizeof(T) == 2 ? 3 : 2) : (sizeof(T) == 2 ? 2 : 1))
+void tree_attn_kernel(TreeAttnParams p) {
+  constexpr bool kMat32 = sizeof(T) == 4;
+  constexpr int kTile = kTreeTile, kGran = kTile / 8;  // tokens, granules of a tile
+  constexpr int kU = kMat32 ? 2 : 1;                   // granules of a lane
+  constexpr int BU = kMat32 ? 1 : 2;                   // score blocks of 16 keys of a granule
+  constexpr int M = D / 16;                            // blocks of output dims
   // bf16 parts of a weight. One rounds it by up to 2^-8, about what the result's own rounding adds; two
-  // leave 2^-16. fp32 queries take three (2^-24); fp32 caches none (their products are of fp32).
-  constexpr int kWParts = H == kCodesF32 ? 3 : (kCols == 1 ? 2 : 1);
-  constexpr int KC = H == kF32 ? D / 16 : (kEight ? D / 64 : D / 32);  // 16-byte pieces of a key row a lane
+  // leave 2^-16. (fp32: none, its products are of fp32.)
+  constexpr int kWParts = kCols == 1 ? 2 : 1;
   constexpr int kRows = 16 * kCols, OS = D + 4;
   constexpr int kThreads = 64 * kWaves;
-  __shared__ int2 pages[kTreePages];                // slot and first token of the listed pages
+  __shared__ TreePage pages[kTreePages];
   __shared__ uint32_t bits[kRows][kMaskWords + 1];  // mask rows of the item's nodes
-  __shared__ __attribute__((aligned(16))) float osm[kWaves * 16 * OS];
+  // the queries; at the end 16 rows of each wave's output
+  constexpr int QC = kMat32 ? D / 16 : D / 32;  // 16-byte pieces of a row that a lane takes
+  constexpr int kSm = std::max(kCols * QC * 64, kWaves * 16 * OS / 4);
+  __shared__ u32x4 qsm[kSm];
+  float* osm = reinterpret_cast<float*>(qsm);
   __shared__ float msm[kWaves][kRows], lsm[kWaves][kRows];
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -171,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_ke
   const int split = __builtin_amdgcn_readfirstlane(group / heads), bh = group - split * heads;
   if (split >= p.n_split) return;
   const int b = __builtin_amdgcn_readfirstlane(bh / p.Hk), h = bh - b * p.Hk;
-  const TreeWalk w = tree_walk<kTile>(p, b, h, lane);
+  const TreeWalk w = tree_walk(p, b, h, lane);
   const int row0 = rt * kRows;
   if (row0 >= w.q_len * p.G) return;
   const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
@@ -185,23 +225,15 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_ke
     for (int x = tid; x < nodes * p.words; x += kThreads) bits[x / p.words][x % p.words] = src[x];
   }
 
-  // queries
-  u32x4 qf[kCols][kMat32 ? 1 : D / 32][kParts];
-  f32x4 qs[kCols][kMat32 ? D / 16 : 1];
+  // Queries, as the operands that the lanes of every wave take each tile. (In registers they would cost
+  // those that hold a tile.)
   int node[kCols];  // of the column's row
 #pragma unroll
-  for (int n = 0; n < kCols; ++n) {
-    const int r = row0 + 16 * n + c16, i = min(r / p.G, w.q_len - 1);
-    node[n] = i;
+  for (int n = 0; n < kCols; ++n) node[n] = min((row0 + 16 * n + c16) / p.G, w.q_len - 1);
+  for (int x = wave; x < kCols * QC; x += kWaves) {
+    const int n = x / QC, c = x % QC, r = row0 + 16 * n + c16, i = min(r / p.G, w.q_len - 1);
     const T* q = static_cast<const T*>(p.q) + (((size_t)b * p.n_q + i) * p.H + h * p.G + r % p.G) * D;
-    if constexpr (kMat32) {
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) qs[n][c] = *reinterpret_cast<const f32x4*>(q + 16 * c + 4 * g);
-    } else {
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c)  // (a lane's 16 codes are dims 16 g.. of 64)
-        split_row<T, kParts>(q + (kEight ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g), qf[n][c]);
-    }
+    qsm[x * 64 + lane] = ld_global16(q + (kMat32 ? 16 * c + 4 * g : 32 * c + 8 * g));
   }
 
   f32x4 acc[kCols][M];
@@ -215,95 +247,197 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_ke
     l_run[n] = 0.f;
   }
 
-  u32x4 kc[NI][KC], vc[M][kEight ? 1 : 2];
-  float ksc[2], vsc[2];
-  // granules of the lane's key rows and of its values, for half u
-  auto key_granule = [&](int u) { return kMat32 ? 2 * u + (c16 >> 3) : kEight ? 2 * (c16 >> 2) + u : 4 * u + (c16 >> 2); };
-  auto val_granule = [&](int u) { return kMat32 ? 2 * u + (g >> 1) : kEight ? 2 * g + u : 4 * u + g; };
-  // the next tile's places: slots, tokens within the page, first tokens of the value granules (INT_MAX
-  // - 8 where no page is listed)
-  int ks[2], ko[2], vs[2], vo[2], vt[2];
-  auto look_up = [&](int li, int at) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int xk = at + key_granule(u), xv = at + val_granule(u);
-      const int pk = p.gpp >= 8 ? (xk >= p.gpp) : (xk * p.gmul) >> 16, pv = p.gpp >= 8 ? (xv >= p.gpp) : (xv * p.gmul) >> 16;
-      const int2 ek = pages[li + pk], ev = pages[li + pv];
-      ks[u] = ek.x;
-      ko[u] = 8 * (xk - pk * p.gpp);
-      vs[u] = ev.x;
-      vo[u] = 8 * (xv - pv * p.gpp);
-      vt[u] = ev.y < 0 ? INT_MAX - 8 : ev.y + vo[u];
+  u32x4 kc[kU * BU][QC], vc[M][kU];
+  // granules of the lane's key rows and of its values
+  auto key_granule = [&](int u) { return kMat32 ? 2 * u + (c16 >> 3) : c16 >> 2; };
+  auto val_granule = [&](int u) { return kMat32 ? 2 * u + (g >> 1) : g; };
+  // the next tile, and a lane's bytes within one page: its key rows of part u, its value row's granules
+  TreePlace to;
+  constexpr int E = (int)sizeof(T);
+  const uint8_t *const kp = static_cast<const uint8_t*>(p.k), *const vp = static_cast<const uint8_t*>(p.v);
+  const int sub = kMat32 ? c16 & 7 : c16 & 3, kcol = (kMat32 ? 4 : 8) * g, vsub = kMat32 ? 4 * (g & 1) : 0;
+  auto load_keys = [&](int u) {
+    const uint8_t* kb;
+    uint32_t mine;
+    if (to.one) {
+      kb = kp + (to.base + (int64_t)to.off * D) * E;
+      mine = ((8 * key_granule(u) + sub) * D + kcol) * E;
+    } else {
+      int off;
+      const TreePage e = tree_granule(p, pages, to, key_granule(u), off);
+      kb = kp + (e.at + (int64_t)off * D) * E;
+      mine = (sub * D + kcol) * E;
     }
-  };
-  auto load_keys = [&]() {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const size_t head = (size_t)ks[u] * p.Hk + h;
-      if constexpr (kMat32) {
-        const float* kb = static_cast<const float*>(p.k) + (head * p.P + ko[u] + (c16 & 7)) * D + 4 * g;
+    for (int i = 0; i < BU; ++i)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) kc[u][c] = ld_global16(kb + 16 * c);
-      } else if constexpr (kEight) {
-        const uint8_t* kb = static_cast<const uint8_t*>(p.k) + (head * p.P + ko[u] + (c16 & 3)) * D + 16 * g;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int c = 0; c < KC; ++c) kc[2 * u + i][c] = ld_global16(kb + 4 * i * D + 64 * c);
-        ksc[u] = scale_of(p.k_exp[head * p.nb + (ko[u] >> 6)]);
-      } else {
-        const uint16_t* kb = static_cast<const uint16_t*>(p.k) + (head * p.P + ko[u] + (c16 & 3)) * D + 8 * g;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int c = 0; c < KC; ++c) kc[2 * u + i][c] = ld_global16(kb + 4 * i * D + 32 * c);
-      }
-    }
+      for (int c = 0; c < QC; ++c) kc[BU * u + i][c] = ld_at(kb, mine + 4 * i * D * E + 64 * c);
   };
   auto load_values = [&]() {
+    const int64_t next = (int64_t)16 * p.P * E;  // to the next block of dims
+    if (to.one) {
+      const uint8_t* vb = vp + (to.base + to.off) * E;
+      const uint32_t row = (uint32_t)c16 * p.P;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const size_t head = (size_t)vs[u] * p.Hk + h;
-      if constexpr (kMat32) {
-        const float* vb = static_cast<const float*>(p.v) + (head * D + c16) * p.P + vo[u] + 4 * (g & 1);
+      for (int m = 0; m < M; ++m) {
 #pragma unroll
-        for (int m = 0; m < M; ++m) vc[m][u] = ld_global16(vb + (size_t)(16 * m) * p.P);
-      } else if constexpr (kEight) {
-        const uint8_t* vb = static_cast<const uint8_t*>(p.v) + (head * D + c16) * p.P + vo[u];
+        for (int u = 0; u < kU; ++u) vc[m][u] = ld_at(vb, (row + 8 * val_granule(u) + vsub) * E);
+        vb += next;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        int off;
+        const TreePage e = tree_granule(p, pages, to, val_granule(u), off);
+        const uint8_t* vb = vp + (e.at + (int64_t)c16 * p.P + off + vsub) * E;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-          const u32x2a8 x = *reinterpret_cast<const u32x2a8*>(vb + (size_t)(16 * m) * p.P);
-          vc[m][0][2 * u] = x[0];
-          vc[m][0][2 * u + 1] = x[1];
+          vc[m][u] = ld_global16(vb);
+          vb += next;
         }
-        vsc[u] = scale_of(p.v_exp[head * p.nb + (vo[u] >> 6)]);
-      } else {
-        const uint16_t* vb = static_cast<const uint16_t*>(p.v) + (head * D + c16) * p.P + vo[u];
-#pragma unroll
-        for (int m = 0; m < M; ++m) vc[m][u] = ld_global16(vb + (size_t)(16 * m) * p.P);
       }
     }
   };
-  // the value operand of dim block m, half u
-  auto values = [&](int m, int u) {
-    if constexpr (kEight) return codes_to_bf16(vc[m][0][2 * u], vc[m][0][2 * u + 1], vsc[u]);
-    else return vc[m][u];
-  };
-  // Bit j: whether node i (row `row` of bits) sees token t0 + j.
-  auto sees = [&](int row, int i, int t0) -> uint32_t {
-    if (t0 >= w.len) return 0u;
-    const int rel = t0 - w.base;  // (t0 below len: no overflow)
-    if (rel <= -8) return 0xffu;
-    uint32_t on;
-    if (p.mask) {
-      const int x = rel >> 5, sh = rel & 31;
-      const uint32_t lo = x < 0 ? ~0u : x < p.words ? bits[row][x] : 0u;
-      const uint32_t hi = x + 1 < 0 ? ~0u : x + 1 < p.words ? bits[row][x + 1] : 0u;
-      on = (uint32_t)(((uint64_t)hi << 32 | lo) >> sh);
+  // Values of a granule's tokens that are not in `in_len` become 0, and those of `nodes` that are no finite
+  // numbers, which are noted.
+  uint32_t wild = 0;
+  auto clean_values = [&](int m, int u, uint32_t in_len, uint32_t nodes) {
+    if constexpr (kMat32) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t x = vc[m][u][j];
+        const uint32_t bad = ((x & 0x7f800000u) + 0x00800000u) & (nodes >> (4 * (g & 1)) << (31 - j) & 0x80000000u);
+        wild |= bad;
+        vc[m][u][j] = x & ones_if(in_len >> (4 * (g & 1)), j) & ~ones_if(bad, 31);
+      }
     } else {
-      on = low_bits(i + 1 - rel);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t x = vc[m][u][j];
+        const uint32_t bad = ((x & 0x7f807f80u) + 0x00800080u) & halves2(nodes >> (2 * j));
+        wild |= bad;
+        vc[m][u][j] = x & fill16(halves2(in_len >> (2 * j))) & ~fill16(bad);
+      }
     }
-    return on & low_bits(min(w.len - t0, 8));
+  };
+  auto sees = [&](int n, int t0) { return tree_sees(p, w, bits[node[n] - i0], node[n], t0); };
+
+  // A tile whose granules begin at tokens tok (partly: which some row may not see): scores, softmax, output.
+  // `after` runs once the keys are done with.
+  auto step = [&](bool partly, const int (&tok)[kU], auto&& after) __attribute__((always_inline)) {
+    f32x4 s[kCols][kU * BU];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n)
+#pragma unroll
+      for (int i = 0; i < kU * BU; ++i) s[n][i] = f32x4{0};
+#pragma unroll
+    for (int c = 0; c < QC; ++c) {
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) {
+        const u32x4 q = qsm[(n * QC + c) * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < kU * BU; ++i) {
+          if constexpr (kMat32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[n][i] = mfma4(__uint_as_float(kc[i][c][j]), __uint_as_float(q[j]), s[n][i]);
+          } else {
+            s[n][i] = mfma16(kc[i][c], q, s[n][i]);
+          }
+        }
+      }
+    }
+    // The reference maximum moves only when a score exceeds it by more than 8 in exp2 units:
+    // exponentials stay below 256, and the division by the sum is exact for any reference.
+    auto raise = [&](int n) __attribute__((always_inline)) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kU * BU; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[n][i][r]);
+      if (__any(mx * c2 > m_run[n] * c2 + 8.f)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = mx * c2 > m_run[n] * c2 + 8.f ? mx : m_run[n];
+        const float alpha = __builtin_amdgcn_exp2f((m_run[n] - m_new) * c2);
+        l_run[n] *= alpha;
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[n][m] *= alpha;
+        m_run[n] = m_new;
+      }
+    };
+    // What a node does not see. (tok + 8 does not overflow.)
+    if (__builtin_expect(partly, 0)) {
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const uint32_t on = sees(n, tok[u]) >> (kMat32 ? 4 * (g & 1) : 0);
+#pragma unroll
+          for (int x = 0; x < 4 * BU; ++x) s[n][u * BU + (x >> 2)][x & 3] = hidden(on, x, s[n][u * BU + (x >> 2)][x & 3]);
+        }
+      // What lies past the sequence's end may be anything, and becomes 0 (a weight of 0 would not take a NaN
+      // out); so does what not every row sees and is no finite number: it reaches its rows at the end.
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const uint32_t in_len = low_bits(clampi(w.len - min(tok[u], w.len), 0, 8));
+        const uint32_t node_bits = in_len & ~low_bits(clampi(w.base - min(tok[u], w.base), 0, 8));
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          __builtin_amdgcn_sched_barrier(0);  // (one block at a time: registers)
+          clean_values(m, u, in_len, node_bits);
+        }
+      }
+    }
+    after();
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) raise(n);
+    u32x4 pk[kCols][kU][kWParts];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      const float mc = m_run[n] * c2;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kU * BU; ++i) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          // (fp32: subtracted before it is scaled, so that large scores lose nothing)
+          s[n][i][r] = __builtin_amdgcn_exp2f(sizeof(T) == 2 ? fmaf(s[n][i][r], c2, -mc) : (s[n][i][r] - m_run[n]) * c2);
+        sum += (s[n][i][0] + s[n][i][1]) + (s[n][i][2] + s[n][i][3]);
+      }
+      l_run[n] += sum;
+      if constexpr (!kMat32) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int k = 0; k < kWParts; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f32x4& e = s[n][2 * u + (i >> 1)];
+              const uint32_t pair = pack_bf16(e[2 * (i & 1)], e[2 * (i & 1) + 1]);
+              pk[n][u][k][i] = pair;
+              if (k + 1 < kWParts) {
+                e[2 * (i & 1)] -= bf16_lo(pair);
+                e[2 * (i & 1) + 1] -= bf16_hi(pair);
+              }
+            }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        if constexpr (kMat32) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) acc[n][m] = mfma4(__uint_as_float(vc[m][u][j]), s[n][u][j], acc[n][m]);
+        } else {
+#pragma unroll
+          for (int n = 0; n < kCols; ++n)
+#pragma unroll
+            for (int k = 0; k < kWParts; ++k) acc[n][m] = mfma16(vc[m][u], pk[n][u][k], acc[n][m]);
+        }
+      }
   };
 
   const int chunk = ((kTreePages - 2) * p.gpp) / kGran;  // tiles whose pages fit the table
@@ -312,203 +446,56 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_ke
     const int li0 = __builtin_amdgcn_readfirstlane(c_lo * kGran / p.gpp), at0 = c_lo * kGran - li0 * p.gpp;
     const int n_pages = (at0 + (c_hi - c_lo) * kGran - 1) / p.gpp + 1;
     if (c_lo > t_lo) __syncthreads();
-    for (int x = tid; x < n_pages; x += kThreads) {
-      const int li = min(li0 + x, w.n_list - 1);
-      const int page = li < w.n_sel ? p.sel[((size_t)b * p.Hk + h) * p.k_max + li] : p.cur_first + li - w.n_sel;
-      const int slot = clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1);
-      pages[x] = int2{slot, li0 + x < w.n_list ? page * p.P : -1};
-    }
+    tree_pages(p, w, b, h, li0, n_pages, D, tid, kThreads, pages);
     __syncthreads();
-    int at = at0 + wave * kGran, li = __builtin_amdgcn_readfirstlane(at / p.gpp);
-    at -= li * p.gpp;
+    to.at = at0 + wave * kGran;
+    to.li = __builtin_amdgcn_readfirstlane(to.at / p.gpp);
+    to.at -= to.li * p.gpp;
     const int on_pages = __builtin_amdgcn_readfirstlane(kWaves * kGran / p.gpp), on_rest = kWaves * kGran - on_pages * p.gpp;
     if (c_lo + wave < c_hi) {
-      look_up(li, at);
-      load_keys();
+      tree_place(p, pages, kGran, to);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) load_keys(u);
       load_values();
     }
     for (int t = c_lo + wave; t < c_hi; t += kWaves) {
       const bool more = t + kWaves < c_hi;
-      const int tok[2] = {vt[0], vt[1]};
-      at += on_rest;
-      li += on_pages;
-      if (at >= p.gpp) {
-        at -= p.gpp;
-        ++li;
+      const TreePlace now = to;
+      to.at += on_rest;
+      to.li += on_pages;
+      if (to.at >= p.gpp) {
+        to.at -= p.gpp;
+        ++to.li;
       }
-      if (more) look_up(li, at);
-      f32x4 s[kCols][NI];
+      if (more) tree_place(p, pages, kGran, to);
+      const bool partly = !now.one || now.first + kTile > w.base;  // (some row may not see all of it)
+      int tok[kU];
+      if (partly) {
 #pragma unroll
-      for (int n = 0; n < kCols; ++n)
-#pragma unroll
-        for (int i = 0; i < NI; ++i) s[n][i] = f32x4{0};
-      if constexpr (kMat32) {
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-              for (int n = 0; n < kCols; ++n) s[n][i] = mfma4(__uint_as_float(kc[i][c][j]), qs[n][c][j], s[n][i]);
-      } else {
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            u32x4 a;
-            if constexpr (kEight) a = codes_to_bf16(kc[i][c >> 1][2 * (c & 1)], kc[i][c >> 1][2 * (c & 1) + 1], ksc[i >> 1]);
-            else a = kc[i][c];
-#pragma unroll
-            for (int n = 0; n < kCols; ++n)
-#pragma unroll
-              for (int k = 0; k < kParts; ++k) s[n][i] = mfma16(a, qf[n][c][k], s[n][i]);
-          }
+        for (int u = 0; u < kU; ++u) tok[u] = tree_token(p, pages, now, val_granule(u));
       }
-      if (more) load_keys();
-      // What a node does not see. (tok + 8 does not overflow.)
-      bool wild = false;  // some value that not every row sees is no finite number
-      uint32_t seen[kCols][2];
-      if (__any(max(tok[0], tok[1]) + 8 > w.base)) {
+      step(partly, tok, [&]() __attribute__((always_inline)) {
+        if (more) {
 #pragma unroll
-        for (int n = 0; n < kCols; ++n)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t on = sees(node[n] - i0, node[n], tok[u]);
-            seen[n][u] = on;
-            if constexpr (kMat32) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (!(on >> (4 * (g & 1) + r) & 1u)) s[n][u][r] = -INFINITY;
-            } else {
-#pragma unroll
-              for (int x = 0; x < 8; ++x)
-                if (!(on >> x & 1u)) s[n][2 * u + (x >> 2)][x & 3] = -INFINITY;
-            }
-          }
-        // What lies past the sequence's end may be anything; a weight of 0 would not take a NaN out.
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t in_len = low_bits(clampi(w.len - min(tok[u], w.len), 0, 8));
-#pragma unroll
-          for (int m = 0; m < M; ++m) {
-            if constexpr (kMat32) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if (!(in_len >> (4 * (g & 1) + j) & 1u)) vc[m][u][j] = 0u;
-                wild |= (vc[m][u][j] & 0x7f800000u) == 0x7f800000u;
-              }
-            } else if constexpr (kEight) {
-              const uint32_t m4 = ((in_len & 15u) * 0x00204081u & 0x01010101u) * 255u;
-              const uint32_t m8 = ((in_len >> 4) * 0x00204081u & 0x01010101u) * 255u;
-              vc[m][0][2 * u] &= m4;
-              vc[m][0][2 * u + 1] &= m8;
-              const u32x4 v = values(m, u);
-              wild |= wild2(v[0]) || wild2(v[1]) || wild2(v[2]) || wild2(v[3]);
-            } else {
-              vc[m][u] = keep8(vc[m][u], in_len);
-              wild |= wild2(vc[m][u][0]) || wild2(vc[m][u][1]) || wild2(vc[m][u][2]) || wild2(vc[m][u][3]);
-            }
-          }
+          for (int u = 0; u < kU; ++u) load_keys(u);
         }
-        wild = __any(wild);
-      }
-      u32x4 pk[kCols][2][kWParts];
-#pragma unroll
-      for (int n = 0; n < kCols; ++n) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[n][i][r]);
-        // The reference maximum moves only when a score exceeds it by more than 8 in exp2 units:
-        // exponentials stay below 256, and the division by the sum is exact for any reference.
-        if (__any(mx * c2 > m_run[n] * c2 + 8.f)) {
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const float m_new = mx * c2 > m_run[n] * c2 + 8.f ? mx : m_run[n];
-          const float alpha = __builtin_amdgcn_exp2f((m_run[n] - m_new) * c2);
-          l_run[n] *= alpha;
-#pragma unroll
-          for (int m = 0; m < M; ++m) acc[n][m] *= alpha;
-          m_run[n] = m_new;
-        }
-        const float mc = m_run[n] * c2;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            // (fp32: subtracted before it is scaled, so that large scores lose nothing)
-            s[n][i][r] = __builtin_amdgcn_exp2f(sizeof(T) == 2 ? fmaf(s[n][i][r], c2, -mc) : (s[n][i][r] - m_run[n]) * c2);
-          sum += (s[n][i][0] + s[n][i][1]) + (s[n][i][2] + s[n][i][3]);
-        }
-        l_run[n] += sum;
-        if constexpr (!kMat32) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int k = 0; k < kWParts; ++k)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                f32x4& e = s[n][2 * u + (i >> 1)];
-                const uint32_t pair = pack_bf16(e[2 * (i & 1)], e[2 * (i & 1) + 1]);
-                pk[n][u][k][i] = pair;
-                if (k + 1 < kWParts) {
-                  e[2 * (i & 1)] -= bf16_lo(pair);
-                  e[2 * (i & 1) + 1] -= bf16_hi(pair);
-                }
-              }
-        }
-      }
-      if (__builtin_expect(!wild, 1)) {
-#pragma unroll
-        for (int m = 0; m < M; ++m)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if constexpr (kMat32) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < kCols; ++n) acc[n][m] = mfma4(__uint_as_float(vc[m][u][j]), s[n][u][j], acc[n][m]);
-            } else {
-              const u32x4 a = values(m, u);
-#pragma unroll
-              for (int n = 0; n < kCols; ++n)
-#pragma unroll
-                for (int k = 0; k < kWParts; ++k) acc[n][m] = mfma16(a, pk[n][u][k], acc[n][m]);
-            }
-          }
-      } else {
-        // Row by row, each with the values that it sees (0 times an infinity is NaN).
-#pragma unroll
-        for (int n = 0; n < kCols; ++n)
-          for (int c = 0; c < 16; ++c) {
-            const uint32_t on0 = (uint32_t)__shfl((int)seen[n][0], 16 * g + c), on1 = (uint32_t)__shfl((int)seen[n][1], 16 * g + c);
-#pragma unroll
-            for (int m = 0; m < M; ++m) {
-              f32x4 one = f32x4{0};
-#pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const uint32_t on = u ? on1 : on0;
-                if constexpr (kMat32) {
-#pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    one = mfma4(on >> (4 * (g & 1) + j) & 1u ? __uint_as_float(vc[m][u][j]) : 0.f, s[n][u][j], one);
-                } else {
-                  const u32x4 a = keep8(values(m, u), on);
-#pragma unroll
-                  for (int k = 0; k < kWParts; ++k) one = mfma16(a, pk[n][u][k], one);
-                }
-              }
-              if (c16 == c) acc[n][m] += one;
-            }
-          }
-      }
+      });
       if (more) load_values();
     }
   }
 
+  // (the waves' tiles are not each other's: any of them may have seen one)
+  if (__syncthreads_or(wild != 0) && wave == 0)
+    tree_wild(p, w, b, h, D, t_lo * kGran, t_hi * kGran, [&](size_t, size_t at, int) { return pool_value<T>(p, at); }, [&](int t0, int j, auto&& value) {
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+        if (sees(n, t0) >> j & 1u) {
+#pragma unroll
+          for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[n][m][r] += value(16 * m + 4 * g + r);
+        }
+    });
   // Join the waves: 16 rows at a time through LDS, then kShare threads a row.
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
@@ -552,9 +539,321 @@ __global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : 1) void tree_attn_ke
   }
 }
 
+// More rows: 32 kRG rows of one key head (kRG = 2 or 4) against a range of its tiles of 64 tokens. Four waves, two
+// workgroups a CU; a tile is turned into bf16 once, on its way from the registers that it arrived in to LDS, and read from
+// there by all waves: with kRG = 4 each takes 32 rows, with two 32 rows and half of the tile's tokens.
+//
+// Products are transposed as above, 32x32x16, with key rows in an order that makes a lane's scores the
+// weights' operand. A tile's loads are two tiles ahead of its products.
+template <int D, int kRG>
+struct TreeWide {
+  static constexpr int kThreads = 256, kRows = 32 * kRG;
+  static constexpr int kRowK = 2 * D, kTileK = 64 * kRowK, kRowV = 128, kTileV = D * kRowV;  // bytes
+  static constexpr int kBytes = 2 * (kTileK + kTileV);
+  // 16-byte pieces of a tile that a thread loads, keys and values alike
+  static constexpr int kPieces = 64 * D * 2 / 16 / kThreads;
+  // 16-byte chunks of a row, permuted so that rows read together fall on their own banks
+  static __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int swz_v(int row) { return (row >> 1) & 7; }
+};
+
+template <int D, int kRG>
+__global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
+  using L = TreeWide<D, kRG>;
+  constexpr int KK = D / 16, NM = D / 32, NP = L::kPieces, kRows = L::kRows;
+  constexpr int KH = kRG / 2;  // halves of a tile that a wave takes
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
+  __shared__ TreePage pages[kTreePages];
+  __shared__ uint32_t bits[kRows][kMaskWords + 1];
+  __shared__ int wild;  // whether a value that not every row sees is no finite number
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int per8 = 8 * p.n_rt;
+  const int oct = __builtin_amdgcn_readfirstlane(blockIdx.x / per8), in = blockIdx.x - oct * per8;
+  const int rt = in >> 3, group = oct * 8 + (in & 7), heads = p.B * p.Hk;
+  const int split = __builtin_amdgcn_readfirstlane(group / heads), bh = group - split * heads;
+  if (split >= p.n_split) return;
+  const int b = __builtin_amdgcn_readfirstlane(bh / p.Hk), h = bh - b * p.Hk;
+  const TreeWalk w = tree_walk(p, b, h, lane);
+  const int row0 = rt * kRows, rows = w.q_len * p.G;
+  if (row0 >= rows) return;
+  const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
+  if (split > 0 && t_lo >= w.n_tiles) return;
+  const bool whole = w.n_tiles <= p.split_tiles;
+
+  const int i0 = __builtin_amdgcn_readfirstlane(row0 / p.G);
+  if (p.mask) {
+    const int nodes = min((row0 + kRows - 1) / p.G, w.q_len - 1) - i0 + 1;
+    const uint32_t* src = p.mask + ((size_t)b * p.n_q + i0) * p.words;
+    for (int x = tid; x < nodes * p.words; x += 256) bits[x / p.words][x % p.words] = src[x];
+  }
+  if (tid == 0) wild = 0;
+
+  // the wave's rows, and with kRG = 2 its half of a tile
+  const int wrow = row0 + 32 * (wave % kRG), kh0 = kRG == 2 ? wave >> 1 : 0;
+  const bool active = wrow < rows;
+  const int r = wrow + l32, node = min(r / p.G, w.q_len - 1);
+  u32x4 qf[KK];
+  {
+    const uint16_t* q =
+        static_cast<const uint16_t*>(p.q) + (((size_t)b * p.n_q + node) * p.H + h * p.G + min(r, rows - 1) % p.G) * D + 8 * half;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[kk] = ld_global16(q + 16 * kk);
+  }
+  f32x16 acc[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) acc[m] = f32x16{0};
+  const float c2 = p.scale_log2;
+  float m_run = softmax_floor(c2), l_run = 0.f;
+
+  // Bit j: whether the lane's row sees token t0 + j.
+  auto sees = [&](int t0) __attribute__((always_inline)) { return tree_sees(p, w, bits[p.mask ? node - i0 : 0], node, t0); };
+
+  // A thread's pieces of a tile: key row and chunk, value row and granule (two of codes).
+  u32x4 kc[NP], vc[NP];
+  auto krow_of = [&](int i) { return (tid + 256 * i) / (D / 8); };
+  const int kcol = tid % (D / 8);
+  const int vgran = tid & 7;
+  auto vrow_of = [&](int i) { return (tid + 256 * i) / 8; };
+  constexpr int E = 2;
+  const uint8_t *const kp = static_cast<const uint8_t*>(p.k), *const vp = static_cast<const uint8_t*>(p.v);
+  const uint32_t vrow = vrow_of(0) * (uint32_t)p.P * E + 8 * vgran * E;  // (within one page)
+  auto load = [&](const TreePlace& t) __attribute__((always_inline)) {
+    const int64_t next = (int64_t)32 * p.P * E;  // to the thread's next value row
+    if (t.one) {
+      const uint8_t *kb = kp + (t.base + (int64_t)t.off * D) * E, *vb = vp + (t.base + t.off) * E;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        kc[i] = ld_at(kb, 16 * (tid + 256 * i));
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        vc[i] = ld_at(vb, vrow);
+        vb += next;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        int off;
+        const int row = krow_of(i);
+        const TreePage e = tree_granule(p, pages, t, row >> 3, off);
+        kc[i] = ld_global16(kp + (e.at + (int64_t)(off + (row & 7)) * D + kcol * (16 / E)) * E);
+      }
+      int off;
+      const TreePage e = tree_granule(p, pages, t, vgran, off);
+      const uint8_t* vb = vp + (e.at + (int64_t)vrow_of(0) * p.P + off) * E;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        vc[i] = ld_global16(vb);
+        vb += next;
+      }
+    }
+  };
+  // What lies past the sequence's end may be anything, and becomes 0; so does what not every row sees and
+  // is no finite number (it reaches the rows that see it at the end).
+  auto clean = [&](u32x4 v, int t0) __attribute__((always_inline)) {
+    uint32_t on = low_bits(clampi(w.len - min(t0, w.len), 0, 8));
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const bool bad = (v[x >> 1] >> (16 * (x & 1)) & 0x7f80u) == 0x7f80u;
+      if (bad && t0 + x >= w.base && (on >> x & 1u)) {
+        on &= ~(1u << x);
+        wild = 1;
+      }
+    }
+    return keep8(v, on);
+  };
+  auto put = [&](int buf, const TreePlace& t) __attribute__((always_inline)) {
+    uint8_t* ksm = smem + buf * (L::kTileK + L::kTileV);
+    uint8_t* vsm = ksm + L::kTileK;
+    const bool some = !t.one || t.first + 64 > w.base;  // (some row may not see all of it)
+    const int t0 = some ? tree_token(p, pages, t, vgran) : 0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int row = krow_of(i), dim = vrow_of(i);
+      uint8_t* kd = ksm + row * L::kRowK;
+      uint8_t* vd = vsm + dim * L::kRowV;
+      *reinterpret_cast<u32x4*>(kd + ((kcol ^ L::swz_k(row)) << 4)) = kc[i];
+      *reinterpret_cast<u32x4*>(vd + ((vgran ^ L::swz_v(dim)) << 4)) = __builtin_expect(some, 0) ? clean(vc[i], t0) : vc[i];
+    }
+  };
+
+  const int krow = (l32 & ~12) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);  // bits 2 and 3 swapped
+  auto compute = [&](const TreePlace& t, int buf) __attribute__((always_inline)) {
+    const uint8_t* ksm = smem + buf * (L::kTileK + L::kTileV);
+    const uint8_t* vsm = ksm + L::kTileK;
+    f32x16 s[KH];
+#pragma unroll
+    for (int x = 0; x < KH; ++x) {
+      s[x] = f32x16{0};
+      const uint8_t* row = ksm + (32 * (kh0 + x) + krow) * L::kRowK;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s[x] = mfma32(ld_lds16(row + (((2 * kk + half) ^ L::swz_k(krow)) << 4)), qf[kk], s[x]);
+    }
+    if (__builtin_expect(!t.one || t.first + 64 > w.base, 0)) {
+#pragma unroll
+      for (int x = 0; x < KH; ++x)
+#pragma unroll
+        for (int gr = 0; gr < 2; ++gr) {
+          const uint32_t on = sees(tree_token(p, pages, t, 4 * (kh0 + x) + 2 * gr + half));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s[x][8 * gr + j] = hidden(on, j, s[x][8 * gr + j]);
+        }
+    }
+    // The reference maximum moves only when a score exceeds it by more than 8 in exp2 units.
+    float mx = s[0][0];
+#pragma unroll
+    for (int x = 0; x < KH; ++x)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[x][j]);
+    if (__any(mx * c2 > m_run * c2 + 8.f)) {
+      const float top = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = top * c2 > m_run * c2 + 8.f ? top : m_run;
+      const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c2);
+      l_run *= alpha;
+#pragma unroll
+      for (int m = 0; m < NM; ++m) acc[m] *= alpha;
+      m_run = m_new;
+    }
+    const float mc = m_run * c2;
+    u32x4 pk[KH][2];
+#pragma unroll
+    for (int x = 0; x < KH; ++x)
+#pragma unroll
+      for (int gr = 0; gr < 2; ++gr) {
+        float sum[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[x][8 * gr + 2 * j], c2, -mc));
+          const float f = __builtin_amdgcn_exp2f(fmaf(s[x][8 * gr + 2 * j + 1], c2, -mc));
+          sum[j] = e + f;
+          pk[x][gr][j] = pack_bf16(e, f);
+        }
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+#pragma unroll
+    for (int x = 0; x < KH; ++x)
+#pragma unroll
+      for (int gr = 0; gr < 2; ++gr)
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+          acc[m] = mfma32(ld_lds16(vsm + (32 * m + l32) * L::kRowV +
+                                   (((4 * (kh0 + x) + 2 * gr + half) ^ L::swz_v(l32)) << 4)), pk[x][gr], acc[m]);
+  };
+
+  const int chunk = ((kTreePages - 2) * p.gpp) / 8;  // tiles whose pages fit the table
+  for (int c_lo = t_lo; c_lo < t_hi; c_lo += chunk) {
+    const int n = min(chunk, t_hi - c_lo);
+    const int li0 = __builtin_amdgcn_readfirstlane(c_lo * 8 / p.gpp), at0 = c_lo * 8 - li0 * p.gpp;
+    if (c_lo > t_lo) __syncthreads();
+    tree_pages(p, w, b, h, li0, (at0 + n * 8 - 1) / p.gpp + 1, D, tid, 256, pages);
+    __syncthreads();
+    const int on_pages = __builtin_amdgcn_readfirstlane(8 / p.gpp), on_rest = 8 - on_pages * p.gpp;
+    auto next = [&](const TreePlace& from) {
+      TreePlace t = from;
+      t.at += on_rest;
+      t.li += on_pages;
+      if (t.at >= p.gpp) {
+        t.at -= p.gpp;
+        ++t.li;
+      }
+      tree_place(p, pages, 8, t);
+      return t;
+    };
+    TreePlace now, ahead;  // the tile computed, the one after it (its loads are on their way)
+    now.li = 0;
+    now.at = at0;
+    tree_place(p, pages, 8, now);
+    load(now);
+    put(0, now);
+    if (n > 1) {
+      ahead = next(now);
+      load(ahead);
+    }
+    lds_barrier();
+    for (int t = 0; t < n; ++t) {
+      if (active) compute(now, t & 1);
+      if (t + 1 < n) {
+        put((t + 1) & 1, ahead);
+        now = ahead;
+      }
+      if (t + 2 < n) {
+        ahead = next(now);
+        load(ahead);
+      }
+      lds_barrier();
+    }
+  }
+  __syncthreads();
+  if (wild && active && kh0 == 0) {
+    // (what was taken out of the tiles, for the rows that see it)
+    tree_wild(p, w, b, h, D, t_lo * 8, t_hi * 8, [&](size_t, size_t at, int) { return pool_value<uint16_t>(p, at); }, [&](int t0, int j, auto&& value) {
+      if (sees(t0) >> j & 1u) {
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) acc[m][x] += value(32 * m + 8 * (x >> 2) + 4 * half + (x & 3));
+      }
+    });
+  }
+  const int row = wrow + l32, i = row / p.G;
+  float l = l_run + __shfl_xor(l_run, 32);
+  if constexpr (kRG == 2) {
+    // join the two halves of the tiles: the second one's sums go through LDS
+    __syncthreads();
+    float* osm = reinterpret_cast<float*>(smem) + (wave & 1) * (32 * D + 64);
+    if (kh0 == 1) {
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)  // [dims / 4][row], so that lanes write side by side
+          *reinterpret_cast<f32x4*>(osm + ((8 * m + 2 * x + half) * 32 + l32) * 4) =
+              f32x4{acc[m][4 * x], acc[m][4 * x + 1], acc[m][4 * x + 2], acc[m][4 * x + 3]};
+      if (half == 0) {
+        osm[32 * D + l32] = m_run;
+        osm[32 * D + 32 + l32] = l;
+      }
+    }
+    __syncthreads();
+    if (kh0 == 1) return;
+    const float m_other = osm[32 * D + l32], top = fmaxf(m_run, m_other);
+    const float a = __builtin_amdgcn_exp2f((m_run - top) * c2), c = __builtin_amdgcn_exp2f((m_other - top) * c2);
+    l = a * l + c * osm[32 * D + 32 + l32];
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * x + half) * 32 + l32) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[m][4 * x + e] = a * acc[m][4 * x + e] + c * y[e];
+      }
+    m_run = top;
+  }
+  if (!active || i >= w.q_len) return;
+  if (whole) {
+    const int head = h * p.G + row % p.G;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float o[4] = {acc[m][4 * x], acc[m][4 * x + 1], acc[m][4 * x + 2], acc[m][4 * x + 3]};
+        tree_store<uint16_t, 4>(p, D, b, i, head, 32 * m + 8 * x + 4 * half, o, m_run, l, m == 0 && x == 0 && half == 0);
+      }
+  } else {
+    const size_t part = ((size_t)bh * p.n_split + split) * p.part_rows + row;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<f32x4*>(p.part_o + part * D + 32 * m + 8 * x + 4 * half) =
+            f32x4{acc[m][4 * x], acc[m][4 * x + 1], acc[m][4 * x + 2], acc[m][4 * x + 3]};
+    if (half == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_run, l};
+  }
+}
+
 // Joins the pieces of a row in an order that does not depend on the launch's timing: kW groups of D / 4
 // lanes a row, four dims a lane, each every kW-th piece, then the groups in order.
-template <typename T, int D, int kTile, int kW>
+template <typename T, int D, int kW>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kW);
   __shared__ __attribute__((aligned(16))) float osm[kW == 1 ? 1 : kRows * kW * D];
@@ -563,7 +862,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   const int tiles = (p.part_rows + kRows - 1) / kRows;
   const int bh = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles), b = __builtin_amdgcn_readfirstlane(bh / p.Hk);
   const int h = bh - b * p.Hk;
-  const TreeWalk w = tree_walk<kTile>(p, b, h, lane);
+  const TreeWalk w = tree_walk(p, b, h, lane);
   if (w.n_tiles <= p.split_tiles) return;
   const int row = tid / (kLanes * kW), r = (blockIdx.x - bh * tiles) * kRows + row;
   const int grp = tid / kLanes % kW, d0 = 4 * (tid % kLanes), i = r / p.G;
@@ -608,28 +907,22 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   if (mine) tree_store<T, 4>(p, D, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
 
-template <int H, int D, int kCols>
-void launch_tree(const TreeAttnParams& p, hipStream_t s) {
-  const int groups = p.n_split * p.B * p.Hk;
-  tree_attn_kernel<H, D, kCols, 4><<<(groups + 7) / 8 * 8 * p.n_rt, 256, 0, s>>>(p);
-}
-
-template <int H, int D>
-hipError_t launch_held(const TreeAttnParams& p, hipStream_t s) {
-  const int cols = p.rows_per_item / 16;
-  if (cols == 1) launch_tree<H, D, 1>(p, s);
-  else if (cols == 2) launch_tree<H, D, 2>(p, s);
-  else if constexpr (H == kCodes || H == kBf16) launch_tree<H, D, 4>(p, s);
+template <typename T, int D>
+hipError_t launch_pool(const TreeAttnParams& p, hipStream_t s) {
+  const int grid = (p.n_split * p.B * p.Hk + 7) / 8 * 8 * p.n_rt;
+  if (p.rows_per_item == 16) tree_attn_kernel<T, D, 1, 4><<<grid, 256, 0, s>>>(p);
+  else if (p.rows_per_item == 32) tree_attn_kernel<T, D, 2, 4><<<grid, 256, 0, s>>>(p);
+  else if constexpr (sizeof(T) == 2) {
+    if (p.rows_per_item == 64) tree_wide_kernel<D, 2><<<grid, 256, 0, s>>>(p);
+    else tree_wide_kernel<D, 4><<<grid, 256, 0, s>>>(p);
+  }
   if (p.n_split > 1) {
-    constexpr int kTile = H == kF32 ? 32 : 64;
-    // eight groups a row while the rows alone do not fill the chip
-    if ((int64_t)p.B * p.Hk * p.part_rows <= 8192) {
-      constexpr int kRows = 256 / (D / 4 * (D == 128 ? 8 : 16));
-      tree_join_kernel<QType<H>, D, kTile, D == 128 ? 8 : 16><<<p.B * p.Hk * ((p.part_rows + kRows - 1) / kRows), 256, 0, s>>>(p);
-    } else {
-      constexpr int kRows = 256 / (D / 4);
-      tree_join_kernel<QType<H>, D, kTile, 1><<<p.B * p.Hk * ((p.part_rows + kRows - 1) / kRows), 256, 0, s>>>(p);
-    }
+    // several groups of lanes a row while the rows alone do not fill the chip
+    constexpr int kMost = 256 / (D / 4);  // rows of a workgroup
+    if ((int64_t)p.B * p.Hk * p.part_rows <= 8192)
+      tree_join_kernel<T, D, kMost><<<p.B * p.Hk * p.part_rows, 256, 0, s>>>(p);
+    else
+      tree_join_kernel<T, D, 1><<<p.B * p.Hk * ((p.part_rows + kMost - 1) / kMost), 256, 0, s>>>(p);
   }
   return hipGetLastError();
 }
@@ -641,33 +934,26 @@ hipError_t launch_tree_mask(int B, const TreeMaskParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-int tree_tile(int dtype, bool eight) { return dtype == HSA_DTYPE_F32 && !eight ? 32 : 64; }
-
-int64_t plan_tree(TreeAttnParams& p, int dtype, bool eight, int64_t list) {
-  p.nb = (p.P + kScaleTok - 1) / kScaleTok;
+int64_t plan_tree(TreeAttnParams& p, int dtype, int64_t list) {
   p.gpp = p.P / 8;
   p.gmul = 65536 / p.gpp + 1;
   const int64_t rows = (int64_t)p.n_q * p.G;
-  p.rows_per_item = rows <= 16 ? 16 : (rows <= 32 || dtype == HSA_DTYPE_F32 ? 32 : 64);
+  p.rows_per_item = rows <= 16 ? 16 : (rows <= 32 || dtype == HSA_DTYPE_F32 ? 32 : (rows <= 64 ? 64 : 128));
   p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
   p.part_rows = p.n_rt * p.rows_per_item;
-  const int tile = tree_tile(dtype, eight);
-  const int64_t tiles = std::max<int64_t>(1, (list * p.P + tile - 1) / tile);
+  p.tile = p.rows_per_item > 32 ? 64 : kTreeTile;
+  const int64_t tiles = std::max<int64_t>(1, (list * p.P + p.tile - 1) / p.tile);
   const int64_t items = (int64_t)p.B * p.Hk * p.n_rt;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kTreeMaxSplit, tiles / 16));
-  const int64_t n = std::min((1024 + items - 1) / items, most);
+  const int64_t n = std::min((4096 + items - 1) / items, most);
   p.split_tiles = (int)((tiles + n - 1) / n);
   p.n_split = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
   return n * p.part_rows;
 }
 
-hipError_t launch_tree_attention(int dtype, int d, bool eight, const TreeAttnParams& p, hipStream_t s) {
-  if (eight) {
-    if (dtype == HSA_DTYPE_BF16) return d == 128 ? launch_held<kCodes, 128>(p, s) : launch_held<kCodes, 64>(p, s);
-    return d == 128 ? launch_held<kCodesF32, 128>(p, s) : launch_held<kCodesF32, 64>(p, s);
-  }
-  if (dtype == HSA_DTYPE_BF16) return d == 128 ? launch_held<kBf16, 128>(p, s) : launch_held<kBf16, 64>(p, s);
-  return d == 128 ? launch_held<kF32, 128>(p, s) : launch_held<kF32, 64>(p, s);
+hipError_t launch_tree_attention(int dtype, int d, const TreeAttnParams& p, hipStream_t s) {
+  if (dtype == HSA_DTYPE_BF16) return d == 128 ? launch_pool<uint16_t, 128>(p, s) : launch_pool<uint16_t, 64>(p, s);
+  return d == 128 ? launch_pool<float, 128>(p, s) : launch_pool<float, 64>(p, s);
 }
 
 }  // namespace hsa
