@@ -1445,10 +1445,11 @@ hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_hea
   p.words = (n_q + 31) / 32;
   p.k_max = k_max;
   p.n_cur = n_cur;
-  const int64_t parts = plan_tree(p, cfg->dtype, (int64_t)k_max + n_cur);
+  plan_tree(p, cfg->dtype, cfg->head_dim, (int64_t)k_max + n_cur);
   const int64_t heads = (int64_t)cfg->batch * kv_heads;
   if (heads * p.n_split * p.n_rt + 8 * p.n_rt > kMaxGrid || heads * p.part_rows > kMaxGrid) return HSA_ERR_UNSUPPORTED;
-  ws = parts > p.part_rows ? align_up((size_t)(parts * heads * (cfg->head_dim + 2)) * 4) : 0;
+  const int64_t parts = tree_part_rows(cfg->dtype, cfg->head_dim, p.P, heads, (int64_t)n_q * p.G, (int64_t)k_max + n_cur);
+  ws = align_up((size_t)(parts * heads * (cfg->head_dim + 2)) * 4);
   return HSA_OK;
 }
 

@@ -78,21 +78,39 @@ __global__ __launch_bounds__(kThreads) void keep_pool_kernel(TokenKeepParams p) 
   }
 }
 
-// A code in units of another scale, 2^shift of its own.
+// Four codes in units of another scale.
+__device__ __forceinline__ uint32_t recode4(uint32_t w, float shift) {
+  return codes4(saturate(code_to_f32(w & 255u) * shift, kCodeMax), saturate(code_to_f32(w >> 8 & 255u) * shift, kCodeMax),
+                saturate(code_to_f32(w >> 16 & 255u) * shift, kCodeMax), saturate(code_to_f32(w >> 24) * shift, kCodeMax), 1.f);
+}
 __device__ __forceinline__ uint8_t recode(uint32_t code, float shift) {
   return (uint8_t)codes2(saturate(code_to_f32(code) * shift, kCodeMax), 0.f, 1.f);
 }
+// Magnitudes of four codes, NaN as 0.
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w) {
+  w &= 0x7f7f7f7fu;
+  return w & ~((((w + 0x01010101u) & 0x80808080u) >> 7) * 255u);
+}
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {  // of two 16-bit numbers each
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+constexpr int kKeepBlocks = HSA_MAX_TREE / 8 + 2;  // scale blocks that a run of tokens touches (pages of 8)
 
 // The 8-bit cache: the keys or values of one head. The kept tokens' numbers are appended as
 // hsa_cache8_write appends them: a block that begins with them takes the smallest scale that holds
-// them, one with older tokens keeps the larger of its own and that. A wave takes a block.
+// them, one with older tokens keeps the larger of its own and that. Codes wait in shared memory, keys as [token][dim] in
+// 16-byte pieces, values as [dim][token], until every one is there; then they go out, in runs of four where a
+// value row has them.
 template <int D>
 __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p) {
-  __shared__ __attribute__((aligned(16))) uint8_t buf[HSA_MAX_TREE * D];  // [token][dim]
+  extern __shared__ __attribute__((aligned(16))) uint8_t buf[];
   __shared__ TokenPlace from[HSA_MAX_TREE];
-  __shared__ int16_t exps[HSA_MAX_TREE];     // of the token's block, without the bias
-  __shared__ int needs[HSA_MAX_TREE];        // the smallest exponent that holds it
+  __shared__ int exps[HSA_MAX_TREE];      // of the token's block, without the bias
+  __shared__ uint32_t most[HSA_MAX_TREE]; // its largest magnitude
   __shared__ bool ok[HSA_MAX_TREE];
+  __shared__ int block_e[kKeepBlocks], block_old[kKeepBlocks];
   const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y, h = blockIdx.x >> 1;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool values = blockIdx.x & 1;
@@ -105,65 +123,131 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
     TokenPlace to;
     const bool in = place_of(p, b, first + p.index[(size_t)b * p.n + tid], from[tid]);
     ok[tid] = place_of(p, b, first + tid, to) && in;
-    exps[tid] = in ? (int16_t)(pool_exp[(from[tid].slot * p.H + h) * nb + from[tid].off / kScaleTok] - 127) : 0;
+    exps[tid] = in ? (int)pool_exp[(from[tid].slot * p.H + h) * nb + from[tid].off / kScaleTok] - 127 : 0;
+    most[tid] = 0;
   }
   __syncthreads();
+  constexpr int C = D / 16;
   if (!values) {
-    for (int x = tid; x < n * (D / 16); x += kThreads) {
-      const int i = x / (D / 16), c = x % (D / 16);
-      if (ok[i])
-        *reinterpret_cast<u32x4*>(buf + i * D + 16 * c) =
-            ld_global16(pool + ((from[i].slot * p.H + h) * p.P + from[i].off) * D + 16 * c);
+    for (int x = tid; x < n * C; x += kThreads) {
+      const int i = x / C, c = x % C;
+      if (!ok[i]) continue;
+      const u32x4 w = ld_global16(pool + ((from[i].slot * p.H + h) * p.P + from[i].off) * D + 16 * c);
+      *reinterpret_cast<u32x4*>(buf + i * D + 16 * c) = w;
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t y = magnitudes(w[j]);
+        m = max2(m, max2(y & 0x00ff00ffu, y >> 8 & 0x00ff00ffu));
+      }
+      atomicMax(most + i, max(m & 0xffffu, m >> 16));
     }
   } else {
-    for (int x = tid; x < n * D; x += kThreads) {
-      const int c = x / n, i = x - c * n;
-      if (ok[i]) buf[i * D + c] = pool[((from[i].slot * p.H + h) * D + c) * p.P + from[i].off];
+    for (int i = lane; i < n; i += 64) {  // a token a lane, every fourth dim a wave
+      if (!ok[i]) continue;
+      const uint8_t* src = pool + ((from[i].slot * p.H + h) * D + wave) * p.P + from[i].off;
+      uint32_t m = 0;
+#pragma unroll 8
+      for (int c = 0; c < D / 4; ++c) {
+        const uint32_t w = src[(size_t)(4 * c) * p.P];
+        buf[(wave + 4 * c) * n + i] = (uint8_t)w;
+        m = max(m, magnitudes(w));
+      }
+      atomicMax(most + i, m);
     }
   }
-  __syncthreads();
-  if (tid < n) {
-    uint32_t most = 0;  // largest magnitude, NaN apart
-    for (int c = 0; c < D; ++c) {
-      const uint32_t m = buf[tid * D + c] & 0x7fu;
-      most = m != 0x7fu ? max(most, m) : most;
-    }
-    needs[tid] = ok[tid] && most ? clampi(scale_exponent(code_to_f32(most)) + exps[tid], kScaleMin, kScaleMax) : kScaleMin;
-  }
-  __syncthreads();
   // destination blocks: those of tokens [t0, t1) of the table
   const int64_t t0 = first > 0 ? first : 0, cap = (int64_t)p.max_pages * p.P;
   const int64_t t1 = first + n < cap ? first + n : cap;
-  if (t0 >= t1) return;
+  if (t0 >= t1) return;  // (every thread)
   const int page0 = (int)t0 / p.P, g0 = ((int)t0 - page0 * p.P) / kScaleTok;
   const int page1 = (int)(t1 - 1) / p.P, g1 = ((int)(t1 - 1) - page1 * p.P) / kScaleTok;
   const int blocks = (page1 - page0) * nb + g1 - g0 + 1;
+  __syncthreads();
+  struct Block {
+    size_t head;
+    int boff, o0, o1, i0;  // first token in its page; kept tokens [o0, o1) of it, the first of them i0
+  };
+  auto block_of = [&](int u, int& blk) {
+    Block x;
+    const int page = page0 + (g0 + u) / nb;
+    blk = (g0 + u) % nb;
+    x.boff = blk * kScaleTok;
+    const int64_t base = (int64_t)page * p.P + x.boff;
+    const int len = min(kScaleTok, p.P - x.boff);
+    x.o0 = t0 > base ? (int)(t0 - base) : 0;
+    x.o1 = t1 - base < len ? (int)(t1 - base) : len;
+    x.i0 = (int)(base + x.o0 - first);
+    x.head = (size_t)clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1) * p.H + h;
+    return x;
+  };
+  // a wave takes a block's scale: a lane a token
   for (int u = wave; u < blocks; u += kThreads / 64) {
-    const int page = page0 + (g0 + u) / nb, blk = (g0 + u) % nb, boff = blk * kScaleTok;
-    const int64_t base = (int64_t)page * p.P + boff;
-    const int len = min(kScaleTok, p.P - boff);
-    const int o0 = t0 > base ? (int)(t0 - base) : 0, o1 = t1 - base < len ? (int)(t1 - base) : len;
-    const int i0 = (int)(base + o0 - first), ntok = o1 - o0;
-    const size_t slot = clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1);
-    const size_t head = slot * p.H + h;
-    int e = lane < ntok ? needs[i0 + lane] : kScaleMin;
+    int blk;
+    const Block x = block_of(u, blk);
+    int e = kScaleMin;
+    if (lane < x.o1 - x.o0) {
+      const int i = x.i0 + lane;
+      if (ok[i] && most[i]) e = clampi(scale_exponent(code_to_f32(most[i])) + exps[i], kScaleMin, kScaleMax);
+    }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) e = max(e, __shfl_xor(e, m));
-    const int e_old = (int)pool_exp[head * nb + blk] - 127;
-    if (o0 > 0) e = max(e, e_old);
-    if (lane == 0) pool_exp[head * nb + blk] = (uint8_t)(e + 127);
-    const bool grow = o0 > 0 && e > e_old;
-    const float shift = pow2i(e_old - e);
-    const int r0 = grow ? 0 : o0;  // older codes are written again only if the scale grows
-    const int rows = o1 - r0;
-    for (int x = lane; x < rows * D; x += 64) {
-      const int o = r0 + (values ? x % rows : x / D), c = values ? x / rows : x % D;
-      uint8_t* dst = pool + (values ? (head * D + c) * p.P + boff + o : (head * p.P + boff + o) * D + c);
-      if (o < o0) {
-        *dst = recode(*dst, shift);
-      } else {
-        const int i = i0 + o - o0;
-        if (ok[i]) *dst = recode(buf[i * D + c], pow2i(exps[i] - e));
+    uint8_t* at = pool_exp + x.head * nb + blk;
+    const int old = (int)*at - 127;
+    if (x.o0 > 0) e = max(e, old);
+    if (lane == 0) {
+      block_e[u] = e;
+      block_old[u] = old;
+      *at = (uint8_t)(e + 127);
+    }
+  }
+  __syncthreads();
+  for (int u = 0; u < blocks; ++u) {
+    int blk;
+    const Block x = block_of(u, blk);
+    const int e = block_e[u];
+    const float shift = pow2i(block_old[u] - e);
+    const int r0 = x.o0 > 0 && e > block_old[u] ? 0 : x.o0;  // older codes are written again only if the scale grows
+    if (!values) {
+      uint8_t* dst = pool + (x.head * p.P + x.boff) * D;
+      for (int y = tid; y < (x.o1 - r0) * C; y += kThreads) {
+        const int o = r0 + y / C, c = y % C;
+        u32x4* at = reinterpret_cast<u32x4*>(dst + o * D + 16 * c);
+        const int i = x.i0 + o - x.o0;
+        if (o >= x.o0 && !ok[i]) continue;
+        u32x4 w = o < x.o0 ? *at : *reinterpret_cast<const u32x4*>(buf + i * D + 16 * c);
+        const float by = o < x.o0 ? shift : pow2i(exps[i] - e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = recode4(w[j], by);
+        *at = w;
+      }
+    } else {
+      uint8_t* dst = pool + x.head * D * p.P + x.boff;
+      const int q0 = r0 / 4, quads = (x.o1 + 3) / 4 - q0;
+      for (int y = tid; y < quads * D; y += kThreads) {
+        const int c = y / quads, o = 4 * (q0 + y - c * quads);
+        uint8_t* at = dst + (size_t)c * p.P + o;  // (4-byte aligned: rows of 8 tokens, blocks of 64)
+        uint32_t w = 0;
+        bool all = true;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = x.i0 + o + j - x.o0;
+          const bool kept = o + j >= x.o0 && o + j < x.o1 && ok[max(i, 0)], older = o + j >= r0 && o + j < x.o0;
+          uint32_t code = 0;
+          if (kept) code = recode(buf[c * n + i], pow2i(exps[i] - e));
+          else if (older) code = recode(at[j], shift);
+          else all = false;
+          w |= code << (8 * j);
+        }
+        if (all) {
+          *reinterpret_cast<uint32_t*>(at) = w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = x.i0 + o + j - x.o0;
+            if (o + j >= r0 && o + j < x.o1 && (o + j < x.o0 || ok[i])) at[j] = (uint8_t)(w >> (8 * j));
+          }
+        }
       }
     }
   }
@@ -173,8 +257,8 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
 
 hipError_t launch_token_keep(int dtype, int d, int B, bool eight, const TokenKeepParams& p, hipStream_t s) {
   if (eight) {
-    if (d == 128) keep_codes_kernel<128><<<dim3(2 * p.H, B), kThreads, 0, s>>>(p);
-    else keep_codes_kernel<64><<<dim3(2 * p.H, B), kThreads, 0, s>>>(p);
+    if (d == 128) keep_codes_kernel<128><<<dim3(2 * p.H, B), kThreads, p.n * 128, s>>>(p);
+    else keep_codes_kernel<64><<<dim3(2 * p.H, B), kThreads, p.n * 64, s>>>(p);
     return hipGetLastError();
   }
   const bool half = dtype == HSA_DTYPE_BF16;

@@ -293,12 +293,15 @@ struct TreeAttnParams {
   int32_t gpp, gmul;          // granules (8 tokens) per page, 65536 / gpp + 1
   int32_t rows_per_item, n_rt, part_rows;
   int32_t tile;               // tokens of a tile
+  int32_t waves;              // of a workgroup of up to 32 rows
   int32_t split_tiles, n_split;  // tiles per piece of an item, pieces of the longest item
 };
 
-// Plans the launch for lists of at most `list` pages. Returns rows of partial outputs that a key head
-// needs at most, for this list or a shorter one.
-int64_t plan_tree(TreeAttnParams& p, int dtype, int64_t list);
+// Plans the launch for lists of at most `list` pages.
+void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list);
+// Most rows of partial outputs (n_split * part_rows) that plan_tree gives a key head for any list up to `list` pages.
+// heads: B * Hk, rows: n_q * G.
+int64_t tree_part_rows(int dtype, int d, int P, int64_t heads, int64_t rows, int64_t list);
 hipError_t launch_tree_attention(int dtype, int d, const TreeAttnParams& p, hipStream_t s);
 
 // ------------------------------------------------------------ kept tokens

@@ -38,6 +38,8 @@ __device__ __forceinline__ int scan_all(int x, int* buf, int& total) {
   return before + sum - x;
 }
 
+typedef int32_t i32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
+
 // The first `most` slots s with test(refs[s]), ascending, in out; returns how many there are (up to
 // `most`). Each thread takes kEach consecutive slots a round.
 template <typename Test>
@@ -47,11 +49,15 @@ __device__ __forceinline__ int list_slots(const int32_t* refs, int lo, int hi, i
   for (int s0 = lo; s0 < hi && found < most; s0 += kPlan * kEach) {
     const int mine = s0 + (int)threadIdx.x * kEach;
     uint32_t on = 0;
-    int r[kEach];
+    if (mine + kEach <= hi) {
+      i32x4a4 r[kEach / 4];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) r[i] = mine + i < hi ? refs[mine + i] : 0;
+      for (int i = 0; i < kEach / 4; ++i) r[i] = *reinterpret_cast<const i32x4a4*>(refs + mine + 4 * i);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) on |= (uint32_t)(mine + i < hi && test(r[i])) << i;
+      for (int i = 0; i < kEach; ++i) on |= (test(r[i >> 2][i & 3]) ? 1u : 0u) << i;
+    } else {
+      for (int i = 0; mine + i < hi; ++i) on |= (test(refs[mine + i]) ? 1u : 0u) << i;
+    }
     int total;
     int at = found + scan_all(__popc(on), buf, total);
     for (; on; on &= on - 1, ++at)
@@ -77,95 +83,152 @@ __device__ __forceinline__ RowPages row_pages(const SlotsParams& p, int b) {
 }
 
 // One workgroup: the wanted entries of all rows are numbered in order; what is shared is counted before
-// anything changes. ws: wanting entries and the last of them for each slot, an entry's rank among those
-// that get a slot, the free slots.
+// anything changes. Entries are taken in rounds of up to kEach a thread, 1024 apart, and stay in registers if one round
+// holds them all. ws: wanting entries and the last of them for each slot, an entry's rank among those that get a slot, the free
+// slots. Bound: a launch, and a few loads and sums of the workgroup that wait for each other.
+template <int kEach>
 __global__ __launch_bounds__(kPlan) void slots_take_kernel(SlotsParams p) {
+  constexpr int kWaves = kPlan / 64;
   __shared__ int starts[kSlotsMaxBatch + 1];  // number of a row's first wanted entry
-  __shared__ int buf[kPlan / 64];
-  const int tid = threadIdx.x;
+  __shared__ int pages[kSlotsMaxBatch];       // its page, less that number
+  __shared__ int buf[kWaves];
+  __shared__ int counts[kEach * kWaves];      // entries in need, of each wave and step of a round; sums before it
+  __shared__ int any_shared;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* wants = p.ws;
   int32_t* last = wants + p.num_slots;
   int32_t* ranks = last + p.num_slots;
   int32_t* free_slots = ranks + (size_t)p.B * p.max_pages;
+  if (tid == 0) any_shared = 0;
   int n = 0;  // wanted entries
   for (int b0 = 0; b0 < p.B; b0 += kPlan) {
     int total;
     const int b = b0 + tid;
-    const int at = n + scan_all(b < p.B ? row_pages(p, b).n : 0, buf, total);
-    if (b < p.B) starts[b] = at;
+    const RowPages r = b < p.B ? row_pages(p, b) : RowPages{0, 0, 0};
+    const int at = n + scan_all(r.n, buf, total);
+    if (b < p.B) {
+      starts[b] = at;
+      pages[b] = r.lo - at;
+    }
     n += total;
   }
   if (tid == 0) starts[p.B] = n;
   __syncthreads();
-  // row and table entry of wanted entry x
-  auto entry = [&](int x, int& b, int& page) {
-    int lo = 0, hi = p.B;  // the last row that starts at or before x
+  // The row of wanted entry x: the last one that starts at or before it, searched for, or from the row `b` of an
+  // entry before it on.
+  auto row_of = [&](int x) __attribute__((always_inline)) {
+    int lo = 0, hi = p.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (starts[mid] <= x) lo = mid;
       else hi = mid;
     }
-    b = lo;
-    page = (p.first ? max(p.first[b], 0) : 0) / p.P + x - starts[b];
-    return (size_t)b * p.max_pages + page;
+    return lo;
   };
-  // whether a slot that an entry holds is held by others too
-  auto shared = [&](int slot) { return slot >= 0 && slot < p.num_slots && p.refs[slot] > 1; };
-  for (int x = tid; x < n; x += kPlan) {
-    int b, page;
-    const int slot = p.page_table[entry(x, b, page)];
-    if (shared(slot)) {
-      wants[slot] = 0;
-      last[slot] = -1;
+  auto row_from = [&](int b, int x) __attribute__((always_inline)) {
+    while (b + 1 < p.B && starts[b + 1] <= x) ++b;
+    return b;
+  };
+  auto entry = [&](int b, int x) __attribute__((always_inline)) { return (size_t)b * p.max_pages + x + pages[b]; };
+  // a round's entries r0 + 1024 j + tid, j < steps: slots (INT32_MAX: no entry), and how many entries hold them (0: none,
+  // or past the pool)
+  const int rounds = (n + kPlan * kEach - 1) / (kPlan * kEach);
+  int slot[kEach], refs[kEach], steps = 0;
+  auto load = [&](int r0) __attribute__((always_inline)) {
+    steps = min((n - r0 + kPlan - 1) / kPlan, kEach);
+    int b = row_of(r0 + tid);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (j < steps) {
+        const int x = r0 + kPlan * j + tid;
+        b = row_from(b, x);
+        slot[j] = x < n ? p.page_table[entry(b, x)] : INT32_MAX;
+      }
     }
-  }
-  __syncthreads();
-  for (int x = tid; x < n; x += kPlan) {
-    int b, page;
-    const int slot = p.page_table[entry(x, b, page)];
-    if (shared(slot)) {
-      atomicAdd(wants + slot, 1);
-      atomicMax(last + slot, x);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (j < steps) refs[j] = slot[j] >= 0 && slot[j] < p.num_slots ? p.refs[slot[j]] : 0;
     }
-  }
+  };
+  auto each = [&](int r0, bool again, auto&& f) __attribute__((always_inline)) {
+    if (again) load(r0);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (j < steps) f(j, r0 + kPlan * j + tid);
+    }
+  };
+  for (int r = 0; r < rounds; ++r)
+    each(r * kPlan * kEach, true, [&](int j, int) {
+      if (refs[j] > 1) {
+        wants[slot[j]] = 0;
+        last[slot[j]] = -1;
+        any_shared = 1;
+      }
+    });
   __syncthreads();
+  const bool again = rounds > 1;
+  if (any_shared) {
+    for (int r = 0; r < rounds; ++r)
+      each(r * kPlan * kEach, again, [&](int j, int x) {
+        if (refs[j] > 1) {
+          atomicAdd(wants + slot[j], 1);
+          atomicMax(last + slot[j], x);
+        }
+      });
+    __syncthreads();
+  }
   // An entry needs a slot if it has none, or shares one: but the last of the entries that hold it, if
   // all of them want it, keeps it.
   int needs = 0;
-  for (int x0 = 0; x0 < n; x0 += kPlan) {
-    const int x = x0 + tid;
-    bool need = false;
-    if (x < n) {
-      int b, page;
-      const int slot = p.page_table[entry(x, b, page)];
-      need = slot < 0;
-      if (shared(slot)) need = !(ld_fresh(wants + slot) == p.refs[slot] && ld_fresh(last + slot) == x);
-    }
+  for (int r = 0; r < rounds; ++r) {
+    uint32_t need = 0;
+    each(r * kPlan * kEach, again, [&](int j, int x) {
+      bool is = slot[j] < 0;
+      if (refs[j] > 1) is = !(ld_fresh(wants + slot[j]) == refs[j] && ld_fresh(last + slot[j]) == x);
+      need |= (is ? 1u : 0u) << j;
+      const uint64_t all = __ballot(is);
+      if (lane == 0) counts[j * kWaves + wave] = __popcll(all);
+    });
+    __syncthreads();
     int total;
-    const int rank = needs + scan_all(need ? 1 : 0, buf, total);
-    if (x < n) ranks[x] = need ? rank : -1;
+    const int before = scan_all(tid < steps * kWaves ? counts[tid] : 0, buf, total);
+    if (tid < steps * kWaves) counts[tid] = before;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (j < steps) {
+        const bool is = need >> j & 1u;
+        const uint64_t all = __ballot(is);
+        const int x = r * kPlan * kEach + kPlan * j + tid;
+        if (x < n) ranks[x] = is ? needs + counts[j * kWaves + wave] + __popcll(all & ((1ull << lane) - 1)) : -1;
+      }
+    }
     needs += total;
+    if (again) __syncthreads();
   }
   const int n_free = list_slots(p.refs, 0, p.num_slots, needs, free_slots, buf, [](int r) { return r == 0; });
   if (p.moves)
     for (int x = tid; x < 3 * p.B; x += kPlan) p.moves[x] = -1;
   __syncthreads();
-  for (int x = tid; x < n; x += kPlan) {
-    const int rank = ranks[x];
-    if (rank < 0 || rank >= n_free) continue;
-    int b, page;
-    const size_t at = entry(x, b, page);
-    const int was = p.page_table[at], now = free_slots[rank];
-    p.page_table[at] = now;
-    p.refs[now] = 1;
-    if (was < 0) continue;
-    atomicSub(p.refs + was, 1);
-    const RowPages r = row_pages(p, b);
-    if (p.moves && page == r.lo && r.inside > 0) {
-      p.moves[3 * b] = was;
-      p.moves[3 * b + 1] = now;
-      p.moves[3 * b + 2] = r.inside;
-    }
+  for (int r = 0; r < rounds; ++r) {
+    int b = row_of(r * kPlan * kEach + tid);
+    each(r * kPlan * kEach, again, [&](int j, int x) {
+      const int rank = x < n ? ranks[x] : -1;
+      if (rank < 0 || rank >= n_free) return;
+      b = row_from(b, x);
+      const size_t at = entry(b, x);
+      const int was = slot[j], now = free_slots[rank];
+      p.page_table[at] = now;
+      p.refs[now] = 1;
+      if (was < 0) return;
+      atomicSub(p.refs + was, 1);
+      const RowPages w = row_pages(p, b);
+      if (p.moves && x == starts[b] && w.inside > 0) {
+        p.moves[3 * b] = was;
+        p.moves[3 * b + 1] = now;
+        p.moves[3 * b + 2] = w.inside;
+      }
+    });
   }
   if (p.missing && tid == 0) *p.missing = needs - n_free;
 }
@@ -307,7 +370,9 @@ size_t slots_fork_ints(const SlotsParams& p) { return (size_t)p.B * p.max_pages;
 size_t slots_compact_ints(const SlotsParams& p) { return 4 * (size_t)p.num_slots; }
 
 hipError_t launch_slots_take(const SlotsParams& p, hipStream_t s) {
-  slots_take_kernel<<<1, kPlan, 0, s>>>(p);
+  // (short code where there are few entries; 128 rows of 512: 57 us with 32 a thread, 82 with 8, 64 rows of 16 13.9 and 11)
+  if ((int64_t)p.B * p.max_pages <= 4 * kPlan) slots_take_kernel<4><<<1, kPlan, 0, s>>>(p);
+  else slots_take_kernel<32><<<1, kPlan, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -152,8 +152,9 @@ __device__ __forceinline__ void tree_store(const TreeAttnParams& p, int D, int b
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int e = 0; e < N; ++e) dst[e] = o[e] * inv;
+  } else if constexpr (N == 1) {
+    *dst = (uint16_t)pack_bf16(o[0] * inv, 0.f);
   } else {
-    static_assert(N % 2 == 0, "pairs");
     uint32_t* w = reinterpret_cast<uint32_t*>(dst);
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
@@ -170,6 +171,7 @@ __device__ __forceinline__ float pool_value(const TreeAttnParams& p, size_t at) 
 }
 
 constexpr int kTreeTile = 32;  // tokens of a tile of up to 32 rows
+constexpr int kBriefItems = 256, kBriefTiles = 128;  // little work: most items of 16 rows, tiles of one
 
 // Up to 16 kCols rows of one key head against a range of its tiles. A wave takes every kWaves-th tile and
 // keeps an online softmax of its own; the workgroup joins them at the end.
@@ -181,7 +183,7 @@ constexpr int kTreeTile = 32;  // tokens of a tile of up to 32 rows
 // from memory to the registers of the wave that uses them; the next tile's keys are asked for once this
 // one's scores are done with their registers, the values after its output.
 template <typename T, int D, int kCols, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kCols == 1 ? (sizeof(T) == 2 ? 3 : 2) : (sizeof(T) == 2 ? 2 : 1))
+__global__ __launch_bounds__(64 * kWaves, kWaves > 4 ? kWaves / 4 : kCols == 1 ? (sizeof(T) == 2 ? 3 : 2) : (sizeof(T) == 2 ? 2 : 1))
 void tree_attn_kernel(TreeAttnParams p) {
   constexpr bool kMat32 = sizeof(T) == 4;
   constexpr int kTile = kTreeTile, kGran = kTile / 8;  // tokens, granules of a tile
@@ -907,10 +909,27 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   if (mine) tree_store<T, 4>(p, D, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
 
+// Waves of a workgroup where the whole call is little work: as many as the registers allow.
+constexpr int brief_waves(size_t size, int d) { return size == 4 || d == 128 ? 8 : 16; }
+
+// Whether items of 16 rows with so many tiles of 32 tokens are little work (up to 16 rows a key head: less of it, there the
+// other kernel reads every token once too).
+int64_t brief_tiles(int64_t items16, int64_t rows) {
+  return items16 > kBriefItems ? 0 : rows <= 16 ? 4096 / items16 : std::min<int64_t>(kBriefTiles, 16384 / items16);
+}
+// Rows of an item otherwise, and the pieces that its list is cut into.
+int tree_rows(int dtype, int64_t rows) {
+  return rows <= 16 ? 16 : (rows <= 32 || dtype == HSA_DTYPE_F32 ? 32 : (rows <= 64 ? 64 : 128));
+}
+int64_t tree_pieces(int64_t items, int64_t tiles) {
+  return std::max<int64_t>(1, std::min<int64_t>({kTreeMaxSplit, tiles / 16, (4096 + items - 1) / items}));
+}
+
 template <typename T, int D>
 hipError_t launch_pool(const TreeAttnParams& p, hipStream_t s) {
   const int grid = (p.n_split * p.B * p.Hk + 7) / 8 * 8 * p.n_rt;
-  if (p.rows_per_item == 16) tree_attn_kernel<T, D, 1, 4><<<grid, 256, 0, s>>>(p);
+  if (p.waves > 4) tree_attn_kernel<T, D, 1, brief_waves(sizeof(T), D)><<<grid, 64 * brief_waves(sizeof(T), D), 0, s>>>(p);
+  else if (p.rows_per_item == 16) tree_attn_kernel<T, D, 1, 4><<<grid, 256, 0, s>>>(p);
   else if (p.rows_per_item == 32) tree_attn_kernel<T, D, 2, 4><<<grid, 256, 0, s>>>(p);
   else if constexpr (sizeof(T) == 2) {
     if (p.rows_per_item == 64) tree_wide_kernel<D, 2><<<grid, 256, 0, s>>>(p);
@@ -934,21 +953,56 @@ hipError_t launch_tree_mask(int B, const TreeMaskParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t plan_tree(TreeAttnParams& p, int dtype, int64_t list) {
+void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list) {
   p.gpp = p.P / 8;
   p.gmul = 65536 / p.gpp + 1;
   const int64_t rows = (int64_t)p.n_q * p.G;
-  p.rows_per_item = rows <= 16 ? 16 : (rows <= 32 || dtype == HSA_DTYPE_F32 ? 32 : (rows <= 64 ? 64 : 128));
+  auto tiles_of = [&](int tile) { return std::max<int64_t>(1, (list * p.P + tile - 1) / tile); };
+  // Little work: what counts is how many tiles a wave does after one another, and a second launch if they
+  // are cut.
+  const int64_t items16 = (int64_t)p.B * p.Hk * ((rows + 15) / 16), tiles32 = tiles_of(kTreeTile);
+  const bool brief = tiles32 <= brief_tiles(items16, rows);
+  p.waves = brief ? brief_waves(dtype == HSA_DTYPE_BF16 ? 2 : 4, d) : 4;
+  p.rows_per_item = brief ? 16 : tree_rows(dtype, rows);
   p.n_rt = (int)((rows + p.rows_per_item - 1) / p.rows_per_item);
   p.part_rows = p.n_rt * p.rows_per_item;
   p.tile = p.rows_per_item > 32 ? 64 : kTreeTile;
-  const int64_t tiles = std::max<int64_t>(1, (list * p.P + p.tile - 1) / p.tile);
-  const int64_t items = (int64_t)p.B * p.Hk * p.n_rt;
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kTreeMaxSplit, tiles / 16));
-  const int64_t n = std::min((4096 + items - 1) / items, most);
+  const int64_t tiles = tiles_of(p.tile), items = (int64_t)p.B * p.Hk * p.n_rt;
+  // pieces that little work may be cut into
+  auto may = [&](int64_t k) { return k <= kTreeMaxSplit && k * items16 <= 512 && p.waves * (k - 1) < tiles32; };
+  int64_t n = 1;
+  if (brief) {
+    // in us: a tile after another 1.7, the join 4.5
+    double best = 1e300;
+    for (int64_t k = 1; k == 1 || may(k); ++k) {
+      const double t = 1.7 * (double)((tiles + p.waves * k - 1) / (p.waves * k)) + (k > 1 ? 4.5 : 0.0);
+      if (t < best) {
+        best = t;
+        n = k;
+      }
+    }
+  } else {
+    n = tree_pieces(items, tiles);
+  }
   p.split_tiles = (int)((tiles + n - 1) / n);
   p.n_split = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
-  return n * p.part_rows;
+}
+
+int64_t tree_part_rows(int dtype, int d, int P, int64_t heads, int64_t rows, int64_t list) {
+  const int64_t items16 = heads * ((rows + 15) / 16), tiles32 = (list * P + kTreeTile - 1) / kTreeTile;
+  int64_t most = 0;
+  auto take = [&](int64_t pieces, int64_t per_item) {
+    if (pieces > 1) most = std::max(most, pieces * ((rows + per_item - 1) / per_item * per_item));
+  };
+  if (items16 <= kBriefItems) {  // as many pieces as the longest list of little work may be cut into
+    const int64_t longest = std::min(tiles32, brief_tiles(items16, rows)), waves = brief_waves(dtype == HSA_DTYPE_BF16 ? 2 : 4, d);
+    take(std::min<int64_t>({kTreeMaxSplit, 512 / items16, (longest - 1) / waves + 1}), 16);
+  }
+  if (tiles32 > brief_tiles(items16, rows)) {
+    const int64_t per = tree_rows(dtype, rows), tile = per > 32 ? 64 : kTreeTile;
+    take(tree_pieces(heads * ((rows + per - 1) / per), (list * P + tile - 1) / tile), per);
+  }
+  return most;
 }
 
 hipError_t launch_tree_attention(int dtype, int d, const TreeAttnParams& p, hipStream_t s) {

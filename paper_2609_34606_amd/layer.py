@@ -37,10 +37,17 @@ class HsaLayer:
         self.page_kmean = torch.zeros((batch, heads, self.max_pages, head_dim), dtype=torch.float64,
                                       device=device)
         self._ws = {}
+        self._pool, self._pool_of = None, None
 
     @property
     def pool(self) -> _h.HsaKvPool:
-        return _h.kv_pool(self.k_pool, self.v_pool, self.page_table, self.cfg)
+        """The pool's descriptor, checked anew when one of its tensors is another one."""
+        k, v, pt = self.k_pool, self.v_pool, self.page_table
+        of = (k.data_ptr(), v.data_ptr(), pt.data_ptr(), k.shape, v.shape, pt.shape, k.stride(), v.stride(), pt.stride(),
+              k.dtype, v.dtype, pt.dtype)
+        if of != self._pool_of:
+            self._pool, self._pool_of = _h.kv_pool(k, v, pt, self.cfg), of
+        return self._pool
 
     def workspace(self, key, nbytes: int):
         if nbytes == 0:
@@ -325,6 +332,9 @@ class HsaSlots:
             raise ValueError("the table's tensors must be on one device")
         self.cfg = _h.config(batch, 1, 64, page_size, _h.HSA_DTYPE_BF16)
         self.table = _h.slot_table(page_table, refs, self.cfg)
+        # (calls on one table follow each other, so one workspace serves them all)
+        self._ws = torch.empty(_h.hsa_slots_workspace_size(self.cfg, self.table.num_slots, self.table.max_pages),
+                               dtype=torch.uint8, device=device)
 
     def take(self, first, end, moves=None, stream=None):
         """Makes the pages that hold tokens [first[b], end[b]) of each row (int32 [B]) its own before they are
@@ -332,13 +342,14 @@ class HsaSlots:
         _same_device(end, self.refs)
         if moves is None:
             moves = _h.empty_on((self.cfg.batch, 3), self.torch.int32, end.device, stream)
-        _h.hsa_slots_take(self.cfg, self.table, first, end, moves=moves, missing=self.missing, stream=stream)
+        _h.hsa_slots_take(self.cfg, self.table, first, end, moves=moves, missing=self.missing, ws=self._ws,
+                          stream=stream)
         return moves
 
     def fork(self, parent, stream=None):
         """Row b becomes what row parent[b] (int32 [B]; outside [0, B): itself) was, sharing its slots."""
         _same_device(parent, self.refs)
-        _h.hsa_slots_fork(self.cfg, self.table, parent, stream=stream)
+        _h.hsa_slots_fork(self.cfg, self.table, parent, ws=self._ws, stream=stream)
 
     def free(self, keep, stream=None):
         """Row b lets go of its pages behind its first keep[b] tokens (int32 [B]; 0: all, below 0: none)."""
@@ -350,5 +361,5 @@ class HsaSlots:
         new table and counts go to table_out and refs_out, or in place."""
         _same_device(moves, self.refs)
         _h.hsa_slots_compact(self.cfg, self.table, moves, moves.shape[0], table_out=table_out, refs_out=refs_out,
-                             stream=stream)
+                             ws=self._ws, stream=stream)
         return moves
