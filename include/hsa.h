@@ -886,8 +886,8 @@ hsa_status_t hsa_cache8_keep(const hsa_config_t* cfg, const hsa_cache8_t* cache,
  * num_slots; hsa_page_copy then does each layer's part of the moves. Everything is decided in a fixed order, so
  * the same tables give the same tables. A pool whose table a tier keeps (hsa_tier_*) is not for these calls.
  * Calls on one table are ordered by the caller (one stream). Of cfg, batch and page_size count. Entries
- * at or past num_slots are left alone. Errors: INVALID_ARG (NULL, sizes below 1), UNSUPPORTED (B above 8192 for
- * take and above 65535, B * max_pages or num_slots above 2^30, max_pages * P above 2^31 - 257), WORKSPACE. ws (256-byte aligned) is
+ * at or past num_slots are left alone. Errors: INVALID_ARG (NULL, sizes below 1), UNSUPPORTED (B above 65535,
+ * B * max_pages or num_slots above 2^30, max_pages * P above 2^31 - 257), WORKSPACE. ws (256-byte aligned) is
  * hsa_slots_workspace_size(...) bytes for every call that takes one; its contents do not matter.
  */
 typedef struct hsa_slots {

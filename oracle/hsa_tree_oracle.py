@@ -5,6 +5,7 @@ loops over nodes, tokens and entries, written from the definitions; attention in
 from __future__ import annotations
 
 import numpy as np
+import torch
 
 from . import hsa_cache8_oracle as C8
 
@@ -71,6 +72,45 @@ def attend(q, k, v, page_table, pages, kv_len, q_len, bits, scale):
                         lse[b, h, i] = s.max() + np.log(p.sum())
                         sa[b, h, i] = (np.abs(kk[see]) @ np.abs(q[b, i, h])).max() * scale
                         vm[b, h, i] = np.abs(vv[see]).max()
+    return o, lse, va, sa, vm
+
+
+def attend_many(q, k, v, page_table, pages, kv_len, q_len, bits, scale, device="cpu"):
+    """attend for larger calls: the same numbers, a key head's rows at once in torch's fp64."""
+    B, n_q, H, d = q.shape
+    Hk, P = k.shape[1], k.shape[2]
+    G = H // Hk
+    o, va = np.full(q.shape, np.nan), np.full(q.shape, np.nan)
+    lse, sa, vm = np.full((B, H, n_q), np.nan), np.zeros((B, H, n_q)), np.zeros((B, H, n_q))
+    put = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(device)
+    for b in range(B):
+        base, n = kv_len[b] - q_len[b], q_len[b]
+        for hk in range(Hk if n else 0):
+            pg = np.asarray([p for p in pages[b][hk] if p * P < kv_len[b]], np.int64)
+            t = (pg[:, None] * P + np.arange(P)).ravel()
+            slots, use = page_table[b, pg], t < kv_len[b]
+            kk, vv, t = put(k[slots, hk].reshape(-1, d)[use]), put(v[slots, hk].reshape(-1, d)[use]), t[use]
+            i, j = np.arange(n)[:, None], np.clip(t - base, 0, n_q - 1)
+            see = put((t < base)[None] | (j <= i if bits is None else bits[b, :n][:, j]))
+            good, any_ = torch.isfinite(vv), see.any(1)
+            for h in range(hk * G, hk * G + G):
+                qq = put(q[b, :n, h])
+                s = torch.where(see, qq @ kk.T * scale, -torch.inf)
+                top = torch.where(any_, s.max(1).values if len(t) else 0.0, 0.0)
+                p = torch.where(see, torch.exp(s - top[:, None]), 0.0)
+                l = p.sum(1)
+                x, y = p @ torch.where(good, vv, 0.0), p @ torch.where(good, vv, 0.0).abs()
+                for w in torch.nonzero(~good.all(1)).ravel().tolist():  # (values only their seers have)
+                    bad, who = torch.where(good[w], 0.0, vv[w]), see[:, w]
+                    x[who] += torch.where(good[w], 0.0, p[who, w, None] * bad)
+                    y[who] += torch.where(good[w], 0.0, p[who, w, None] * bad.abs())
+                none = ~any_[:, None]
+                o[b, :n, h] = torch.where(none, 0.0, x / l[:, None]).cpu().numpy()
+                va[b, :n, h] = torch.where(none, 0.0, y / l[:, None]).cpu().numpy()
+                lse[b, h, :n] = torch.where(any_, top + torch.log(l), -torch.inf).cpu().numpy()
+                if len(t):
+                    sa[b, h, :n] = torch.where(see, qq.abs() @ kk.abs().T, 0.0).max(1).values.cpu().numpy() * scale
+                    vm[b, h, :n] = torch.where(see, vv.abs().max(1).values, 0.0).max(1).values.cpu().numpy()
     return o, lse, va, sa, vm
 
 

@@ -1786,7 +1786,6 @@ hsa_status_t hsa_slots_take(const hsa_config_t* cfg, const hsa_slots_t* slots, c
   hsa_status_t st = slots_call(cfg, slots, p);
   if (st != HSA_OK) return st;
   if (!end) return HSA_ERR_INVALID_ARG;
-  if (p.B > kSlotsMaxBatch) return HSA_ERR_UNSUPPORTED;
   if ((st = check_ws(ws, ws_bytes, slots_ws(p))) != HSA_OK) return st;
   p.first = first;
   p.end = end;

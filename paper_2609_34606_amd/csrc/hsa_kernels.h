@@ -344,7 +344,6 @@ struct SlotsParams {
   int32_t* refs_out;
   int32_t* ws;
 };
-constexpr int kSlotsMaxBatch = 8192;
 size_t slots_take_ints(const SlotsParams& p);
 size_t slots_fork_ints(const SlotsParams& p);
 size_t slots_compact_ints(const SlotsParams& p);

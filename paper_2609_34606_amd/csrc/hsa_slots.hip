@@ -82,23 +82,36 @@ __device__ __forceinline__ RowPages row_pages(const SlotsParams& p, int b) {
   return r;
 }
 
-// One workgroup: the wanted entries of all rows are numbered in order; what is shared is counted before
-// anything changes. Entries are taken in rounds of up to kEach a thread, 1024 apart, and stay in registers if one round
-// holds them all. ws: wanting entries and the last of them for each slot, an entry's rank among those that get a slot, the free
-// slots. Bound: a launch, and a few loads and sums of the workgroup that wait for each other.
-template <int kEach>
+// An entry gets a slot of its own in the place of `was`. lead: it is the row's first wanted one.
+__device__ __forceinline__ void take_slot(const SlotsParams& p, int b, int page, int was, int now, bool lead) {
+  p.page_table[(size_t)b * p.max_pages + page] = now;
+  p.refs[now] = 1;
+  if (was < 0) return;
+  atomicSub(p.refs + was, 1);
+  const RowPages r = row_pages(p, b);
+  if (p.moves && lead && r.inside > 0) {
+    p.moves[3 * b] = was;
+    p.moves[3 * b + 1] = now;
+    p.moves[3 * b + 2] = r.inside;
+  }
+}
+
+// Small tables: one workgroup. The wanted entries of all rows are numbered in order, kEach a thread, 1024 apart, and
+// stay in registers; what is shared is counted before anything changes. ws: wanting entries and the last of them for each
+// slot, the free slots. Bound: a launch, and a few loads and sums of the workgroup that wait for each other (64
+// rows of 16 pages, a page each that most rows share: 9.2 us).
+constexpr int kSmallTable = 4 * kPlan;
 __global__ __launch_bounds__(kPlan) void slots_take_kernel(SlotsParams p) {
-  constexpr int kWaves = kPlan / 64;
-  __shared__ int starts[kSlotsMaxBatch + 1];  // number of a row's first wanted entry
-  __shared__ int pages[kSlotsMaxBatch];       // its page, less that number
+  constexpr int kEach = kSmallTable / kPlan, kWaves = kPlan / 64;
+  __shared__ int starts[kSmallTable + 1];  // number of a row's first wanted entry
+  __shared__ int pages[kSmallTable];       // its page, less that number
   __shared__ int buf[kWaves];
-  __shared__ int counts[kEach * kWaves];      // entries in need, of each wave and step of a round; sums before it
+  __shared__ int counts[kEach * kWaves];   // entries in need, of each wave and step; sums before it
   __shared__ int any_shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* wants = p.ws;
   int32_t* last = wants + p.num_slots;
-  int32_t* ranks = last + p.num_slots;
-  int32_t* free_slots = ranks + (size_t)p.B * p.max_pages;
+  int32_t* free_slots = last + p.num_slots;
   if (tid == 0) any_shared = 0;
   int n = 0;  // wanted entries
   for (int b0 = 0; b0 < p.B; b0 += kPlan) {
@@ -114,123 +127,201 @@ __global__ __launch_bounds__(kPlan) void slots_take_kernel(SlotsParams p) {
   }
   if (tid == 0) starts[p.B] = n;
   __syncthreads();
-  // The row of wanted entry x: the last one that starts at or before it, searched for, or from the row `b` of an
-  // entry before it on.
-  auto row_of = [&](int x) __attribute__((always_inline)) {
-    int lo = 0, hi = p.B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (starts[mid] <= x) lo = mid;
-      else hi = mid;
-    }
-    return lo;
-  };
-  auto row_from = [&](int b, int x) __attribute__((always_inline)) {
-    while (b + 1 < p.B && starts[b + 1] <= x) ++b;
-    return b;
-  };
-  auto entry = [&](int b, int x) __attribute__((always_inline)) { return (size_t)b * p.max_pages + x + pages[b]; };
-  // a round's entries r0 + 1024 j + tid, j < steps: slots (INT32_MAX: no entry), and how many entries hold them (0: none,
-  // or past the pool)
-  const int rounds = (n + kPlan * kEach - 1) / (kPlan * kEach);
-  int slot[kEach], refs[kEach], steps = 0;
-  auto load = [&](int r0) __attribute__((always_inline)) {
-    steps = min((n - r0 + kPlan - 1) / kPlan, kEach);
-    int b = row_of(r0 + tid);
+  // the entries 1024 j + tid: rows, slots (INT32_MAX: no entry), and how many entries hold them (0: none, or
+  // past the pool)
+  int row[kEach], slot[kEach], refs[kEach];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (j < steps) {
-        const int x = r0 + kPlan * j + tid;
-        b = row_from(b, x);
-        slot[j] = x < n ? p.page_table[entry(b, x)] : INT32_MAX;
+  for (int j = 0; j < kEach; ++j) {
+    const int x = kPlan * j + tid;
+    slot[j] = INT32_MAX;
+    row[j] = 0;
+    if (x < n) {
+      int lo = 0, hi = p.B;  // the last row that starts at or before x
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= x) lo = mid;
+        else hi = mid;
       }
+      row[j] = lo;
+      slot[j] = p.page_table[(size_t)lo * p.max_pages + x + pages[lo]];
     }
+  }
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (j < steps) refs[j] = slot[j] >= 0 && slot[j] < p.num_slots ? p.refs[slot[j]] : 0;
+  for (int j = 0; j < kEach; ++j) {
+    refs[j] = slot[j] >= 0 && slot[j] < p.num_slots ? p.refs[slot[j]] : 0;
+    if (refs[j] > 1) {
+      wants[slot[j]] = 0;
+      last[slot[j]] = -1;
+      any_shared = 1;
     }
-  };
-  auto each = [&](int r0, bool again, auto&& f) __attribute__((always_inline)) {
-    if (again) load(r0);
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (j < steps) f(j, r0 + kPlan * j + tid);
-    }
-  };
-  for (int r = 0; r < rounds; ++r)
-    each(r * kPlan * kEach, true, [&](int j, int) {
-      if (refs[j] > 1) {
-        wants[slot[j]] = 0;
-        last[slot[j]] = -1;
-        any_shared = 1;
-      }
-    });
+  }
   __syncthreads();
-  const bool again = rounds > 1;
   if (any_shared) {
-    for (int r = 0; r < rounds; ++r)
-      each(r * kPlan * kEach, again, [&](int j, int x) {
-        if (refs[j] > 1) {
-          atomicAdd(wants + slot[j], 1);
-          atomicMax(last + slot[j], x);
-        }
-      });
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (refs[j] > 1) {
+        atomicAdd(wants + slot[j], 1);
+        atomicMax(last + slot[j], kPlan * j + tid);
+      }
     __syncthreads();
   }
   // An entry needs a slot if it has none, or shares one: but the last of the entries that hold it, if
   // all of them want it, keeps it.
-  int needs = 0;
-  for (int r = 0; r < rounds; ++r) {
-    uint32_t need = 0;
-    each(r * kPlan * kEach, again, [&](int j, int x) {
-      bool is = slot[j] < 0;
-      if (refs[j] > 1) is = !(ld_fresh(wants + slot[j]) == refs[j] && ld_fresh(last + slot[j]) == x);
-      need |= (is ? 1u : 0u) << j;
-      const uint64_t all = __ballot(is);
-      if (lane == 0) counts[j * kWaves + wave] = __popcll(all);
-    });
-    __syncthreads();
-    int total;
-    const int before = scan_all(tid < steps * kWaves ? counts[tid] : 0, buf, total);
-    if (tid < steps * kWaves) counts[tid] = before;
-    __syncthreads();
+  uint32_t need = 0;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (j < steps) {
-        const bool is = need >> j & 1u;
-        const uint64_t all = __ballot(is);
-        const int x = r * kPlan * kEach + kPlan * j + tid;
-        if (x < n) ranks[x] = is ? needs + counts[j * kWaves + wave] + __popcll(all & ((1ull << lane) - 1)) : -1;
-      }
-    }
-    needs += total;
-    if (again) __syncthreads();
+  for (int j = 0; j < kEach; ++j) {
+    bool is = slot[j] < 0;
+    if (refs[j] > 1) is = !(ld_fresh(wants + slot[j]) == refs[j] && ld_fresh(last + slot[j]) == kPlan * j + tid);
+    need |= (is ? 1u : 0u) << j;
+    const uint64_t all = __ballot(is);
+    if (lane == 0) counts[j * kWaves + wave] = __popcll(all);
   }
+  __syncthreads();
+  int needs;
+  const int before = scan_all(tid < kEach * kWaves ? counts[tid] : 0, buf, needs);
+  if (tid < kEach * kWaves) counts[tid] = before;
   const int n_free = list_slots(p.refs, 0, p.num_slots, needs, free_slots, buf, [](int r) { return r == 0; });
   if (p.moves)
     for (int x = tid; x < 3 * p.B; x += kPlan) p.moves[x] = -1;
   __syncthreads();
-  for (int r = 0; r < rounds; ++r) {
-    int b = row_of(r * kPlan * kEach + tid);
-    each(r * kPlan * kEach, again, [&](int j, int x) {
-      const int rank = x < n ? ranks[x] : -1;
-      if (rank < 0 || rank >= n_free) return;
-      b = row_from(b, x);
-      const size_t at = entry(b, x);
-      const int was = slot[j], now = free_slots[rank];
-      p.page_table[at] = now;
-      p.refs[now] = 1;
-      if (was < 0) return;
-      atomicSub(p.refs + was, 1);
-      const RowPages w = row_pages(p, b);
-      if (p.moves && x == starts[b] && w.inside > 0) {
-        p.moves[3 * b] = was;
-        p.moves[3 * b + 1] = now;
-        p.moves[3 * b + 2] = w.inside;
-      }
-    });
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const bool is = need >> j & 1u;
+    const uint64_t all = __ballot(is);
+    const int rank = counts[j * kWaves + wave] + __popcll(all & ((1ull << lane) - 1));
+    if (is && rank < n_free) {
+      const int x = kPlan * j + tid;
+      take_slot(p, row[j], x + pages[row[j]], slot[j], free_slots[rank], x == starts[row[j]]);
+    }
   }
   if (p.missing && tid == 0) *p.missing = needs - n_free;
+}
+
+// Larger tables, in four launches: a row of the table or 4096 slots a workgroup. ws: as above, an entry's rank
+// among those of its row that get a slot, a row's number of them, free slots of each 4096.
+constexpr int kRow = 256, kPerChunk = 4096;
+struct TakeWs {
+  int32_t *wants, *last, *free_slots, *ranks, *row_needs, *chunk_free;
+  int chunks;
+};
+__host__ __device__ __forceinline__ TakeWs take_ws(const SlotsParams& p) {
+  TakeWs w;
+  w.wants = p.ws;
+  w.last = w.wants + p.num_slots;
+  w.free_slots = w.last + p.num_slots;
+  w.ranks = w.free_slots + p.num_slots;
+  w.row_needs = w.ranks + (size_t)p.B * p.max_pages;
+  w.chunk_free = w.row_needs + p.B;
+  w.chunks = (p.num_slots + kPerChunk - 1) / kPerChunk;
+  return w;
+}
+// Sum over the workgroup of kRow threads. Every thread must call it.
+__device__ __forceinline__ int sum_row(int x, int* buf) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
+  __syncthreads();
+  const int total = buf[0] + buf[1] + buf[2] + buf[3];
+  __syncthreads();
+  return total;
+}
+// Numbers of set flags in the threads before this one; total: of all.
+__device__ __forceinline__ int rank_row(bool is, int* buf, int& total) {
+  const uint64_t all = __ballot(is);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0) buf[wave] = __popcll(all);
+  __syncthreads();
+  int before = __popcll(all & ((1ull << lane) - 1));
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kRow / 64; ++w) {
+    before += w < wave ? buf[w] : 0;
+    total += buf[w];
+  }
+  __syncthreads();
+  return before;
+}
+
+__global__ __launch_bounds__(kRow) void take_clear_kernel(SlotsParams p) {
+  __shared__ int buf[kRow / 64];
+  const TakeWs w = take_ws(p);
+  const int s0 = blockIdx.x * kPerChunk, hi = min(s0 + kPerChunk, p.num_slots);
+  int free = 0;
+  for (int s = s0 + threadIdx.x; s < hi; s += kRow) {
+    w.wants[s] = 0;
+    w.last[s] = -1;
+    free += p.refs[s] == 0;
+  }
+  free = sum_row(free, buf);
+  if (threadIdx.x == 0) w.chunk_free[blockIdx.x] = free;
+}
+__global__ __launch_bounds__(kRow) void take_count_kernel(SlotsParams p) {
+  const TakeWs w = take_ws(p);
+  const int b = blockIdx.x;
+  const RowPages r = row_pages(p, b);
+  for (int i = threadIdx.x; i < r.n; i += kRow) {
+    const int at = b * p.max_pages + r.lo + i, slot = p.page_table[at];  // (a table has at most 2^30 entries)
+    if (slot >= 0 && slot < p.num_slots && p.refs[slot] > 1) {
+      atomicAdd(w.wants + slot, 1);
+      atomicMax(w.last + slot, at);
+    }
+  }
+}
+__global__ __launch_bounds__(kRow) void take_decide_kernel(SlotsParams p) {
+  __shared__ int buf[kRow / 64];
+  const TakeWs w = take_ws(p);
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < p.B) {
+    const int b = blockIdx.x;
+    const RowPages r = row_pages(p, b);
+    int needs = 0;
+    for (int i0 = 0; i0 < r.n; i0 += kRow) {
+      const int at = b * p.max_pages + r.lo + i0 + tid;
+      bool is = false;
+      if (i0 + tid < r.n) {
+        const int slot = p.page_table[at], refs = slot >= 0 && slot < p.num_slots ? p.refs[slot] : 0;
+        is = slot < 0 || (refs > 1 && !(w.wants[slot] == refs && w.last[slot] == at));
+      }
+      int total;
+      const int rank = rank_row(is, buf, total);
+      if (i0 + tid < r.n) w.ranks[at] = is ? needs + rank : -1;
+      needs += total;
+    }
+    if (tid == 0) w.row_needs[b] = needs;
+    return;
+  }
+  // the free slots of a chunk, behind those of the chunks before it
+  const int c = blockIdx.x - p.B;
+  int before = 0;
+  for (int x = tid; x < c; x += kRow) before += w.chunk_free[x];
+  before = sum_row(before, buf);
+  const int hi = min((c + 1) * kPerChunk, p.num_slots);
+  for (int s0 = c * kPerChunk; s0 < hi; s0 += kRow) {
+    int total;
+    const bool is = s0 + tid < hi && p.refs[s0 + tid] == 0;
+    const int rank = rank_row(is, buf, total);
+    if (is) w.free_slots[before + rank] = s0 + tid;
+    before += total;
+  }
+}
+__global__ __launch_bounds__(kRow) void take_apply_kernel(SlotsParams p) {
+  __shared__ int buf[kRow / 64];
+  const TakeWs w = take_ws(p);
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const RowPages r = row_pages(p, b);
+  int before = 0, n_free = 0;
+  for (int x = tid; x < b; x += kRow) before += w.row_needs[x];
+  for (int x = tid; x < w.chunks; x += kRow) n_free += w.chunk_free[x];
+  before = sum_row(before, buf);
+  n_free = sum_row(n_free, buf);
+  if (p.moves && tid < 3) p.moves[3 * b + tid] = -1;
+  __syncthreads();
+  for (int i = tid; i < r.n; i += kRow) {
+    const int at = b * p.max_pages + r.lo + i, rank = w.ranks[at];
+    if (rank >= 0 && before + rank < n_free)
+      take_slot(p, b, r.lo + i, p.page_table[at], w.free_slots[before + rank], i == 0);
+  }
+  if (p.missing && b == p.B - 1 && tid == 0) *p.missing = max(before + w.row_needs[b] - n_free, 0);
 }
 
 // ---------------------------------------------------------------- fork, free
@@ -363,16 +454,22 @@ __global__ __launch_bounds__(256) void page_copy_kernel(PageCopyParams p, int pa
 }  // namespace
 
 size_t slots_take_ints(const SlotsParams& p) {
-  const size_t entries = (size_t)p.B * p.max_pages;
-  return 2 * (size_t)p.num_slots + entries + (entries < (size_t)p.num_slots ? entries : (size_t)p.num_slots);
+  const TakeWs w = take_ws(p);
+  return 3 * (size_t)p.num_slots + (size_t)p.B * p.max_pages + p.B + w.chunks;
 }
 size_t slots_fork_ints(const SlotsParams& p) { return (size_t)p.B * p.max_pages; }
 size_t slots_compact_ints(const SlotsParams& p) { return 4 * (size_t)p.num_slots; }
 
 hipError_t launch_slots_take(const SlotsParams& p, hipStream_t s) {
-  // (short code where there are few entries; 128 rows of 512: 57 us with 32 a thread, 82 with 8, 64 rows of 16 13.9 and 11)
-  if ((int64_t)p.B * p.max_pages <= 4 * kPlan) slots_take_kernel<4><<<1, kPlan, 0, s>>>(p);
-  else slots_take_kernel<32><<<1, kPlan, 0, s>>>(p);
+  if ((int64_t)p.B * p.max_pages <= kSmallTable) {
+    slots_take_kernel<<<1, kPlan, 0, s>>>(p);
+  } else {
+    const int chunks = take_ws(p).chunks;
+    take_clear_kernel<<<chunks, kRow, 0, s>>>(p);
+    take_count_kernel<<<p.B, kRow, 0, s>>>(p);
+    take_decide_kernel<<<p.B + chunks, kRow, 0, s>>>(p);
+    take_apply_kernel<<<p.B, kRow, 0, s>>>(p);
+  }
   return hipGetLastError();
 }
 

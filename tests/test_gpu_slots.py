@@ -34,7 +34,7 @@ def same(s, table, refs):
 
 
 SIZES = [(1, 1, 1, 8), (1, 5, 4, 16), (3, 7, 12, 64), (8, 40, 200, 8), (64, 16, 1200, 256), (130, 33, 5000, 24), (2000, 3, 40000, 40),
-         (5, 2100, 9000, 8)]
+         (5, 2100, 9000, 8), (4096, 1, 3000, 8), (1, 4097, 5000, 8), (9000, 2, 20000, 16)]
 
 
 @pytest.mark.parametrize("B,pages,slots,P_", SIZES)

@@ -79,7 +79,7 @@ def make(kind, seed, B, H, kv, d, P_, dt, pages, lens, spread):
 
 
 def run_case(kind, seed, B, H, kv, d, P_, n_q, dt, pages, first=0, n=None, k_h=None, k_max=0, kv_len=None,
-             q_len=None, mask="tree", spread=0.3, scale=0.0, sel_valid=None, change=None):
+             q_len=None, mask="tree", spread=0.3, scale=0.0, sel_valid=None, change=None, many=False):
     n = pages - first if n is None else n
     r = np.random.default_rng(seed)
     lens = [pages * P_] * B if kv_len is None else kv_len
@@ -116,13 +116,14 @@ def run_case(kind, seed, B, H, kv, d, P_, n_q, dt, pages, first=0, n=None, k_h=N
                   kv_len=None if kv_len is None else i32(kv_len), q_len=None if q_len is None else i32(q_len),
                   out=out, lse=lse)
     ol = [(first + n) * P_ if kv_len is None else x for x in lens]
-    check(q, out, lse, k, v, pt, listed, ol, ql, bits, scale or d ** -0.5)
+    check(q, out, lse, k, v, pt, listed, ol, ql, bits, scale or d ** -0.5, many)
     return c, q, out, lse
 
 
-def check(q, out, lse, k, v, pt, listed, kv_len, q_len, bits, scale):
+def check(q, out, lse, k, v, pt, listed, kv_len, q_len, bits, scale, many=False):
     d = q.shape[-1]
-    o, l, va, S, vm = O.attend(host(q), k, v, pt, listed, kv_len, q_len, bits, scale)
+    attend = (lambda *a: O.attend_many(*a, device=DEV)) if many else O.attend
+    o, l, va, S, vm = attend(host(q), k, v, pt, listed, kv_len, q_len, bits, scale)
     got, gl = host(out), host(lse)
     past = np.isnan(va) & np.isnan(o) & (np.arange(o.shape[1])[None, :] >= np.array(q_len)[:, None])[..., None, None]
     assert (got[past] == 3.0).all()  # rows past q_len stay
@@ -237,6 +238,84 @@ def test_what_a_node_does_not_see_does_not_reach_it(d, kind, dt):
         _, _, out, _ = run_case(kind, n_q + H, 2, H, kv, d, 40, n_q, dt, 6, kv_len=[130, 225], q_len=[30, 25], change=change)
         fine = torch.isfinite(out[0]).all(-1).all(-1)
         assert fine.any() and not fine.all() and torch.isfinite(out[1, :25]).all()
+
+
+# rows of a key head 16, 30, 64, 100 and 250: every kernel of calls that are not little work
+MUCH = pytest.mark.parametrize("B,H,kv,n_q", [(33, 16, 8, 8), (18, 16, 8, 15), (9, 16, 8, 32), (20, 32, 16, 50), (10, 32, 16, 125)])
+
+
+@kinds
+@MUCH
+@pytest.mark.parametrize("d", [64, 128])
+def test_much_work(B, H, kv, n_q, d, kind, dt):
+    """Ragged batches of many rows over pages of several sizes, selected pages, masks of any bits, rows
+    that see nothing."""
+    print(B, H, kv, n_q, d, kind, dt, flush=True)
+    r = np.random.default_rng(n_q)
+    for P_, mask in ((64, "tree"), (40, "any"), (136, None)):
+        pages = -(-1152 // P_)
+        kv_len = [1152, n_q, n_q + 1, 0] + r.integers(n_q, 1153, B - 4).tolist()
+        q_len = [n_q, n_q, n_q, 0] + r.integers(0, n_q + 1, B - 4).tolist()
+        run_case(kind, P_ + n_q, B, H, kv, d, P_, n_q, dt, pages, kv_len=kv_len, q_len=q_len, mask=mask, many=True)
+    kv_len[1:3] = [1100, n_q - 1]
+    run_case(kind, n_q, B, H, kv, d, 72, n_q, dt, 16, first=10, k_max=9, k_h=[9 - h % 9 for h in range(kv)], kv_len=kv_len, q_len=q_len, many=True)
+    run_case(kind, n_q, B, H, kv, d, 8, n_q, dt, 144, mask="any", many=True)
+
+
+@kinds
+@pytest.mark.parametrize("B,H,kv,n_q", [(8, 16, 8, 8), (8, 16, 4, 8), (8, 16, 8, 32), (4, 8, 4, 125)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_much_work_in_pieces(B, H, kv, n_q, d, kind, dt):
+    """Long lists of many rows; captured calls follow lengths and masks."""
+    print(B, H, kv, n_q, d, kind, dt, flush=True)
+    P_, pages = 200, 42
+    kv_len = [8301, n_q, 5000, 8400, 0, 1, 6000, 7777][:B]
+    q_len = [n_q, n_q, n_q - 1, n_q, 0, 1, 3, n_q][:B]
+    c, q, out, lse = run_case(kind, n_q, B, H, kv, d, P_, n_q, dt, pages, kv_len=kv_len, q_len=q_len, many=True)
+    run_case(kind, n_q, B, H, kv, d, P_, n_q, dt, pages, mask="any", many=True)
+    lens, nodes, words_ = i32(kv_len), i32(q_len), -(-n_q // 32)
+    mask = torch.zeros((B, n_q, words_), dtype=torch.int32, device=DEV)
+    got = torch.empty_like(out)
+    call = lambda to: c.attend_tree(q, pages, mask=mask, kv_len=lens, q_len=nodes, out=to)
+    call(got)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(got)
+    r = np.random.default_rng(0)
+    for i in range(3):
+        lens.copy_(i32(r.permutation(kv_len).tolist()))
+        nodes.copy_(i32(r.permutation(q_len).tolist()))
+        mask.copy_(words(r.random((B, n_q, n_q)) < 0.5))
+        out.fill_(2.0)
+        got.fill_(2.0)
+        call(out)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bits_of(got), bits_of(out))
+
+
+@kinds
+@MUCH
+@pytest.mark.parametrize("d", [64, 128])
+def test_much_work_and_what_a_node_does_not_see(B, H, kv, n_q, d, kind, dt):
+    """NaN and infinities among the nodes, as above, of every kernel of larger calls."""
+    nan, inf = float("nan"), float("inf")
+    print(B, H, kv, n_q, d, kind, dt, flush=True)
+
+    def change(c, pt):
+        for t, key, value in ((603, nan, 1.0), (605, 1.0, nan), (606, 1.0, inf)):  # nodes 3, 5, 6
+            s, o = int(pt[1, t // 40]), t % 40
+            if kind == "codes":
+                c.k[s, :, o] = 0x7f if key != key else 0x30
+                c.v[s, :, :, o] = 0x7f if value != 1.0 else 0x30
+            else:
+                c.k_pool[s, :, o] = key
+                c.v_pool[s, :, :, o] = value
+    kv_len = [1160 - b for b in range(B)]
+    kv_len[1] = 600 + n_q
+    _, _, out, _ = run_case(kind, n_q, B, H, kv, d, 40, n_q, dt, 29, kv_len=kv_len, change=change, many=True)
+    fine = torch.isfinite(out[1]).all(-1).all(-1)
+    assert fine.any() and not fine.all() and torch.isfinite(out[0]).all() and torch.isfinite(out[2:]).all()
 
 
 def bits_of(t):

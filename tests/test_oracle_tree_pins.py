@@ -96,3 +96,24 @@ def test_copied_pages():
     O.page_copy(a, [[0, 2, 3], [-1, 1, 16], [0, 1, 0]], 16)
     assert a["k"][2, 0, :, 0].tolist() == list(range(8)) + list(range(40, 48))
     assert a["v"][1, 0, 0].tolist() == list(range(16, 32))
+
+
+def test_both_forms_of_the_attention():
+    r = np.random.default_rng(3)
+    B, n_q, H, kv, d, P = 4, 9, 4, 2, 8, 8
+    k, v = r.standard_normal((9, kv, P, d)), r.standard_normal((9, kv, P, d))
+    q, table = r.standard_normal((B, n_q, H, d)), r.integers(0, 9, (B, 4))
+    k[table[0, 2], 1, 3], v[table[0, 2], :, 5], v[table[0, 2], 0, 6, 2] = np.nan, np.nan, np.inf
+    kv_len, q_len, bits = [25, 5, 0, 32], [9, 9, 3, 1], r.random((B, n_q, n_q)) < 0.4
+    bits[:, ::4] = False
+    pages = [[[2, 0, 1, 3], [3, 2]], [[0], [1]], [[0, 1], []], [[0, 1, 2, 3], [0, 1, 2, 3]]]
+    for m in (bits, None):
+        a = O.attend(q, k, v, table, pages, kv_len, q_len, m, 0.7)
+        b = O.attend_many(q, k, v, table, pages, kv_len, q_len, m, 0.7)
+        use = np.isfinite(a[0])
+        assert np.array_equal(use, np.isfinite(b[0])) and np.array_equal(np.isinf(a[0]), np.isinf(b[0]))
+        assert (~use).any() and use.any()
+        rows = use.all(-1).transpose(0, 2, 1)
+        for x, y in zip(a, b):
+            w = use if x.ndim == 4 else rows
+            assert np.allclose(x[w], y[w], rtol=1e-12, atol=1e-13)
