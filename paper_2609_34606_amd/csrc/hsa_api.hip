@@ -1433,7 +1433,7 @@ hsa_status_t validate_kept(const hsa_config_t* c, const int32_t* page_table, int
 }
 
 hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k_max, int32_t n_cur,
-                            TreeAttnParams& p, size_t& ws) {
+                            bool ragged, TreeAttnParams& p, size_t& ws) {
   if (n_q > HSA_MAX_TREE || cfg->batch > kMaxGridY) return HSA_ERR_UNSUPPORTED;
   if (((int64_t)k_max + n_cur) * cfg->page_size >= (1LL << 31) - 256) return HSA_ERR_UNSUPPORTED;
   p.B = cfg->batch;
@@ -1445,7 +1445,7 @@ hsa_status_t plan_tree_call(const hsa_config_t* cfg, int32_t n_q, int32_t kv_hea
   p.words = (n_q + 31) / 32;
   p.k_max = k_max;
   p.n_cur = n_cur;
-  plan_tree(p, cfg->dtype, cfg->head_dim, (int64_t)k_max + n_cur);
+  plan_tree(p, cfg->dtype, cfg->head_dim, (int64_t)k_max + n_cur, ragged);
   const int64_t heads = (int64_t)cfg->batch * kv_heads;
   if (heads * p.n_split * p.n_rt + 8 * p.n_rt > kMaxGrid || heads * p.part_rows > kMaxGrid) return HSA_ERR_UNSUPPORTED;
   const int64_t parts = tree_part_rows(cfg->dtype, cfg->head_dim, p.P, heads, (int64_t)n_q * p.G, (int64_t)k_max + n_cur);
@@ -1458,7 +1458,7 @@ size_t tree_ws(const hsa_config_t* cfg, int32_t n_q, int32_t kv_heads, int32_t k
   if (cfg->num_heads % kv_heads != 0 || (int64_t)k_max + n_cur < 1) return 0;
   TreeAttnParams p{};
   size_t ws = 0;
-  return plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur, p, ws) == HSA_OK ? ws : 0;
+  return plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur, true, p, ws) == HSA_OK ? ws : 0;
 }
 
 // The pool's pages as the descriptor that the calls over either cache take.
@@ -1705,7 +1705,7 @@ hsa_status_t hsa_tree_attn(const hsa_config_t* cfg, const void* q, int32_t n_q, 
   if (n_q == 0) return HSA_OK;
   TreeAttnParams p{};
   size_t need = 0;
-  if ((st = plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur_pages, p, need)) != HSA_OK) return st;
+  if ((st = plan_tree_call(cfg, n_q, kv_heads, k_max, n_cur_pages, kv_len != nullptr, p, need)) != HSA_OK) return st;
   if ((st = check_ws(ws, ws_bytes, need)) != HSA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if ((st = validate_cache8(cfg, &pages, sel, k_max, k_h, cur_first_page, n_cur_pages, kv_len, s)) != HSA_OK) return st;

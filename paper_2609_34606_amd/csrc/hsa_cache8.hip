@@ -502,32 +502,31 @@ struct ManyLayout {
 
 constexpr int many_rows(int d) { return d == 128 ? 256 : 128; }  // query rows of a many-rows item
 
+// What an item's workgroup keeps in LDS.
 template <int D, bool kSmallP, bool kTree>
-__global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_rows_kernel(Cache8AttnParams p) {
+struct ManyLds {
+  uint8_t tiles[ManyLayout<D>::kBytes];
+  int2 first[kSmallP ? 8 : 1][4];                       // first tokens of the granules of eight tiles
+  uint32_t bits[kTree ? many_rows(D) : 1][kMaskWords + 1];  // mask rows of the item's nodes
+  int wild;                                             // whether a node's value is no finite number
+};
+
+// The item of rows from rt * kRows of key head h, piece `split`. kPair: a tree's item of up to half as many
+// rows, two waves a 32 rows, each with half of every tile's keys (d = 128, 32 sequences of 8192 tokens, 8 key heads,
+// 128 rows: 224 to 232 us, by four waves beside four idle ones 238; a ragged batch of up to 256 rows over up to 16384
+// tokens 437 and 451. With d = 64 three workgroups share a CU).
+template <int D, bool kSmallP, bool kTree, bool kPair>
+__device__ __forceinline__ void many_rows_item(const Cache8AttnParams& p, ManyLds<D, kSmallP, kTree>& lds, const Cache8Walk& w,
+                                               int b, int h, int rt, int split) {
   using L = ManyLayout<D>;
   constexpr int KK = D / 16, NM = D / 32;
   constexpr int kRows = many_rows(D);  // (32 a wave; 4 D threads: 16 codes of a tile's keys each, 16 of its values)
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[L::kBytes];
-  __shared__ int2 first_sm[kSmallP ? 8 : 1][4];  // first tokens of the granules of eight tiles
-  __shared__ uint32_t bits[kTree ? kRows : 1][kMaskWords + 1];  // mask rows of the item's nodes
-  __shared__ int wild;                                          // whether a node's value is no finite number
+  uint8_t* const smem = lds.tiles;
+  auto& first_sm = lds.first;
+  auto& bits = lds.bits;
+  int& wild = lds.wild;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // workgroup i runs on XCD i % 8: an XCD takes an eighth of the items in a row, which share
-  // their pages in its L2, first pieces first (a causal item's last pieces may be empty: the
-  // workgroups of a CU, 32 apart, should not all be first pieces)
-  const int n_wg = gridDim.x, x8 = blockIdx.x & 7;
-  const int id = x8 * (n_wg >> 3) + min(x8, n_wg & 7) + (blockIdx.x >> 3);
-  const int n_items = p.Hk * p.n_rt, share = (n_items + 7) >> 3;
-  // (a quotient comes from the vector unit, and its uses would stay there)
-  const int group = __builtin_amdgcn_readfirstlane(id / (share * p.n_split)), in = id - group * share * p.n_split;
-  const int members = min(share, n_items - group * share);
-  const int split = __builtin_amdgcn_readfirstlane(in / members), item = group * share + in - split * members;
-  const int b = blockIdx.y;
-  const int h = __builtin_amdgcn_readfirstlane(item / p.n_rt);
-  const int rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
-  const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, lane);
-  if (w.rows <= 0) return;
   const int t_lo = split * p.split_tiles, t_hi = min(t_lo + p.split_tiles, w.n_tiles);
   if (split > 0 && t_lo >= w.n_tiles) return;
   const bool whole = w.n_tiles <= p.split_tiles;
@@ -546,7 +545,9 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
   // queries
   u32x4 qf[KK];
   int lim;
-  const int row0 = rt * kRows + wave * 32;
+  constexpr int kHalfWaves = D / 32;
+  const int kh0 = kPair && wave >= kHalfWaves ? 1 : 0;
+  const int row0 = rt * kRows + (wave - kh0 * kHalfWaves) * 32;
   {
     const int r = row0 + l32, i = min(r / p.G, w.q_len - 1);
     lim = kTree ? i : cache8_limit(p, w, i);  // (a tree: the row's node)
@@ -830,6 +831,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
   // compiler reads operands right before their use.
   auto half_step = [&](int vb, int kh, const f32x16& s, int kb, int nh, const Tile& nt, f32x16& sn,
                        auto&& tail) __attribute__((always_inline)) {
+    // kh and nh: constants, or, of a pair, both the half that the wave has
     constexpr int NP = KK + 2 * NM;            // matrix instructions
     constexpr int kFirst = KK / 2;             // of them, beside the weights of the first 16 keys
     constexpr int kSecond = KK + NM - kFirst;  // and of the second
@@ -868,7 +870,8 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
       }
       if (i >= KK + NM) {  // (the scores were complete NM instructions ago)
 #pragma unroll
-        for (int x = (i - KK - NM) * 16 / NM; x < (i - KK - NM + 1) * 16 / NM; ++x) mx = fmaxf(mx, sn[x]);
+        for (int x = 0; x < 16; ++x)
+          if (x * NM / 16 == i - KK - NM) mx = fmaxf(mx, sn[x]);
         asm volatile("" : "+v"(mx));
       }
       if (i == KK) tail();
@@ -905,9 +908,20 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
       return;
     }
     // (tile t is ring[1] before load_k, ring[0] after it)
-    half_step(par, 0, sa, k0, 1, ring[1], sb, next_v);
-    const Tile ahead = ring[2];
-    half_step(par, 1, sb, k1, 0, ahead, sa, next_k);
+    if constexpr (kPair) {
+      // the wave's half of tile t, and the scores of that half of t + 1
+      const Tile ahead = ring[2];
+      auto next = [&]() __attribute__((always_inline)) {
+        next_v();
+        next_k();
+      };
+      if constexpr (par == 0) half_step(par, kh0, sa, k1, kh0, ahead, sb, next);
+      else half_step(par, kh0, sb, k1, kh0, ahead, sa, next);
+    } else {
+      half_step(par, 0, sa, k0, 1, ring[1], sb, next_v);
+      const Tile ahead = ring[2];
+      half_step(par, 1, sb, k1, 0, ahead, sa, next_k);
+    }
   };
 
   if (n > 0) {
@@ -930,8 +944,8 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
     if (active) {
       sa = f32x16{0};
 #pragma unroll
-      for (int j = 0; j < KK; ++j) sa = mfma32(kop(kfirst, 0, j), qf[j], sa);
-      if (beyond(ring[1], lim_first)) mask(ring[1], 0, sa);
+      for (int j = 0; j < KK; ++j) sa = mfma32(kop(kfirst, kh0, j), qf[j], sa);
+      if (beyond(ring[1], lim_first)) mask(ring[1], kh0, sa);
       raise(largest(sa));
     }
     for (int t = 0; t < n; t += 2) {
@@ -941,7 +955,7 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
   }
   if constexpr (kTree) {
     __syncthreads();
-    if (wild && active)
+    if (wild && active && kh0 == 0)
       tree_wild(p, w, b, h, D, t_lo * 8, t_hi * 8,
                 [&](size_t head, size_t at, int off) { return code_value(p, head, at, off); },
                 [&](int t0, int j, auto&& value) {
@@ -953,9 +967,42 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
                   }
                 });
   }
+  float l = l_run + __shfl_xor(l_run, 32);
+  if constexpr (kPair) {
+    // the second halves' sums go through LDS, [dims / 4][row], so that lanes write side by side
+    __syncthreads();
+    float* osm = reinterpret_cast<float*>(smem) + (wave & (kHalfWaves - 1)) * (32 * D + 64);
+    if (active && kh0 == 1) {
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(osm + ((8 * m + 2 * g + half) * 32 + l32) * 4) =
+              f32x4{acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]};
+      if (half == 0) {
+        osm[32 * D + l32] = m_run;
+        osm[32 * D + 32 + l32] = l;
+      }
+    }
+    __syncthreads();
+    if (kh0 == 1) return;
+    if (active) {
+      const float m_other = osm[32 * D + l32], top = fmaxf(m_run, m_other);
+      const float mine = __builtin_amdgcn_exp2f((m_run - top) * c2), other = __builtin_amdgcn_exp2f((m_other - top) * c2);
+      l = mine * l + other * osm[32 * D + 32 + l32];
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * g + half) * 32 + l32) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][4 * g + e] = mine * acc[m][4 * g + e] + other * y[e];
+        }
+      m_run = top;
+    }
+  }
   if (!active) return;
   const int r = row0 + l32, i = r / p.G;
-  const float l = l_run + __shfl_xor(l_run, 32);
   if (i >= w.q_len) return;
   if (whole) {
     const int head = h * p.G + r % p.G;
@@ -976,6 +1023,34 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
             f32x4{acc[m][4 * g], acc[m][4 * g + 1], acc[m][4 * g + 2], acc[m][4 * g + 3]};
     if (half == 0) reinterpret_cast<f32x2*>(p.part_ml)[part] = f32x2{m_run, l};
   }
+}
+
+template <int D, bool kSmallP, bool kTree>
+__global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_rows_kernel(Cache8AttnParams p) {
+  constexpr int kRows = many_rows(D);
+  __shared__ __attribute__((aligned(1024))) ManyLds<D, kSmallP, kTree> lds;
+  // workgroup i runs on XCD i % 8: an XCD takes an eighth of the items in a row, which share
+  // their pages in its L2, first pieces first (a causal item's last pieces may be empty: the
+  // workgroups of a CU, 32 apart, should not all be first pieces)
+  const int n_wg = gridDim.x, x8 = blockIdx.x & 7;
+  const int id = x8 * (n_wg >> 3) + min(x8, n_wg & 7) + (blockIdx.x >> 3);
+  const int n_items = p.Hk * p.n_rt, share = (n_items + 7) >> 3;
+  // (a quotient comes from the vector unit, and its uses would stay there)
+  const int group = __builtin_amdgcn_readfirstlane(id / (share * p.n_split)), in = id - group * share * p.n_split;
+  const int members = min(share, n_items - group * share);
+  const int split = __builtin_amdgcn_readfirstlane(in / members), item = group * share + in - split * members;
+  const int b = blockIdx.y;
+  const int h = __builtin_amdgcn_readfirstlane(item / p.n_rt);
+  const int rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
+  const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, threadIdx.x & 63);
+  if (w.rows <= 0) return;
+  if constexpr (kTree && D == 128) {
+    if (w.rows <= kRows / 2) {
+      many_rows_item<D, kSmallP, kTree, true>(p, lds, w, b, h, rt, split);
+      return;
+    }
+  }
+  many_rows_item<D, kSmallP, kTree, false>(p, lds, w, b, h, rt, split);
 }
 
 // Joins the pieces of a row whose tokens were split, in an order that does not depend on

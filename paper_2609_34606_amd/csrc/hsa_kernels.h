@@ -298,7 +298,7 @@ struct TreeAttnParams {
 };
 
 // Plans the launch for lists of at most `list` pages.
-void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list);
+void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list, bool ragged);
 // Most rows of partial outputs (n_split * part_rows) that plan_tree gives a key head for any list up to `list` pages.
 // heads: B * Hk, rows: n_q * G.
 int64_t tree_part_rows(int dtype, int d, int P, int64_t heads, int64_t rows, int64_t list);

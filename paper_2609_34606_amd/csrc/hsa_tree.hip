@@ -953,7 +953,7 @@ hipError_t launch_tree_mask(int B, const TreeMaskParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list) {
+void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list, bool ragged) {
   p.gpp = p.P / 8;
   p.gmul = 65536 / p.gpp + 1;
   const int64_t rows = (int64_t)p.n_q * p.G;
@@ -983,6 +983,20 @@ void plan_tree(TreeAttnParams& p, int dtype, int d, int64_t list) {
     }
   } else {
     n = tree_pieces(items, tiles);
+    if (!ragged && p.rows_per_item > 32) {
+      // Equal lists, two workgroups a CU: rounds of them, each of its tiles and about eight more for its start, end and
+      // part of the join (64 nodes of 12 heads over 187200 tokens: 42 pieces, one round, 217 us, 85 241, 128 249; of
+      // 32 heads, 8 key heads, over 65536, 106 and, in 64, 116). Pieces of ragged lists end at different times
+      // anyway, and many short ones balance.
+      int64_t best = INT64_MAX;
+      for (int64_t k = 1, most = n; k <= most; ++k) {
+        const int64_t t = (items * k + 511) / 512 * ((tiles + k - 1) / k + 8);
+        if (t < best) {
+          best = t;
+          n = k;
+        }
+      }
+    }
   }
   p.split_tiles = (int)((tiles + n - 1) / n);
   p.n_split = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
