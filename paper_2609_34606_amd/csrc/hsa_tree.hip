@@ -25,7 +25,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // ---------------------------------------------------------------- ancestors
 // A node's row is its own bit and its parent's row. Rows double the path they hold with every
 // round (row |= row of the node at the end of the path), so a chain of n nodes takes log2(n) rounds, through
-// shared memory, a thread a node. Bound: a launch's latency.
+// shared memory, a thread a node. Bound: a launch's latency (64 trees of up to 256 nodes: 4.4 us).
 __global__ __launch_bounds__(HSA_MAX_TREE) void tree_mask_kernel(TreeMaskParams p) {
   __shared__ uint32_t rows[HSA_MAX_TREE][kMaskWords + 1];
   __shared__ int jump[HSA_MAX_TREE];
@@ -182,6 +182,11 @@ constexpr int kBriefItems = 256, kBriefTiles = 128;  // little work: most items 
 // of the tile: weights become the second product's operand without an exchange between lanes. Tiles go
 // from memory to the registers of the wave that uses them; the next tile's keys are asked for once this
 // one's scores are done with their registers, the values after its output.
+//
+// Bound: of much work, reading the tokens (32 sequences of 8192 tokens, 8 key heads, d = 128: rows 4 to 32 212 to 248 us,
+// 5.1 to 4.3 TB/s; 12 heads, 187200 tokens, 1 and 16 rows 223 and 240 us, 5.2 and 4.8 TB/s); of little, the latency of
+// the loads that wait for each other, lengths, page table, tokens (12 heads, one row, 1024 tokens: 10.3 us and the join
+// 3.7). Through shared memory, which items of more rows use, each wave would wait for all of them.
 template <typename T, int D, int kCols, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kWaves > 4 ? kWaves / 4 : kCols == 1 ? (sizeof(T) == 2 ? 3 : 2) : (sizeof(T) == 2 ? 2 : 1))
 void tree_attn_kernel(TreeAttnParams p) {
@@ -546,7 +551,12 @@ void tree_attn_kernel(TreeAttnParams p) {
 // there by all waves: with kRG = 4 each takes 32 rows, with two 32 rows and half of the tile's tokens.
 //
 // Products are transposed as above, 32x32x16, with key rows in an order that makes a lane's scores the
-// weights' operand. A tile's loads are two tiles ahead of its products.
+// weights' operand. A tile's loads are two tiles ahead of its products (three spilled registers: 159 and 288 us for the
+// calls below).
+// Bound: up to 64 rows, reading the tokens (64 rows, 12 heads over 187200 tokens: 203 to 222 us, 5.7 to 5.2 TB/s; a ragged
+// batch of up to 64 rows over up to 8192 tokens 127 to 134 us, 4.4 TB/s, the first kernel here, whose waves each
+// loaded 64 rows' tiles for themselves, 250); of more, the matrix and vector instructions, which the two
+// workgroups of a CU overlap in part (256 rows, 32 sequences of 8192 tokens, 8 key heads: 452 us, 600 TFLOP/s).
 template <int D, int kRG>
 struct TreeWide {
   static constexpr int kThreads = 256, kRows = 32 * kRG;
@@ -854,7 +864,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
 }
 
 // Joins the pieces of a row in an order that does not depend on the launch's timing: kW groups of D / 4
-// lanes a row, four dims a lane, each every kW-th piece, then the groups in order.
+// lanes a row, four dims a lane, each every kW-th piece, then the groups in order. Bound: reading the pieces
+// (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us).
 template <typename T, int D, int kW>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kW);
@@ -909,15 +920,20 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   if (mine) tree_store<T, 4>(p, D, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
 
-// Waves of a workgroup where the whole call is little work: as many as the registers allow.
+// Waves of a workgroup where the whole call is little work: as many as the registers allow (12 heads, one query, 1024
+// tokens, d = 128: 8 waves 14.1 us, 16, which spill, 24.7).
 constexpr int brief_waves(size_t size, int d) { return size == 4 || d == 128 ? 8 : 16; }
 
-// Whether items of 16 rows with so many tiles of 32 tokens are little work (up to 16 rows a key head: less of it, there the
-// other kernel reads every token once too).
+// Tiles of 32 tokens up to which items of 16 rows are little work. (Up to 16 rows a key head the other workgroups read
+// every token once too.) In us, as little work and not: 12 heads, one row, 1024 tokens 13.8 and 15.8; 8 key heads, 64
+// rows, 1024 and 4096 tokens 13.6 and 24.0, 22.7 and 27.8; 4 sequences of 2000, 4 key heads, 240 rows, d = 64 21.6 and
+// 30.9; fp32, 2 sequences of 2000, 8 heads, one row 20.8 and 25.9.
 int64_t brief_tiles(int64_t items16, int64_t rows) {
   return items16 > kBriefItems ? 0 : rows <= 16 ? 4096 / items16 : std::min<int64_t>(kBriefTiles, 16384 / items16);
 }
-// Rows of an item otherwise, and the pieces that its list is cut into.
+// Rows of an item otherwise, and the most pieces that its list is cut into: of 16 tiles, which balance ragged lists (up to
+// 64 rows, up to 8192 tokens: pieces of 16 tiles 139 us, of 8 154), while they make fewer than 4096 workgroups (1024:
+// 149 us; 2048 to 8192: 139). fp32 has registers for 32 rows.
 int tree_rows(int dtype, int64_t rows) {
   return rows <= 16 ? 16 : (rows <= 32 || dtype == HSA_DTYPE_F32 ? 32 : (rows <= 64 ? 64 : 128));
 }
@@ -936,9 +952,10 @@ hipError_t launch_pool(const TreeAttnParams& p, hipStream_t s) {
     else tree_wide_kernel<D, 4><<<grid, 256, 0, s>>>(p);
   }
   if (p.n_split > 1) {
-    // several groups of lanes a row while the rows alone do not fill the chip
+    // several groups of lanes a row while the rows alone do not fill the chip (12 heads, 187200 tokens, 16 and 1 rows, in
+    // us of both kernels: 240 and 223, with one group 255 and 238; 4096 rows of 16 pieces 35.0 and 30.6)
     constexpr int kMost = 256 / (D / 4);  // rows of a workgroup
-    if ((int64_t)p.B * p.Hk * p.part_rows <= 8192)
+    if ((int64_t)p.B * p.Hk * p.part_rows <= 2048)
       tree_join_kernel<T, D, kMost><<<p.B * p.Hk * p.part_rows, 256, 0, s>>>(p);
     else
       tree_join_kernel<T, D, 1><<<p.B * p.Hk * ((p.part_rows + kMost - 1) / kMost), 256, 0, s>>>(p);
