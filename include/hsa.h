@@ -827,10 +827,10 @@ hsa_status_t hsa_tree_mask(const hsa_config_t* cfg, const int32_t* parent, int32
  * kv_len: device int32 [B], NULL: (cur_first_page + n_cur_pages) * P. q_len: device int32 [B] in
  * [0, n_q], NULL: n_q; rows of o and lse at or past q_len[b] stay as they were.
  * Products of bf16 operands summed in fp32; a bf16 call rounds the softmax weights to bf16 (in two parts
- * where a key head has up to 16 rows n_q * num_heads / kv_heads); an fp32 call's products are of fp32. Sums are
+ * where a key head has up to 16 rows n_q * num_heads / kv_heads, and in calls of little work); an fp32 call's products are of fp32. Sums are
  * joined in a fixed order: the same call gives the same bits. ws: hsa_tree_attn_workspace_size(...)
  * bytes, 256-byte aligned; the size for a program's longest list serves every shorter one of the same cfg,
- * n_q and kv_heads. It does not grow with n_q (see hsa_cache8_attn). Errors as hsa_cache8_attn; q, o, pool->k and
+ * n_q and kv_heads, but a step of fewer nodes may need more (as hsa_cache8_attn's). Errors as hsa_cache8_attn; q, o, pool->k and
  * pool->v are 16-byte aligned, and the listed pages hold fewer than 2^31 - 256 tokens (UNSUPPORTED).
  * Kernels read kv_len, q_len and mask, so a captured call follows them.
  */

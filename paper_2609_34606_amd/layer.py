@@ -37,17 +37,10 @@ class HsaLayer:
         self.page_kmean = torch.zeros((batch, heads, self.max_pages, head_dim), dtype=torch.float64,
                                       device=device)
         self._ws = {}
-        self._pool, self._pool_of = None, None
 
     @property
     def pool(self) -> _h.HsaKvPool:
-        """The pool's descriptor, checked anew when one of its tensors is another one."""
-        k, v, pt = self.k_pool, self.v_pool, self.page_table
-        of = (k.data_ptr(), v.data_ptr(), pt.data_ptr(), k.shape, v.shape, pt.shape, k.stride(), v.stride(), pt.stride(),
-              k.dtype, v.dtype, pt.dtype)
-        if of != self._pool_of:
-            self._pool, self._pool_of = _h.kv_pool(k, v, pt, self.cfg), of
-        return self._pool
+        return _h.kv_pool(self.k_pool, self.v_pool, self.page_table, self.cfg)
 
     def workspace(self, key, nbytes: int):
         if nbytes == 0:
