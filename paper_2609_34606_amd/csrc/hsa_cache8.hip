@@ -513,8 +513,7 @@ struct ManyLds {
 
 // The item of rows from rt * kRows of key head h, piece `split`. kPair: a tree's item of up to half as many
 // rows, two waves a 32 rows, each with half of every tile's keys (d = 128, 32 sequences of 8192 tokens, 8 key heads,
-// 128 rows: 224 to 232 us, by four waves beside four idle ones 238; a ragged batch of up to 256 rows over up to 16384
-// tokens 437 and 451. With d = 64 three workgroups share a CU).
+// 128 rows: 224 to 232 us, by four waves beside four idle ones 238. With d = 64 three workgroups share a CU).
 template <int D, bool kSmallP, bool kTree, bool kPair>
 __device__ __forceinline__ void many_rows_item(const Cache8AttnParams& p, ManyLds<D, kSmallP, kTree>& lds, const Cache8Walk& w,
                                                int b, int h, int rt, int split) {
@@ -1038,8 +1037,16 @@ __global__ __launch_bounds__(4 * D, D == 128 ? 1 : (kSmallP ? 2 : 3)) void many_
   // (a quotient comes from the vector unit, and its uses would stay there)
   const int group = __builtin_amdgcn_readfirstlane(id / (share * p.n_split)), in = id - group * share * p.n_split;
   const int members = min(share, n_items - group * share);
-  const int split = __builtin_amdgcn_readfirstlane(in / members), item = group * share + in - split * members;
-  const int b = blockIdx.y;
+  int split = __builtin_amdgcn_readfirstlane(in / members), item = group * share + in - split * members;
+  int b = blockIdx.y;
+  if constexpr (kTree) {
+    // Neighbours on an XCD go round its four shader engines: pieces in the same order for every sequence would give the
+    // last ones, which short sequences lack, to the same engines each time, and a third of the chip's time to
+    // nothing (32 sequences of up to 256 rows over up to 16384 tokens 437 us and, so, 378; 100 over up to 4096 415 and
+    // 343; 50 of up to 160 rows over up to 8192 397 and 287). Odd numbers of pieces go round by themselves.
+    if (p.n_split % 2 == 0)
+      split = __builtin_amdgcn_readfirstlane((split + (p.n_split % 4 == 0 ? b : b >> 1)) % p.n_split);
+  }
   const int h = __builtin_amdgcn_readfirstlane(item / p.n_rt);
   const int rt = p.n_rt - 1 - (item - h * p.n_rt);  // (causal: the longest first)
   const Cache8Walk w = cache8_walk(p, b, h, rt * kRows, kRows, threadIdx.x & 63);
@@ -1221,8 +1228,9 @@ int64_t cache8_slots(int d, int P, bool ragged) { return d == 128 ? 256 : (ragge
 // Most pieces of such a call, their ends counted (see plan_cache8).
 constexpr int kManyPieces = 16;
 constexpr double kManyEnds = 6.0, kManyJoin = 4.0, kManyGain = 0.97;
-// Pieces of a ragged batch's trees, which end at different times: of 32 tiles, up to some 2048 (a batch of up to 256 rows over
-// up to 16384 tokens: 451 us, planned as equal lists 549; pieces of 16 tiles 451, of 64 545; up to 4096 of 16 459).
+// Pieces of a ragged batch's trees, which end at different times: of 32 tiles, up to some 2048 (in us, of 32 tiles, 16,
+// 48, and 24 up to 4096: 32 sequences of up to 256 rows over up to 16384 tokens 381, 380, 369, 397; 100 over up to
+// 4096 343, 356, 329, 343; 50 of up to 160 rows over up to 8192 287, 302, 309, 290).
 constexpr int kTreeTiles = 32, kTreeItems = 2048;
 int64_t cache8_tree_pieces(int64_t items, int64_t tiles) {
   return std::max<int64_t>(1, std::min<int64_t>({kManyPieces, tiles / kTreeTiles, (kTreeItems + items - 1) / items}));

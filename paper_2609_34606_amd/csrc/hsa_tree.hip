@@ -582,9 +582,15 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int per8 = 8 * p.n_rt;
   const int oct = __builtin_amdgcn_readfirstlane(blockIdx.x / per8), in = blockIdx.x - oct * per8;
-  const int rt = in >> 3, group = oct * 8 + (in & 7), heads = p.B * p.Hk;
-  const int split = __builtin_amdgcn_readfirstlane(group / heads), bh = group - split * heads;
+  // (Neighbours on an XCD go round its four shader engines: a ragged batch's last row tiles and pieces take turns
+  // at which engine has them: 32 sequences of up to 256 rows over up to 8192 tokens 231 us and, so, 207; 100 of up to 160
+  // over up to 4096 317 and 261. The register kernel gains nothing by it: one node each 132
+  // and 136.)
+  const int rt = __builtin_amdgcn_readfirstlane(((in >> 3) + oct + (oct >> 1)) % p.n_rt);
+  const int group = oct * 8 + (in & 7), heads = p.B * p.Hk;
+  const int split = __builtin_amdgcn_readfirstlane(group / heads);
   if (split >= p.n_split) return;
+  const int bh = __builtin_amdgcn_readfirstlane((group - split * heads + 8 * split) % heads);
   const int b = __builtin_amdgcn_readfirstlane(bh / p.Hk), h = bh - b * p.Hk;
   const TreeWalk w = tree_walk(p, b, h, lane);
   const int row0 = rt * kRows, rows = w.q_len * p.G;

@@ -318,11 +318,12 @@ def kv_pool(k_pool, v_pool, page_table, cfg: Optional[HsaConfig] = None) -> HsaK
     if cfg is not None:
         H, P, d = cfg.num_heads, cfg.page_size, cfg.head_dim
         slots = int(k_pool.shape[0])
-        dt = _elem_dtype(cfg)
+        lib()
+        dt = _elem(cfg)
         for name, t, shape in (("k_pool", k_pool, (slots, H, P, d)), ("v_pool", v_pool, (slots, H, d, P))):
-            if t.shape != shape or str(t.dtype) != dt:
+            if t.dtype is not dt or t.shape != shape:
                 raise ValueError(f"{name} must be {dt} {shape}, got {t.dtype} {tuple(t.shape)}")
-        if page_table.dim() != 2 or page_table.shape[0] != cfg.batch or str(page_table.dtype) != "torch.int32":
+        if page_table.dtype is not _torch.int32 or page_table.dim() != 2 or page_table.shape[0] != cfg.batch:
             raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "
                              f"{page_table.dtype} {tuple(page_table.shape)}")
     return HsaKvPool(_ptr(k_pool), _ptr(v_pool), _ptr(page_table), int(k_pool.shape[0]),
