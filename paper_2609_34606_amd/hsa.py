@@ -315,19 +315,18 @@ def kv_pool(k_pool, v_pool, page_table, cfg: Optional[HsaConfig] = None) -> HsaK
     """The pool descriptor. With cfg, the tensors are checked against it
     first: k_pool [slots, H, P, d] and v_pool [slots, H, d, P] of the config's
     dtype, page_table [B, max_pages] int32."""
+    ks, ps = k_pool.shape, page_table.shape
     if cfg is not None:
-        H, P, d = cfg.num_heads, cfg.page_size, cfg.head_dim
-        slots = int(k_pool.shape[0])
         lib()
-        dt = _elem(cfg)
-        for name, t, shape in (("k_pool", k_pool, (slots, H, P, d)), ("v_pool", v_pool, (slots, H, d, P))):
-            if t.dtype is not dt or t.shape != shape:
-                raise ValueError(f"{name} must be {dt} {shape}, got {t.dtype} {tuple(t.shape)}")
-        if page_table.dtype is not _torch.int32 or page_table.dim() != 2 or page_table.shape[0] != cfg.batch:
+        H, P, d, dt, slots = cfg.num_heads, cfg.page_size, cfg.head_dim, _elem(cfg), ks[0]
+        for name, t, got, shape in (("k_pool", k_pool, ks, (slots, H, P, d)),
+                                    ("v_pool", v_pool, v_pool.shape, (slots, H, d, P))):
+            if t.dtype is not dt or got != shape:
+                raise ValueError(f"{name} must be {dt} {shape}, got {t.dtype} {tuple(got)}")
+        if page_table.dtype is not _torch.int32 or len(ps) != 2 or ps[0] != cfg.batch:
             raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "
-                             f"{page_table.dtype} {tuple(page_table.shape)}")
-    return HsaKvPool(_ptr(k_pool), _ptr(v_pool), _ptr(page_table), int(k_pool.shape[0]),
-                     int(page_table.shape[-1]))
+                             f"{page_table.dtype} {tuple(ps)}")
+    return HsaKvPool(_ptr(k_pool), _ptr(v_pool), _ptr(page_table), ks[0], ps[-1])
 
 
 # ------------------------------------------------------------------ C ABI calls
