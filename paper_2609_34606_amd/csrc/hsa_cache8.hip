@@ -456,6 +456,16 @@ void few_rows_kernel(Cache8AttnParams p) {
 #pragma unroll
       for (int e = 0; e < N; ++e) o[e] += wt * osm[(x * 16 + col) * OS + d0 + e];
     }
+    if (__builtin_expect(!all_finite(o), 0)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) o[e] = 0.f;
+#pragma unroll 1
+      for (int x = 0; x < kWaves; ++x) {
+        const float wt = __builtin_amdgcn_exp2f((msm[x][row] - m_all) * c2);
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] = add_share(o[e], osm[(x * 16 + col) * OS + d0 + e], wt);
+      }
+    }
     if (i >= w.q_len) continue;
     if (whole) {
       cache8_store<T, N>(p, b, i, h * p.G + r % p.G, d0, o, m_all, l, d0 == 0);
@@ -989,14 +999,22 @@ __device__ __forceinline__ void many_rows_item(const Cache8AttnParams& p, ManyLd
       const float m_other = osm[32 * D + l32], top = fmaxf(m_run, m_other);
       const float mine = __builtin_amdgcn_exp2f((m_run - top) * c2), other = __builtin_amdgcn_exp2f((m_other - top) * c2);
       l = mine * l + other * osm[32 * D + 32 + l32];
+      if (__builtin_expect(__any(fminf(mine, other) == 0.f), 0)) {
 #pragma unroll
-      for (int m = 0; m < NM; ++m)
+        for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * g + half) * 32 + l32) * 4);
+          for (int x = 0; x < 16; ++x)
+            acc[m][x] = add_share(add_share(0.f, acc[m][x], mine), osm[((8 * m + 2 * (x >> 2) + half) * 32 + l32) * 4 + (x & 3)], other);
+      } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[m][4 * g + e] = mine * acc[m][4 * g + e] + other * y[e];
-        }
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * g + half) * 32 + l32) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][4 * g + e] = fmaf(other, y[e], mine * acc[m][4 * g + e]);
+          }
+      }
       m_run = top;
     }
   }
@@ -1118,6 +1136,17 @@ __global__ __launch_bounds__(512) void join_row_kernel(Cache8AttnParams p) {
       }
     }
   }
+  if (__builtin_expect(!all_finite(o), 0)) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int s = wave; s < n; s += kW) {
+      const float share = __builtin_amdgcn_exp2f((ml[part0 + (size_t)s * p.part_rows][0] - m_all) * p.scale_log2);
+      const float* y = p.part_o + (part0 + (size_t)s * p.part_rows) * D + E * lane;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = add_share(o[e], y[e], share);
+    }
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e) osm[wave][E * lane + e] = o[e];
   __syncthreads();
@@ -1158,6 +1187,17 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Cache8AttnParams p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = o[e] * was + add * y[e];
     m = top;
+  }
+  if (__builtin_expect(!all_finite(o), 0)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < n; ++s) {
+      const float share = __builtin_amdgcn_exp2f((ml[part0 + (size_t)s * p.part_rows][0] - m) * p.scale_log2);
+      const float* y = p.part_o + (part0 + (size_t)s * p.part_rows) * D + d0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = add_share(o[e], y[e], share);
+    }
   }
   cache8_store<T, 4>(p, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }

@@ -144,6 +144,19 @@ __device__ __forceinline__ float softmax_floor(float c2) { return c2 > 1.f ? -0.
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
+// sum + share x, of joins of weighted sums: a share that rounds to 0 takes no infinity (or NaN) out of its sum, whose
+// token the row does see (0 * inf would be NaN). Joins do without, and are done again with it if all_finite says no.
+__device__ __forceinline__ float add_share(float sum, float x, float share) {
+  return fabsf(x) < INFINITY ? fmaf(share, x, sum) : sum + x;
+}
+template <int N>
+__device__ __forceinline__ bool all_finite(const float (&x)[N]) {
+  float zero = 0.f;  // (x - x: NaN of no finite number)
+#pragma unroll
+  for (int i = 0; i < N; ++i) zero += x[i] - x[i];
+  return zero == 0.f;
+}
+
 // Eight elements of T in kParts bf16 operands whose sum is the element: one for
 // bf16, three for fp32 (3 x 8 significant bits).
 template <typename T, int kParts>

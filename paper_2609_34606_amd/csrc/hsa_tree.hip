@@ -532,7 +532,7 @@ void tree_attn_kernel(TreeAttnParams p) {
       const float wt = __builtin_amdgcn_exp2f((msm[x][row] - m_all) * c2);
       l += wt * lsm[x][row];
 #pragma unroll
-      for (int e = 0; e < N; ++e) o[e] += wt * osm[(x * 16 + col) * OS + d0 + e];
+      for (int e = 0; e < N; ++e) o[e] = add_share(o[e], osm[(x * 16 + col) * OS + d0 + e], wt);
     }
     if (i >= w.q_len) continue;
     if (whole) {
@@ -837,14 +837,22 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
     const float m_other = osm[32 * D + l32], top = fmaxf(m_run, m_other);
     const float a = __builtin_amdgcn_exp2f((m_run - top) * c2), c = __builtin_amdgcn_exp2f((m_other - top) * c2);
     l = a * l + c * osm[32 * D + 32 + l32];
+    if (__builtin_expect(__any(fminf(a, c) == 0.f), 0)) {
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+      for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * x + half) * 32 + l32) * 4);
+        for (int x = 0; x < 16; ++x)
+          acc[m][x] = add_share(add_share(0.f, acc[m][x], a), osm[((8 * m + 2 * (x >> 2) + half) * 32 + l32) * 4 + (x & 3)], c);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[m][4 * x + e] = a * acc[m][4 * x + e] + c * y[e];
-      }
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(osm + ((8 * m + 2 * x + half) * 32 + l32) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][4 * x + e] = a * acc[m][4 * x + e] + c * y[e];
+        }
+    }
     m_run = top;
   }
   if (!active || i >= w.q_len) return;
@@ -873,7 +881,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
 // lanes a row, four dims a lane, each every kW-th piece, then the groups in order. Bound: reading the pieces
 // (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us).
 template <typename T, int D, int kW>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
+__global__ __launch_bounds__(256, kW == 1 ? 8 : 1) void tree_join_kernel(TreeAttnParams p) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kW);
   __shared__ __attribute__((aligned(16))) float osm[kW == 1 ? 1 : kRows * kW * D];
   __shared__ f32x2 mlsm[kW == 1 ? 1 : kRows * kW];
@@ -922,6 +930,17 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
       for (int e = 0; e < 4; ++e) o[e] += wt * osm[(row * kW + x) * D + d0 + e];
     }
     m = top;
+  }
+  if (__builtin_expect(mine && !all_finite(o), 0)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < n; ++s) {
+      const float share = __builtin_amdgcn_exp2f((ml[part0 + (size_t)s * p.part_rows][0] - m) * p.scale_log2);
+      const float* y = p.part_o + (part0 + (size_t)s * p.part_rows) * D + d0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = add_share(o[e], y[e], share);
+    }
   }
   if (mine) tree_store<T, 4>(p, D, b, i, h * p.G + r % p.G, d0, o, m, l, d0 == 0);
 }
