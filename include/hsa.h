@@ -873,7 +873,8 @@ hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, 
  * hsa_cache8_keep -- the same in the 8-bit cache. The result is that of appending the kept tokens'
  * numbers (code * 2^(exponent byte - 127)) at first[b] with hsa_cache8_write: a block that begins with
  * kept tokens takes the smallest scale that holds them, one with older tokens before them keeps the larger of
- * its own and that (older codes scaled down). A number changes only if its code becomes subnormal. Codes of a block
+ * its own and that (older codes scaled down), as does one with tokens among them whose source lies outside the table, and
+ * which stay; a block of which none is kept keeps its scale. A number changes only if its code becomes subnormal. Codes of a block
  * behind the kept tokens stay as they are, and what they stand for is lost if the scale changes.
  */
 hsa_status_t hsa_cache8_keep(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* first,

@@ -115,40 +115,60 @@ def attend_many(q, k, v, page_table, pages, kv_len, q_len, bits, scale, device="
 
 
 # ---------------------------------------------------------------- kept tokens
+def _place(page_table, b, t, P):
+    """(slot, token of the page) of a sequence's token, None outside the table."""
+    return (int(page_table[b, t // P]), t % P) if 0 <= t < page_table.shape[1] * P else None
+
+
 def _kept(page_table, P, first, index, count):
-    """(batch entry, i, source slot, source offset) of the tokens that are read, -1 where one is not."""
-    cap = page_table.shape[1] * P
+    """(batch entry, place that is read, place that is written) of the tokens that are kept."""
     for b in range(page_table.shape[0]):
         for i in range(count[b]):
-            t = int(first[b]) + int(index[b, i])
-            yield b, i, t, 0 <= t < cap
+            src = _place(page_table, b, int(first[b]) + int(index[b, i]), P)
+            dst = _place(page_table, b, int(first[b]) + i, P)
+            if src and dst:
+                yield b, src, dst
 
 
 def keep(k_pool, v_pool, page_table, first, index, count):
     """The pool [slots, H, P, d] / [slots, H, d, P], changed in place."""
-    P = k_pool.shape[2]
-    cap = page_table.shape[1] * P
     old_k, old_v = k_pool.copy(), v_pool.copy()
-    for b, i, t, read in _kept(page_table, P, first, index, count):
-        to = int(first[b]) + i
-        if read and 0 <= to < cap:
-            s, w = page_table[b, t // P], page_table[b, to // P]
-            k_pool[w, :, to % P] = old_k[s, :, t % P]
-            v_pool[w, :, :, to % P] = old_v[s, :, :, t % P]
+    for _, (s, o), (w, x) in _kept(page_table, k_pool.shape[2], first, index, count):
+        k_pool[w, :, x] = old_k[s, :, o]
+        v_pool[w, :, :, x] = old_v[s, :, :, o]
 
 
 def keep8(cache, page_table, first, index, count):
-    """cache: dict of uint8 k, v, k_exp, v_exp, changed in place, as by an append of the kept tokens'
-    numbers. Every index has to be a token of the table."""
+    """cache: dict of uint8 k, v, k_exp, v_exp, changed in place, as by an append of the kept tokens' numbers.
+    Tokens that stay before or among a block's kept ones keep its scale from shrinking, and their numbers."""
     P = cache["k"].shape[2]
-    k, v = C8.dequantise(cache)
-    B, n = index.shape
-    new_k, new_v = np.zeros((B, n) + (k.shape[1], k.shape[3])), np.zeros((B, n) + (k.shape[1], k.shape[3]))
-    for b, i, t, read in _kept(page_table, P, first, index, count):
-        assert read
-        s = page_table[b, t // P]
-        new_k[b, i], new_v[b, i] = k[s, :, t % P], v[s, :, t % P]
-    return C8.write8(cache, page_table, new_k, new_v, first, count)
+    numbers = dict(zip("kv", C8.dequantise(cache)))
+    kept = list(_kept(page_table, P, first, index, count))
+    for b in range(page_table.shape[0]):
+        to = {dst: src for c, src, dst in kept if c == b}
+        last = {}  # of each block, the last token of the run that the call brings
+        for t in range(int(first[b]), int(first[b]) + int(count[b])):
+            at = _place(page_table, b, t, P)
+            if at:
+                last[at[0], at[1] // C8.BLOCK] = at[1]
+        for (slot, blk), o1 in last.items():
+            run = range(blk * C8.BLOCK, o1 + 1)
+            if not any((slot, o) in to for o in run):
+                continue
+            stay = [o for o in run if (slot, o) not in to]
+            for name, x in numbers.items():
+                codes = cache[name] if name == "k" else cache[name].transpose(0, 1, 3, 2)
+                for h in range(codes.shape[1]):
+                    new = {o: x[to[slot, o][0], h, to[slot, o][1]] for o in run if (slot, o) in to}
+                    e = C8.exponent(C8.finite_max(np.stack(list(new.values()))))
+                    old = int(cache[name + "_exp"][slot, h, blk]) - 127
+                    if stay:
+                        e = max(e, old)
+                        if e > old:
+                            codes[slot, h, stay] = C8.encode(C8.decode(codes[slot, h, stay]) * 2.0 ** (old - e))
+                    cache[name + "_exp"][slot, h, blk] = e + 127
+                    for o, y in new.items():
+                        codes[slot, h, o] = C8.encode(y * 2.0 ** -e)
 
 
 # ---------------------------------------------------------------- page tables

@@ -98,12 +98,14 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {  // of two 16
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
+constexpr int kNoneKept = -1024;  // in the place of a block's exponent
 constexpr int kKeepBlocks = HSA_MAX_TREE / 8 + 2;  // scale blocks that a run of tokens touches (pages of 8)
 
 // The 8-bit cache: the keys or values of one head. The kept tokens' numbers are appended as
 // hsa_cache8_write appends them: a block that begins with them takes the smallest scale that holds
-// them, one with older tokens keeps the larger of its own and that. Codes wait in shared memory, keys as [token][dim] in
-// 16-byte pieces, values as [dim][token], until every one is there; then they go out, in runs of four where a
+// them, one with tokens that stay (older ones, and those whose source is no token) the larger of its own and
+// that, and one of which none is kept stays as it is. Codes wait in shared memory, keys as [token][dim] in 16-byte
+// pieces, values as [dim][token], until every one is there; then they go out, in runs of four where a
 // value row has them (64 sequences' paths of up to 100 tokens, 8 heads, d = 128: 17.7 us, 25.8 with the ends of the
 // runs in the same loop, where every wave waits for its few lanes that have one; the loads alone take 10).
 template <int D>
@@ -196,15 +198,21 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
     int blk;
     const Block x = block_of(u, blk);
     int e = kScaleMin;
-    if (lane < x.o1 - x.o0) {
+    const bool one = lane < x.o1 - x.o0 && ok[x.i0 + lane];
+    if (one) {
       const int i = x.i0 + lane;
-      if (ok[i] && most[i]) e = clampi(scale_exponent(code_to_f32(most[i])) + exps[i], kScaleMin, kScaleMax);
+      if (most[i]) e = clampi(scale_exponent(code_to_f32(most[i])) + exps[i], kScaleMin, kScaleMax);
+    }
+    const int kept = __popcll(__ballot(one));
+    if (kept == 0) {
+      if (lane == 0) block_e[u] = kNoneKept;
+      continue;
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) e = max(e, __shfl_xor(e, m));
     uint8_t* at = pool_exp + x.head * nb + blk;
     const int old = (int)*at - 127;
-    if (x.o0 > 0) e = max(e, old);
+    if (kept < x.o1) e = max(e, old);  // (some of its tokens up to the last one stay)
     if (lane == 0) {
       block_e[u] = e;
       block_old[u] = old;
@@ -221,17 +229,20 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
     int blk;
     const Block x = block_of(u, blk);
     const int e = block_e[u];
+    if (e == kNoneKept) continue;
     const float shift = pow2i(block_old[u] - e);
-    const int r0 = x.o0 > 0 && e > block_old[u] ? 0 : x.o0;  // older codes are written again only if the scale grows
+    const bool grows = e > block_old[u];  // then, and only then, codes that stay are written again
+    const int r0 = x.o0 > 0 && grows ? 0 : x.o0;
     if (!values) {
       uint8_t* dst = pool + (x.head * p.P + x.boff) * D;
       for (int y = tid; y < (x.o1 - r0) * C; y += kThreads) {
         const int o = r0 + y / C, c = y % C;
         u32x4* at = reinterpret_cast<u32x4*>(dst + o * D + 16 * c);
         const int i = x.i0 + o - x.o0;
-        if (o >= x.o0 && !ok[i]) continue;
-        u32x4 w = o < x.o0 ? *at : *reinterpret_cast<const u32x4*>(buf + i * D + 16 * c);
-        const float by = o < x.o0 ? shift : shifts[i];
+        const bool stays = o < x.o0 || !ok[i];
+        if (stays && !grows) continue;
+        u32x4 w = stays ? *at : *reinterpret_cast<const u32x4*>(buf + i * D + 16 * c);
+        const float by = stays ? shift : shifts[i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = recode4(w[j], by);
         *at = w;
@@ -246,6 +257,7 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
           const int i = x.i0 + o + j - x.o0;
           if (o + j >= x.o0 && o + j < x.o1) {
             if (ok[i]) at[j] = recode(buf[c * n + i], shifts[i]);
+            else if (grows) at[j] = recode(at[j], shift);
           } else if (o + j >= r0 && o + j < x.o0) {
             at[j] = recode(at[j], shift);
           }
