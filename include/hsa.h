@@ -24,9 +24,12 @@
  *
  * Errors: calls return an hsa_status_t. Arguments are validated on the host
  * before any launch; on an error nothing is launched and no output is
- * written. Kernels clamp physical slots into [0, num_slots) so that a corrupt
- * page table cannot fault the GPU (results are then meaningless; HSA_CHECK=1
- * reports HSA_ERR_OUT_OF_RANGE instead). A launch failure is HSA_ERR_DEVICE.
+ * written. A page whose table entry lies outside [0, num_slots), as -1 does, has
+ * no slot: tokens that hsa_page_write, hsa_token_write, hsa_cache8_write,
+ * hsa_token_keep or hsa_cache8_keep bring to such a page are dropped. Where kernels
+ * read through an entry they clamp it into [0, num_slots), so that a corrupt
+ * page table cannot fault the GPU (results are then meaningless). HSA_CHECK=1
+ * reports HSA_ERR_OUT_OF_RANGE for either. A launch failure is HSA_ERR_DEVICE.
  *
  * Shapes: B batch, H heads (1..64), d head dim (64 or 128), P page size
  * (a multiple of 8, >= 8), n_q queries in the chunk. Element type of q, k, v
@@ -689,8 +692,8 @@ hsa_status_t hsa_rope_apply(const hsa_config_t* cfg, const hsa_rope_t* rope, con
  * hsa_token_write -- appends any run of tokens to the pool, keys rotated on the
  * way (hsa_page_write without whole pages): tokens i < count[b] of batch entry
  * b become tokens first[b] + i of its sequence, token t in page t / P of its
- * row of the page table. Tokens outside [0, max_pages * P) are dropped; the rest of
- * the pages stays as it was. rope: NULL for keys as they are; pos as in
+ * row of the page table. Tokens outside [0, max_pages * P) and of pages without a slot are dropped;
+ * the rest of the pages stays as it was. rope: NULL for keys as they are; pos as in
  * hsa_rope_apply, its default the token's place in the sequence.
  * k_src, v_src: device, cfg->dtype, [B, n, H, d] with strides in elements as in
  * hsa_rope_apply. first: device int32 [B], NULL: 0. count: device int32 [B] in
@@ -861,8 +864,8 @@ hsa_status_t hsa_cache8_tree_attn(const hsa_config_t* cfg, const void* q, int32_
  * index may occur twice). With first the base of a tree and index the nodes of the accepted path, the path becomes
  * the sequence's next tokens. Keys are moved as they are: a node's position is that of its depth already. first:
  * device int32 [B], NULL: 0. index: device int32 [B, n]. count: device int32 [B] in [0, n], NULL: n. n in
- * [0, HSA_MAX_TREE] (UNSUPPORTED above). Tokens outside [0, max_pages * P) are neither read nor written (nor is
- * what they would have gone to). No two entries may write to the same page. cfg->num_heads are
+ * [0, HSA_MAX_TREE] (UNSUPPORTED above). Tokens outside [0, max_pages * P) and of pages without a slot are neither
+ * read nor written (nor is what they would have gone to). No two entries may write to the same page. cfg->num_heads are
  * the pool's heads. pool->k and pool->v 16-byte aligned (UNSUPPORTED). n == 0 is a no-op. Kernels read
  * first, index and count, so a captured call follows them.
  */
@@ -873,7 +876,7 @@ hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, 
  * hsa_cache8_keep -- the same in the 8-bit cache. The result is that of appending the kept tokens'
  * numbers (code * 2^(exponent byte - 127)) at first[b] with hsa_cache8_write: a block that begins with
  * kept tokens takes the smallest scale that holds them, one with older tokens before them keeps the larger of
- * its own and that (older codes scaled down), as does one with tokens among them whose source lies outside the table, and
+ * its own and that (older codes scaled down), as does one with tokens among them whose source is not read, and
  * which stay; a block of which none is kept keeps its scale. A number changes only if its code becomes subnormal. Codes of a block
  * behind the kept tokens stay as they are, and what they stand for is lost if the scale changes.
  */
@@ -909,7 +912,8 @@ size_t hsa_slots_workspace_size(const hsa_config_t* cfg, int32_t num_slots, int3
  * slot, new slot, first[b] % P} for hsa_page_copy, {-1, -1, -1} otherwise (device int32 [B, 3], nullable: such
  * tokens are then lost). If the free slots do not suffice, the entries that come last stay as they were and
  * *missing (device int32, nullable) is their number, else 0: a program that can run out of slots
- * reads it before it writes. Pages past max_pages are not taken. first: device int32 [B], NULL: 0.
+ * reads it before it writes (tokens for pages without a slot are dropped; an entry that went on sharing its slot is
+ * written where the others read it). Pages past max_pages are not taken. first: device int32 [B], NULL: 0.
  * end: device int32 [B]; end[b] <= first[b] takes nothing.
  */
 hsa_status_t hsa_slots_take(const hsa_config_t* cfg, const hsa_slots_t* slots, const int32_t* first,

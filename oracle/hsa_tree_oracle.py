@@ -115,17 +115,19 @@ def attend_many(q, k, v, page_table, pages, kv_len, q_len, bits, scale, device="
 
 
 # ---------------------------------------------------------------- kept tokens
-def _place(page_table, b, t, P):
-    """(slot, token of the page) of a sequence's token, None outside the table."""
-    return (int(page_table[b, t // P]), t % P) if 0 <= t < page_table.shape[1] * P else None
+def _place(page_table, b, t, P, slots):
+    """(slot, token of the page) of a sequence's token, None outside the table and of a page without a slot."""
+    if not 0 <= t < page_table.shape[1] * P or not 0 <= page_table[b, t // P] < slots:
+        return None
+    return int(page_table[b, t // P]), t % P
 
 
-def _kept(page_table, P, first, index, count):
+def _kept(page_table, P, slots, first, index, count):
     """(batch entry, place that is read, place that is written) of the tokens that are kept."""
     for b in range(page_table.shape[0]):
         for i in range(count[b]):
-            src = _place(page_table, b, int(first[b]) + int(index[b, i]), P)
-            dst = _place(page_table, b, int(first[b]) + i, P)
+            src = _place(page_table, b, int(first[b]) + int(index[b, i]), P, slots)
+            dst = _place(page_table, b, int(first[b]) + i, P, slots)
             if src and dst:
                 yield b, src, dst
 
@@ -133,7 +135,7 @@ def _kept(page_table, P, first, index, count):
 def keep(k_pool, v_pool, page_table, first, index, count):
     """The pool [slots, H, P, d] / [slots, H, d, P], changed in place."""
     old_k, old_v = k_pool.copy(), v_pool.copy()
-    for _, (s, o), (w, x) in _kept(page_table, k_pool.shape[2], first, index, count):
+    for _, (s, o), (w, x) in _kept(page_table, k_pool.shape[2], len(k_pool), first, index, count):
         k_pool[w, :, x] = old_k[s, :, o]
         v_pool[w, :, :, x] = old_v[s, :, :, o]
 
@@ -141,14 +143,14 @@ def keep(k_pool, v_pool, page_table, first, index, count):
 def keep8(cache, page_table, first, index, count):
     """cache: dict of uint8 k, v, k_exp, v_exp, changed in place, as by an append of the kept tokens' numbers.
     Tokens that stay before or among a block's kept ones keep its scale from shrinking, and their numbers."""
-    P = cache["k"].shape[2]
+    slots, _, P, _ = cache["k"].shape
     numbers = dict(zip("kv", C8.dequantise(cache)))
-    kept = list(_kept(page_table, P, first, index, count))
+    kept = list(_kept(page_table, P, slots, first, index, count))
     for b in range(page_table.shape[0]):
         to = {dst: src for c, src, dst in kept if c == b}
         last = {}  # of each block, the last token of the run that the call brings
         for t in range(int(first[b]), int(first[b]) + int(count[b])):
-            at = _place(page_table, b, t, P)
+            at = _place(page_table, b, t, P, slots)
             if at:
                 last[at[0], at[1] // C8.BLOCK] = at[1]
         for (slot, blk), o1 in last.items():

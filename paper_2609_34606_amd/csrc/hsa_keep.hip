@@ -17,17 +17,19 @@ constexpr int kThreads = 256;
 template <typename T>
 constexpr int kSliceOf = 128 / (int)sizeof(T);
 
-// Slot and place within its page of a sequence's token; false outside the table.
+// Slot and place within its page of a sequence's token; false outside the table, and if its page has no slot (the place is
+// one of the pool all the same).
 struct TokenPlace {
   size_t slot;
   int off;
 };
 __device__ __forceinline__ bool place_of(const TokenKeepParams& p, int b, int64_t t, TokenPlace& at) {
-  if (t < 0 || t >= (int64_t)p.max_pages * p.P) return false;
-  const int page = (int)t / p.P;
-  at.off = (int)t - page * p.P;
-  at.slot = clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1);
-  return true;
+  const bool in = t >= 0 && t < (int64_t)p.max_pages * p.P;
+  const int token = in ? (int)t : 0, page = token / p.P;
+  at.off = token - page * p.P;
+  const int slot = p.page_table[(size_t)b * p.max_pages + page];
+  at.slot = clampi(slot, 0, p.num_slots - 1);
+  return in & (slot >= 0) & (slot < p.num_slots);
 }
 
 // The pool: a slice of the dims of one head's keys or values. T: an element's bits. (32 sequences' paths of up to 8
@@ -129,11 +131,12 @@ __global__ __launch_bounds__(kThreads) void keep_codes_kernel(TokenKeepParams p)
   bool mine = false;
   if (tid <= HSA_MAX_TREE / 32) ok_words[tid] = 0;
   if (tid < n) {
-    TokenPlace to;
-    const bool in = place_of(p, b, first + p.index[(size_t)b * p.n + tid], from[tid]);
-    mine = place_of(p, b, first + tid, to) && in;
+    TokenPlace at, to;
+    const bool there = place_of(p, b, first + tid, to);
+    mine = place_of(p, b, first + p.index[(size_t)b * p.n + tid], at) & there;
+    from[tid] = at;
     ok[tid] = mine;
-    exps[tid] = in ? (int)pool_exp[(from[tid].slot * p.H + h) * nb + from[tid].off / kScaleTok] - 127 : 0;
+    exps[tid] = (int)pool_exp[(at.slot * p.H + h) * nb + at.off / kScaleTok] - 127;
     most[tid] = 0;
   }
   __syncthreads();

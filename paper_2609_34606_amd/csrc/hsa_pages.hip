@@ -58,8 +58,7 @@ __global__ __launch_bounds__(256) void page_write_kernel(PageWriteParams p) {
   const int b = blockIdx.z / p.n_pages, pg = blockIdx.z % p.n_pages;
   const int i0 = run * kTok;
   const int n = min(kTok, p.P - i0);             // a multiple of 8
-  const int slot = clampi(ld_const(p.page_table + (size_t)b * p.max_pages + p.first_page + pg), 0,
-                          p.num_slots - 1);
+  const int slot = ld_const(p.page_table + (size_t)b * p.max_pages + p.first_page + pg);
   const T* ksrc = static_cast<const T*>(p.k_src);
   const T* vsrc = static_cast<const T*>(p.v_src);
   T* kdst = static_cast<T*>(p.k) + ((size_t)slot * p.H + h) * p.P * D;
@@ -77,6 +76,7 @@ __global__ __launch_bounds__(256) void page_write_kernel(PageWriteParams p) {
   for (int l = 0; l < NLD; ++l) v[l] = *reinterpret_cast<const V16*>(vsrc + row[l] * D + tid % CPR * E);
 #pragma unroll
   for (int l = 0; l < NLD; ++l) k[l] = *reinterpret_cast<const V16*>(ksrc + row[l] * D + tid % CPR * E);
+  if (slot < 0 || slot >= p.num_slots) return;  // (the whole workgroup: a page without a slot)
 #pragma unroll
   for (int l = 0; l < NLD; ++l) {
     uint32_t* dst = vs + (tid + 256 * l) / CPR * RW + tid % CPR * 4;

@@ -115,8 +115,8 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
     }
   };
   load(h_lo);
-  const size_t slot =
-      clampi(ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page), 0, p.num_slots - 1);
+  const int slot = ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page);
+  if (slot < 0 || slot >= p.num_slots) return;  // (the whole workgroup: a page without a slot)
   it.frequencies(r);
   float cs[NK][Item::NP], sn[NK][Item::NP];
   auto angles = [&](int i, int k) { it.angles(r, rope_positions(r, t.b, t.i0 + i, p.n), cs[k], sn[k]); };
@@ -126,7 +126,7 @@ __device__ __forceinline__ void write_keys(const TokenWriteParams& p, const Toke
       if (tk + k * step < ntok) angles(tk + k * step, k);
   }
   for (int h = h_lo; h < h_hi; ++h) {
-    const size_t head = slot * p.H + h;
+    const size_t head = (size_t)slot * p.H + h;
     int e_old = kScaleMin;
     if (kEight && t.o0 > 0) e_old = (int)p.k_exp[head * t.nb + t.blk] - 127;
     float mk = 0.f;
@@ -249,9 +249,9 @@ __device__ __forceinline__ void write_values(const TokenWriteParams& p, const To
   for (int l = 0; l < NLD; ++l)
     v[l] = *reinterpret_cast<const V16*>(src + (int64_t)min((tid + kThreads * l) / CPR, ntok - 1) * p.v_token +
                                          tid % CPR * E);
-  const size_t slot =
-      clampi(ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page), 0, p.num_slots - 1);
-  const size_t head = slot * p.H + h;
+  const int slot = ld_const(p.page_table + (size_t)t.b * p.max_pages + t.page);
+  if (slot < 0 || slot >= p.num_slots) return;  // (the whole workgroup: a page without a slot)
+  const size_t head = (size_t)slot * p.H + h;
   int e_old = kScaleMin;
   if (kEight && o0 > 0) e_old = (int)p.v_exp[head * t.nb + t.blk] - 127;
   uint32_t mv = 0;
