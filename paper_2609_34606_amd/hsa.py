@@ -698,11 +698,12 @@ def _call(fn, dev: int, stream, *args) -> int:
         raise ValueError("the tensors must be on a GPU")
     if dev != _torch.cuda.current_device():
         with _torch.cuda.device(dev):
-            return fn(*args, _raw_stream(dev, stream))
-    return fn(*args, _raw_stream(dev, stream))
+            return fn(*args, raw_stream(dev, stream))
+    return fn(*args, raw_stream(dev, stream))
 
 
-def _raw_stream(dev: int, stream) -> int:
+def raw_stream(dev: int, stream) -> int:
+    """The handle of stream (None: the current one of device dev)."""
     if stream is not None:
         return int(getattr(stream, "cuda_stream", stream))
     return _torch._C._cuda_getCurrentRawStream(dev)
@@ -714,10 +715,29 @@ def _empty(shape, dtype, device, stream):
     what is queued there, and the launch does not wait for that."""
     if stream is None:
         return _torch.empty(shape, dtype=dtype, device=device)
-    if not isinstance(stream, _torch.cuda.Stream):
-        stream = _torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
-    with _torch.cuda.stream(stream):
+    with _torch.cuda.stream(_torch_stream(stream, device)):
         return _torch.empty(shape, dtype=dtype, device=device)
+
+
+def _torch_stream(stream, device):
+    if isinstance(stream, _torch.cuda.Stream):
+        return stream
+    return _torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+
+
+def used_on(stream, *tensors):
+    """Tensors of a GPU that calls on stream (None: the current one) read or write and that may be let go before those
+    have run: their memory then waits for the stream."""
+    device = tensors[0].device
+    on = _torch.cuda.current_stream(device) if stream is None else _torch_stream(stream, device)
+    for t in tensors:
+        t.record_stream(on)
+
+
+def empty_of(nbytes, device, stream):
+    """Memory of stream (None: the current one), and whether the stream is being captured."""
+    with _torch.cuda.stream(None if stream is None else _torch_stream(stream, device)), _torch.cuda.device(device):
+        return _torch.empty(nbytes, dtype=_torch.uint8, device=device), _torch.cuda.is_current_stream_capturing()
 
 
 def empty_on(shape, dtype, device, stream=None):

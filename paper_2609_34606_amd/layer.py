@@ -325,34 +325,45 @@ class HsaSlots:
             raise ValueError("the table's tensors must be on one device")
         self.cfg = _h.config(batch, 1, 64, page_size, _h.HSA_DTYPE_BF16)
         self.table = _h.slot_table(page_table, refs, self.cfg)
-        # (calls on one table follow each other, so one workspace serves them all)
-        self._ws = torch.empty(_h.hsa_slots_workspace_size(self.cfg, self.table.num_slots, self.table.max_pages),
-                               dtype=torch.uint8, device=device)
+        # Calls on one table follow each other, so those of a stream share a workspace, which is that stream's memory.
+        self._ws, self._ws_bytes = {}, _h.hsa_slots_workspace_size(self.cfg, self.table.num_slots, self.table.max_pages)
+
+    def _workspace(self, t, stream):
+        """The workspace of a call with t on stream."""
+        dev = self.refs.get_device()
+        if t.get_device() != dev or dev < 0:
+            return _same_device(t, self.refs)
+        ws = self._ws.get(_h.raw_stream(dev, stream))
+        return self._first_call(_h.raw_stream(dev, stream), stream) if ws is None else ws
+
+    def _first_call(self, at, stream):
+        _h.used_on(stream, self.page_table, self.refs, self.missing)
+        ws, captured = _h.empty_of(self._ws_bytes, self.refs.device, stream)
+        if not captured:  # (memory of a graph stays the graph's)
+            self._ws[at] = ws
+        return ws
 
     def take(self, first, end, moves=None, stream=None):
         """Makes the pages that hold tokens [first[b], end[b]) of each row (int32 [B]) its own before they are
         written; returns the moves (int32 [B, 3]) that carry over what a shared first page holds."""
-        _same_device(end, self.refs)
+        ws = self._workspace(end, stream)
         if moves is None:
             moves = _h.empty_on((self.cfg.batch, 3), self.torch.int32, end.device, stream)
-        _h.hsa_slots_take(self.cfg, self.table, first, end, moves=moves, missing=self.missing, ws=self._ws,
-                          stream=stream)
+        _h.hsa_slots_take(self.cfg, self.table, first, end, moves=moves, missing=self.missing, ws=ws, stream=stream)
         return moves
 
     def fork(self, parent, stream=None):
         """Row b becomes what row parent[b] (int32 [B]; outside [0, B): itself) was, sharing its slots."""
-        _same_device(parent, self.refs)
-        _h.hsa_slots_fork(self.cfg, self.table, parent, ws=self._ws, stream=stream)
+        _h.hsa_slots_fork(self.cfg, self.table, parent, ws=self._workspace(parent, stream), stream=stream)
 
     def free(self, keep, stream=None):
         """Row b lets go of its pages behind its first keep[b] tokens (int32 [B]; 0: all, below 0: none)."""
-        _same_device(keep, self.refs)
+        self._workspace(keep, stream)
         _h.hsa_slots_free(self.cfg, self.table, keep, stream=stream)
 
     def compact(self, moves, table_out=None, refs_out=None, stream=None):
         """Moves the slots in use to the front of the pool, at most as many as moves (int32 [n, 3]) has rows; the
         new table and counts go to table_out and refs_out, or in place."""
-        _same_device(moves, self.refs)
         _h.hsa_slots_compact(self.cfg, self.table, moves, moves.shape[0], table_out=table_out, refs_out=refs_out,
-                             ws=self._ws, stream=stream)
+                             ws=self._workspace(moves, stream), stream=stream)
         return moves
