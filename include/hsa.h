@@ -952,7 +952,8 @@ hsa_status_t hsa_slots_compact(const hsa_config_t* cfg, const hsa_slots_t* slots
  * page); the rest of the page at `to` stays as it was. A move with a slot outside [0, num_slots) or no tokens
  * copies nothing. No slot may be written by two moves, or written by one and read by another.
  * cfg->num_heads are the pool's heads. pool->k and pool->v 16-byte aligned. A compressed pool is copied
- * with cfg->page_size = rank. n == 0 is a no-op. pool->page_table is not used.
+ * with cfg->page_size = rank and moves of `rank` tokens: its rows are projections of a whole page, and the first few of
+ * them are not those of its first tokens. n == 0 is a no-op. pool->page_table is not used.
  */
 hsa_status_t hsa_page_copy(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* moves, int32_t n,
                            void* stream);

@@ -963,6 +963,14 @@ def hsa_cache8_page_copy(cfg, cache, moves, n, stream=None, check=True) -> int:
                        _i32s(moves, 3 * n, moves.get_device(), "moves"), n)
 
 
+def whole_pages(moves, page_size: int, stream=None):
+    """The moves with whole pages of page_size rows for those that copy any token."""
+    with _torch.cuda.stream(None if stream is None else _torch_stream(stream, moves.device)):
+        whole = moves.clone()
+        whole[:, 2].clamp_(0, 1).mul_(page_size)
+        return whole
+
+
 def slot_table(page_table, refs, cfg: HsaConfig) -> HsaSlotTable:
     """The descriptor of a page table (int32 [B, max_pages]) and its slots' counts (int32 [num_slots])."""
     if page_table.dim() != 2 or page_table.shape[0] != cfg.batch or str(page_table.dtype) != "torch.int32":

@@ -110,14 +110,15 @@ class HsaLayer:
         _h.hsa_token_keep(self.cfg, self.pool, first, index, index.shape[1], count=count, stream=stream)
 
     def copy_pages(self, moves, stream=None):
-        """Copies pages between slots (moves int32 [n, 3] of HsaSlots), compressed pages as well."""
+        """Copies pages between slots (moves int32 [n, 3] of HsaSlots). Compressed pages go along whole, whatever part of
+        a page is copied: their rows are projections of all its tokens."""
         _same_device(moves, self.k_pool)
         _h.hsa_page_copy(self.cfg, self.pool, moves, moves.shape[0], stream=stream)
         if getattr(self, "ck", None) is not None:
             c = self.cfg
-            whole = _h.HsaConfig(c.batch, c.num_heads, c.head_dim, self.rank, c.dtype, c.sm_scale, 0)
-            _h.hsa_page_copy(whole, _h.kv_pool(self.ck, self.cv, self.page_table), moves, moves.shape[0],
-                             stream=stream)
+            cfg = _h.HsaConfig(c.batch, c.num_heads, c.head_dim, self.rank, c.dtype, c.sm_scale, 0)
+            whole = _h.whole_pages(moves, self.rank, stream)
+            _h.hsa_page_copy(cfg, _h.kv_pool(self.ck, self.cv, self.page_table), whole, whole.shape[0], stream=stream)
 
     def forward(self, q, n_cand: int, n_cur: int, k_h: Sequence[int], k_max: Optional[int] = None,
                 g_lin=None, g_sp=None, out=None, sel_out=None, stream=None):
