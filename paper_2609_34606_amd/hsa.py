@@ -317,13 +317,16 @@ def kv_pool(k_pool, v_pool, page_table, cfg: Optional[HsaConfig] = None) -> HsaK
     dtype, page_table [B, max_pages] int32."""
     ks, ps = k_pool.shape, page_table.shape
     if cfg is not None:
-        lib()
-        H, P, d, dt, slots = cfg.num_heads, cfg.page_size, cfg.head_dim, _elem(cfg), ks[0]
+        torch = _torch
+        if torch is None:  # (the library need not be there)
+            import torch
+        dt = torch.bfloat16 if cfg.dtype == HSA_DTYPE_BF16 else torch.float32
+        H, P, d, slots = cfg.num_heads, cfg.page_size, cfg.head_dim, ks[0]
         for name, t, got, shape in (("k_pool", k_pool, ks, (slots, H, P, d)),
                                     ("v_pool", v_pool, v_pool.shape, (slots, H, d, P))):
             if t.dtype is not dt or got != shape:
                 raise ValueError(f"{name} must be {dt} {shape}, got {t.dtype} {tuple(got)}")
-        if page_table.dtype is not _torch.int32 or len(ps) != 2 or ps[0] != cfg.batch:
+        if page_table.dtype is not torch.int32 or len(ps) != 2 or ps[0] != cfg.batch:
             raise ValueError(f"page_table must be int32 [B={cfg.batch}, max_pages], got "
                              f"{page_table.dtype} {tuple(ps)}")
     return HsaKvPool(_ptr(k_pool), _ptr(v_pool), _ptr(page_table), ks[0], ps[-1])
