@@ -157,33 +157,4 @@ __device__ __forceinline__ bool all_finite(const float (&x)[N]) {
   return zero == 0.f;
 }
 
-// Eight elements of T in kParts bf16 operands whose sum is the element: one for
-// bf16, three for fp32 (3 x 8 significant bits).
-template <typename T, int kParts>
-__device__ __forceinline__ void split_row(const T* p, u32x4 (&f)[kParts]) {
-  if constexpr (kParts == 1) {
-    f[0] = ld_global16(p);
-  } else {
-    float x[8];
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-#pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[k][i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        x[2 * i] -= bf16_lo(f[k][i]);
-        x[2 * i + 1] -= bf16_hi(f[k][i]);
-      }
-      // an infinity is its first part alone
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? x[i] : 0.f;
-    }
-  }
-}
-
 }  // namespace hsa

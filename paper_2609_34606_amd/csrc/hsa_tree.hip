@@ -7,7 +7,7 @@
 //   o_i = sum_j softmax_j(scale q_i . k_j) v_j over the tokens it sees.
 //
 // The H / Hk query heads that share a key head are rows of one product (row r of key head h is head
-// h G + r % G of node r / G), so that every key and value is read once for up to 64 rows.
+// h G + r % G of node r / G), so that every key and value is read once for up to 128 rows.
 #include <limits.h>
 
 #include <algorithm>
@@ -90,11 +90,11 @@ __device__ __forceinline__ TreeWalk tree_walk(const TreeAttnParams& p, int b, in
   return w;
 }
 
-// A listed page: where its numbers of the key head begin (of keys and values alike), the head's index in the
-// cache, the page's first token (-1 past the list, where it repeats the last page).
+// A listed page: where its numbers of the key head begin (of keys and values alike), the page's first token (-1 past
+// the list, where it repeats the last page).
 struct TreePage {
   int64_t at;
-  int head, first;
+  int first;
 };
 __device__ __forceinline__ void tree_pages(const TreeAttnParams& p, const TreeWalk& w, int b, int h, int li0, int n,
                                            int D, int tid, int threads, TreePage* pages) {
@@ -103,7 +103,7 @@ __device__ __forceinline__ void tree_pages(const TreeAttnParams& p, const TreeWa
     const int page = li < w.n_sel ? p.sel[((size_t)b * p.Hk + h) * p.k_max + li] : p.cur_first + li - w.n_sel;
     const int slot = clampi(p.page_table[(size_t)b * p.max_pages + page], 0, p.num_slots - 1);
     const int64_t head = (int64_t)slot * p.Hk + h;
-    pages[x] = TreePage{head * p.P * D, (int)head, li0 + x < w.n_list ? page * p.P : -1};
+    pages[x] = TreePage{head * p.P * D, li0 + x < w.n_list ? page * p.P : -1};
   }
 }
 
@@ -112,8 +112,8 @@ __device__ __forceinline__ void tree_pages(const TreeAttnParams& p, const TreeWa
 struct TreePlace {
   int li, at;
   bool one;       // the whole tile is in one page
-  int64_t base;   // (one) its first token's place among the page's tokens, and the page's
-  int head, off, first;
+  int64_t base;   // (one) where the page's numbers begin
+  int off, first; // (one) the tile's first token, within the page and of the sequence
 };
 __device__ __forceinline__ void tree_place(const TreeAttnParams& p, const TreePage* pages, int grans, TreePlace& t) {
   t.one = t.at + grans <= p.gpp;
@@ -121,7 +121,6 @@ __device__ __forceinline__ void tree_place(const TreeAttnParams& p, const TreePa
     const TreePage e = pages[t.li];
     t.base = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)e.at) |
              (int64_t)__builtin_amdgcn_readfirstlane((int)(e.at >> 32)) << 32;
-    t.head = __builtin_amdgcn_readfirstlane(e.head);
     t.off = 8 * t.at;
     t.first = __builtin_amdgcn_readfirstlane(e.first) + t.off;
   }
@@ -547,7 +546,7 @@ void tree_attn_kernel(TreeAttnParams p) {
 }
 
 // More rows: 32 kRG rows of one key head (kRG = 2 or 4) against a range of its tiles of 64 tokens. Four waves, two
-// workgroups a CU; a tile is turned into bf16 once, on its way from the registers that it arrived in to LDS, and read from
+// workgroups a CU; a tile goes once from the registers that it arrived in to LDS, and is read from
 // there by all waves: with kRG = 4 each takes 32 rows, with two 32 rows and half of the tile's tokens.
 //
 // Products are transposed as above, 32x32x16, with key rows in an order that makes a lane's scores the
@@ -627,7 +626,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
   // Bit j: whether the lane's row sees token t0 + j.
   auto sees = [&](int t0) __attribute__((always_inline)) { return tree_sees(p, w, bits[p.mask ? node - i0 : 0], node, t0); };
 
-  // A thread's pieces of a tile: key row and chunk, value row and granule (two of codes).
+  // A thread's pieces of a tile: key row and chunk, value row and granule.
   u32x4 kc[NP], vc[NP];
   auto krow_of = [&](int i) { return (tid + 256 * i) / (D / 8); };
   const int kcol = tid % (D / 8);
@@ -655,7 +654,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
         int off;
         const int row = krow_of(i);
         const TreePage e = tree_granule(p, pages, t, row >> 3, off);
-        kc[i] = ld_global16(kp + (e.at + (int64_t)(off + (row & 7)) * D + kcol * (16 / E)) * E);
+        kc[i] = ld_global16(kp + (e.at + (int64_t)(off + (row & 7)) * D + kcol * 8) * E);
       }
       int off;
       const TreePage e = tree_granule(p, pages, t, vgran, off);
