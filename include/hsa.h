@@ -877,8 +877,9 @@ hsa_status_t hsa_token_keep(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, 
  * numbers (code * 2^(exponent byte - 127)) at first[b] with hsa_cache8_write: a block that begins with
  * kept tokens takes the smallest scale that holds them, one with older tokens before them keeps the larger of
  * its own and that (older codes scaled down), as does one with tokens among them whose source is not read, and
- * which stay; a block of which none is kept keeps its scale. A number changes only if its code becomes subnormal. Codes of a block
- * behind the kept tokens stay as they are, and what they stand for is lost if the scale changes.
+ * which stay; a block of which none is kept keeps its scale. A number changes only if its code becomes
+ * subnormal. Codes of a block behind the kept tokens stay as they are, and what they stand for is lost if
+ * the scale changes.
  */
 hsa_status_t hsa_cache8_keep(const hsa_config_t* cfg, const hsa_cache8_t* cache, const int32_t* first,
                              const int32_t* index, int32_t n, const int32_t* count, void* stream);
@@ -952,8 +953,8 @@ hsa_status_t hsa_slots_compact(const hsa_config_t* cfg, const hsa_slots_t* slots
  * page); the rest of the page at `to` stays as it was. A move with a slot outside [0, num_slots) or no tokens
  * copies nothing. No slot may be written by two moves, or written by one and read by another.
  * cfg->num_heads are the pool's heads. pool->k and pool->v 16-byte aligned. A compressed pool is copied
- * with cfg->page_size = rank and moves of `rank` tokens: its rows are projections of a whole page, and the first few of
- * them are not those of its first tokens. n == 0 is a no-op. pool->page_table is not used.
+ * with cfg->page_size = rank and moves of `rank` tokens: its rows are projections of a whole page, and the first
+ * few of them are not those of its first tokens. n == 0 is a no-op. pool->page_table is not used.
  */
 hsa_status_t hsa_page_copy(const hsa_config_t* cfg, const hsa_kv_pool_t* pool, const int32_t* moves, int32_t n,
                            void* stream);

@@ -882,7 +882,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
 
 // Joins the pieces of a row in an order that does not depend on the launch's timing: kW groups of D / 4
 // lanes a row, four dims a lane, each every kW-th piece, then the groups in order. Bound: reading the pieces
-// (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us).
+// (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us). Eight waves
+// a SIMD for kW = 1: with seven (66 registers; the check at the end takes two) the ragged batch above took 144 us for 139.
 template <typename T, int D, int kW>
 __global__ __launch_bounds__(256, kW == 1 ? 8 : 1) void tree_join_kernel(TreeAttnParams p) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kW);
