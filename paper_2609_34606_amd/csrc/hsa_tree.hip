@@ -840,6 +840,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
     const float m_other = osm[32 * D + l32], top = fmaxf(m_run, m_other);
     const float a = __builtin_amdgcn_exp2f((m_run - top) * c2), c = __builtin_amdgcn_exp2f((m_other - top) * c2);
     l = a * l + c * osm[32 * D + 32 + l32];
+    // (a choice for each number instead: the ragged batch above 144 us for 139)
     if (__builtin_expect(__any(fminf(a, c) == 0.f), 0)) {
 #pragma unroll
       for (int m = 0; m < NM; ++m)
@@ -882,10 +883,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(TreeAttnParams p) {
 
 // Joins the pieces of a row in an order that does not depend on the launch's timing: kW groups of D / 4
 // lanes a row, four dims a lane, each every kW-th piece, then the groups in order. Bound: reading the pieces
-// (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us). Eight waves
-// a SIMD for kW = 1: with seven (66 registers; the check at the end takes two) the ragged batch above took 144 us for 139.
+// (16384 rows of up to 8: 9.1 us), of few rows a launch and a few loads after another (12 rows of 6: 2.8 us).
 template <typename T, int D, int kW>
-__global__ __launch_bounds__(256, kW == 1 ? 8 : 1) void tree_join_kernel(TreeAttnParams p) {
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeAttnParams p) {
   constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kW);
   __shared__ __attribute__((aligned(16))) float osm[kW == 1 ? 1 : kRows * kW * D];
   __shared__ f32x2 mlsm[kW == 1 ? 1 : kRows * kW];
